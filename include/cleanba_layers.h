@@ -145,6 +145,43 @@ impala_status_t impala_maxpool_bwd(impala_prec_t prec, int64_t n, int32_t H, int
                                    const uint8_t* arg, const void* dy, void* dx,
                                    hipStream_t stream);
 
+/* Group norm with an activation, for residual networks whose convolutions are normalised. Per
+ * frame and group of C / groups channels, over the group's N = H W C / groups elements:
+ *   mean = sum(x) / N, rstd = 1 / sqrt(sum((x - mean)^2) / N + eps),
+ *   z = (x - mean) rstd gamma[c] + beta[c],  y = act(z);
+ * the activation is z, max(z, 0) or z / (1 + exp(-z)). Statistics are float32 sums in two passes
+ * (the mean, then the squares about it), in both precisions.
+ * x, y: [n, H, W, C]; gamma, beta: float [C] or NULL (1 and 0); mean, rstd: float [n, groups], what
+ * the backward pass reads, or NULL where none follows. y may be x itself; any other overlap of the
+ * two is IMPALA_EINVAL. eps >= 0. 1 <= C <= 1024 with groups dividing C, H * W <= 2^24, any of them
+ * odd; addresses aligned to an element (16-byte aligned ones, with C a multiple of 8 in bf16 or 4 in
+ * float32, are read 16 bytes at a time). ws: device scratch of
+ * impala_groupnorm_fwd_workspace_bytes() bytes (0 where a frame fits one workgroup: ws may then be
+ * NULL). */
+typedef enum { IMPALA_ACT_NONE = 0, IMPALA_ACT_RELU = 1, IMPALA_ACT_SILU = 2 } impala_act_t;
+size_t impala_groupnorm_fwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                            int32_t groups);
+impala_status_t impala_groupnorm_fwd(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                     int32_t groups, const void* x, const float* gamma, const float* beta,
+                                     float eps, int32_t act, void* y, float* mean, float* rstd, void* ws,
+                                     size_t ws_bytes, hipStream_t stream);
+
+/* Backward of impala_groupnorm_fwd from the gradient dy at y and the mean and rstd it left. With
+ * xh = (x - mean) rstd, da = dy act'(z) (relu: dy where z > 0, decided in 64 bits next to zero) and
+ * h = da gamma[c]:
+ *   dbeta[c] = sum da,  dgamma[c] = sum da xh  (over frames and pixels),
+ *   dx = rstd (h - mean_group(h) - xh mean_group(h xh)).
+ * dy, x, dx: [n, H, W, C]; dx may be dy itself; any other overlap of dx with dy or x is
+ * IMPALA_EINVAL. dgamma, dbeta: float [C], overwritten (zero for n = 0), or NULL where not wanted.
+ * ws: impala_groupnorm_bwd_workspace_bytes() bytes. Shapes and alignment as the forward. */
+size_t impala_groupnorm_bwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                            int32_t groups);
+impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                     int32_t groups, const void* dy, const void* x, const float* gamma,
+                                     const float* beta, const float* mean, const float* rstd, int32_t act,
+                                     void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                                     hipStream_t stream);
+
 /* Where a training-mode impala_cnn_fwd on n_frames frames (workspace laid out by
  * impala_workspace_bytes(net, n_frames, prec, 1)) leaves the activations that impala_cnn_bwd
  * reads, so a caller can inspect them or replace them between the two calls: the backward

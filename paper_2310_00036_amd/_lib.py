@@ -17,6 +17,7 @@ PREC_BF16, PREC_FP32 = 0, 1
 LEARNER_PPO, LEARNER_IMPALA = 0, 1
 LEARNER_OPT_ADAM, LEARNER_OPT_RMSPROP = 0, 1
 X_PLAIN, X_RELU, X_U8 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 STATUS = {0: "OK", -1: "EINVAL", -2: "EWORKSPACE", -3: "EUNSUPPORTED", -4: "EHIP"}
 
 
@@ -100,6 +101,12 @@ _SIGS = {
                                                _P]),
     "impala_maxpool_fwd": (C.c_int, [C.c_int, _I64, _I32, _I32, _I32, _P, _P, _P, _P]),
     "impala_maxpool_bwd": (C.c_int, [C.c_int, _I64, _I32, _I32, _I32, _P, _P, _P, _P]),
+    "impala_groupnorm_fwd_workspace_bytes": (_SZ, [C.c_int, _I64, _I32, _I32, _I32, _I32]),
+    "impala_groupnorm_fwd": (C.c_int, [C.c_int, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _F, _I32, _P, _P, _P, _P,
+                                       _SZ, _P]),
+    "impala_groupnorm_bwd_workspace_bytes": (_SZ, [C.c_int, _I64, _I32, _I32, _I32, _I32]),
+    "impala_groupnorm_bwd": (C.c_int, [C.c_int, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _I32, _P, _P,
+                                       _P, _P, _SZ, _P]),
     "impala_gumbel_sample": (C.c_int, [_I64, _I32, _P, _P, _P, _P, _P]),
     "impala_action_logp": (C.c_int, [_I64, _I32, _P, _P, _P, _P]),
     "impala_profile_begin": (C.c_int, [C.c_char_p, _I32]),
@@ -400,6 +407,28 @@ def impala_maxpool_fwd(prec, n, H, W, C_, x, y, arg, stream=None):
 def impala_maxpool_bwd(prec, n, H, W, C_, arg, dy, dx, stream=None):
     _check("impala_maxpool_bwd", lib.impala_maxpool_bwd(prec, n, H, W, C_, ptr(arg), ptr(dy), ptr(dx),
                                                         stream_handle(stream)))
+
+
+def impala_groupnorm_fwd_workspace_bytes(prec, n, H, W, C_, groups) -> int:
+    return int(lib.impala_groupnorm_fwd_workspace_bytes(prec, n, H, W, C_, groups))
+
+
+def impala_groupnorm_fwd(prec, n, H, W, C_, groups, x, gamma, beta, eps, act, y, mean=None, rstd=None, ws=None,
+                         stream=None):
+    _check("impala_groupnorm_fwd", lib.impala_groupnorm_fwd(
+        prec, n, H, W, C_, groups, ptr(x), ptr(gamma), ptr(beta), eps, act, ptr(y), ptr(mean), ptr(rstd), *_ws_args(ws),
+        stream_handle(stream)))
+
+
+def impala_groupnorm_bwd_workspace_bytes(prec, n, H, W, C_, groups) -> int:
+    return int(lib.impala_groupnorm_bwd_workspace_bytes(prec, n, H, W, C_, groups))
+
+
+def impala_groupnorm_bwd(prec, n, H, W, C_, groups, dy, x, gamma, beta, mean, rstd, act, dx, dgamma, dbeta, ws,
+                         stream=None):
+    _check("impala_groupnorm_bwd", lib.impala_groupnorm_bwd(
+        prec, n, H, W, C_, groups, ptr(dy), ptr(x), ptr(gamma), ptr(beta), ptr(mean), ptr(rstd), act, ptr(dx),
+        ptr(dgamma), ptr(dbeta), *_ws_args(ws), stream_handle(stream)))
 
 
 def impala_gumbel_sample(n, A, logits, gumbel, actions, logp, stream=None):

@@ -825,6 +825,83 @@ impala_status_t impala_conv3x3_pool_wgrad_u8(impala_prec_t prec, int64_t n, int3
     return hip_status(pool_wgrad_u8(cout, a, stream), "impala_conv3x3_pool_wgrad_u8");
 }
 
+static impala_status_t check_groupnorm(const char* fn, int prec, int64_t n, int H, int W, int C, int G, int act) {
+    if (!valid_prec(prec)) return fail(IMPALA_EINVAL, "%s: bad prec", fn);
+    if (n < 0 || n > (int64_t(1) << 24) || H < 1 || W < 1 || int64_t(H) * W > (int64_t(1) << 24))
+        return fail(IMPALA_EINVAL, "%s: shape out of range", fn);
+    if (C < 1 || G < 1 || C % G) return fail(IMPALA_EINVAL, "%s: groups must divide C (got C=%d groups=%d)", fn, C, G);
+    if (C > kGnMaxC) return fail(IMPALA_EUNSUPPORTED, "%s: at most %d channels (got %d)", fn, kGnMaxC, C);
+    if (act < IMPALA_ACT_NONE || act > IMPALA_ACT_SILU) return fail(IMPALA_EINVAL, "%s: bad act %d", fn, act);
+    if (groupnorm_blocks(prec, n, H, W, C, G) > (int64_t(1) << 31) - 1)
+        return fail(IMPALA_EUNSUPPORTED, "%s: too many elements for one call", fn);
+    return IMPALA_OK;
+}
+
+// Whether the byte ranges [a, a + bytes) and [b, b + bytes) overlap without being the same.
+static bool partial_overlap(const void* a, const void* b, size_t bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x != y && x < y + bytes && y < x + bytes;
+}
+
+size_t impala_groupnorm_fwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                            int32_t groups) {
+    if (check_groupnorm(__func__, prec, n, H, W, C, groups, 0) != IMPALA_OK) return 0;
+    ok();
+    return groupnorm_ws_bytes(prec, n, H, W, C, groups, 0);
+}
+
+impala_status_t impala_groupnorm_fwd(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                     int32_t groups, const void* x, const float* gamma, const float* beta,
+                                     float eps, int32_t act, void* y, float* mean, float* rstd, void* ws,
+                                     size_t ws_bytes, hipStream_t stream) {
+    impala_status_t st = check_groupnorm(__func__, prec, n, H, W, C, groups, act);
+    if (st) return st;
+    if (!(eps >= 0.f)) return fail(IMPALA_EINVAL, "impala_groupnorm_fwd: eps must be >= 0");
+    if (n == 0) return ok();
+    CHECK_PTR(x); CHECK_PTR(y);
+    const size_t bytes = size_t(n) * H * W * C * (prec == IMPALA_PREC_BF16 ? 2 : 4);
+    if (partial_overlap(x, y, bytes)) return fail(IMPALA_EINVAL, "impala_groupnorm_fwd: x and y overlap");
+    const size_t need = groupnorm_ws_bytes(prec, n, H, W, C, groups, 0);
+    if (need > 0) CHECK_PTR(ws);
+    if (ws_bytes < need)
+        return fail(IMPALA_EWORKSPACE, "impala_groupnorm_fwd: workspace %zu < %zu bytes", ws_bytes, need);
+    GnArgs a{};
+    a.x = x; a.y = y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd; a.eps = eps; a.act = act;
+    a.n = n; a.C = C; a.G = groups;
+    return hip_status(groupnorm_fwd(prec, H, W, a, ws, stream), "impala_groupnorm_fwd");
+}
+
+size_t impala_groupnorm_bwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                            int32_t groups) {
+    if (check_groupnorm(__func__, prec, n, H, W, C, groups, 0) != IMPALA_OK) return 0;
+    ok();
+    return groupnorm_ws_bytes(prec, n, H, W, C, groups, 1);
+}
+
+impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
+                                     int32_t groups, const void* dy, const void* x, const float* gamma,
+                                     const float* beta, const float* mean, const float* rstd, int32_t act,
+                                     void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                                     hipStream_t stream) {
+    impala_status_t st = check_groupnorm(__func__, prec, n, H, W, C, groups, act);
+    if (st) return st;
+    GnArgs a{};
+    a.gamma = gamma; a.beta = beta; a.act = act; a.n = n; a.C = C; a.G = groups;
+    if (n > 0) {
+        CHECK_PTR(dy); CHECK_PTR(x); CHECK_PTR(mean); CHECK_PTR(rstd); CHECK_PTR(dx);
+        const size_t bytes = size_t(n) * H * W * C * (prec == IMPALA_PREC_BF16 ? 2 : 4);
+        if (partial_overlap(dx, dy, bytes) || dx == x || partial_overlap(dx, x, bytes))
+            return fail(IMPALA_EINVAL, "impala_groupnorm_bwd: dx overlaps dy or x");
+        const size_t need = groupnorm_ws_bytes(prec, n, H, W, C, groups, 1);
+        CHECK_PTR(ws);
+        if (ws_bytes < need)
+            return fail(IMPALA_EWORKSPACE, "impala_groupnorm_bwd: workspace %zu < %zu bytes", ws_bytes, need);
+        a.x = x; a.dy = dy; a.y = dx;
+        a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+    }
+    return hip_status(groupnorm_bwd(prec, H, W, a, dgamma, dbeta, ws, stream), "impala_groupnorm_bwd");
+}
+
 impala_status_t impala_maxpool_fwd(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
                                    const void* x, void* y, uint8_t* arg, hipStream_t stream) {
     impala_status_t st = check_layer(__func__, prec, n, H, W, C, C);

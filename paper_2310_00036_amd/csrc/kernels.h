@@ -169,6 +169,27 @@ hipError_t maxpool_fwd(int prec, int n, int H, int W, int C, const void* x, void
 hipError_t maxpool_bwd(int prec, int n, int H, int W, int C, const uint8_t* arg, const void* dy,
                        void* dx, hipStream_t s);
 
+// ---- group norm with an activation, channels last; x, y, dy [n, HW, C] in the storage type
+constexpr int kGnMaxC = 1024;
+struct GnArgs {
+    const void* x; const void* dy; void* y;        // backward: y is dx
+    const float* gamma; const float* beta;         // [C] or NULL (1, 0)
+    float* mean; float* rstd;                      // [n, G]; forward: may be NULL
+    float eps;
+    int act;                                       // 0 none, 1 relu, 2 silu
+    int64_t n;
+    int HW, C, G, cg;                              // cg = C / G channels per group
+    // filled by the launcher: columns of V channels per pixel, padded to cvp = 2^cvs; pixels and
+    // number of a frame's chunks; workspace
+    int cv, cvp, cvs, crows, chunks;
+    float* part; float* fsum; float* smean; float* srstd;
+};
+size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd);
+int64_t groupnorm_blocks(int prec, int64_t n, int H, int W, int C, int G);   // workgroups at most
+hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t s);
+// n == 0: dgamma and dbeta are cleared. Either may be NULL.
+hipError_t groupnorm_bwd(int prec, int H, int W, GnArgs a, float* dgamma, float* dbeta, void* ws, hipStream_t s);
+
 // ---- GEMM D[m][n] = sum_k A(m,k) B(k,n) on MFMA, output out[n*ld + m]
 struct GemmArgs {
     const void* a; int a_f32; int a_kcontig; int64_t lda;   // A(m,k) = a[m*lda+k] or a[k*lda+m]

@@ -1,0 +1,323 @@
+"""Group norm with an activation, forward and backward, against the formulas in 64 bits.
+
+Tolerances. u = 2^-24 is float32's half step; a value stored in bf16 adds 2^-8 of itself. The kernels' sums are
+trees of at most 100 roundings (64 in a thread, the rest across threads), so a group's mean is off by at most
+100 u mean|x| and its rstd by 60 u of itself; K = 128 covers these and the few roundings of one element:
+  forward   |dy| <= K u ((|x| + mean|x|) rstd |gamma| + |z| + |beta|), half a step of the stored type, and for the
+            sigmoid 8 u (1 + |z|) |z| (an exponential whose argument is rounded, a reciprocal); act' is below 1.1
+  backward  |ddx| <= 2 K u rstd (|h| + mean|h| + |xh| mean|h xh| + |da'| terms) with h as large as 1.1 |dy gamma|
+  dbeta, dgamma: K u sum|terms| (the frames are added in 64 bits)
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+from tests import gpu_util as G  # noqa: E402
+
+P = pytest.importorskip("paper_2310_00036_amd")
+
+U, K, EPS = 2.0 ** -24, 128.0, 1e-5
+ACTS = {"none": 0, "relu": 1, "silu": 2}
+
+
+def _act(z, act):
+    with np.errstate(over="ignore"):
+        return {"none": z, "relu": np.maximum(z, 0), "silu": z / (1 + np.exp(-z))}[act]
+
+
+def _dact(z, act):
+    with np.errstate(over="ignore"):
+        s = 1 / (1 + np.exp(-z))
+    return {"none": np.ones_like(z), "relu": (z > 0) * 1.0, "silu": s * (1 + z * (1 - s))}[act]
+
+
+def _per_channel(stat, C):
+    """[n, G] -> [n, 1, C]"""
+    return np.repeat(stat, C // stat.shape[1], axis=1)[:, None, :]
+
+
+def _group_mean(v, groups):
+    """mean over pixels and the channels of a group: [n, HW, C] -> [n, G]"""
+    n, hw, C = v.shape
+    return v.reshape(n, hw, groups, C // groups).mean((1, 3))
+
+
+def _half(prec, v):
+    return (2.0 ** -8 if prec == G.BF16 else U) * np.abs(v)
+
+
+def _inputs(prec, n, H, W, C, seed, mean=0.5, scale=1.0):
+    rng = np.random.default_rng(seed)
+    x = G.q((rng.standard_normal((n, H * W, C)) + mean * rng.standard_normal(C)) * scale, prec)
+    dy = G.q(rng.standard_normal((n, H * W, C)), prec)
+    gamma = (1 + 0.3 * rng.standard_normal(C)).astype(np.float32).astype(np.float64)
+    beta = (0.3 * rng.standard_normal(C)).astype(np.float32).astype(np.float64)
+    return x, dy, gamma, beta
+
+
+def _stats(x, groups, eps=EPS):
+    mu = _group_mean(x, groups)
+    var = _group_mean((x - _per_channel(mu, x.shape[2])) ** 2, groups)
+    return mu, 1 / np.sqrt(var + eps)
+
+
+def _ws(fn, *dims):
+    return G.ws_bytes(fn(*dims))
+
+
+def _fwd(prec, dims, groups, x, gamma, beta, act, eps=EPS, shift=0, stats=True):
+    t = G.torch()
+    n, H, W, C = dims
+    buf = t.zeros(x.size + shift, dtype=t.bfloat16 if prec == G.BF16 else t.float32, device="cuda:0")
+    dx = buf[shift:]
+    dx.copy_(G.dev_act(x, prec).reshape(-1))
+    y = G.empty_act(x.shape, prec)
+    mean, rstd = (G.dev_f32(np.full((n, groups), 7.0)) for _ in range(2)) if stats else (None, None)
+    g, b = (None if v is None else G.dev_f32(v) for v in (gamma, beta))
+    ws = _ws(P.impala_groupnorm_fwd_workspace_bytes, prec, n, H, W, C, groups)
+    P.impala_groupnorm_fwd(prec, n, H, W, C, groups, dx, g, b, eps, ACTS[act], y, mean, rstd, ws)
+    G.sync()
+    return G.host(y), *((G.host(mean), G.host(rstd)) if stats else (None, None))
+
+
+def _check_fwd(prec, dims, groups, act, seed=1, mean=0.5, scale=1.0, affine=True, shift=0):
+    n, H, W, C = dims
+    x, _, gamma, beta = _inputs(prec, n, H, W, C, seed, mean, scale)
+    if not affine:
+        gamma = beta = None
+    y, gm, gr = _fwd(prec, dims, groups, x, gamma, beta, act, shift=shift)
+    ga, be = (np.ones(C), np.zeros(C)) if not affine else (gamma, beta)
+    mu, rstd = _stats(x, groups)
+    ax = _group_mean(np.abs(x), groups)
+    assert np.all(np.abs(gm - mu) <= 2 * K * U * (ax + 1e-30)), np.abs(gm - mu).max()
+    assert np.all(np.abs(gr - rstd) <= K * U * rstd * (1 + ax * rstd))
+    rc = _per_channel(rstd, C)
+    z = (x - _per_channel(mu, C)) * rc * ga + be
+    want = _act(z, act)
+    tol = K * U * ((np.abs(x) + _per_channel(ax, C)) * rc * np.abs(ga) + np.abs(z) + np.abs(be))
+    tol = 1.1 * tol + 8 * U * (1 + np.abs(z)) * np.abs(z) + _half(prec, want)
+    assert np.all(np.abs(y - want) <= tol), (dims, groups, act, (np.abs(y - want) - tol).max())
+
+
+def _bwd_want(x, dy, ga, be, mu, rstd, groups, act):
+    C = x.shape[2]
+    rc = _per_channel(rstd, C)
+    xh = (x - _per_channel(mu, C)) * rc
+    z = xh * ga + be
+    da = dy * _dact(z, act)
+    h = da * ga
+    m1, m2 = (_per_channel(_group_mean(v, groups), C) for v in (h, h * xh))
+    dx = rc * (h - m1 - xh * m2)
+    a1, a2 = (_per_channel(_group_mean(np.abs(v), groups), C) for v in (h, h * xh))
+    sig = np.abs(dy * ga) * (1 + np.abs(z)) if act == "silu" else 0.0
+    tol = 2 * K * U * rc * (np.abs(h) + sig / 8 + a1 + np.abs(xh) * a2)
+    return dx, (da * xh).sum((0, 1)), da.sum((0, 1)), tol, np.abs(da * xh).sum((0, 1)), np.abs(da).sum((0, 1))
+
+
+def _bwd(prec, dims, groups, x, dy, gamma, beta, mu, rstd, act, params=True, inplace=False):
+    n, H, W, C = dims
+    dx_, d_ = G.dev_act(x, prec), G.dev_act(dy, prec)
+    dx = d_ if inplace else G.empty_act(x.shape, prec)
+    dg, db = (G.dev_f32(np.full(C, 9.0)) if params else None for _ in range(2))
+    g, b = (None if v is None else G.dev_f32(v) for v in (gamma, beta))
+    ws = _ws(P.impala_groupnorm_bwd_workspace_bytes, prec, n, H, W, C, groups)
+    P.impala_groupnorm_bwd(prec, n, H, W, C, groups, d_, dx_, g, b, G.dev_f32(mu), G.dev_f32(rstd), ACTS[act], dx, dg,
+                           db, ws)
+    G.sync()
+    return G.host(dx), *((G.host(dg), G.host(db)) if params else (None, None))
+
+
+def _check_bwd(prec, dims, groups, act, seed=2, affine=True, mean=0.5):
+    n, H, W, C = dims
+    x, dy, gamma, beta = _inputs(prec, n, H, W, C, seed, mean)
+    if not affine:
+        gamma = beta = None
+    ga, be = (np.ones(C), np.zeros(C)) if not affine else (gamma, beta)
+    mu, rstd = (v.astype(np.float32).astype(np.float64) for v in _stats(x, groups))
+    dx, dg, db = _bwd(prec, dims, groups, x, dy, gamma, beta, mu, rstd, act)
+    wx, wg, wb, tol, ag, ab = _bwd_want(x, dy, ga, be, mu, rstd, groups, act)
+    assert np.all(np.abs(dx - wx) <= tol + _half(prec, wx)), (dims, groups, act)
+    sig = 2.0 if act == "silu" else 1.0
+    assert np.all(np.abs(dg - wg) <= sig * K * U * (ag + 1e-30) * (1 + mean)), np.abs(dg - wg).max()
+    assert np.all(np.abs(db - wb) <= sig * K * U * (ab + 1e-30)), np.abs(db - wb).max()
+
+
+PREC = pytest.mark.parametrize("prec", [G.BF16, G.FP32], ids=["bf16", "fp32"])
+# every size of register chunk, frames cut into chunks, ragged last rows, one pixel, columns that are no
+# power of two, one channel to a column, groups of one channel, of all, and across columns
+SHAPES = [((3, 1, 1, 16), 4), ((2, 5, 7, 16), 4), ((5, 11, 11, 32), 8), ((2, 21, 21, 64), 16), ((2, 42, 42, 16), 1),
+          ((2, 42, 41, 32), 32), ((1, 84, 84, 16), 4), ((2, 67, 83, 48), 4), ((1, 128, 128, 64), 2), ((3, 9, 9, 7), 7),
+          ((2, 13, 5, 15), 3), ((1, 33, 31, 20), 5), ((2, 6, 6, 1), 1), ((1, 3, 3, 1024), 32), ((2, 4, 5, 1000), 8),
+          ((1, 40, 40, 1021), 1), ((1, 30, 30, 96), 12), ((2, 8, 9, 24), 8), ((1, 9, 300, 40), 5), ((300, 2, 3, 16), 2)]
+
+
+@PREC
+@pytest.mark.parametrize("dims,groups", SHAPES, ids=lambda v: str(v).replace(" ", ""))
+def test_forward(prec, dims, groups):
+    for act in ACTS:
+        _check_fwd(prec, dims, groups, act)
+
+
+@PREC
+@pytest.mark.parametrize("dims,groups", SHAPES, ids=lambda v: str(v).replace(" ", ""))
+def test_backward(prec, dims, groups):
+    for act in ACTS:
+        _check_bwd(prec, dims, groups, act)
+
+
+@PREC
+def test_without_scale_and_shift(prec):
+    _check_fwd(prec, (2, 10, 9, 32), 4, "relu", affine=False)
+    _check_bwd(prec, (2, 10, 9, 32), 4, "silu", affine=False)
+
+
+@PREC
+@pytest.mark.parametrize("dims", [(2, 12, 12, 16), (1, 120, 120, 32)], ids=["whole", "chunks"])
+def test_large_mean_keeps_the_variance(prec, dims):
+    """Means of 100 and 1000 over a spread of one: a sum of squares less a squared mean would lose the spread."""
+    _check_fwd(prec, dims, 4, "none", mean=100.0)
+    if prec == G.FP32:
+        _check_fwd(prec, dims, 4, "none", mean=1000.0)
+
+
+@PREC
+def test_unaligned_address_and_statistics_left_out(prec):
+    for shift in (1, 3):
+        _check_fwd(prec, (2, 9, 9, 32), 4, "relu", shift=shift)
+    x, _, gamma, beta = _inputs(prec, 2, 9, 9, 32, 3)
+    a = _fwd(prec, (2, 9, 9, 32), 4, x, gamma, beta, "relu")[0]
+    b = _fwd(prec, (2, 9, 9, 32), 4, x, gamma, beta, "relu", stats=False)[0]
+    assert np.array_equal(a, b)
+
+
+@PREC
+@pytest.mark.parametrize("dims", [(2, 9, 9, 32), (1, 120, 120, 32)], ids=["whole", "chunks"])
+def test_in_place(prec, dims):
+    t = G.torch()
+    n, H, W, C = dims
+    x, dy, gamma, beta = _inputs(prec, n, H, W, C, 4)
+    want = _fwd(prec, dims, 4, x, gamma, beta, "silu")
+    d = G.dev_act(x, prec)
+    ws = _ws(P.impala_groupnorm_fwd_workspace_bytes, prec, n, H, W, C, 4)
+    P.impala_groupnorm_fwd(prec, n, H, W, C, 4, d, G.dev_f32(gamma), G.dev_f32(beta), EPS, 2, d, None, None, ws)
+    G.sync()
+    assert np.array_equal(G.host(d), want[0])
+    mu, rstd = _stats(x, 4)
+    a = _bwd(prec, dims, 4, x, dy, gamma, beta, mu, rstd, "silu")
+    b = _bwd(prec, dims, 4, x, dy, gamma, beta, mu, rstd, "silu", inplace=True)
+    assert all(np.array_equal(p, q) for p, q in zip(a, b))
+    c = _bwd(prec, dims, 4, x, dy, gamma, beta, mu, rstd, "silu", params=False)
+    assert np.array_equal(a[0], c[0])
+    assert t.cuda.is_available()
+
+
+def test_gradient_against_differences():
+    """Backward against central differences of the forward's formula (not of the kernel): the loss sum(dy y) in 64
+    bits, step 1e-6 on values of one, so the differences are good to 1e-8; the kernel's own bound on top."""
+    n, H, W, C, groups = 2, 3, 4, 6, 2
+    x, dy, gamma, beta = _inputs(G.FP32, n, H, W, C, 5)
+    mu, rstd = _stats(x, groups)
+
+    def loss(x, gamma, beta):
+        m, r = _stats(x, groups)
+        return (dy * _act((x - _per_channel(m, C)) * _per_channel(r, C) * gamma + beta, "silu")).sum()
+
+    dx, dg, db = _bwd(G.FP32, (n, H, W, C), groups, x, dy, gamma, beta, mu, rstd, "silu")
+    e = 1e-6
+    for got, k in ((dx, 0), (dg, 1), (db, 2)):
+        args = [x, gamma, beta]
+        for i in range(args[k].size):
+            v = []
+            for s in (e, -e):
+                a = [q.copy() for q in args]
+                a[k].reshape(-1)[i] += s
+                v.append(loss(*a))
+            want = (v[0] - v[1]) / (2 * e)
+            assert abs(got.reshape(-1)[i] - want) <= 1e-5 * (1 + abs(want)) * 3, (k, i)
+
+
+def test_relu_decision_next_to_zero():
+    """z = xh gamma + beta cancels to far less than float32's step of its terms: the decision is the 64-bit one of the
+    float32 statistics that both sides read."""
+    n, H, W, C = 1, 64, 64, 16
+    rng = np.random.default_rng(6)
+    x = rng.standard_normal((n, H * W, C)).astype(np.float32).astype(np.float64)
+    mu, rstd = np.full((1, 1), np.float32(0.1), np.float64), np.full((1, 1), np.float32(1.3), np.float64)
+    gamma = np.full(C, np.float32(0.7), np.float64)
+    beta = np.float64(np.float32(0.25)) * np.ones(C)
+    edge = (mu[0, 0] - beta[0] / (rstd[0, 0] * gamma[0]))
+    near = np.float32(edge) + np.float32(2.0 ** -27) * rng.integers(-8, 9, x.shape).astype(np.float32)
+    x[:, ::2] = near[:, ::2].astype(np.float64)
+    dy = rng.standard_normal(x.shape).astype(np.float32).astype(np.float64)
+    dx, dg, db = _bwd(G.FP32, (n, H, W, C), 1, x, dy, gamma, beta, mu, rstd, "relu")
+    wx, wg, wb, tol, ag, ab = _bwd_want(x, dy, gamma, beta, mu, rstd, 1, "relu")
+    assert np.all(np.abs(dx - wx) <= tol + U * np.abs(wx))
+    assert np.all(np.abs(db - wb) <= K * U * ab)
+
+
+@PREC
+def test_constant_input_and_non_finite_frames(prec):
+    """A constant frame has variance zero: rstd = eps^-1/2, y = act(beta). A frame with a NaN or an infinity is NaN in
+    that group only; others keep their values."""
+    n, H, W, C = 3, 6, 6, 16
+    x, _, gamma, beta = _inputs(prec, n, H, W, C, 7)
+    want = _fwd(prec, (n, H, W, C), 4, x, gamma, beta, "none")[0]
+    bad = x.copy()
+    bad[0] = 2.0
+    bad[1, 3, 5] = np.nan
+    bad[2, 0, 15] = np.inf
+    y, mean, rstd = _fwd(prec, (n, H, W, C), 4, bad, gamma, beta, "none")
+    assert np.array_equal(mean[0], np.full(4, 2.0)) and np.allclose(rstd[0], EPS ** -0.5, rtol=4 * U, atol=0)
+    assert np.all(np.abs(y[0] - beta) <= _half(prec, beta) + 2 * U * np.abs(beta))
+    assert np.isnan(y[1][:, 4:8]).all() and np.isnan(y[2][:, 12:]).all()
+    assert np.array_equal(y[1][:, :4], want[1][:, :4]) and np.array_equal(y[1][:, 8:], want[1][:, 8:])
+    assert np.array_equal(y[2][:, :12], want[2][:, :12])
+
+
+def test_no_frames():
+    t = G.torch()
+    dg, db = (G.dev_f32(np.full(16, 3.0)) for _ in range(2))
+    P.impala_groupnorm_fwd(G.BF16, 0, 4, 4, 16, 4, None, None, None, EPS, 0, None)
+    P.impala_groupnorm_bwd(G.BF16, 0, 4, 4, 16, 4, None, None, None, None, None, None, 0, None, dg, db, None)
+    G.sync()
+    assert not dg.any() and not db.any() and t.cuda.is_available()
+
+
+@pytest.mark.parametrize("dims", [(9, 11, 11, 32), (2, 100, 90, 64)], ids=["whole", "chunks"])
+def test_captured_and_replayed_on_another_stream(dims):
+    """Both passes captured into one graph and replayed on new inputs equal the eager calls, bit for bit; eager work
+    with the same workspaces runs between the replays."""
+    t = G.torch()
+    n, H, W, C = dims
+    x = t.zeros((n, H, W, C), dtype=t.bfloat16, device="cuda:0")
+    dy, y, dx = t.zeros_like(x), t.empty_like(x), t.empty_like(x)
+    gamma, beta = (G.dev_f32(v) for v in _inputs(G.BF16, *dims, 8)[2:])
+    mean, rstd = (t.empty((n, 8), device="cuda:0") for _ in range(2))
+    dg, db = (t.empty(C, device="cuda:0") for _ in range(2))
+    wf = _ws(P.impala_groupnorm_fwd_workspace_bytes, G.BF16, *dims, 8)
+    wb = _ws(P.impala_groupnorm_bwd_workspace_bytes, G.BF16, *dims, 8)
+
+    def both():
+        P.impala_groupnorm_fwd(G.BF16, *dims, 8, x, gamma, beta, EPS, 1, y, mean, rstd, wf)
+        P.impala_groupnorm_bwd(G.BF16, *dims, 8, dy, x, gamma, beta, mean, rstd, 1, dx, dg, db, wb)
+
+    s = t.cuda.Stream()
+    with t.cuda.stream(s):
+        both()
+    s.synchronize()
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        both()
+    for k in range(3):
+        x.normal_()
+        dy.normal_()
+        both()
+        G.sync()
+        want = [v.clone() for v in (y, mean, rstd, dx, dg, db)]
+        for v in (y, mean, rstd, dx, dg, db):
+            v.fill_(5)
+        G.sync()
+        graph.replay()
+        G.sync()
+        assert all(t.equal(a, b) for a, b in zip(want, (y, mean, rstd, dx, dg, db))), k
