@@ -6,7 +6,8 @@
  * Learning Platform", Algorithm 1 learning phase, Appendix A objective, Appendix B
  * hyperparameter tables): the IMPALA-ResNet forward and backward over uint8 Atari
  * frames, GAE or V-trace targets, the PPO clipped-surrogate or IMPALA policy-gradient
- * loss with value and entropy terms, global-norm gradient clipping and Adam.
+ * loss with value and entropy terms, global-norm gradient clipping and Adam (or RMSprop, or
+ * Muon's orthogonalised updates).
  *
  * Conventions shared by every call
  * --------------------------------
@@ -208,8 +209,72 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
                              float lr, float decay, float eps, float max_grad_norm, float* stats,
                              void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* Orthogonalised matrices: y = the polynomial iteration of Newton and Schulz on each x,
+ *   X_0 = x / max(||x||_F, eps),  X_k = a_k X + (b_k A + c_k A^2) X with A = X X^T,  y = X_steps,
+ * which moves every singular value towards one and keeps the singular vectors (the update of the
+ * Muon optimiser). x, y: [batch, rows, cols], row-major, in the storage type (bf16 or float32); y
+ * may be x itself, any other overlap is IMPALA_EINVAL.
+ * coeffs: HOST float [steps][3], row k = (a_k, b_k, c_k), or NULL for (3.4445, -4.7750, 2.0315) in
+ * every step. 1 <= steps <= 16. Coefficients that let a singular value of [0, 1] grow past 2^10, or
+ * the product of the steps' polynomials past 10^15, are IMPALA_EUNSUPPORTED.
+ * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included;
+ * batch * rows * cols <= 2^34.
+ * Precision: the products run on f16 matrix cores, each operand as the sum of two f16 numbers, with
+ * float32 accumulation; ||x|| is a 64-bit sum. IMPALA_PREC_FP32 results differ from the exact ones
+ * by about what a float32 evaluation does; IMPALA_PREC_BF16 results by about their own rounding. A
+ * zero matrix gives zeros; one with an element that is not finite gives NaN in all of its own.
+ * ws: device scratch of muon_orthogonalize_workspace_bytes() bytes. */
+size_t muon_orthogonalize_workspace_bytes(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
+                                          int32_t steps);
+impala_status_t muon_orthogonalize(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
+                                   const void* x, int32_t steps, const float* coeffs, float eps, void* y,
+                                   void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* A matrix of a flat float32 buffer: rows x cols, row-major, from float `offset` on. A dense layer's
+ * weights are [in, out]; a conv kernel's HWIO [3,3,cin,cout] are a (9 cin) x cout matrix. */
+typedef struct muon_matrix {
+    int64_t offset;
+    int32_t rows, cols;
+} muon_matrix_t;
+
+typedef enum {
+    MUON_SCALE_SPECTRAL = 0,  /* sqrt(max(1, cols / rows)) */
+    MUON_SCALE_RMS = 1        /* 0.2 sqrt(max(rows, cols)): entries the size of Adam's */
+} muon_scale_t;
+
+typedef struct muon_cfg {
+    float lr, momentum, weight_decay;
+    int32_t nesterov;         /* 0 or 1 */
+    int32_t steps;            /* Newton-Schulz steps, 1 .. 16 */
+    int32_t scale;            /* muon_scale_t */
+    float eps;                /* of muon_orthogonalize */
+    float adam_lr, beta1, beta2, adam_eps;   /* what no matrix covers */
+    float max_grad_norm;      /* <= 0: no clipping */
+    const float* coeffs;      /* HOST, of muon_orthogonalize, or NULL */
+} muon_cfg_t;
+
+/* Global-norm clip over all of grads (as adam_step), then for each matrix
+ *   m <- momentum m + (1 - momentum) g;  u = momentum m + (1 - momentum) g if nesterov, else m;
+ *   p <- p (1 - lr weight_decay) - lr scale O(u),  O as muon_orthogonalize in float32,
+ * and one Adam step (step 1-based, adam_lr, no weight decay) on every parameter that no matrix
+ * covers. params, m, v are updated in place; v is left alone inside the matrices; grads is read
+ * only. mats: HOST array of n_mats matrices in any order, disjoint, inside the buffer; at most 512,
+ * sides as muon_orthogonalize. cfg is HOST memory and, like mats, not kept after the call returns.
+ * stats as adam_step. ws: device scratch of muon_workspace_bytes() bytes. */
+size_t muon_workspace_bytes(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
+                            const muon_cfg_t* cfg);
+impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
+                          const muon_cfg_t* cfg, float* params, const float* grads, float* m, float* v,
+                          int32_t step, float* stats, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The matrices of a net's parameter buffer that learner_step orthogonalises with
+ * LEARNER_OPT_MUON: the 15 conv kernels and the dense layer's weights (the two heads and the biases
+ * are left to Adam). Writes at most `cap` into out (host) and returns their number, 16, or a
+ * negative status. */
+int muon_net_matrices(const impala_net_t* net, muon_matrix_t* out, int cap);
+
 typedef enum { LEARNER_PPO = 0, LEARNER_IMPALA = 1 } learner_algo_t;
-typedef enum { LEARNER_OPT_ADAM = 0, LEARNER_OPT_RMSPROP = 1 } learner_opt_t;
+typedef enum { LEARNER_OPT_ADAM = 0, LEARNER_OPT_RMSPROP = 1, LEARNER_OPT_MUON = 2 } learner_opt_t;
 
 /* One learning phase's hyperparameters (Appendix A nomenclature; Appendix B values). */
 typedef struct learner_cfg {
@@ -227,9 +292,13 @@ typedef struct learner_cfg {
     float rho_bar, c_bar, pg_rho_bar; /* IMPALA importance-weight clips */
     float lr, beta1, beta2, adam_eps;
     float max_grad_norm;      /* omega; <= 0 disables clipping */
-    int32_t optimizer;        /* learner_opt_t: Adam (Appendix B's PPO table) or RMSprop (its
-                                 IMPALA table) */
+    int32_t optimizer;        /* learner_opt_t: Adam (Appendix B's PPO table), RMSprop (its IMPALA
+                                 table), or muon_step on muon_net_matrices with lr, beta1, beta2,
+                                 adam_eps for the rest */
     float rms_decay, rms_eps; /* RMSprop (Appendix B: 0.99, 0.01) */
+    /* read with LEARNER_OPT_MUON only; muon_eps and the default coefficients as muon_cfg_t */
+    float muon_lr, muon_momentum, muon_weight_decay, muon_eps;
+    int32_t muon_nesterov, muon_steps, muon_scale;
 } learner_cfg_t;
 
 /* The rollout one learning phase consumes (Algorithm 1's D plus the bootstrap state). */
@@ -255,7 +324,7 @@ size_t learner_workspace_bytes(const impala_net_t* net, const learner_cfg_t* cfg
  * rollout frames and E/N bootstrap frames, target log-probs, V-trace, loss over the rollout
  * rows, backward (bootstrap rows get no gradient), clip, optimiser step.
  * params, m, v: float [param_count], updated in place (RMSprop: v holds its nu, m is unused and
- * may be NULL). step: HOST int32, 1-based count of
+ * may be NULL; Muon: as muon_step). step: HOST int32, 1-based count of
  * updates done so far (incremented). perm: int32 [update_epochs, T*E] (PPO; NULL for IMPALA),
  * every entry in [0, T*E) (not checked: it indexes the frames and the rollout arrays on the
  * device; each row of perm is normally a permutation).

@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(HERE, "libcleanba_learner.so")
 
 PREC_BF16, PREC_FP32 = 0, 1
 LEARNER_PPO, LEARNER_IMPALA = 0, 1
-LEARNER_OPT_ADAM, LEARNER_OPT_RMSPROP = 0, 1
+LEARNER_OPT_ADAM, LEARNER_OPT_RMSPROP, LEARNER_OPT_MUON = 0, 1, 2
+MUON_SCALE_SPECTRAL, MUON_SCALE_RMS = 0, 1
 X_PLAIN, X_RELU, X_U8 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 STATUS = {0: "OK", -1: "EINVAL", -2: "EWORKSPACE", -3: "EUNSUPPORTED", -4: "EHIP"}
@@ -48,7 +49,21 @@ class LearnerCfg(C.Structure):
                 ("rho_bar", C.c_float), ("c_bar", C.c_float), ("pg_rho_bar", C.c_float),
                 ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
                 ("adam_eps", C.c_float), ("max_grad_norm", C.c_float),
-                ("optimizer", C.c_int32), ("rms_decay", C.c_float), ("rms_eps", C.c_float)]
+                ("optimizer", C.c_int32), ("rms_decay", C.c_float), ("rms_eps", C.c_float),
+                ("muon_lr", C.c_float), ("muon_momentum", C.c_float), ("muon_weight_decay", C.c_float),
+                ("muon_eps", C.c_float), ("muon_nesterov", C.c_int32), ("muon_steps", C.c_int32),
+                ("muon_scale", C.c_int32)]
+
+
+class MuonMatrix(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
+class MuonCfg(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32),
+                ("steps", C.c_int32), ("scale", C.c_int32), ("eps", C.c_float), ("adam_lr", C.c_float),
+                ("beta1", C.c_float), ("beta2", C.c_float), ("adam_eps", C.c_float), ("max_grad_norm", C.c_float),
+                ("coeffs", C.POINTER(C.c_float))]
 
 
 class Rollout(C.Structure):
@@ -78,6 +93,12 @@ _SIGS = {
     "adam_step_noalloc": (C.c_int, [_I64, _P, _P, _P, _P, _I32, _F, _F, _F, _F, _F, _P, _P]),
     "rmsprop_workspace_bytes": (_SZ, [_I64]),
     "rmsprop_step": (C.c_int, [_I64, _P, _P, _P, _F, _F, _F, _F, _P, _P, _SZ, _P]),
+    "muon_orthogonalize_workspace_bytes": (_SZ, [C.c_int, _I64, _I32, _I32, _I32]),
+    "muon_orthogonalize": (C.c_int, [C.c_int, _I64, _I32, _I32, _P, _I32, C.POINTER(_F), _F, _P, _P, _SZ, _P]),
+    "muon_workspace_bytes": (_SZ, [_I64, C.POINTER(MuonMatrix), _I32, C.POINTER(MuonCfg)]),
+    "muon_step": (C.c_int, [_I64, C.POINTER(MuonMatrix), _I32, C.POINTER(MuonCfg), _P, _P, _P, _P, _I32, _P, _P, _SZ,
+                            _P]),
+    "muon_net_matrices": (C.c_int, [_NETP, C.POINTER(MuonMatrix), C.c_int]),
     "learner_workspace_bytes": (_SZ, [_NETP, C.POINTER(LearnerCfg)]),
     "learner_step": (C.c_int, [_NETP, C.POINTER(LearnerCfg), C.POINTER(Rollout), _P, _P, _P,
                                C.POINTER(_I32), _P, _P, _SZ, _P, _P]),
@@ -287,6 +308,62 @@ def rmsprop_step(n_params, params, grads, nu, lr, decay, eps, max_grad_norm, sta
         ws.numel() * ws.element_size(), stream_handle(stream)))
 
 
+def _coeff_array(steps: int, coeffs):
+    """A host float array [steps][3] from a sequence of (a, b, c), or None."""
+    if coeffs is None:
+        return None
+    flat = [float(v) for row in coeffs for v in row]
+    if len(flat) != 3 * steps:
+        raise ValueError(f"coeffs must have {steps} rows of three")
+    return (C.c_float * len(flat))(*flat)
+
+
+def muon_orthogonalize_workspace_bytes(prec, batch, rows, cols, steps=5) -> int:
+    return int(lib.muon_orthogonalize_workspace_bytes(prec, batch, rows, cols, steps))
+
+
+def muon_orthogonalize(prec, batch, rows, cols, x, y, ws, steps=5, coeffs=None, eps=1e-7, stream=None):
+    _check("muon_orthogonalize", lib.muon_orthogonalize(
+        prec, batch, rows, cols, ptr(x), steps, _coeff_array(steps, coeffs), eps, ptr(y), *_ws_args(ws),
+        stream_handle(stream)))
+
+
+def muon_matrices(mats):
+    """The host array that muon_step takes, from a sequence of (offset, rows, cols)."""
+    mats = list(mats)
+    return (MuonMatrix * len(mats))(*(MuonMatrix(*m) for m in mats))
+
+
+def muon_net_matrices(net):
+    """The matrices of a net's parameters that learner_step orthogonalises, for muon_step."""
+    out = (MuonMatrix * 16)()
+    k = lib.muon_net_matrices(C.byref(net_struct(net)), out, 16)
+    if k < 0:
+        raise LibraryError("muon_net_matrices", k)
+    return out
+
+
+def muon_cfg(lr, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, scale=MUON_SCALE_SPECTRAL, eps=1e-7,
+             adam_lr=2.5e-4, beta1=0.9, beta2=0.999, adam_eps=1e-5, max_grad_norm=0.0, coeffs=None) -> MuonCfg:
+    c = MuonCfg(lr, momentum, weight_decay, int(nesterov), steps, scale, eps, adam_lr, beta1, beta2, adam_eps,
+                max_grad_norm)
+    rows = _coeff_array(steps, coeffs)
+    if rows is not None:
+        c.coeffs = C.cast(rows, C.POINTER(C.c_float))   # the structure keeps the array alive
+    return c
+
+
+def muon_workspace_bytes(n_params, mats, cfg: MuonCfg) -> int:
+    return int(lib.muon_workspace_bytes(n_params, mats, len(mats), C.byref(cfg)))
+
+
+def muon_step(n_params, mats, cfg: MuonCfg, params, grads, m, v, step, stats, ws, stream=None):
+    """mats: muon_matrices(...) or muon_net_matrices(net)."""
+    _check("muon_step", lib.muon_step(
+        n_params, mats, len(mats), C.byref(cfg), ptr(params), ptr(grads), ptr(m), ptr(v), step, ptr(stats),
+        *_ws_args(ws), stream_handle(stream)))
+
+
 def learner_cfg(wl, prec: int) -> LearnerCfg:
     """LearnerCfg from a workload description (synth.Workload or anything alike)."""
     c = LearnerCfg()
@@ -300,8 +377,13 @@ def learner_cfg(wl, prec: int) -> LearnerCfg:
     c.rho_bar, c.c_bar, c.pg_rho_bar = wl.rho_bar, wl.c_bar, wl.pg_rho_bar
     c.lr, c.beta1, c.beta2, c.adam_eps = wl.lr, wl.beta1, wl.beta2, wl.adam_eps
     c.max_grad_norm = wl.max_grad_norm
-    c.optimizer = LEARNER_OPT_RMSPROP if getattr(wl, "optimizer", "adam") == "rmsprop" else LEARNER_OPT_ADAM
+    c.optimizer = {"adam": LEARNER_OPT_ADAM, "rmsprop": LEARNER_OPT_RMSPROP,
+                   "muon": LEARNER_OPT_MUON}[getattr(wl, "optimizer", "adam")]
     c.rms_decay, c.rms_eps = getattr(wl, "rms_decay", 0.99), getattr(wl, "rms_eps", 0.01)
+    c.muon_lr, c.muon_momentum = getattr(wl, "muon_lr", 0.02), getattr(wl, "muon_momentum", 0.95)
+    c.muon_weight_decay, c.muon_eps = getattr(wl, "muon_weight_decay", 0.0), getattr(wl, "muon_eps", 1e-7)
+    c.muon_nesterov, c.muon_steps = int(getattr(wl, "muon_nesterov", True)), getattr(wl, "muon_steps", 5)
+    c.muon_scale = getattr(wl, "muon_scale", MUON_SCALE_SPECTRAL)
     return c
 
 

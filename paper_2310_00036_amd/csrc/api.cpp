@@ -1,5 +1,6 @@
 // C-ABI of the learner-update library: argument validation on the host (before any HIP
 // call), workspace planning, and the learning-phase orchestration of Algorithm 1.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -45,6 +46,12 @@ impala_status_t hip_status(hipError_t e, const char* where) {
 
 bool valid_prec(int p) { return p == IMPALA_PREC_BF16 || p == IMPALA_PREC_FP32; }
 
+// Whether the byte ranges [a, a + bytes) and [b, b + bytes) overlap without being the same.
+bool partial_overlap(const void* a, const void* b, size_t bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x != y && x < y + bytes && y < x + bytes;
+}
+
 // Learner workspace layout (bytes from the start of ws).
 struct LearnerLayout {
     NetPlan plan;
@@ -52,11 +59,83 @@ struct LearnerLayout {
     size_t rows, gact, gmu, grew, gdone, gnd;   // IMPALA minibatch gathers (more than one)
     size_t lossws;                               // the loss kernels' statistics and row terms
     size_t advms;                                // PPO: every update's advantage mean / std
+    size_t muon;                                 // Muon: the step's workspace
     size_t total;
     int64_t fwd_rows, mb;
 };
 
 size_t a256(size_t x) { return (x + 255) / 256 * 256; }
+
+// ---- the Muon step's arguments
+
+constexpr int64_t kMuonMaxSize = int64_t(1) << 28;   // elements of one matrix
+constexpr int kMuonMaxSide = 16384, kMuonMaxMats = 512, kMuonMaxSteps = 16;
+
+bool muon_shape_ok(int64_t rows, int64_t cols) {
+    return rows >= 1 && cols >= 1 && rows * cols <= kMuonMaxSize && std::min(rows, cols) <= kMuonMaxSide;
+}
+
+muon_cfg_t muon_of(const learner_cfg_t& c) {
+    muon_cfg_t m{};
+    m.lr = c.muon_lr; m.momentum = c.muon_momentum; m.weight_decay = c.muon_weight_decay; m.eps = c.muon_eps;
+    m.nesterov = c.muon_nesterov; m.steps = c.muon_steps; m.scale = c.muon_scale;
+    m.adam_lr = c.lr; m.beta1 = c.beta1; m.beta2 = c.beta2; m.adam_eps = c.adam_eps;
+    m.max_grad_norm = c.max_grad_norm;
+    return m;
+}
+
+std::string check_muon(const muon_cfg_t& c) {
+    if (!(c.lr >= 0.f) || !(c.momentum >= 0.f && c.momentum < 1.f) || !(c.weight_decay >= 0.f) || !(c.eps >= 0.f))
+        return "Muon hyperparameters out of range";
+    if (c.nesterov != 0 && c.nesterov != 1) return "Muon's nesterov must be 0 or 1";
+    if (c.steps < 1 || c.steps > kMuonMaxSteps) return "Muon needs 1 to 16 Newton-Schulz steps";
+    if (c.scale != MUON_SCALE_SPECTRAL && c.scale != MUON_SCALE_RMS) return "Muon's scale must be SPECTRAL or RMS";
+    if (!(c.adam_lr >= 0.f) || !(c.adam_eps >= 0.f) || !(c.beta1 >= 0.f && c.beta1 < 1.f) ||
+        !(c.beta2 >= 0.f && c.beta2 < 1.f))
+        return "Muon's Adam hyperparameters out of range";
+    return "";
+}
+
+// The matrices sorted by offset; an error text where they are not valid.
+std::string muon_mats(int64_t n_params, const muon_matrix_t* mats, int n_mats, std::vector<MuonMat>& out) {
+    if (n_mats < 0 || n_mats > kMuonMaxMats) return "between 0 and 512 matrices";
+    if (n_mats > 0 && !mats) return "mats is NULL";
+    out.clear();
+    for (int i = 0; i < n_mats; ++i) {
+        const muon_matrix_t& m = mats[i];
+        if (!muon_shape_ok(m.rows, m.cols)) return "matrix " + std::to_string(i) + " has unsupported sides";
+        if (m.offset < 0 || m.offset > n_params || int64_t(m.rows) * m.cols > n_params - m.offset)
+            return "matrix " + std::to_string(i) + " lies outside the buffer";
+        out.push_back({m.offset, m.rows, m.cols});
+    }
+    std::sort(out.begin(), out.end(), [](const MuonMat& a, const MuonMat& b) { return a.offset < b.offset; });
+    for (size_t i = 1; i < out.size(); ++i)
+        if (out[i - 1].offset + int64_t(out[i - 1].rows) * out[i - 1].cols > out[i].offset) return "matrices overlap";
+    return "";
+}
+
+std::vector<MuonMat> net_mats(const ParamOffsets& po, const impala_net_t& net) {
+    std::vector<MuonMat> v;
+    int cin = net.in_c;
+    for (int s = 0; s < 3; ++s) {
+        for (int k = 0; k < 5; ++k) v.push_back({po.conv_w[s][k], 9 * (k == 0 ? cin : net.ch[s]), net.ch[s]});
+        cin = net.ch[s];
+    }
+    v.push_back({po.dense_w, int((po.dense_b - po.dense_w) / net.hidden), net.hidden});
+    return v;
+}
+
+MuonStep muon_step_of(const muon_cfg_t& c, const OptArgs& adam, float* stats) {
+    MuonStep m{};
+    m.n = adam.n; m.adam = adam;
+    m.lr = c.lr; m.decay = float(1.0 - double(c.lr) * c.weight_decay);
+    // 1 - momentum from the decimal that the float stands for would be another number; the float's own
+    // complement is exact in double
+    m.momentum = c.momentum; m.omu = float(1.0 - double(c.momentum));
+    m.nesterov = c.nesterov; m.steps = c.steps; m.scale_mode = c.scale; m.eps = c.eps; m.coeffs = c.coeffs;
+    m.stats = stats;
+    return m;
+}
 
 std::string check_cfg(const learner_cfg_t* c) {
     if (!c) return "cfg is NULL";
@@ -73,10 +152,14 @@ std::string check_cfg(const learner_cfg_t* c) {
         if (c->num_minibatches < 1 || c->E % c->num_minibatches)
             return "IMPALA needs num_minibatches >= 1 dividing E (minibatches are env blocks)";
     }
-    if (c->optimizer != LEARNER_OPT_ADAM && c->optimizer != LEARNER_OPT_RMSPROP)
-        return "cfg.optimizer must be ADAM or RMSPROP";
+    if (c->optimizer != LEARNER_OPT_ADAM && c->optimizer != LEARNER_OPT_RMSPROP && c->optimizer != LEARNER_OPT_MUON)
+        return "cfg.optimizer must be ADAM, RMSPROP or MUON";
     if (!(c->lr >= 0.f)) return "cfg.lr must be >= 0";
-    if (c->optimizer == LEARNER_OPT_ADAM &&
+    if (c->optimizer == LEARNER_OPT_MUON) {
+        const std::string e = check_muon(muon_of(*c));
+        if (!e.empty()) return e;
+    }
+    if (c->optimizer != LEARNER_OPT_RMSPROP &&
         (!(c->adam_eps >= 0.f) || !(c->beta1 >= 0.f && c->beta1 < 1.f) || !(c->beta2 >= 0.f && c->beta2 < 1.f)))
         return "cfg Adam hyperparameters out of range";
     if (c->optimizer == LEARNER_OPT_RMSPROP && (!(c->rms_eps >= 0.f) || !(c->rms_decay >= 0.f && c->rms_decay < 1.f)))
@@ -114,6 +197,8 @@ LearnerLayout learner_layout(const impala_net_t& net, const learner_cfg_t& c) {
     L.gnd = take(gather ? size_t(Eb) : 0);
     L.lossws = take(loss_ws_bytes(L.mb));
     L.advms = take(c.algo == LEARNER_PPO ? size_t(2) * c.update_epochs * c.num_minibatches * sizeof(float) : 0);
+    L.muon = take(c.optimizer == LEARNER_OPT_MUON
+                      ? muon_step_ws_bytes(L.plan.po.total, net_mats(L.plan.po, net), c.muon_steps) : 0);
     L.total = off;
     return L;
 }
@@ -473,6 +558,92 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
     return hip_status(clip_opt_step(OPT_RMSPROP, a, stats, static_cast<float*>(ws), stream), "rmsprop_step");
 }
 
+static std::string check_orth(int prec, int64_t batch, int rows, int cols, int steps) {
+    if (!valid_prec(prec)) return "bad prec";
+    if (batch < 0 || rows < 1 || cols < 1) return "batch >= 0 and sides >= 1";
+    if (steps < 1 || steps > kMuonMaxSteps) return "steps must be in [1, 16]";
+    return "";
+}
+static bool orth_supported(int64_t batch, int rows, int cols) {
+    return muon_shape_ok(rows, cols) && batch <= (int64_t(1) << 24) && batch * rows * cols <= (int64_t(1) << 34);
+}
+
+size_t muon_orthogonalize_workspace_bytes(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
+                                          int32_t steps) {
+    const std::string e = check_orth(prec, batch, rows, cols, steps);
+    if (!e.empty()) { fail(IMPALA_EINVAL, "muon_orthogonalize_workspace_bytes: %s", e.c_str()); return 0; }
+    if (!orth_supported(batch, rows, cols)) {
+        fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize_workspace_bytes: too large");
+        return 0;
+    }
+    ok();
+    return muon_orth_ws_bytes(prec, batch > 0 ? batch : 1, rows, cols, steps);
+}
+
+impala_status_t muon_orthogonalize(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
+                                   const void* x, int32_t steps, const float* coeffs, float eps, void* y,
+                                   void* ws, size_t ws_bytes, hipStream_t stream) {
+    const std::string e = check_orth(prec, batch, rows, cols, steps);
+    if (!e.empty()) return fail(IMPALA_EINVAL, "muon_orthogonalize: %s", e.c_str());
+    if (!(eps >= 0.f)) return fail(IMPALA_EINVAL, "muon_orthogonalize: eps must be >= 0");
+    if (!orth_supported(batch, rows, cols)) return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: too large");
+    if (!muon_coeffs_ok(steps, coeffs))
+        return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: the coefficients let singular values grow without bound");
+    if (batch == 0) return ok();
+    CHECK_PTR(x); CHECK_PTR(y); CHECK_PTR(ws);
+    if (partial_overlap(x, y, size_t(batch) * rows * cols * (prec == IMPALA_PREC_BF16 ? 2 : 4)))
+        return fail(IMPALA_EINVAL, "muon_orthogonalize: x and y overlap");
+    const size_t need = muon_orth_ws_bytes(prec, batch, rows, cols, steps);
+    if (ws_bytes < need)
+        return fail(IMPALA_EWORKSPACE, "muon_orthogonalize: workspace %zu < %zu bytes", ws_bytes, need);
+    return hip_status(muon_orth(prec, batch, rows, cols, x, steps, coeffs, eps, y, ws, stream), "muon_orthogonalize");
+}
+
+static std::string check_muon_call(int64_t n_params, const muon_matrix_t* mats, int n_mats, const muon_cfg_t* cfg,
+                                   std::vector<MuonMat>& out) {
+    if (!cfg) return "cfg is NULL";
+    if (n_params < 0) return "n_params must be >= 0";
+    const std::string e = check_muon(*cfg);
+    return e.empty() ? muon_mats(n_params, mats, n_mats, out) : e;
+}
+
+size_t muon_workspace_bytes(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
+                            const muon_cfg_t* cfg) {
+    std::vector<MuonMat> v;
+    const std::string e = check_muon_call(n_params, mats, n_mats, cfg, v);
+    if (!e.empty()) { fail(IMPALA_EINVAL, "muon_workspace_bytes: %s", e.c_str()); return 0; }
+    ok();
+    return muon_step_ws_bytes(n_params, v, cfg->steps);
+}
+
+impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
+                          const muon_cfg_t* cfg, float* params, const float* grads, float* m, float* v,
+                          int32_t step, float* stats, void* ws, size_t ws_bytes, hipStream_t stream) {
+    std::vector<MuonMat> mv;
+    const std::string e = check_muon_call(n_params, mats, n_mats, cfg, mv);
+    if (!e.empty()) return fail(IMPALA_EINVAL, "muon_step: %s", e.c_str());
+    if (step < 1) return fail(IMPALA_EINVAL, "muon_step: step is 1-based (got %d)", step);
+    if (!muon_coeffs_ok(cfg->steps, cfg->coeffs))
+        return fail(IMPALA_EUNSUPPORTED, "muon_step: the coefficients let singular values grow without bound");
+    if (n_params == 0) return ok();
+    CHECK_PTR(params); CHECK_PTR(grads); CHECK_PTR(m); CHECK_PTR(v); CHECK_PTR(ws);
+    const size_t need = muon_step_ws_bytes(n_params, mv, cfg->steps);
+    if (ws_bytes < need) return fail(IMPALA_EWORKSPACE, "muon_step: workspace %zu < %zu bytes", ws_bytes, need);
+    const OptArgs oa = adam_args(n_params, params, grads, m, v, step, cfg->adam_lr, cfg->beta1, cfg->beta2,
+                                 cfg->adam_eps, cfg->max_grad_norm);
+    return hip_status(muon_update(muon_step_of(*cfg, oa, stats), mv, ws, stream), "muon_step");
+}
+
+int muon_net_matrices(const impala_net_t* net, muon_matrix_t* out, int cap) {
+    const std::string e = check_net(net);
+    if (!e.empty()) return fail(IMPALA_EINVAL, "muon_net_matrices: %s", e.c_str());
+    if (!out && cap > 0) return fail(IMPALA_EINVAL, "muon_net_matrices: out is NULL");
+    const std::vector<MuonMat> v = net_mats(param_offsets(*net), *net);
+    for (size_t i = 0; i < v.size() && int(i) < cap; ++i) out[i] = muon_matrix_t{v[i].offset, v[i].rows, v[i].cols};
+    ok();
+    return int(v.size());
+}
+
 size_t learner_workspace_bytes(const impala_net_t* net, const learner_cfg_t* cfg) {
     std::string e = check_net(net);
     if (e.empty()) e = check_cfg(cfg);
@@ -490,7 +661,7 @@ impala_status_t learner_step(const impala_net_t* net, const learner_cfg_t* cfg,
     if (!e.empty()) return fail(IMPALA_EINVAL, "learner_step: %s", e.c_str());
     CHECK_PTR(ro); CHECK_PTR(params); CHECK_PTR(v); CHECK_PTR(step); CHECK_PTR(ws);
     CHECK_PTR(stats);
-    if (cfg->optimizer == LEARNER_OPT_ADAM) CHECK_PTR(m);
+    if (cfg->optimizer != LEARNER_OPT_RMSPROP) CHECK_PTR(m);
     CHECK_PTR(ro->obs); CHECK_PTR(ro->actions); CHECK_PTR(ro->behav_logp); CHECK_PTR(ro->rewards);
     CHECK_PTR(ro->dones); CHECK_PTR(ro->next_done);
     if (*step < 0) return fail(IMPALA_EINVAL, "learner_step: *step must be >= 0");
@@ -521,7 +692,7 @@ impala_status_t learner_step(const impala_net_t* net, const learner_cfg_t* cfg,
     // first forward of the call casts them
     bool dense_ready = false;
     auto opt_step = [&](float* st) {
-        OptArgs oa = c.optimizer == LEARNER_OPT_ADAM
+        OptArgs oa = c.optimizer != LEARNER_OPT_RMSPROP
                          ? adam_args(P.po.total, params, grads, m, v, *step, c.lr, c.beta1, c.beta2, c.adam_eps,
                                      c.max_grad_norm)
                          : rmsprop_args(P.po.total, params, grads, v, c.lr, c.rms_decay, c.rms_eps, c.max_grad_norm);
@@ -530,8 +701,10 @@ impala_status_t learner_step(const impala_net_t* net, const learner_cfg_t* cfg,
             oa.mir_off = P.po.dense_w;
             oa.mir_len = int64_t(P.flat) * P.hidden;
         }
-        const hipError_t e = clip_opt_step(c.optimizer == LEARNER_OPT_ADAM ? OPT_ADAM : OPT_RMSPROP, oa, st, apart,
-                                           stream);
+        const hipError_t e =
+            c.optimizer == LEARNER_OPT_MUON
+                ? muon_update(muon_step_of(muon_of(c), oa, st), net_mats(P.po, *net), w + L.muon, stream)
+                : clip_opt_step(c.optimizer == LEARNER_OPT_ADAM ? OPT_ADAM : OPT_RMSPROP, oa, st, apart, stream);
         dense_ready = e == hipSuccess && P.prec == BF16;
         return e;
     };
@@ -835,12 +1008,6 @@ static impala_status_t check_groupnorm(const char* fn, int prec, int64_t n, int 
     if (groupnorm_blocks(prec, n, H, W, C, G) > (int64_t(1) << 31) - 1)
         return fail(IMPALA_EUNSUPPORTED, "%s: too many elements for one call", fn);
     return IMPALA_OK;
-}
-
-// Whether the byte ranges [a, a + bytes) and [b, b + bytes) overlap without being the same.
-static bool partial_overlap(const void* a, const void* b, size_t bytes) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x != y && x < y + bytes && y < x + bytes;
 }
 
 size_t impala_groupnorm_fwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,

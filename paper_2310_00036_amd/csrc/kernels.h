@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <vector>
+
 #include "prof.h"
 
 namespace cb {
@@ -302,6 +304,28 @@ struct OptArgs {
 };
 // Global-norm clip then one optimiser step; stats [2] = [pre-clip norm, nonfinite] or NULL.
 hipError_t clip_opt_step(int opt, const OptArgs& a, float* stats, float* partial, hipStream_t s);
+
+// ---- orthogonalised updates (Newton-Schulz products) and the Muon step
+// steps in [1, 16]; coeffs: host [steps][3] or NULL (the default quintic in every step)
+bool muon_coeffs_ok(int steps, const float* coeffs);   // singular values stay bounded
+size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps);
+hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,
+                     float eps, void* y, void* ws, hipStream_t s);
+struct MuonMat { int64_t offset; int rows, cols; };   // a matrix of the flat buffer
+struct MuonStep {
+    int64_t n;
+    OptArgs adam;             // buffers, the clip, Adam's constants for what no matrix covers, the mirror
+    float lr, decay;          // p <- decay p - lr scale O
+    float momentum, omu;      // momentum, 1 - momentum (formed in double)
+    int nesterov, steps, scale_mode;
+    float eps;
+    const float* coeffs;
+    float* stats;
+};
+size_t muon_step_ws_bytes(int64_t n_params, const std::vector<MuonMat>& mats, int steps);
+// mats sorted by offset, disjoint.
+hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void* ws, hipStream_t s);
+
 // Largest dynamic LDS allocation per workgroup on the current device (bytes).
 size_t lds_limit();
 // Compute units of the current device.

@@ -1,0 +1,47 @@
+// Internal interface of the orthogonalised updates (muon.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace cb {
+
+constexpr int kNsGroups = 8;       // shapes per pass
+constexpr int kNsMats = 64;        // matrices with offsets of their own per pass
+constexpr int kNsMaxSteps = 16;
+
+// Matrices of one shape. rp x cp: the shape padded to whole tiles; m <= n the sides, mp and np padded.
+struct NsGroup {
+    int rows, cols, rp, cp, m, n, mp, np, tall;   // tall: rows > cols
+    int batch, first;                 // first: index of its first matrix in the call
+    int bt, tiles, splits, kchunk;    // tile, tiles of a symmetric m x m product, the Gram product's k split
+    int table, nsum, part0;           // 1 + its first offset in NsArgs::off (0: b * rows * cols); its blocks of the sums
+    float scale;                      // the update's factor (muon_step)
+    int64_t x[2], part, a, t, p, q[2];   // workspace byte offsets of the first matrix
+    int64_t xs, ms, ps;                  // bytes of one X plane, one m x m plane, one matrix's partials
+};
+
+struct NsArgs {
+    NsGroup g[kNsGroups];
+    int64_t off[kNsMats];             // element offsets of matrices with a table
+    int ng;
+    int start[kNsGroups + 1];         // workgroups of this launch by group
+    char* ws;
+    int64_t info, sums;               // workspace byte offsets: two floats a matrix; 3 doubles a block of the sums
+};
+
+struct MuonElem {                     // the elementwise part of muon_step
+    int64_t n_params;
+    float* p; const float* g; float* m; float* v;
+    float mu, omu, c1, c2;            // momentum, 1 - momentum; u = c1 s g + c2 m
+    int nesterov;
+    float b1, b2, omb1, omb2, bc1, bc2, alr, aeps;   // Adam for the rest
+    float max_norm, eps;
+    float* stats;
+    uint16_t* mir; int64_t mir_off, mir_len;
+    int nblocks;                      // blocks of the sums in the whole call
+    int64_t gap[kNsMats + 1], gap_len[kNsMats + 1];   // what no matrix covers
+    int ngaps, gap_start[kNsMats + 2];
+};
+
+}  // namespace cb

@@ -1,0 +1,1164 @@
+// Orthogonalised updates: Newton-Schulz products on gfx950 matrix cores, and the Muon step over the
+// flat parameter buffer that they serve.
+//
+// One Newton-Schulz step is X <- (a I + b A + c A^2) X with A = X X^T on the smaller side m <= n. The
+// factors of all steps are polynomials of the first Gram matrix, so a segment of L steps needs X twice:
+//   A = X X^T;  per step  P = a I + b A + c A^2,  Q <- P Q,  A <- P A P;  then X <- Q X,
+// 3 m^2 n + (4 L - 3) m^3 operations with the symmetric products computed by halves, against
+// L (3 m^2 n + m^3) for the steps one by one. What bounds L is rounding: A squares the singular values
+// and P A P grows what is small by a^2 a step, the rounding of A along with it. A's error is 2^-24 of
+// its norm, so a segment has at most kSeg = 3 steps, the next one starting from a fresh Gram matrix: two
+// segments of 3 and 2 steps come as near the exact result as the steps one by one in float32 do, where
+// one segment of 5 is off by 2^-7 for singular values spread over six decades (more than bf16 resolves).
+//
+// Every matrix is held as two f16 planes, v = hi + lo with lo = f16(v - hi): 22 bits and more under a
+// power-of-two scale that keeps values in f16's normal range (at least 2^-40 of a matrix's bound is
+// resolved). A product is hi hi + hi lo + lo hi in f16 MFMAs with float32 accumulation, at a third of
+// the f16 rate, where float32 MFMAs run at a sixteenth. bf16 inputs are exact in one plane (their 8
+// bits under a power-of-two scale), so they need one product in the Gram matrix and two with Q.
+// Sums of squares, norms and the clip are 64 bits.
+//
+// Launches of a pass: sums of squares; planes of X (for muon_step with the momentum update and Adam
+// for the rest); and per segment the Gram product (split over k), its sum, the m x m products, and
+// Q X, whose last form writes the result or the updated parameters. Matrices of up to 64 on the
+// smaller side have their whole m x m part in one workgroup's LDS, in float32, inside the launch that
+// sums the others' Gram partials. All matrices of a call go through the same launches.
+#include "common.h"
+#include "kernels.h"
+#include "muon.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+namespace cb {
+
+namespace {
+
+constexpr int kSeg = 3;
+
+typedef _Float16 ns_f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 ns_f16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t ns_u32x4 __attribute__((ext_vector_type(4)));
+
+CB_DEV cb_f32x4 ns_mma(uint4 a, uint4 b, cb_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ns_f16x8, a), __builtin_bit_cast(ns_f16x8, b), c,
+                                                  0, 0, 0);
+}
+
+// Four values to their planes. Each value is made final first: joined with the product that formed it,
+// its conversion would round once where the difference takes the twice rounded hi, and the two planes
+// would miss an f16 step of each other now and then.
+CB_DEV void ns_split(const float (&v)[4], uint2& hi, uint2& lo) {
+    ns_f16x4 h, l;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float x = v[r];
+        asm("" : "+v"(x));
+        h[r] = static_cast<_Float16>(x);
+        l[r] = static_cast<_Float16>(x - static_cast<float>(h[r]));
+    }
+    hi = __builtin_bit_cast(uint2, h);
+    lo = __builtin_bit_cast(uint2, l);
+}
+CB_DEV void ns_join(uint2 hi, uint2 lo, float (&v)[4]) {
+    const ns_f16x4 h = __builtin_bit_cast(ns_f16x4, hi), l = __builtin_bit_cast(ns_f16x4, lo);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = static_cast<float>(h[r]) + static_cast<float>(l[r]);
+}
+
+// This workgroup's group; blk becomes its index within the group.
+CB_DEV int ns_group(const NsArgs& a, int& blk) {
+    int g = 0;
+    while (g + 1 < a.ng && blk >= a.start[g + 1]) ++g;
+    blk -= a.start[g];
+    return g;
+}
+CB_DEV int64_t ns_offset(const NsArgs& a, const NsGroup& G, int b) {
+    return G.table ? a.off[G.table - 1 + b] : int64_t(b) * G.rows * G.cols;
+}
+// Tile t of the lower triangle, row by row.
+CB_DEV void ns_tile(int t, int& ti, int& tj) {
+    ti = 0;
+    while (t > ti) { t -= ti + 1; ++ti; }
+    tj = t;
+}
+
+// ------------------------------------------------------------------ the tile product
+//
+// acc += A B^T over k in [k0, k1) for a BT x BT tile, four waves of BT/2 x BT/2. An operand is NP planes
+// (`plane` bytes apart) of a padded matrix, either [rows][k] or (KM) [k][rows], leading dimension ld
+// elements; padding is zero, so there are no edges. Tiles go from memory into an LDS ring of ST stages
+// by direct loads that stay in flight across barriers (one wait per stage, counted), in the layout they
+// have in memory; 16-byte slots are permuted within a row so that a fragment read meets every bank.
+
+// 16 bytes a lane to LDS at lds + 16 lane. Inline so that the compiler, which cannot tell a ring's
+// stages apart, does not wait for every load in flight before an LDS read; the waits are written out.
+// (The s_nop is the wait state between the write of m0 and its use. Nothing else here uses m0, which
+// the compiler keeps out of its allocation.)
+CB_DEV void ns_dma16(ns_u32x4 rsrc, uint32_t lds, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"(off), "s"(rsrc) : "memory");
+}
+template <int N>
+CB_DEV void ns_wait() {
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
+}
+CB_DEV ns_u32x4 ns_rsrc(const char* base, int64_t bytes) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base);
+    return ns_u32x4{uint32_t(p), uint32_t(p >> 32), uint32_t(bytes), 0x00020000u};
+}
+CB_DEV uint32_t ns_lds(const unsigned char* p) { return uint32_t(reinterpret_cast<uintptr_t>((lds_t*)(p))); }
+
+template <int BT, int BK, int KM>
+struct NsOperand {
+    static constexpr int BYTES = BT * BK * 2;              // of a plane's tile
+    static constexpr int NI = BYTES / 4096;                // direct loads a wave and plane
+    static constexpr int SPR = (KM ? BT : BK) / 8;         // 16-byte slots per LDS row
+    static_assert(BYTES % 4096 == 0, "whole loads");
+    uint32_t base[NI], step;
+    // the slot that holds chunk c of row r (its own inverse)
+    static CB_DEV int swz(int r, int c) {
+        if (KM) return c ^ ((r & (SPR / 2 - 1)) << 1);
+        return BK == 64 ? c ^ (r & 7) : c ^ ((r >> 1) & 3);
+    }
+    CB_DEV NsOperand(int ld, int row0, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int s = (wave + 4 * i) * 64 + lane, r = s / SPR, c = swz(r, s % SPR);
+            base[i] = KM ? (uint32_t(r) * uint32_t(ld) + uint32_t(row0 + c * 8)) * 2u
+                         : (uint32_t(row0 + r) * uint32_t(ld) + uint32_t(c * 8)) * 2u;
+        }
+        step = KM ? uint32_t(ld) * 2u : 2u;
+    }
+    CB_DEV void issue(ns_u32x4 rs, uint32_t lds, int k, bool live, int wave) const {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+            ns_dma16(rs, lds + (wave + 4 * i) * 1024, live ? base[i] + uint32_t(k) * step : kOOB);
+    }
+    // 8 consecutive k (step ks of 32, lane group g) of tile row `row` (row % 16 == lane % 16)
+    static CB_DEV uint4 frag(const unsigned char* t, int row, int ks, int lane) {
+        const int g = lane >> 4;
+        if (!KM) return *reinterpret_cast<const uint4*>(t + row * (BK * 2) + swz(row, ks * 4 + g) * 16);
+        // transpose read: lane 4j+q of the 16-lane group addresses k = base + j, rows 4q..4q+3
+        const int r16 = lane & 15, j = r16 >> 2, rb = row - r16 + 4 * (r16 & 3);
+        const int k = ks * 32 + g * 8 + j;
+        const uint2 lo = lds_read_tr16(t + k * (BT * 2) + swz(k, rb >> 3) * 16 + (rb & 7) * 2);
+        const uint2 hi = lds_read_tr16(t + (k + 4) * (BT * 2) + swz(k + 4, rb >> 3) * 16 + (rb & 7) * 2);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+};
+
+template <int BT, int BK, int ST, int NA, int NB>
+constexpr int ns_lds_bytes() { return ST * (NA + NB) * BT * BK * 2; }
+
+template <int BT, int BK, int ST, int NA, int NB, int KMA, int KMB>
+CB_DEV void ns_gemm(const char* A, int64_t aplane, int lda, int arow, const char* B, int64_t bplane, int ldb, int brow,
+                    int k0, int k1, unsigned char* smem, cb_f32x4 (&acc)[BT / 32][BT / 32]) {
+    constexpr int F = BT / 32;
+    using OA = NsOperand<BT, BK, KMA>;
+    using OB = NsOperand<BT, BK, KMB>;
+    constexpr int STAGE = NA * OA::BYTES + NB * OB::BYTES, LPS = NA * OA::NI + NB * OB::NI;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, wm = wave >> 1, wn = wave & 1;
+    const OA oa(lda, arow, wave, lane);
+    const OB ob(ldb, brow, wave, lane);
+    ns_u32x4 ra[NA], rb[NB];
+#pragma unroll
+    for (int p = 0; p < NA; ++p) ra[p] = ns_rsrc(A + p * aplane, aplane);
+#pragma unroll
+    for (int p = 0; p < NB; ++p) rb[p] = ns_rsrc(B + p * bplane, bplane);
+    const uint32_t lds0 = ns_lds(smem);
+    const int nb = (k1 - k0) / BK;
+    // past the end the loads are out of range (zeros), so every stage counts the same loads
+    auto issue = [&](int it) CB_INLINE_LAMBDA {
+        const uint32_t l = lds0 + uint32_t(it % ST) * STAGE;
+#pragma unroll
+        for (int p = 0; p < NA; ++p) oa.issue(ra[p], l + p * OA::BYTES, k0 + it * BK, it < nb, wave);
+#pragma unroll
+        for (int p = 0; p < NB; ++p) ob.issue(rb[p], l + NA * OA::BYTES + p * OB::BYTES, k0 + it * BK, it < nb, wave);
+    };
+    for (int s = 0; s < ST - 1; ++s) issue(s);
+    for (int it = 0; it < nb; ++it) {
+        ns_wait<(ST - 2) * LPS>();   // this stage's loads (this wave's) are in LDS
+        lds_barrier();               // all waves' are, and the stage before is read
+        issue(it + ST - 1);
+        const unsigned char* cur = smem + (it % ST) * STAGE;
+#pragma unroll
+        for (int ks = 0; ks < BK / 32; ++ks) {
+            uint4 af[NA][F], bf[NB][F];
+#pragma unroll
+            for (int p = 0; p < NA; ++p)
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+                    af[p][i] = OA::frag(cur + p * OA::BYTES, wm * (BT / 2) + i * 16 + r16, ks, lane);
+#pragma unroll
+            for (int p = 0; p < NB; ++p)
+#pragma unroll
+                for (int j = 0; j < F; ++j)
+                    bf[p][j] = OB::frag(cur + NA * OA::BYTES + p * OB::BYTES, wn * (BT / 2) + j * 16 + r16, ks, lane);
+#pragma unroll
+            for (int q = 0; q < NA + NB - 1; ++q)   // hi hi, then lo hi and hi lo where there are planes for them
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int j = 0; j < F; ++j) {
+                        const int pa = q > 0 && q < NA ? q : 0, pb = q >= NA ? q - NA + 1 : 0;
+                        acc[i][j] = ns_mma(af[pa][i], bf[pb][j], acc[i][j]);
+                    }
+        }
+    }
+    ns_wait<0>();
+    lds_barrier();
+}
+
+template <int F>
+CB_DEV void ns_clear(cb_f32x4 (&acc)[F][F]) {
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) acc[i][j] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// f(M, N, acc[i][j]) for every group of four rows M .. M+3 of column N that this lane holds (local).
+template <int BT, class Fn>
+CB_DEV void ns_each(cb_f32x4 (&acc)[BT / 32][BT / 32], Fn&& f) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int g = lane >> 4, r16 = lane & 15, wm = wave >> 1, wn = wave & 1;
+#pragma unroll
+    for (int i = 0; i < BT / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < BT / 32; ++j)
+            f(wm * (BT / 2) + i * 16 + 4 * g, wn * (BT / 2) + j * 16 + r16, acc[i][j]);
+}
+
+// ------------------------------------------------------------------ Gram product
+
+// part [split][tile][N][M] float32: the k range of one split of one tile of X X^T (smaller side).
+template <int BT, int BK, int ST, int NP>
+__global__ __launch_bounds__(256) void ns_gram_kernel(NsArgs a, int src) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    int blk = blockIdx.x;
+    const NsGroup& G = a.g[ns_group(a, blk)];
+    const int z = blk % G.splits, t = blk / G.splits % G.tiles, b = blk / (G.splits * G.tiles);
+    int ti, tj;
+    ns_tile(t, ti, tj);
+    const char* X = a.ws + G.x[src] + int64_t(b) * NP * G.xs;
+    const int k0 = z * G.kchunk, k1 = min(G.np, k0 + G.kchunk);
+    cb_f32x4 acc[BT / 32][BT / 32];
+    ns_clear(acc);
+    if (G.tall)
+        ns_gemm<BT, BK, ST, NP, NP, 1, 1>(X, G.xs, G.cp, ti * BT, X, G.xs, G.cp, tj * BT, k0, k1, smem, acc);
+    else
+        ns_gemm<BT, BK, ST, NP, NP, 0, 0>(X, G.xs, G.cp, ti * BT, X, G.xs, G.cp, tj * BT, k0, k1, smem, acc);
+    float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.tiles + t) * (BT * BT);
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        *reinterpret_cast<float4*>(part + N * BT + M) = make_float4(v[0], v[1], v[2], v[3]);
+    });
+}
+
+// ------------------------------------------------------------------ the m x m products
+
+struct NsSeg {                 // one segment's polynomials and scales (host constants)
+    int len;
+    float c[kSeg][3];
+    float sa, sp, st, sq;      // power-of-two scales of A, P, P A and Q
+    float alpha;               // the Gram matrix's scale where X's planes have a static one, else 0
+};
+
+// X is held as X / rho with rho = ||x|| / max(||x||, eps), so that it keeps its bits where eps is far above
+// the norm; info[mat] = (what undoes the first planes' scale and divides by the norm, rho).
+CB_DEV float2 ns_info(const NsArgs& a, int mat) { return reinterpret_cast<const float2*>(a.ws + a.info)[mat]; }
+CB_DEV float ns_alpha(const NsArgs& a, const NsSeg& s, int mat) {
+    const float2 i = ns_info(a, mat);
+    const float f = s.alpha > 0.f ? i.y : i.x * i.y;
+    return s.alpha > 0.f ? s.alpha * f * f : f * f;
+}
+
+// A whole segment's m x m part of one matrix with m <= 64 in LDS, float32: five m x m buffers of pitch
+// 68 (the fragment reads of 16 rows by 4 k meet 64 different banks).
+constexpr int kSmPitch = 68, kSmBuf = 64 * kSmPitch;
+constexpr int kSmLds = 5 * kSmBuf * int(sizeof(float));
+
+// f(N, M, v): four rows M .. M+3 of column N of L R^T, tiles of 16 in turn over the waves.
+template <class Fn>
+CB_DEV void ns_small_mul(const float* L, const float* R, int mt, Fn&& f) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r16 = lane & 15;
+    for (int t = wave; t < mt * mt; t += 4) {
+        const int i = t / mt, j = t - i * mt;
+        const float* l = L + (i * 16 + r16) * kSmPitch + g;
+        const float* r = R + (j * 16 + r16) * kSmPitch + g;
+        cb_f32x4 acc{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < mt * 16; k += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(l[k], r[k], acc, 0, 0, 0);
+        f(j * 16 + r16, i * 16 + 4 * g, acc);
+    }
+}
+
+CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, float* sm) {
+    float *A = sm, *T = sm + kSmBuf, *P = sm + 2 * kSmBuf, *Q = sm + 3 * kSmBuf, *Q2 = sm + 4 * kSmBuf;
+    const int mt = (G.m + 15) / 16;
+    const float alpha = ns_alpha(a, s, G.first + b);
+    const float* part = reinterpret_cast<const float*>(a.ws + G.part + int64_t(b) * G.ps);
+    for (int e = threadIdx.x * 4; e < 64 * 64; e += 1024) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int z = 0; z < G.splits; ++z) {
+            const float4 q = *reinterpret_cast<const float4*>(part + z * 4096 + e);
+            v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
+        }
+        *reinterpret_cast<float4*>(A + (e >> 6) * kSmPitch + (e & 63)) =
+            make_float4(v.x * alpha, v.y * alpha, v.z * alpha, v.w * alpha);
+    }
+    __syncthreads();
+    auto put = [&](float* D) {
+        return [=](int N, int M, cb_f32x4 v) CB_INLINE_LAMBDA {
+            *reinterpret_cast<float4*>(D + N * kSmPitch + M) = make_float4(v[0], v[1], v[2], v[3]);
+        };
+    };
+    for (int t = 0; t < s.len; ++t) {
+        float* D = t == 0 ? Q : P;
+        const float ca = s.c[t][0], cb = s.c[t][1], cc = s.c[t][2];
+        ns_small_mul(A, A, mt, [&](int N, int M, cb_f32x4 v) CB_INLINE_LAMBDA {
+            const float4 q = *reinterpret_cast<const float4*>(A + N * kSmPitch + M);
+            *reinterpret_cast<float4*>(D + N * kSmPitch + M) =
+                make_float4(cb * q.x + cc * v[0] + (N == M ? ca : 0.f), cb * q.y + cc * v[1] + (N == M + 1 ? ca : 0.f),
+                            cb * q.z + cc * v[2] + (N == M + 2 ? ca : 0.f), cb * q.w + cc * v[3] + (N == M + 3 ? ca : 0.f));
+        });
+        __syncthreads();
+        if (t > 0) {
+            ns_small_mul(P, Q, mt, put(Q2));
+            float* w = Q; Q = Q2; Q2 = w;
+        }
+        if (t + 1 < s.len) {
+            const float* F = t == 0 ? Q : P;   // the first P is Q
+            ns_small_mul(F, A, mt, put(T));
+            __syncthreads();
+            ns_small_mul(T, F, mt, put(A));
+        }
+        __syncthreads();
+    }
+    char* q = a.ws + G.q[0] + int64_t(b) * 2 * G.ms;
+    for (int e = threadIdx.x * 4; e < 64 * 64; e += 1024) {
+        const int N = e >> 6, M = e & 63;
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = N < G.m && M + r < G.m ? Q[N * kSmPitch + M + r] * s.sq : 0.f;
+        uint2 hi, lo;
+        ns_split(v, hi, lo);
+        *reinterpret_cast<uint2*>(q + e * 2) = hi;
+        *reinterpret_cast<uint2*>(q + G.ms + e * 2) = lo;
+    }
+}
+
+// Sums the Gram partials in split order. m <= 64: and goes on to Q. Else A's planes, 16 columns of a
+// tile a workgroup, with the mirror image of an off-diagonal tile.
+__global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    int blk = blockIdx.x;
+    const NsGroup& G = a.g[ns_group(a, blk)];
+    if (G.mp == 64) {
+        ns_small(a, G, s, blk, reinterpret_cast<float*>(smem));
+        return;
+    }
+    float* sh = reinterpret_cast<float*>(smem);   // [BT][17]
+    const int bt = G.bt, strips = bt / 16;
+    const int n0 = (blk % strips) * 16, t = blk / strips % G.tiles, b = blk / (strips * G.tiles);
+    int ti, tj;
+    ns_tile(t, ti, tj);
+    const float alpha = ns_alpha(a, s, G.first + b) * s.sa;
+    const float* part = reinterpret_cast<const float*>(a.ws + G.part + int64_t(b) * G.ps) + int64_t(t) * bt * bt;
+    char* A = a.ws + G.a + int64_t(b) * 2 * G.ms;
+    for (int e = threadIdx.x * 4; e < 16 * bt; e += 1024) {
+        const int N = n0 + e / bt, M = e % bt;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int z = 0; z < G.splits; ++z) {
+            const float4 q = *reinterpret_cast<const float4*>(part + int64_t(z) * G.tiles * bt * bt + N * bt + M);
+            v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            v[r] *= alpha;
+            sh[(M + r) * 17 + e / bt] = v[r];
+        }
+        uint2 hi, lo;
+        ns_split(v, hi, lo);
+        const int64_t o = (int64_t(tj * bt + N) * G.mp + ti * bt + M) * 2;
+        *reinterpret_cast<uint2*>(A + o) = hi;
+        *reinterpret_cast<uint2*>(A + G.ms + o) = lo;
+    }
+    if (ti == tj) return;
+    __syncthreads();
+    for (int e = threadIdx.x * 4; e < 16 * bt; e += 1024) {
+        const int M = e / 16, q = e % 16;
+        const float v[4] = {sh[M * 17 + q], sh[M * 17 + q + 1], sh[M * 17 + q + 2], sh[M * 17 + q + 3]};
+        uint2 hi, lo;
+        ns_split(v, hi, lo);
+        const int64_t o = (int64_t(ti * bt + M) * G.mp + tj * bt + n0 + q) * 2;
+        *reinterpret_cast<uint2*>(A + o) = hi;
+        *reinterpret_cast<uint2*>(A + G.ms + o) = lo;
+    }
+}
+
+enum { NS_A = 0, NS_T, NS_P, NS_Q0, NS_Q1 };
+struct NsJob {                 // dst = lhs rhs (scaled), or with poly diag I + fa A + f lhs rhs
+    int lhs, rhs, dst, poly;
+    float f, fa, diag;
+};
+struct NsJobs { int n; NsJob j[2]; };
+
+CB_DEV char* ns_buf(const NsArgs& a, const NsGroup& G, int id, int b) {
+    const int64_t o = id == NS_A ? G.a : id == NS_T ? G.t : id == NS_P ? G.p : id == NS_Q0 ? G.q[0] : G.q[1];
+    return a.ws + o + int64_t(b) * 2 * G.ms;
+}
+
+// Products of symmetric matrices that commute: the lower triangle's tiles, and their mirror images.
+template <int BT, int BK, int ST>
+__global__ __launch_bounds__(256) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    int blk = blockIdx.x;
+    const NsGroup& G = a.g[ns_group(a, blk)];
+    const NsJob& J = jobs.j[blk % jobs.n];
+    const int t = blk / jobs.n % G.tiles, b = blk / (jobs.n * G.tiles);
+    int ti, tj;
+    ns_tile(t, ti, tj);
+    cb_f32x4 acc[BT / 32][BT / 32];
+    ns_clear(acc);
+    ns_gemm<BT, BK, ST, 2, 2, 0, 0>(ns_buf(a, G, J.lhs, b), G.ms, G.mp, ti * BT, ns_buf(a, G, J.rhs, b), G.ms, G.mp,
+                                    tj * BT, 0, G.mp, smem, acc);
+    char* D = ns_buf(a, G, J.dst, b);
+    const char* A = ns_buf(a, G, NS_A, b);
+    const float f = J.f, fa = J.fa, diag = J.diag;
+    const int poly = J.poly;
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        const int m = ti * BT + M, n = tj * BT + N;
+        const int64_t o = (int64_t(n) * G.mp + m) * 2;
+        float w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r] = f * v[r];
+        if (poly) {
+            float q[4];
+            ns_join(*reinterpret_cast<const uint2*>(A + o), *reinterpret_cast<const uint2*>(A + G.ms + o), q);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[r] += fa * q[r] + (m + r == n ? diag : 0.f);
+        }
+        uint2 hi, lo;
+        ns_split(w, hi, lo);
+        *reinterpret_cast<uint2*>(D + o) = hi;
+        *reinterpret_cast<uint2*>(D + G.ms + o) = lo;
+        if (ti != tj) {
+            const uint16_t h[4] = {uint16_t(hi.x), uint16_t(hi.x >> 16), uint16_t(hi.y), uint16_t(hi.y >> 16)};
+            const uint16_t l[4] = {uint16_t(lo.x), uint16_t(lo.x >> 16), uint16_t(lo.y), uint16_t(lo.y >> 16)};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t m2 = (int64_t(m + r) * G.mp + n) * 2;
+                *reinterpret_cast<uint16_t*>(D + m2) = h[r];
+                *reinterpret_cast<uint16_t*>(D + G.ms + m2) = l[r];
+            }
+        }
+    });
+}
+
+// ------------------------------------------------------------------ Q X
+
+enum { NS_OUT_MID = 0, NS_OUT_F32, NS_OUT_BF16, NS_OUT_STEP };
+struct NsApply {
+    int out, src, dst, q;      // X buffer read, X buffer written (MID), Q buffer of the large groups
+    float f;                   // 1 / (scale of Q, of X where static), times the new scale (MID)
+    int use_inv;               // X carries its matrix's own scale (info)
+    void* y;
+    float* p;                  // parameters (STEP)
+    float decay, lr;
+    uint16_t* mir; int64_t mir_off, mir_len;
+};
+
+template <int BT, int BK, int ST, int NP>
+__global__ __launch_bounds__(256) void ns_apply_kernel(NsArgs a, NsApply ap) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    int blk = blockIdx.x;
+    const NsGroup& G = a.g[ns_group(a, blk)];
+    const int tn = G.rp / BT, tm = G.cp / BT;   // N over the rows, M over the columns
+    const int jt = blk % tn, it = blk / tn % tm, b = blk / (tn * tm);
+    const char* X = a.ws + G.x[ap.src] + int64_t(b) * NP * G.xs;
+    const char* Q = a.ws + (G.mp == 64 ? G.q[0] : G.q[ap.q]) + int64_t(b) * 2 * G.ms;
+    cb_f32x4 acc[BT / 32][BT / 32];
+    ns_clear(acc);
+    if (G.tall)   // rows of X by Q: both k-contiguous
+        ns_gemm<BT, BK, ST, 2, NP, 0, 0>(Q, G.ms, G.mp, it * BT, X, G.xs, G.cp, jt * BT, 0, G.mp, smem, acc);
+    else          // columns of X by Q
+        ns_gemm<BT, BK, ST, NP, 2, 1, 0>(X, G.xs, G.cp, it * BT, Q, G.ms, G.mp, jt * BT, 0, G.mp, smem, acc);
+    float f = ap.f;
+    const float2 info = ns_info(a, G.first + b);
+    if (ap.use_inv) f *= info.x;
+    if (ap.out != NS_OUT_MID) f *= info.y;
+    if (ap.out == NS_OUT_MID) {
+        char* D = a.ws + G.x[ap.dst] + int64_t(b) * 2 * G.xs;
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+            const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+            uint2 hi, lo;
+            ns_split(w, hi, lo);
+            const int64_t o = (int64_t(jt * BT + N) * G.cp + it * BT + M) * 2;
+            *reinterpret_cast<uint2*>(D + o) = hi;
+            *reinterpret_cast<uint2*>(D + G.xs + o) = lo;
+        });
+        return;
+    }
+    const int64_t off = ns_offset(a, G, b);
+    const int rows = G.rows, cols = G.cols;
+    if (ap.out == NS_OUT_BF16) {
+        uint16_t* y = static_cast<uint16_t*>(ap.y) + off;
+        const bool vec = cols % 4 == 0 && (reinterpret_cast<uintptr_t>(y) & 7) == 0;
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+            const int r = jt * BT + N, c = it * BT + M;
+            if (r >= rows) return;
+            uint16_t* o = y + int64_t(r) * cols + c;
+            if (vec && c < cols) store4(o, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < cols) o[e] = f2bf(v[e] * f);
+        });
+        return;
+    }
+    if (ap.out == NS_OUT_F32) {
+        float* y = static_cast<float*>(ap.y) + off;
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+            const int r = jt * BT + N, c = it * BT + M;
+            if (r >= rows) return;
+            float* o = y + int64_t(r) * cols + c;
+            if (c + 4 <= cols) {
+                *reinterpret_cast<cb_f32x4_a4*>(o) = cb_f32x4_a4{v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < cols) o[e] = v[e] * f;
+            }
+        });
+        return;
+    }
+    // the parameters: p <- decay p - lr scale O
+    f *= ap.lr * G.scale;
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        const int r = jt * BT + N, c = it * BT + M;
+        if (r >= rows || c >= cols) return;
+        const int64_t o = off + int64_t(r) * cols + c;
+        const int k = min(4, cols - c);
+        float w[4];
+        if (k == 4) {
+            const float4 p = load_f4(ap.p + o);
+            w[0] = ap.decay * p.x - f * v[0]; w[1] = ap.decay * p.y - f * v[1];
+            w[2] = ap.decay * p.z - f * v[2]; w[3] = ap.decay * p.w - f * v[3];
+            *reinterpret_cast<cb_f32x4_a4*>(ap.p + o) = cb_f32x4_a4{w[0], w[1], w[2], w[3]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < k) {
+                    w[e] = ap.decay * ap.p[o + e] - f * v[e];
+                    ap.p[o + e] = w[e];
+                }
+        }
+        if (ap.mir)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t d = o + e - ap.mir_off;
+                if (e < k && d >= 0 && d < ap.mir_len) ap.mir[d] = f2bf(w[e]);
+            }
+    });
+}
+
+// ------------------------------------------------------------------ sums of squares, planes
+
+enum { NS_SRC_F32 = 0, NS_SRC_BF16, NS_SRC_STEP };
+
+// Blocks [0, start[ng]) sum a matrix's elements in G.nsum shares; (STEP) those after them the gaps'.
+// Three doubles a block: sum g^2, sum g m, sum m^2 (others: sum x^2, 0, 0).
+template <int SRC>
+__global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, const void* src, int block0) {
+    __shared__ double sh[256];
+    int64_t at, len;
+    int blk = blockIdx.x;
+    bool both = SRC == NS_SRC_STEP;
+    if (SRC != NS_SRC_STEP || blk < a.start[a.ng]) {
+        const NsGroup& G = a.g[ns_group(a, blk)];
+        const int b = blk / G.nsum, k = blk % G.nsum;
+        const int64_t tot = int64_t(G.rows) * G.cols, per = ((tot + G.nsum - 1) / G.nsum + 3) / 4 * 4;
+        at = ns_offset(a, G, b) + k * per;
+        len = min(per, tot - k * per);
+    } else {
+        blk -= a.start[a.ng];
+        int i = 0;
+        while (i + 1 < e.ngaps && blk >= e.gap_start[i + 1]) ++i;
+        const int nb = e.gap_start[i + 1] - e.gap_start[i], k = blk - e.gap_start[i];
+        const int64_t per = ((e.gap_len[i] + nb - 1) / nb + 3) / 4 * 4;
+        at = e.gap[i] + k * per;
+        len = min(per, e.gap_len[i] - k * per);
+        both = false;
+    }
+    double gg = 0.0, gm = 0.0, mm = 0.0;
+    auto add = [&](float g, float m) CB_INLINE_LAMBDA {
+        gg += double(g) * g;
+        if (SRC == NS_SRC_STEP && both) {
+            gm += double(g) * m;
+            mm += double(m) * m;
+        }
+    };
+    if (SRC == NS_SRC_BF16) {
+        const uint16_t* x = static_cast<const uint16_t*>(src) + at;
+        if ((reinterpret_cast<uintptr_t>(x) & 7) == 0) {
+            for (int64_t i = threadIdx.x * 4; i < len; i += 1024) {
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+                if (i + 4 <= len) load4(x + i, v);
+                else
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (i + q < len) v[q] = bf2f(x[i + q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) add(v[q], 0.f);
+            }
+        } else {
+            for (int64_t i = threadIdx.x; i < len; i += 256) add(bf2f(x[i]), 0.f);
+        }
+    } else {
+        const float* x = (SRC == NS_SRC_STEP ? e.g : static_cast<const float*>(src)) + at;
+        const float* m = e.m + at;
+        for (int64_t i = threadIdx.x * 4; i < len; i += 1024) {
+            if (i + 4 <= len) {
+                const float4 v = load_f4(x + i);
+                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (SRC == NS_SRC_STEP && both) w = load_f4(m + i);
+                add(v.x, w.x); add(v.y, w.y); add(v.z, w.z); add(v.w, w.w);
+            } else {
+                for (int64_t q = i; q < len; ++q) add(x[q], SRC == NS_SRC_STEP && both ? m[q] : 0.f);
+            }
+        }
+    }
+    gg = block_sum<256>(gg, sh);
+    if (SRC == NS_SRC_STEP) {
+        gm = block_sum<256>(gm, sh);
+        mm = block_sum<256>(mm, sh);
+    }
+    if (threadIdx.x == 0) {
+        double* o = reinterpret_cast<double*>(a.ws + a.sums) + int64_t(3) * (block0 + blockIdx.x);
+        o[0] = gg; o[1] = gm; o[2] = mm;
+    }
+}
+
+constexpr int kPrepElems = 8192;   // padded elements a workgroup of the planes
+
+// The power of two that brings a matrix of this norm to a root mean square near one; info as ns_info.
+// A zero matrix: (1, 0).
+CB_DEV float ns_scale(double norm, double elems, float eps, float2& info) {
+    int k = 0;
+    if (norm > 0.0 && isfinite(norm)) k = -int(rint(log2(norm / sqrt(elems))));
+    k = k < -126 ? -126 : k > 126 ? 126 : k;
+    const double f = exp2(double(k));
+    info.x = norm == 0.0 ? 1.f : float(1.0 / (norm * f));
+    info.y = norm == 0.0 ? 0.f : float(norm / (norm > double(eps) || norm != norm ? norm : double(eps)));
+    return float(f);
+}
+
+CB_DEV float ns_adam(float p, float g, float& m, float& v, const MuonElem& e) {
+    m = e.b1 * m + e.omb1 * g;
+    v = e.b2 * v + e.omb2 * g * g;
+    const float mh = m / e.bc1, vh = v / e.bc2;
+    return p - e.alr * mh / (sqrtf(vh) + e.aeps);
+}
+
+// X's planes from the source (STEP: u from the clipped gradient and the momentum, which is updated),
+// padded with zeros; blocks after the matrices' (STEP): Adam on what no matrix covers.
+template <int SRC, int NP>
+__global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, const void* src, float eps, int block0) {
+    __shared__ double sh[256];
+    const double* sums = reinterpret_cast<const double*>(a.ws + a.sums);
+    float clip = 1.f;
+    if (SRC == NS_SRC_STEP) {
+        double s = 0.0;
+        for (int i = threadIdx.x; i < e.nblocks; i += 256) s += sums[3 * i];
+        const double norm = sqrt(block_sum<256>(s, sh));
+        if (blockIdx.x == 0 && block0 == 0 && threadIdx.x == 0 && e.stats) {
+            e.stats[0] = float(norm);
+            e.stats[1] = isfinite(norm) ? 0.f : 1.f;
+        }
+        clip = (e.max_norm > 0.f && norm > double(e.max_norm)) ? float(double(e.max_norm) / norm) : 1.f;
+    }
+    int blk = blockIdx.x;
+    if (SRC == NS_SRC_STEP && blk >= a.start[a.ng]) {
+        blk -= a.start[a.ng];
+        int i = 0;
+        while (i + 1 < e.ngaps && blk >= e.gap_start[i + 1]) ++i;
+        const int nb = e.gap_start[i + 1] - e.gap_start[i], k = blk - e.gap_start[i];
+        for (int64_t q = int64_t(k) * 256 + threadIdx.x; q < e.gap_len[i]; q += int64_t(nb) * 256) {
+            const int64_t o = e.gap[i] + q;
+            float m = e.m[o], v = e.v[o];
+            const float p = ns_adam(e.p[o], e.g[o] * clip, m, v, e);
+            e.p[o] = p; e.m[o] = m; e.v[o] = v;
+            if (e.mir && o >= e.mir_off && o < e.mir_off + e.mir_len) e.mir[o - e.mir_off] = f2bf(p);
+        }
+        return;
+    }
+    const NsGroup& G = a.g[ns_group(a, blk)];
+    const int64_t padded = int64_t(G.rp) * G.cp;
+    const int per = int((padded + kPrepElems - 1) / kPrepElems);
+    const int b = blk / per, k = blk % per;
+    const double* ms = sums + int64_t(3) * (G.part0 + b * G.nsum);
+    double gg = 0.0, gm = 0.0, mm = 0.0;
+    for (int i = threadIdx.x; i < G.nsum; i += 256) {
+        gg += ms[3 * i]; gm += ms[3 * i + 1]; mm += ms[3 * i + 2];
+    }
+    gg = block_sum<256>(gg, sh);
+    double norm = sqrt(gg);
+    if (SRC == NS_SRC_STEP) {
+        gm = block_sum<256>(gm, sh);
+        mm = block_sum<256>(mm, sh);
+        // ||c1 g + c2 m|| from the three sums; where the two all but cancel what is left of it is
+        // their rounding, and a norm no smaller than that keeps the singular values below one
+        const double c1 = double(e.c1) * clip, c2 = e.c2;
+        const double est = c1 * c1 * gg + 2.0 * c1 * c2 * gm + c2 * c2 * mm;
+        const double least = 0x1p-21 * (fabs(c1) * sqrt(gg) + fabs(c2) * sqrt(mm));
+        norm = est < least * least ? least : sqrt(est);
+        eps = e.eps;
+    }
+    float2 info;
+    const float f = ns_scale(norm, double(G.rows) * G.cols, eps, info);
+    if (k == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.ws + a.info)[G.first + b] = info;
+    char* X = a.ws + G.x[0] + int64_t(b) * NP * G.xs;
+    const int64_t off = ns_offset(a, G, b);
+    const int64_t end = min(padded, int64_t(k + 1) * kPrepElems);
+    for (int64_t q = int64_t(k) * kPrepElems + threadIdx.x * 4; q < end; q += 1024) {
+        const int r = int(q / G.cp), c = int(q - int64_t(r) * G.cp);
+        float w[4] = {0.f, 0.f, 0.f, 0.f};
+        if (r < G.rows && c < G.cols) {
+            const int64_t o = off + int64_t(r) * G.cols + c;
+            const int n = min(4, G.cols - c);
+            if (SRC == NS_SRC_BF16) {
+                const uint16_t* x = static_cast<const uint16_t*>(src) + o;
+                if (n == 4 && (reinterpret_cast<uintptr_t>(x) & 7) == 0) load4(x, w);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < n) w[i] = bf2f(x[i]);
+            } else if (SRC == NS_SRC_F32) {
+                const float* x = static_cast<const float*>(src) + o;
+                if (n == 4) {
+                    const float4 v = load_f4(x);
+                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < n) w[i] = x[i];
+                }
+            } else {
+                float gv[4], mv[4];
+                if (n == 4) {
+                    const float4 g = load_f4(e.g + o), m = load_f4(e.m + o);
+                    gv[0] = g.x; gv[1] = g.y; gv[2] = g.z; gv[3] = g.w;
+                    mv[0] = m.x; mv[1] = m.y; mv[2] = m.z; mv[3] = m.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        gv[i] = i < n ? e.g[o + i] : 0.f;
+                        mv[i] = i < n ? e.m[o + i] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < n) {
+                        const float gs = e.omu * (gv[i] * clip);
+                        mv[i] = e.mu * mv[i] + gs;
+                        w[i] = e.nesterov ? e.mu * mv[i] + gs : mv[i];
+                    }
+                if (n == 4) {
+                    *reinterpret_cast<cb_f32x4_a4*>(e.m + o) = cb_f32x4_a4{mv[0], mv[1], mv[2], mv[3]};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < n) e.m[o + i] = mv[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = i < n ? w[i] * f : 0.f;
+        }
+        uint2 hi, lo;
+        ns_split(w, hi, lo);
+        *reinterpret_cast<uint2*>(X + q * 2) = hi;
+        if (NP > 1) *reinterpret_cast<uint2*>(X + G.xs + q * 2) = lo;
+    }
+}
+
+// ------------------------------------------------------------------ host: shapes, layout, launches
+
+int64_t up(int64_t v, int64_t k) { return (v + k - 1) / k * k; }
+int64_t a256(int64_t v) { return up(v, 256); }
+
+// Tiles of 128 where they fill the chip (256 CUs), else of 64: more workgroups, each a quarter of the work.
+int ns_bt(int m, int64_t batch) {
+    const int64_t t = (m + 127) / 128;
+    return m > 64 && batch * t * (t + 1) / 2 >= 192 ? 128 : 64;
+}
+
+void ns_shape(NsGroup& G, int rows, int cols, int batch) {
+    G.rows = rows; G.cols = cols; G.batch = batch;
+    G.tall = rows > cols;
+    G.m = std::min(rows, cols); G.n = std::max(rows, cols);
+    G.bt = ns_bt(G.m, batch);
+    G.rp = int(up(rows, G.bt)); G.cp = int(up(cols, G.bt));
+    G.mp = std::min(G.rp, G.cp); G.np = std::max(G.rp, G.cp);
+    const int t = G.mp / G.bt;
+    G.tiles = t * (t + 1) / 2;
+    // the Gram product's k in splits of at least two 64-blocks, towards two workgroups per CU
+    const int nb = G.np / 64;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::max(1, nb / 2), 512 / (int64_t(batch) * G.tiles)));
+    const int each = int((nb + want - 1) / want);
+    G.kchunk = each * 64;
+    G.splits = (nb + each - 1) / each;
+    // blocks of the sums: 16384 elements each, at most 64 a matrix
+    G.nsum = int(std::max<int64_t>(1, std::min<int64_t>(64, int64_t(rows) * cols / 16384)));
+    G.xs = int64_t(G.rp) * G.cp * 2;
+    G.ms = int64_t(G.mp) * G.mp * 2;
+    G.ps = int64_t(G.splits) * G.tiles * G.bt * G.bt * 4;
+    G.scale = 1.f;
+}
+
+// Lays the group's buffers out from `at`; np0: planes of X as it comes; two: a second X buffer.
+int64_t ns_layout(NsGroup& G, int64_t at, int np0, bool two) {
+    auto take = [&](int64_t bytes) { const int64_t o = at; at += a256(bytes); return o; };
+    const bool big = G.mp > 64;
+    G.x[0] = take(G.batch * G.xs * (two ? 2 : np0));   // a later segment may write it with both planes
+    G.x[1] = take(two ? G.batch * G.xs * 2 : 0);
+    G.part = take(G.batch * G.ps);
+    const int64_t mm = G.batch * G.ms * 2;
+    G.q[0] = take(mm);
+    G.q[1] = take(big ? mm : 0);
+    G.a = take(big ? mm : 0);
+    G.t = take(big ? mm : 0);
+    G.p = take(big ? mm : 0);
+    return at;
+}
+
+struct NsProgram {
+    int nseg;
+    NsSeg seg[(kNsMaxSteps + kSeg - 1) / kSeg];
+    double xscale[(kNsMaxSteps + kSeg - 1) / kSeg];   // scale of X after segment i
+};
+
+double pow2_scale(double bound, int most) {   // the largest power of two (at most 2^most) with bound * it <= 2^15
+    const double e = std::floor(15.0 - std::log2(std::max(bound, 1e-30)));
+    return std::exp2(std::min<double>(e, most));
+}
+
+// The segments of `steps` steps and the scales of their matrices, from bounds on the singular values:
+// they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False where they
+// could grow past 2^10 (planes would no longer resolve them).
+bool ns_program(int steps, const float* coeffs, NsProgram& P) {
+    static const float kDefault[3] = {3.4445f, -4.7750f, 2.0315f};
+    P.nseg = (steps + kSeg - 1) / kSeg;
+    double s = 1.0 + 0x1p-10;
+    int at = 0;
+    for (int k = 0; k < P.nseg; ++k) {
+        NsSeg& g = P.seg[k];
+        std::memset(&g, 0, sizeof(g));
+        g.len = (steps - at + P.nseg - k - 1) / (P.nseg - k);
+        double amax = s * s, pmax = 0, tmax = 0, q = 1, qmax = 0;
+        for (int t = 0; t < g.len; ++t, ++at) {
+            const float* c = coeffs ? coeffs + 3 * at : kDefault;
+            const double a = c[0], b = c[1], cc = c[2], lam = s * s;
+            for (int i = 0; i < 3; ++i) g.c[t][i] = c[i];
+            auto poly = [&](double l) { return std::fabs(a + b * l + cc * l * l); };
+            double p = std::max(poly(0), poly(lam));
+            if (cc != 0) {
+                const double v = -b / (2 * cc);
+                if (v > 0 && v < lam) p = std::max(p, poly(v));
+            }
+            // extrema of s (a + b s^2 + c s^4): a + 3 b l + 5 c l^2 = 0 with l = s^2
+            double ns = s * poly(lam);
+            auto extremum = [&](double l) { if (l > 0 && l < lam) ns = std::max(ns, std::sqrt(l) * poly(l)); };
+            const double d = 9 * b * b - 20 * cc * a;
+            if (cc != 0 && d >= 0) {
+                extremum((-3 * b + std::sqrt(d)) / (10 * cc));
+                extremum((-3 * b - std::sqrt(d)) / (10 * cc));
+            } else if (cc == 0 && b != 0) {
+                extremum(-a / (3 * b));
+            }
+            q *= p;
+            pmax = std::max(pmax, p); qmax = std::max(qmax, q); tmax = std::max(tmax, lam * p);
+            s = ns * (1 + 0x1p-10);
+            if (!(s <= 1024.0) || !(qmax <= 1e15)) return false;
+            if (t + 1 < g.len) amax = std::max(amax, s * s);
+        }
+        g.sa = float(pow2_scale(amax, 14));
+        g.sp = float(pow2_scale(pmax, 14));
+        g.st = float(pow2_scale(tmax, 14));
+        g.sq = float(pow2_scale(qmax, 14));
+        P.xscale[k] = pow2_scale(s, 12);
+        g.alpha = k == 0 ? 0.f : float(1.0 / (P.xscale[k - 1] * P.xscale[k - 1]));
+    }
+    return true;
+}
+
+// The groups of `a` that `take` accepts, with `blocks` workgroups each.
+template <class Take, class Blocks>
+NsArgs ns_select(const NsArgs& a, Take&& take, Blocks&& blocks, int& total) {
+    NsArgs r = a;
+    r.ng = 0;
+    total = 0;
+    for (int g = 0; g < a.ng; ++g)
+        if (take(a.g[g])) {
+            r.g[r.ng] = a.g[g];
+            r.start[r.ng++] = total;
+            total += blocks(a.g[g]);
+        }
+    r.start[r.ng] = total;
+    return r;
+}
+
+#define NS_LAUNCH(K, N, LDS, ...) hipLaunchKernelGGL(K, dim3(unsigned(N)), dim3(256), LDS, s, __VA_ARGS__)
+
+template <int BT, int BK, int ST>
+void ns_gram(const NsArgs& a, int src, int np, hipStream_t s) {
+    int n;
+    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
+                               [](const NsGroup& G) { return G.batch * G.tiles * G.splits; }, n);
+    if (!n) return;
+    if (np == 1) NS_LAUNCH((ns_gram_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 1, 1>()), r, src);
+    else NS_LAUNCH((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, src);
+}
+
+template <int BT, int BK, int ST>
+void ns_prod(const NsArgs& a, const NsJobs& jobs, hipStream_t s) {
+    int n;
+    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT && G.mp > 64; },
+                               [&](const NsGroup& G) { return G.batch * G.tiles * jobs.n; }, n);
+    if (n) NS_LAUNCH((ns_prod_kernel<BT, BK, ST>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, jobs);
+}
+
+template <int BT, int BK, int ST>
+void ns_apply(const NsArgs& a, const NsApply& ap, int np, hipStream_t s) {
+    int n;
+    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
+                               [](const NsGroup& G) { return G.batch * (G.rp / BT) * (G.cp / BT); }, n);
+    if (!n) return;
+    if (np == 1) NS_LAUNCH((ns_apply_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 2, 1>()), r, ap);
+    else NS_LAUNCH((ns_apply_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, ap);
+}
+
+// All segments of one pass, X's planes (np of them) in place; `last` describes the final output.
+hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hipStream_t s) {
+    int src = 0;
+    for (int k = 0; k < P.nseg; ++k) {
+        const NsSeg& g = P.seg[k];
+        ns_gram<64, 64, 4>(a, src, np, s);
+        ns_gram<128, 32, 2>(a, src, np, s);
+        int n;
+        const NsArgs r = ns_select(a, [](const NsGroup&) { return true; }, [](const NsGroup& G) {
+            return G.mp == 64 ? G.batch : G.batch * G.tiles * (G.bt / 16);
+        }, n);
+        bool small = false;
+        for (int i = 0; i < a.ng; ++i) small = small || a.g[i].mp == 64;
+        NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 128 * 17 * int(sizeof(float)), r, g);
+        int q = 0;   // the buffer that holds Q
+        auto prod = [&](NsJobs j) {
+            ns_prod<64, 64, 4>(a, j, s);
+            ns_prod<128, 32, 2>(a, j, s);
+        };
+        for (int t = 0; t < g.len; ++t) {
+            const float sd = t == 0 ? g.sq : g.sp;        // the first P is Q
+            const int p = t == 0 ? NS_Q0 : NS_P;
+            prod({1, {{NS_A, NS_A, p, 1, sd * g.c[t][2] / (g.sa * g.sa), sd * g.c[t][1] / g.sa, sd * g.c[t][0]}}});
+            NsJobs j{};
+            if (t > 0) {
+                j.j[j.n++] = {NS_P, q ? NS_Q1 : NS_Q0, q ? NS_Q0 : NS_Q1, 0, 1.f / g.sp, 0.f, 0.f};
+                q ^= 1;
+            }
+            if (t + 1 < g.len) j.j[j.n++] = {p, NS_A, NS_T, 0, g.st / (sd * g.sa), 0.f, 0.f};
+            if (j.n) prod(j);
+            if (t + 1 < g.len) prod({1, {{NS_T, p, NS_A, 0, g.sa / (g.st * sd), 0.f, 0.f}}});
+        }
+        const bool end = k + 1 == P.nseg;
+        NsApply ap = last;
+        if (!end) ap.out = NS_OUT_MID;
+        ap.src = src; ap.dst = src ^ 1; ap.q = q;
+        ap.use_inv = k == 0;
+        ap.f = float((end ? 1.0 : P.xscale[k]) / (double(g.sq) * (k == 0 ? 1.0 : P.xscale[k - 1])));
+        ns_apply<64, 64, 4>(a, ap, np, s);
+        ns_apply<128, 32, 2>(a, ap, np, s);
+        src ^= 1;
+        np = 2;
+    }
+    return hipGetLastError();
+}
+
+int64_t orth_layout(int prec, int64_t batch, int rows, int cols, int steps, NsArgs& a) {
+    std::memset(&a, 0, sizeof(a));
+    a.ng = 1;
+    NsGroup& G = a.g[0];
+    ns_shape(G, rows, cols, int(batch));
+    a.info = 0;
+    a.sums = a256(batch * 8);
+    return ns_layout(G, a.sums + a256(batch * G.nsum * 24), prec == BF16 ? 1 : 2, steps > kSeg);
+}
+
+}  // namespace
+
+bool muon_coeffs_ok(int steps, const float* coeffs) {
+    NsProgram P;
+    return ns_program(steps, coeffs, P);
+}
+
+size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps) {
+    NsArgs a;
+    return size_t(orth_layout(prec, batch, rows, cols, steps, a));
+}
+
+hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,
+                     float eps, void* y, void* ws, hipStream_t s) {
+    NsArgs a;
+    orth_layout(prec, batch, rows, cols, steps, a);
+    a.ws = static_cast<char*>(ws);
+    NsProgram P;
+    ns_program(steps, coeffs, P);
+    const NsGroup& G = a.g[0];
+    ProfScope ps(s, [&] { return cb_key("muon_orthogonalize", prec, cb_dims(rows, cols) + "x" + std::to_string(batch)); });
+    MuonElem e{};
+    const int64_t sums = batch * G.nsum, planes = batch * ((int64_t(G.rp) * G.cp + kPrepElems - 1) / kPrepElems);
+    if (prec == BF16) {
+        NS_LAUNCH((ns_sums_kernel<NS_SRC_BF16>), sums, 0, a, e, x, 0);
+        NS_LAUNCH((ns_planes_kernel<NS_SRC_BF16, 1>), planes, 0, a, e, x, eps, 0);
+    } else {
+        NS_LAUNCH((ns_sums_kernel<NS_SRC_F32>), sums, 0, a, e, x, 0);
+        NS_LAUNCH((ns_planes_kernel<NS_SRC_F32, 2>), planes, 0, a, e, x, eps, 0);
+    }
+    NsApply ap{};
+    ap.out = prec == BF16 ? NS_OUT_BF16 : NS_OUT_F32;
+    ap.y = y;
+    return ns_run(a, P, prec == BF16 ? 1 : 2, ap, s);
+}
+
+// ------------------------------------------------------------------ the step over the flat buffer
+
+namespace {
+
+struct MuonPlan {
+    struct Pass { NsArgs a; MuonElem e; int block0, sums, planes; };
+    std::vector<Pass> pass;
+    int nblocks = 0;
+    int64_t total = 0;
+};
+
+// Passes of at most kNsMats matrices in kNsGroups shapes; each also has the gaps that lie before its
+// matrices in the buffer (the last one those after). `mats` sorted by offset.
+MuonPlan muon_plan(int64_t n_params, const std::vector<MuonMat>& mats, int steps, int scale_mode) {
+    MuonPlan plan;
+    int64_t at = 0;
+    size_t i = 0;
+    int first = 0;
+    do {
+        MuonPlan::Pass P;
+        std::memset(&P, 0, sizeof(P));
+        struct Shape { int rows, cols; std::vector<int64_t> off; };
+        std::vector<Shape> shapes;
+        auto gap = [&](int64_t to) {
+            if (to > at) {
+                P.e.gap[P.e.ngaps] = at;
+                P.e.gap_len[P.e.ngaps++] = to - at;
+            }
+        };
+        int count = 0;
+        for (; i < mats.size() && count < kNsMats; ++i, ++count) {
+            size_t k = 0;
+            while (k < shapes.size() && !(shapes[k].rows == mats[i].rows && shapes[k].cols == mats[i].cols)) ++k;
+            if (k == shapes.size()) {
+                if (k == size_t(kNsGroups)) break;
+                shapes.push_back({mats[i].rows, mats[i].cols, {}});
+            }
+            shapes[k].off.push_back(mats[i].offset);
+            gap(mats[i].offset);
+            at = mats[i].offset + int64_t(mats[i].rows) * mats[i].cols;
+        }
+        if (i == mats.size()) {
+            gap(n_params);
+            at = n_params;
+        }
+        P.block0 = plan.nblocks;
+        int o = 0;
+        for (const Shape& sh : shapes) {
+            NsGroup& G = P.a.g[P.a.ng];
+            ns_shape(G, sh.rows, sh.cols, int(sh.off.size()));
+            G.first = first + o;
+            G.table = 1 + o;
+            for (int64_t f : sh.off) P.a.off[o++] = f;
+            // the spectral norm that keeps a layer's output as large as its input, or the root mean
+            // square of an Adam update
+            const double fi = sh.rows, fo = sh.cols;
+            G.scale = float(scale_mode == 0 ? std::sqrt(std::max(1.0, fo / fi)) : 0.2 * std::sqrt(std::max(fi, fo)));
+            P.a.start[P.a.ng++] = P.sums;
+            G.part0 = P.block0 + P.sums;
+            P.sums += G.batch * G.nsum;
+            P.planes += G.batch * int((int64_t(G.rp) * G.cp + kPrepElems - 1) / kPrepElems);
+        }
+        P.a.start[P.a.ng] = P.sums;
+        first += o;
+        for (int k = 0; k < P.e.ngaps; ++k) {   // 4096 elements a block, at most 256 a gap
+            P.e.gap_start[k + 1] =
+                P.e.gap_start[k] + int(std::max<int64_t>(1, std::min<int64_t>(256, (P.e.gap_len[k] + 4095) / 4096)));
+        }
+        P.sums += P.e.gap_start[P.e.ngaps];
+        P.planes += P.e.gap_start[P.e.ngaps];
+        plan.nblocks += P.sums;
+        plan.pass.push_back(P);
+    } while (i < mats.size());
+    const int64_t sums = a256(int64_t(first) * 8), base = sums + a256(int64_t(plan.nblocks) * 24);
+    for (MuonPlan::Pass& P : plan.pass) {
+        P.a.info = 0;
+        P.a.sums = sums;
+        int64_t end = base;   // passes follow each other in the same memory
+        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSeg);
+        plan.total = std::max(plan.total, end);
+        P.e.nblocks = plan.nblocks;
+    }
+    return plan;
+}
+
+}  // namespace
+
+size_t muon_step_ws_bytes(int64_t n_params, const std::vector<MuonMat>& mats, int steps) {
+    return size_t(muon_plan(n_params, mats, steps, 0).total);
+}
+
+hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void* ws, hipStream_t s) {
+    if (m.n <= 0) return hipSuccess;
+    MuonPlan plan = muon_plan(m.n, mats, m.steps, m.scale_mode);
+    NsProgram P;
+    ns_program(m.steps, m.coeffs, P);
+    ProfScope ps(s, [&] { return "muon/" + std::to_string(m.n); });
+    for (MuonPlan::Pass& p : plan.pass) {
+        p.a.ws = static_cast<char*>(ws);
+        MuonElem& e = p.e;
+        const OptArgs& o = m.adam;
+        e.n_params = m.n; e.p = o.p; e.g = o.g; e.m = o.m; e.v = o.v;
+        e.mu = m.momentum; e.omu = m.omu; e.nesterov = m.nesterov;
+        e.c1 = m.nesterov ? m.omu * (1.f + m.momentum) : m.omu;
+        e.c2 = m.nesterov ? m.momentum * m.momentum : m.momentum;
+        e.b1 = o.b1; e.b2 = o.b2; e.omb1 = o.omb1; e.omb2 = o.omb2; e.bc1 = o.bc1; e.bc2 = o.bc2;
+        e.alr = o.lr; e.aeps = o.eps; e.max_norm = o.max_norm; e.eps = m.eps;
+        e.stats = m.stats; e.mir = o.mir; e.mir_off = o.mir_off; e.mir_len = o.mir_len;
+        NS_LAUNCH((ns_sums_kernel<NS_SRC_STEP>), p.sums, 0, p.a, e, nullptr, p.block0);
+    }
+    for (const MuonPlan::Pass& p : plan.pass) {
+        // the planes' blocks by group, then the gaps' (counted from start[ng])
+        int n;
+        const NsArgs r = ns_select(p.a, [](const NsGroup&) { return true; }, [](const NsGroup& G) {
+            return G.batch * int((int64_t(G.rp) * G.cp + kPrepElems - 1) / kPrepElems);
+        }, n);
+        NS_LAUNCH((ns_planes_kernel<NS_SRC_STEP, 2>), p.planes, 0, r, p.e, nullptr, 0.f, p.block0);
+        if (p.a.ng == 0) continue;
+        NsApply ap{};
+        ap.out = NS_OUT_STEP;
+        ap.p = m.adam.p;
+        ap.decay = m.decay; ap.lr = m.lr;
+        ap.mir = m.adam.mir; ap.mir_off = m.adam.mir_off; ap.mir_len = m.adam.mir_len;
+        const hipError_t err = ns_run(p.a, P, 2, ap, s);
+        if (err != hipSuccess) return err;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace cb
