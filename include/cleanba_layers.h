@@ -167,7 +167,7 @@ impala_status_t impala_groupnorm_fwd(impala_prec_t prec, int64_t n, int32_t H, i
                                      size_t ws_bytes, hipStream_t stream);
 
 /* Backward of impala_groupnorm_fwd from the gradient dy at y and the mean and rstd it left. With
- * xh = (x - mean) rstd, da = dy act'(z) (relu: dy where z > 0, decided in 64 bits next to zero) and
+ * xh = (x - mean) rstd, da = dy act'(z) (relu: dy where z > 0, decided as the exact z would) and
  * h = da gamma[c]:
  *   dbeta[c] = sum da,  dgamma[c] = sum da xh  (over frames and pixels),
  *   dx = rstd (h - mean_group(h) - xh mean_group(h xh)).

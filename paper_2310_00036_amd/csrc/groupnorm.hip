@@ -13,7 +13,9 @@
 // are two-pass (mean, then the squares about it) and x is still read once. A frame that fits one
 // workgroup is done in one launch; a larger one is cut into chunks whose statistics are combined
 // exactly (sums of squares about the chunks' own means, then about the common one) by a small second
-// launch, and a third applies them.
+// launch, and a third applies them. bf16 elements cost vector instructions before they cost bandwidth
+// (57.8 M elements at 60 instructions are 88 us, their traffic 68), so an element's work is folded into
+// per-channel constants: z = (x - mu) k + beta, dx = da k + (x - mu) c2 + c3.
 //
 // A thread keeps one column of V channels (16 bytes, or one channel where C or an address does not
 // allow it) for all its pixels; columns are padded to a power of two per pixel so that the threads of
@@ -63,31 +65,57 @@ enum { GN_NONE = 0, GN_RELU = 1, GN_SILU = 2 };
 
 CB_DEV float gn_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
-CB_DEV float gn_act(float z, int act) {
+template <int ACT>
+CB_DEV float gn_act(float z, int act_) {
+    const int act = ACT < 0 ? act_ : ACT;
     if (act == GN_RELU) return relu_f(z);
     if (act == GN_SILU) return z * gn_sigmoid(z);
     return z;
 }
 
-// dy act'(z). The relu's decision next to its border is taken in 64 bits: with |z| within rounding
-// of zero, 32 bits would decide by the order of their roundings (one element in 10^6 or so).
-CB_DEV float gn_dact(float dy, float x, float mu, float rs, float ga, float be, float xh, int act) {
-    if (act == GN_NONE) return dy;
-    const float t = xh * ga, z = t + be;
-    if (act == GN_RELU) {
-        bool pos = z > 0.f;
-        if (fabsf(z) <= 0x1p-20f * (fabsf(t) + fabsf(be)))
-            pos = (double(x) - double(mu)) * double(rs) * double(ga) + double(be) > 0.0;
-        return pos ? dy : 0.f;
+// A channel's constants: d = x - mu, xh = d rstd, z = d k + be with k = rstd gamma. The relu's decision
+// z > 0 is x beyond t = mu - be / k on the side that k's sign says: s x > s t with s = +-1. It is taken
+// against the largest float32 that is no larger than s t, formed in 64 bits once a channel, so it is
+// the decision of the exact z for every x, where z itself in 32 bits would decide by its rounding (one
+// element in 10^6); and the sign of s x - T is exact in one fma.
+// bf16 activations (CEN = 0) take x for x - mu with mu in the constants: fewer registers and instructions,
+// and what cancels, 2^-24 |mu| rstd, is far below the 2^-9 |mu| rstd that their own rounding leaves.
+struct GnChannel { float mu, k, p, q; };   // relu: p = s, q = -T; silu: p = be (CEN) or be - mu k
+// da = dy act'(z) of V channels, and d (x itself without CEN). ACT < 0: the activation is a.act.
+template <class Vec, int V, int ACT, int CEN>
+CB_DEV void gn_dact(const GnArgs& a, const typename Vec::Raw& rx, const typename Vec::Raw& rd,
+                    const GnChannel (&ch)[V], float (&d)[V], float (&da)[V]) {
+    const int act = ACT < 0 ? a.act : ACT;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const float x = Vec::get(rx, e);
+        d[e] = CEN ? x - ch[e].mu : x;
+        da[e] = Vec::get(rd, e);
+        if (act == GN_RELU) {
+            da[e] = __builtin_fmaf(x, ch[e].p, ch[e].q) > 0.f ? da[e] : 0.f;
+        } else if (act == GN_SILU) {
+            const float z = __builtin_fmaf(d[e], ch[e].k, ch[e].p), s = gn_sigmoid(z);
+            da[e] *= s * (1.f + z * (1.f - s));
+        }
     }
-    const float s = gn_sigmoid(z);
-    return dy * (s * (1.f + z * (1.f - s)));
 }
 
 // The wave's sum over the lanes that share the low bits below `from` (a power of two).
 CB_DEV float gn_lanes(float v, int from) {
     for (int m = from; m < 64; m <<= 1) v += __shfl_xor(v, m);
     return v;
+}
+
+// ... of V values: their exchanges run together.
+template <int V>
+CB_DEV void gn_lanes_each(float (&v)[V], int from) {
+    for (int m = from; m < 64; m <<= 1) {
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = __shfl_xor(v[e], m);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += o[e];
+    }
 }
 
 // Sums of per-thread column values over the workgroup, by group: val[0..V) are this thread's channels
@@ -103,10 +131,8 @@ CB_DEV void gn_group_sums(const GnArgs& a, float (&val)[V], float scale, float* 
         for (int e = 1; e < V; ++e) val[0] += val[e];
     }
     if (a.cvp < 64) {
-        val[0] = gn_lanes(val[0], a.cvp);
-        if (!one)
-#pragma unroll
-            for (int e = 1; e < V; ++e) val[e] = gn_lanes(val[e], a.cvp);
+        if (one) val[0] = gn_lanes(val[0], a.cvp);
+        else gn_lanes_each<V>(val, a.cvp);
     }
     const int per = a.cvp < 64 ? 64 : a.cvp, row = t / per, R = NT / per;
     if (a.cvp >= 64 || lane < a.cvp) {
@@ -134,10 +160,7 @@ template <int V, int NT>
 CB_DEV void gn_channel_sums(const GnArgs& a, float (&val)[V], float* red, float* out) {
     const int t = threadIdx.x, lane = t & 63, col = t & (a.cvp - 1);
     const int w = a.cvp * V;
-    if (a.cvp < 64) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) val[e] = gn_lanes(val[e], a.cvp);
-    }
+    if (a.cvp < 64) gn_lanes_each<V>(val, a.cvp);
     const int per = a.cvp < 64 ? 64 : a.cvp, row = t / per, R = NT / per;
     if (a.cvp >= 64 || lane < a.cvp)
 #pragma unroll
@@ -156,46 +179,147 @@ template <int NT>
 struct GnPos {
     int64_t base;     // first element of the chunk
     int rows, row, rpp, col;
+    int g0, r0;       // group of the column's first channel, and its place in the group
     bool on;
     CB_DEV GnPos(const GnArgs& a, int64_t f, int ck) {
         const int t = threadIdx.x;
         col = t & (a.cvp - 1);
         row = t >> a.cvs;
         rpp = NT >> a.cvs;
-        const int r0 = ck * a.crows;
-        rows = min(a.crows, a.HW - r0);
-        base = (f * a.HW + r0) * a.C;
+        const int first = ck * a.crows;
+        rows = min(a.crows, a.HW - first);
+        base = (f * a.HW + first) * a.C;
         on = col < a.cv;
+        const int c0 = on ? col * (a.C / a.cv) : 0;
+        g0 = c0 / a.cg;
+        r0 = c0 - g0 * a.cg;
     }
 };
 
+// After each vector of a pass: the next one's work does not start early (its registers would add up).
+CB_DEV void gn_step() { __builtin_amdgcn_sched_barrier(0); }
+
+// The chunk as a buffer resource: what lies past its end, or in a padding column, reads as zero and is not
+// written, without a branch (one around each load would make the wave wait for each).
+template <class Raw>
+CB_DEV Raw gn_get(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    if constexpr (sizeof(Raw) == 16) return __builtin_bit_cast(Raw, buf_load16(r, off));
+    else if constexpr (sizeof(Raw) == 4) return __builtin_bit_cast(Raw, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+    else return __builtin_bit_cast(Raw, __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
+}
+template <class Raw>
+CB_DEV void gn_put(__amdgpu_buffer_rsrc_t r, uint32_t off, Raw v) {
+    if constexpr (sizeof(Raw) == 16) buf_store16(r, off, __builtin_bit_cast(uint4, v));
+    else if constexpr (sizeof(Raw) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, off, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), r, off, 0, 0);
+}
+template <class P, int NT>
+CB_DEV __amdgpu_buffer_rsrc_t gn_rsrc(const void* base, const GnArgs& a, const GnPos<NT>& p) {
+    return buf_rsrc(static_cast<const typename P::T*>(base) + p.base, uint32_t(p.rows) * uint32_t(a.C) * sizeof(typename P::T));
+}
 template <class P, int V, int NV, int NT>
 CB_DEV void gn_load(const void* src, const GnArgs& a, const GnPos<NT>& p, typename GnVec<P, V>::Raw (&raw)[NV]) {
-    using Raw = typename GnVec<P, V>::Raw;
-    const typename P::T* x = static_cast<const typename P::T*>(src) + p.base + p.col * V;
+    const auto rs = gn_rsrc<P, NT>(src, a, p);
+    const uint32_t es = sizeof(typename P::T), step = uint32_t(p.rpp) * uint32_t(a.C) * es;
+    const uint32_t off = p.on ? (uint32_t(p.row) * uint32_t(a.C) + uint32_t(p.col * V)) * es : kOOB;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) raw[j] = gn_get<typename GnVec<P, V>::Raw>(rs, off + uint32_t(j) * step);
+}
+// f(j) -> the vector to store, for every slot that the chunk has.
+template <class P, int V, int NV, int NT, class Fn>
+CB_DEV void gn_store(void* dst, const GnArgs& a, const GnPos<NT>& p, Fn&& f) {
+    const auto rs = gn_rsrc<P, NT>(dst, a, p);
+    const uint32_t es = sizeof(typename P::T), step = uint32_t(p.rpp) * uint32_t(a.C) * es;
+    const uint32_t off = p.on ? (uint32_t(p.row) * uint32_t(a.C) + uint32_t(p.col * V)) * es : kOOB;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (j * p.rpp < p.rows) {
+            gn_put<typename GnVec<P, V>::Raw>(rs, off + uint32_t(j) * step, f(j));
+            gn_step();
+        }
+}
+
+// Before each pass over the register chunk: the values that follow are formed anew from the raw words, where
+// the compiler would keep the floats of the pass before (twice the registers: one workgroup per CU
+// instead of two).
+template <class Raw, int NV>
+CB_DEV void gn_again(Raw (&raw)[NV]) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int r = p.row + j * p.rpp;
-        raw[j] = Raw{};
-        if (p.on && r < p.rows) raw[j] = *reinterpret_cast<const Raw*>(x + int64_t(r) * a.C);
+        if constexpr (sizeof(Raw) == 16) {
+            uint4 u = __builtin_bit_cast(uint4, raw[j]);
+            asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));
+            raw[j] = __builtin_bit_cast(Raw, u);
+        }
     }
 }
 
-// The thread's V channels of a per-channel or (by group) per-group vector.
-template <int V>
-CB_DEV void gn_per_channel(const float* v, int c0, int C, float other, float (&out)[V]) {
+// The thread's V channels of a per-channel vector (NULL: `other`). A column that is on lies inside the
+// channels whole.
+template <int V, class Pos>
+CB_DEV void gn_per_channel(const float* v, const Pos& p, float other, float (&out)[V]) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) out[e] = v && c0 + e < C ? v[c0 + e] : other;
+    for (int e = 0; e < V; ++e) out[e] = other;
+    if (!v || !p.on) return;
+    if constexpr (V == 1) {
+        out[0] = v[p.col];
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+            const float4 q = load_f4(v + p.col * V + e);
+            out[e] = q.x; out[e + 1] = q.y; out[e + 2] = q.z; out[e + 3] = q.w;
+        }
+    }
 }
-template <int V>
-CB_DEV void gn_per_group(const float* v, int c0, int C, int cg, float (&out)[V]) {
+// ... and of a per-group vector: one group where the groups are whole columns, else counted on from the
+// first channel's (a division per channel would be most of the kernel's instructions).
+template <int V, class Pos>
+CB_DEV void gn_per_group(const float* v, const GnArgs& a, const Pos& p, float (&out)[V]) {
+    if (a.cg % V == 0) {
+        const float q = v[p.g0];
 #pragma unroll
-    for (int e = 0; e < V; ++e) out[e] = c0 + e < C ? v[(c0 + e) / cg] : 0.f;
+        for (int e = 0; e < V; ++e) out[e] = q;
+    } else {
+        int g = p.g0, r = p.r0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            out[e] = v[min(g, a.G - 1)];
+            if (++r == a.cg) { r = 0; ++g; }
+        }
+    }
+}
+
+template <int V, int ACT, int CEN, class Pos>
+CB_DEV void gn_channels(const GnArgs& a, int64_t f, const Pos& p, GnChannel (&ch)[V]) {
+    const int act = ACT < 0 ? a.act : ACT;
+    float mu[V], rs[V], ga[V], be[V];
+    gn_per_group<V>(a.mean + f * a.G, a, p, mu);
+    gn_per_group<V>(a.rstd + f * a.G, a, p, rs);
+    gn_per_channel<V>(a.gamma, p, 1.f, ga);
+    gn_per_channel<V>(a.beta, p, 0.f, be);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        ch[e].mu = mu[e];
+        ch[e].k = rs[e] * ga[e];
+        ch[e].p = CEN ? be[e] : __builtin_fmaf(-mu[e], ch[e].k, be[e]);
+        ch[e].q = 0.f;
+        if (act == GN_RELU) {
+            const double k = double(rs[e]) * double(ga[e]);
+            const double t = k == 0.0 ? (be[e] > 0.f ? -__builtin_inf() : __builtin_inf()) : double(mu[e]) - double(be[e]) / k;
+            const double st = k < 0.0 ? -t : t;
+            float T = float(st);
+            if (double(T) > st) T = T > 0.f ? __uint_as_float(__float_as_uint(T) - 1)
+                                    : T < 0.f ? __uint_as_float(__float_as_uint(T) + 1) : -0x1p-149f;
+            ch[e].p = k < 0.0 ? -1.f : 1.f;
+            ch[e].q = -T;
+            gn_step();
+        }
+    }
 }
 
 // Forward statistics of one chunk per workgroup, and (WHOLE: the chunk is the frame) the output.
 // Chunks leave their mean and sum of squares about it in ws [n][chunks][2][G].
-template <class P, int V, int NV, int NT, int WHOLE>
+template <class P, int V, int NV, int NT, int WHOLE, int ACT>
 __global__ __launch_bounds__(NT) void gn_fwd_kernel(GnArgs a) {
     using Vec = GnVec<P, V>;
     __shared__ float red[NT * V];
@@ -205,7 +329,6 @@ __global__ __launch_bounds__(NT) void gn_fwd_kernel(GnArgs a) {
     const GnPos<NT> p(a, f, ck);
     typename Vec::Raw raw[NV];
     gn_load<P, V, NV, NT>(a.x, a, p, raw);
-    const int c0 = p.col * V;
     const float inv = 1.f / (float(p.rows) * float(a.cg));
     float s[V];
 #pragma unroll
@@ -216,17 +339,20 @@ __global__ __launch_bounds__(NT) void gn_fwd_kernel(GnArgs a) {
         for (int e = 0; e < V; ++e) s[e] += Vec::get(raw[j], e);
     gn_group_sums<V, NT>(a, s, inv, red, gmean);
     float mu[V];
-    gn_per_group<V>(gmean, c0, a.C, a.cg, mu);
+    gn_per_group<V>(gmean, a, p, mu);
 #pragma unroll
     for (int e = 0; e < V; ++e) s[e] = 0.f;
+    gn_again(raw);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
         if (p.on && p.row + j * p.rpp < p.rows)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float d = Vec::get(raw[j], e) - mu[e];
-                s[e] += d * d;
+                s[e] = __builtin_fmaf(d, d, s[e]);
             }
+        gn_step();
+    }
     gn_group_sums<V, NT>(a, s, 1.f, red, gm2);
     if constexpr (!WHOLE) {
         float* o = a.part + (f * a.chunks + ck) * 2 * a.G;
@@ -236,26 +362,25 @@ __global__ __launch_bounds__(NT) void gn_fwd_kernel(GnArgs a) {
         }
     } else {
         float ga[V], be[V], rs[V];
-        gn_per_group<V>(gm2, c0, a.C, a.cg, rs);
+        gn_per_group<V>(gm2, a, p, rs);
 #pragma unroll
         for (int e = 0; e < V; ++e) rs[e] = 1.f / sqrtf(rs[e] * inv + a.eps);
         for (int g = threadIdx.x; g < a.G; g += NT) {
             if (a.mean) a.mean[f * a.G + g] = gmean[g];
             if (a.rstd) a.rstd[f * a.G + g] = 1.f / sqrtf(gm2[g] * inv + a.eps);
         }
-        gn_per_channel<V>(a.gamma, c0, a.C, 1.f, ga);
-        gn_per_channel<V>(a.beta, c0, a.C, 0.f, be);
-        typename P::T* y = static_cast<typename P::T*>(a.y) + p.base + c0;
+        gn_per_channel<V>(a.gamma, p, 1.f, ga);
+        gn_per_channel<V>(a.beta, p, 0.f, be);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int r = p.row + j * p.rpp;
-            if (!(p.on && r < p.rows)) continue;
+        for (int e = 0; e < V; ++e) rs[e] *= ga[e];
+        gn_again(raw);
+        gn_store<P, V, NV, NT>(a.y, a, p, [&](int j) CB_INLINE_LAMBDA {
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                v[e] = gn_act((Vec::get(raw[j], e) - mu[e]) * rs[e] * ga[e] + be[e], a.act);
-            *reinterpret_cast<typename Vec::Raw*>(y + int64_t(r) * a.C) = Vec::put(v);
-        }
+                v[e] = gn_act<ACT>(__builtin_fmaf(Vec::get(raw[j], e) - mu[e], rs[e], be[e]), a.act);
+            return Vec::put(v);
+        });
     }
 }
 
@@ -287,159 +412,157 @@ __global__ __launch_bounds__(256) void gn_stats_kernel(GnArgs a) {
     }
 }
 
-template <class P, int V, int NV, int NT>
+template <class P, int V, int NV, int NT, int ACT>
 __global__ __launch_bounds__(NT) void gn_apply_kernel(GnArgs a) {
     using Vec = GnVec<P, V>;
     const int64_t f = blockIdx.x / unsigned(a.chunks);
     const GnPos<NT> p(a, f, int(blockIdx.x % unsigned(a.chunks)));
     typename Vec::Raw raw[NV];
     gn_load<P, V, NV, NT>(a.x, a, p, raw);
-    const int c0 = p.col * V;
     float mu[V], rs[V], ga[V], be[V];
-    gn_per_group<V>(a.smean + f * a.G, c0, a.C, a.cg, mu);
-    gn_per_group<V>(a.srstd + f * a.G, c0, a.C, a.cg, rs);
-    gn_per_channel<V>(a.gamma, c0, a.C, 1.f, ga);
-    gn_per_channel<V>(a.beta, c0, a.C, 0.f, be);
-    typename P::T* y = static_cast<typename P::T*>(a.y) + p.base + c0;
+    gn_per_group<V>(a.smean + f * a.G, a, p, mu);
+    gn_per_group<V>(a.srstd + f * a.G, a, p, rs);
+    gn_per_channel<V>(a.gamma, p, 1.f, ga);
+    gn_per_channel<V>(a.beta, p, 0.f, be);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int r = p.row + j * p.rpp;
-        if (!(p.on && r < p.rows)) continue;
+    for (int e = 0; e < V; ++e) rs[e] *= ga[e];
+    gn_store<P, V, NV, NT>(a.y, a, p, [&](int j) CB_INLINE_LAMBDA {
         float v[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = gn_act((Vec::get(raw[j], e) - mu[e]) * rs[e] * ga[e] + be[e], a.act);
-        *reinterpret_cast<typename Vec::Raw*>(y + int64_t(r) * a.C) = Vec::put(v);
-    }
+        for (int e = 0; e < V; ++e) v[e] = gn_act<ACT>(__builtin_fmaf(Vec::get(raw[j], e) - mu[e], rs[e], be[e]), a.act);
+        return Vec::put(v);
+    });
 }
 
 // Backward. STEP 0: the chunk is the frame: sums, then dx. STEP 1: the chunk's per-channel sums of da
-// and da xh to part [n][chunks][2][C]. STEP 2: dx of the chunk from the frame's means of h and h xh.
-// STEP 0 leaves the frame's channel sums in fsum [n][2][C].
-template <class P, int V, int NV, int NT, int STEP>
-__global__ __launch_bounds__(NT) void gn_bwd_kernel(GnArgs a) {
+// and da xh to part [n][chunks][2][C]. STEP 2: dx of the chunk. The frame's channel sums are in fsum
+// [n][2][C] (left there by STEP 0, read by STEP 2); its means of h and h xh are formed from them.
+template <class P, int V, int NV, int NT, int STEP, int ACT>
+__global__ __launch_bounds__(NT, V == 8 && STEP == 0 ? 4 : 1) void gn_bwd_kernel(GnArgs a) {
     using Vec = GnVec<P, V>;
+    constexpr int CEN = sizeof(typename P::T) == 4;
     __shared__ float red[STEP == 2 ? 1 : NT * V];
-    __shared__ float cb_[STEP == 2 ? 1 : kGnMaxC], cg_[STEP == 2 ? 1 : kGnMaxC];
-    __shared__ float m1s[STEP == 0 ? kGnMaxC : 1], m2s[STEP == 0 ? kGnMaxC : 1];
+    __shared__ float sums[2 * kGnMaxC];
+    __shared__ float m1s[STEP == 1 ? 1 : kGnMaxC], m2s[STEP == 1 ? 1 : kGnMaxC];
     const int64_t f = STEP == 0 ? blockIdx.x : blockIdx.x / unsigned(a.chunks);
     const int ck = STEP == 0 ? 0 : int(blockIdx.x % unsigned(a.chunks));
     const GnPos<NT> p(a, f, ck);
     typename Vec::Raw rx[NV], rd[NV];
     gn_load<P, V, NV, NT>(a.x, a, p, rx);
     gn_load<P, V, NV, NT>(a.dy, a, p, rd);
-    const int c0 = p.col * V;
-    float mu[V], rs[V], ga[V], be[V];
-    gn_per_group<V>(a.mean + f * a.G, c0, a.C, a.cg, mu);
-    gn_per_group<V>(a.rstd + f * a.G, c0, a.C, a.cg, rs);
-    gn_per_channel<V>(a.gamma, c0, a.C, 1.f, ga);
-    gn_per_channel<V>(a.beta, c0, a.C, 0.f, be);
+    GnChannel ch[V];
+    gn_channels<V, ACT, CEN>(a, f, p, ch);
     const int t = threadIdx.x;
     if constexpr (STEP != 2) {
         float sb[V], sg[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) sb[e] = sg[e] = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (p.on && p.row + j * p.rpp < p.rows)
+        for (int j = 0; j < NV; ++j)   // (slots outside the chunk: dy = 0)
+            if (j * p.rpp < p.rows) {
+                float d[V], da[V];
+                gn_dact<Vec, V, ACT, CEN>(a, rx[j], rd[j], ch, d, da);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float x = Vec::get(rx[j], e), xh = (x - mu[e]) * rs[e];
-                    const float da = gn_dact(Vec::get(rd[j], e), x, mu[e], rs[e], ga[e], be[e], xh, a.act);
-                    sb[e] += da;
-                    sg[e] += da * xh;
+                    sb[e] += da[e];
+                    sg[e] = __builtin_fmaf(da[e], d[e], sg[e]);
                 }
-        gn_channel_sums<V, NT>(a, sb, red, cb_);
-        gn_channel_sums<V, NT>(a, sg, red, cg_);
-        float* o = STEP == 0 ? a.fsum + f * 2 * a.C : a.part + (f * a.chunks + ck) * 2 * a.C;
-        for (int c = t; c < a.C; c += NT) {
-            o[c] = cb_[c];
-            o[a.C + c] = cg_[c];
+                gn_step();
+            }
+        gn_again(rx);
+        gn_again(rd);
+        float rs[V];
+        gn_per_group<V>(a.rstd + f * a.G, a, p, rs);
+        if constexpr (!CEN) {
+            float mu[V];
+            gn_per_group<V>(a.mean + f * a.G, a, p, mu);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sg[e] = __builtin_fmaf(-mu[e], sb[e], sg[e]);
         }
+#pragma unroll
+        for (int e = 0; e < V; ++e) sg[e] *= rs[e];
+        gn_channel_sums<V, NT>(a, sb, red, sums);
+        gn_channel_sums<V, NT>(a, sg, red, sums + a.C);
+        float* o = STEP == 0 ? a.fsum + f * 2 * a.C : a.part + (f * a.chunks + ck) * 2 * a.C;
+        for (int c = t; c < 2 * a.C; c += NT) o[c] = sums[c];
+    } else {
+        for (int c = t; c < 2 * a.C; c += NT) sums[c] = a.fsum[f * 2 * a.C + c];
+        __syncthreads();
     }
     if constexpr (STEP == 1) return;
-    float m1[V], m2[V];
-    if constexpr (STEP == 0) {
-        const float inv = 1.f / (float(a.HW) * float(a.cg));
-        for (int g = t >> 6; g < a.G; g += NT / 64) {
-            float u = 0.f, v = 0.f;
-            for (int c = g * a.cg + (t & 63); c < (g + 1) * a.cg; c += 64) {
-                const float gm = a.gamma ? a.gamma[c] : 1.f;
-                u += gm * cb_[c];
-                v += gm * cg_[c];
-            }
-            u = gn_lanes(u, 1);
-            v = gn_lanes(v, 1);
-            if ((t & 63) == 0) {
-                m1s[g] = u * inv;
-                m2s[g] = v * inv;
-            }
+    const float inv = 1.f / (float(a.HW) * float(a.cg));
+    for (int g = t >> 6; g < a.G; g += NT / 64) {
+        float u = 0.f, v = 0.f;
+        for (int c = g * a.cg + (t & 63); c < (g + 1) * a.cg; c += 64) {
+            const float gm = a.gamma ? a.gamma[c] : 1.f;
+            u += gm * sums[c];
+            v += gm * sums[a.C + c];
         }
-        __syncthreads();
-        gn_per_group<V>(m1s, c0, a.C, a.cg, m1);
-        gn_per_group<V>(m2s, c0, a.C, a.cg, m2);
-    } else {
-        gn_per_group<V>(a.smean + f * a.G, c0, a.C, a.cg, m1);
-        gn_per_group<V>(a.srstd + f * a.G, c0, a.C, a.cg, m2);
-    }
-    typename P::T* dx = static_cast<typename P::T*>(a.y) + p.base + c0;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int r = p.row + j * p.rpp;
-        if (!(p.on && r < p.rows)) continue;
-        float v[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float x = Vec::get(rx[j], e), xh = (x - mu[e]) * rs[e];
-            const float da = gn_dact(Vec::get(rd[j], e), x, mu[e], rs[e], ga[e], be[e], xh, a.act);
-            v[e] = rs[e] * (da * ga[e] - m1[e] - xh * m2[e]);
+        u = gn_lanes(u, 1);
+        v = gn_lanes(v, 1);
+        if ((t & 63) == 0) {
+            m1s[g] = u * inv;
+            m2s[g] = v * inv;
         }
-        *reinterpret_cast<typename Vec::Raw*>(dx + int64_t(r) * a.C) = Vec::put(v);
-    }
-}
-
-// A frame's channel sums from its chunks' (fsum [n][2][C]), and its means of h and h xh (smean, srstd
-// [n][G]): one workgroup per frame.
-__global__ __launch_bounds__(256) void gn_bwd_means_kernel(GnArgs a) {
-    __shared__ float ch[2 * kGnMaxC];
-    const int64_t f = blockIdx.x;
-    const float* part = a.part + f * a.chunks * 2 * a.C;
-    for (int c = threadIdx.x; c < 2 * a.C; c += 256) {
-        double s = 0.0;
-        for (int k = 0; k < a.chunks; ++k) s += part[int64_t(k) * 2 * a.C + c];
-        ch[c] = float(s);
-        a.fsum[f * 2 * a.C + c] = float(s);
     }
     __syncthreads();
-    const double inv = 1.0 / (double(a.HW) * a.cg);
-    for (int g = threadIdx.x; g < a.G; g += 256) {
-        double u = 0.0, v = 0.0;
-        for (int c = g * a.cg; c < (g + 1) * a.cg; ++c) {
-            const double gm = a.gamma ? a.gamma[c] : 1.f;
-            u += gm * ch[c];
-            v += gm * ch[a.C + c];
-        }
-        a.smean[f * a.G + g] = float(u * inv);
-        a.srstd[f * a.G + g] = float(v * inv);
+    // dx = rs (da ga - m1 - xh m2) = da k + d c2 + c3; mu and k are read again rather than kept over the
+    // first pass (kept, they spill, and the scratch memory's writes cost more than the loads)
+    float c2[V], c3[V], k[V], rs[V];
+    gn_per_group<V>(m1s, a, p, c3);
+    gn_per_group<V>(m2s, a, p, c2);
+    gn_per_group<V>(a.rstd + f * a.G, a, p, rs);
+    gn_per_channel<V>(a.gamma, p, 1.f, k);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        c3[e] *= -rs[e];
+        c2[e] *= -rs[e] * rs[e];
+        k[e] *= rs[e];
     }
+    if constexpr (!CEN) {
+        float mu[V];
+        gn_per_group<V>(a.mean + f * a.G, a, p, mu);
+#pragma unroll
+        for (int e = 0; e < V; ++e) c3[e] = __builtin_fmaf(-mu[e], c2[e], c3[e]);
+    }
+    gn_store<P, V, NV, NT>(a.y, a, p, [&](int j) CB_INLINE_LAMBDA {
+        float d[V], da[V], v[V];
+        gn_dact<Vec, V, ACT, CEN>(a, rx[j], rd[j], ch, d, da);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf(da[e], k[e], __builtin_fmaf(d[e], c2[e], c3[e]));
+        return Vec::put(v);
+    });
 }
 
-// dbeta and dgamma: the frames' channel sums added in a fixed order, in 64 bits. A workgroup takes 4
-// columns in 64 slices of the frames.
-__global__ __launch_bounds__(256) void gn_params_kernel(GnArgs a, float* dgamma, float* dbeta) {
-    __shared__ double sh[256];
-    const int c = blockIdx.x * 4 + (threadIdx.x & 3), sl = threadIdx.x >> 2;
+// Column sums of x [sets][rows][cols] in a fixed order, in 64 bits: out [sets][cols]; with out2, the
+// columns from `half` on go there. A workgroup takes 4 columns in 256 slices of the rows.
+__global__ __launch_bounds__(1024) void gn_columns_kernel(const float* __restrict__ x, int64_t rows, int cols, int half,
+                                                          float* out, float* out2) {
+    __shared__ double sh[1024];
+    const int blocks = (cols + 3) / 4, c = int(blockIdx.x % blocks) * 4 + (threadIdx.x & 3), sl = threadIdx.x >> 2;
+    const int64_t set = blockIdx.x / blocks;
     double s = 0.0;
-    if (c < 2 * a.C)
-        for (int64_t f = sl; f < a.n; f += 64) s += a.fsum[f * 2 * a.C + c];
+    if (c < cols) {
+        const float* p = x + set * rows * cols + c;
+        int64_t r = sl;
+        for (; r + 7 * 256 < rows; r += 8 * 256) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = p[(r + 256 * u) * cols];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += v[u];
+        }
+        for (; r < rows; r += 256) s += p[r * cols];
+    }
     sh[threadIdx.x] = s;
     __syncthreads();
-    for (int w = 32; w >= 1; w >>= 1) {
+    for (int w = 128; w >= 1; w >>= 1) {
         if (sl < w) sh[threadIdx.x] += sh[threadIdx.x + 4 * w];
         __syncthreads();
     }
-    if (sl == 0 && c < 2 * a.C) {
-        float* o = c < a.C ? dbeta : dgamma;
-        if (o) o[c < a.C ? c : c - a.C] = float(sh[threadIdx.x]);
+    if (sl == 0 && c < cols) {
+        float* o = c < half ? out : out2;
+        if (o) o[set * half + (c < half ? c : c - half)] = float(sh[threadIdx.x]);
     }
 }
 
@@ -499,19 +622,40 @@ bool gn_vec_ok(int prec, int C, std::initializer_list<const void*> ptrs) {
     return true;
 }
 
-template <class P, int V>
+// ACT < 0 (the activation chosen in the kernel) for one-channel columns
+template <class P, int V, int ACT>
 void gn_fwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
     const dim3 grid(unsigned(a.n * a.chunks));
 #define GN_W(K, NT, NV) \
-    if (p.whole && p.shape == K) hipLaunchKernelGGL((gn_fwd_kernel<P, V, NV, NT, 1>), grid, dim3(NT), 0, s, a);
+    if (p.whole && p.shape == K) hipLaunchKernelGGL((gn_fwd_kernel<P, V, NV, NT, 1, ACT>), grid, dim3(NT), 0, s, a);
     GN_W(0, 256, 2) GN_W(1, 256, 8) GN_W(2, 512, 8) GN_W(3, 1024, 8)
 #undef GN_W
     if (p.whole) return;
 #define GN_C(K, NT, NV)                                                                             \
     if (p.shape == K) {                                                                             \
-        hipLaunchKernelGGL((gn_fwd_kernel<P, V, NV, NT, 0>), grid, dim3(NT), 0, s, a);              \
+        hipLaunchKernelGGL((gn_fwd_kernel<P, V, NV, NT, 0, -1>), grid, dim3(NT), 0, s, a);          \
         hipLaunchKernelGGL(gn_stats_kernel, dim3(unsigned(a.n)), dim3(256), 0, s, a);               \
-        hipLaunchKernelGGL((gn_apply_kernel<P, V, NV, NT>), grid, dim3(NT), 0, s, a);               \
+        hipLaunchKernelGGL((gn_apply_kernel<P, V, NV, NT, ACT>), grid, dim3(NT), 0, s, a);          \
+    }
+    GN_C(1, 256, 8)
+    if constexpr (V == 1) { GN_C(2, 512, 8) GN_C(3, 1024, 8) }
+#undef GN_C
+}
+
+template <class P, int V, int ACT>
+void gn_bwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
+    const dim3 grid(unsigned(a.n * a.chunks));
+#define GN_W(K, NT, NV) \
+    if (p.whole && p.shape == K) hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 0, ACT>), grid, dim3(NT), 0, s, a);
+    GN_W(0, 256, 2) GN_W(1, 256, 8) GN_W(2, 512, 8) GN_W(3, 1024, 8)
+#undef GN_W
+    if (p.whole) return;
+#define GN_C(K, NT, NV)                                                                                  \
+    if (p.shape == K) {                                                                                  \
+        hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 1, ACT>), grid, dim3(NT), 0, s, a);              \
+        hipLaunchKernelGGL(gn_columns_kernel, dim3(unsigned(a.n * ((2 * a.C + 3) / 4))), dim3(1024), 0, s, a.part, \
+                           int64_t(a.chunks), 2 * a.C, 2 * a.C, a.fsum, static_cast<float*>(nullptr));  \
+        hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 2, ACT>), grid, dim3(NT), 0, s, a);              \
     }
     GN_C(1, 256, 8)
     if constexpr (V == 1) { GN_C(2, 512, 8) GN_C(3, 1024, 8) }
@@ -519,22 +663,19 @@ void gn_fwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
 }
 
 template <class P, int V>
-void gn_bwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
-    const dim3 grid(unsigned(a.n * a.chunks));
-#define GN_W(K, NT, NV) \
-    if (p.whole && p.shape == K) hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 0>), grid, dim3(NT), 0, s, a);
-    GN_W(0, 256, 2) GN_W(1, 256, 8) GN_W(2, 512, 8) GN_W(3, 1024, 8)
-#undef GN_W
-    if (p.whole) return;
-#define GN_C(K, NT, NV)                                                                             \
-    if (p.shape == K) {                                                                             \
-        hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 1>), grid, dim3(NT), 0, s, a);              \
-        hipLaunchKernelGGL(gn_bwd_means_kernel, dim3(unsigned(a.n)), dim3(256), 0, s, a);           \
-        hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 2>), grid, dim3(NT), 0, s, a);              \
+void gn_launch(const GnPlan& p, const GnArgs& a, int bwd, hipStream_t s) {
+    if constexpr (V == 1) {
+        if (bwd) gn_bwd_launch<P, V, -1>(p, a, s);
+        else gn_fwd_launch<P, V, -1>(p, a, s);
+    } else {
+#define GN_A(ACT)                                     \
+    if (a.act == ACT) {                               \
+        if (bwd) gn_bwd_launch<P, V, ACT>(p, a, s);   \
+        else gn_fwd_launch<P, V, ACT>(p, a, s);       \
     }
-    GN_C(1, 256, 8)
-    if constexpr (V == 1) { GN_C(2, 512, 8) GN_C(3, 1024, 8) }
-#undef GN_C
+        GN_A(GN_NONE) GN_A(GN_RELU) GN_A(GN_SILU)
+#undef GN_A
+    }
 }
 
 std::string gn_key(const char* name, int prec, int H, int W, int C) {
@@ -544,7 +685,8 @@ std::string gn_key(const char* name, int prec, int H, int W, int C) {
 }  // namespace
 
 int64_t groupnorm_blocks(int prec, int64_t n, int H, int W, int C, int G) {
-    return n * gn_plan(prec, n, H, W, C, G, 0, 0, nullptr).chunks;   // one-channel columns: the most chunks
+    // one-channel columns: the most chunks; the column sums take 4 columns of a frame each
+    return std::max(n * gn_plan(prec, n, H, W, C, G, 0, 0, nullptr).chunks, n * ((2 * C + 3) / 4));
 }
 
 size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd) {
@@ -560,11 +702,11 @@ hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t
     a.srstd = reinterpret_cast<float*>(w + p.srstd);
     ProfScope ps(s, [&] { return gn_key("groupnorm_fwd", prec, H, W, a.C); });
     if (prec == BF16) {
-        if (p.V == 8) gn_fwd_launch<PrecBF16, 8>(p, a, s);
-        else gn_fwd_launch<PrecBF16, 1>(p, a, s);
+        if (p.V == 8) gn_launch<PrecBF16, 8>(p, a, 0, s);
+        else gn_launch<PrecBF16, 1>(p, a, 0, s);
     } else {
-        if (p.V == 4) gn_fwd_launch<PrecF32, 4>(p, a, s);
-        else gn_fwd_launch<PrecF32, 1>(p, a, s);
+        if (p.V == 4) gn_launch<PrecF32, 4>(p, a, 0, s);
+        else gn_launch<PrecF32, 1>(p, a, 0, s);
     }
     return hipGetLastError();
 }
@@ -579,16 +721,17 @@ hipError_t groupnorm_bwd(int prec, int H, int W, GnArgs a, float* dgamma, float*
     if (a.n > 0) {
         ProfScope ps(s, [&] { return gn_key("groupnorm_bwd", prec, H, W, a.C); });
         if (prec == BF16) {
-            if (p.V == 8) gn_bwd_launch<PrecBF16, 8>(p, a, s);
-            else gn_bwd_launch<PrecBF16, 1>(p, a, s);
+            if (p.V == 8) gn_launch<PrecBF16, 8>(p, a, 1, s);
+            else gn_launch<PrecBF16, 1>(p, a, 1, s);
         } else {
-            if (p.V == 4) gn_bwd_launch<PrecF32, 4>(p, a, s);
-            else gn_bwd_launch<PrecF32, 1>(p, a, s);
+            if (p.V == 4) gn_launch<PrecF32, 4>(p, a, 1, s);
+            else gn_launch<PrecF32, 1>(p, a, 1, s);
         }
     }
     if (dgamma || dbeta) {
         ProfScope ps(s, [&] { return gn_key("groupnorm_params", prec, H, W, a.C); });
-        hipLaunchKernelGGL(gn_params_kernel, dim3(unsigned((2 * a.C + 3) / 4)), dim3(256), 0, s, a, dgamma, dbeta);
+        hipLaunchKernelGGL(gn_columns_kernel, dim3(unsigned((2 * a.C + 3) / 4)), dim3(1024), 0, s, a.fsum, a.n, 2 * a.C,
+                           a.C, dbeta, dgamma);
     }
     return hipGetLastError();
 }

@@ -7,9 +7,12 @@
 // 3 m^2 n + (4 L - 3) m^3 operations with the symmetric products computed by halves, against
 // L (3 m^2 n + m^3) for the steps one by one. What bounds L is rounding: A squares the singular values
 // and P A P grows what is small by a^2 a step, the rounding of A along with it. A's error is 2^-24 of
-// its norm, so a segment has at most kSeg = 3 steps, the next one starting from a fresh Gram matrix: two
-// segments of 3 and 2 steps come as near the exact result as the steps one by one in float32 do, where
-// one segment of 5 is off by 2^-7 for singular values spread over six decades (more than bf16 resolves).
+// its norm, so the next segment starts from a fresh Gram matrix. Five steps on gradient-like matrices
+// (a few strong directions over noise) come out as near the exact result as the steps one by one in
+// float32 do, 1e-6 of their norm, with segments of 2, 2 and 1 steps (kSegF32); with 3 and 2 (kSegBf16)
+// they are off by 6e-6, which bf16 results and parameters that move by a few per cent do not see; one
+// segment of 5 is off by 2^-7 for singular values spread over six decades, more than bf16 resolves.
+// On square matrices the operations are the same either way; on 15 : 1 they are 1 : 1.4.
 //
 // Every matrix is held as two f16 planes, v = hi + lo with lo = f16(v - hi): 22 bits and more under a
 // power-of-two scale that keeps values in f16's normal range (at least 2^-40 of a matrix's bound is
@@ -36,7 +39,7 @@ namespace cb {
 
 namespace {
 
-constexpr int kSeg = 3;
+constexpr int kSegF32 = 2, kSegBf16 = 3, kMaxSegs = kNsMaxSteps / 2;
 
 typedef _Float16 ns_f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 ns_f16x4 __attribute__((ext_vector_type(4)));
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(256) void ns_gram_kernel(NsArgs a, int src) {
 
 struct NsSeg {                 // one segment's polynomials and scales (host constants)
     int len;
-    float c[kSeg][3];
+    float c[kSegBf16][3];
     float sa, sp, st, sq;      // power-of-two scales of A, P, P A and Q
     float alpha;               // the Gram matrix's scale where X's planes have a static one, else 0
 };
@@ -818,6 +821,9 @@ void ns_shape(NsGroup& G, int rows, int cols, int batch) {
     G.scale = 1.f;
 }
 
+// Steps in one segment at most.
+int ns_most(int prec) { return prec == BF16 ? kSegBf16 : kSegF32; }
+
 // Lays the group's buffers out from `at`; np0: planes of X as it comes; two: a second X buffer.
 int64_t ns_layout(NsGroup& G, int64_t at, int np0, bool two) {
     auto take = [&](int64_t bytes) { const int64_t o = at; at += a256(bytes); return o; };
@@ -836,8 +842,8 @@ int64_t ns_layout(NsGroup& G, int64_t at, int np0, bool two) {
 
 struct NsProgram {
     int nseg;
-    NsSeg seg[(kNsMaxSteps + kSeg - 1) / kSeg];
-    double xscale[(kNsMaxSteps + kSeg - 1) / kSeg];   // scale of X after segment i
+    NsSeg seg[kMaxSegs];
+    double xscale[kMaxSegs];   // scale of X after segment i
 };
 
 double pow2_scale(double bound, int most) {   // the largest power of two (at most 2^most) with bound * it <= 2^15
@@ -848,9 +854,9 @@ double pow2_scale(double bound, int most) {   // the largest power of two (at mo
 // The segments of `steps` steps and the scales of their matrices, from bounds on the singular values:
 // they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False where they
 // could grow past 2^10 (planes would no longer resolve them).
-bool ns_program(int steps, const float* coeffs, NsProgram& P) {
+bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
     static const float kDefault[3] = {3.4445f, -4.7750f, 2.0315f};
-    P.nseg = (steps + kSeg - 1) / kSeg;
+    P.nseg = (steps + most - 1) / most;
     double s = 1.0 + 0x1p-10;
     int at = 0;
     for (int k = 0; k < P.nseg; ++k) {
@@ -993,14 +999,14 @@ int64_t orth_layout(int prec, int64_t batch, int rows, int cols, int steps, NsAr
     ns_shape(G, rows, cols, int(batch));
     a.info = 0;
     a.sums = a256(batch * 8);
-    return ns_layout(G, a.sums + a256(batch * G.nsum * 24), prec == BF16 ? 1 : 2, steps > kSeg);
+    return ns_layout(G, a.sums + a256(batch * G.nsum * 24), prec == BF16 ? 1 : 2, steps > ns_most(prec));
 }
 
 }  // namespace
 
 bool muon_coeffs_ok(int steps, const float* coeffs) {
     NsProgram P;
-    return ns_program(steps, coeffs, P);
+    return ns_program(steps, coeffs, kSegBf16, P);   // (shorter segments have smaller products)
 }
 
 size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps) {
@@ -1014,7 +1020,7 @@ hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x,
     orth_layout(prec, batch, rows, cols, steps, a);
     a.ws = static_cast<char*>(ws);
     NsProgram P;
-    ns_program(steps, coeffs, P);
+    ns_program(steps, coeffs, ns_most(prec), P);
     const NsGroup& G = a.g[0];
     ProfScope ps(s, [&] { return cb_key("muon_orthogonalize", prec, cb_dims(rows, cols) + "x" + std::to_string(batch)); });
     MuonElem e{};
@@ -1110,7 +1116,7 @@ MuonPlan muon_plan(int64_t n_params, const std::vector<MuonMat>& mats, int steps
         P.a.info = 0;
         P.a.sums = sums;
         int64_t end = base;   // passes follow each other in the same memory
-        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSeg);
+        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSegBf16);
         plan.total = std::max(plan.total, end);
         P.e.nblocks = plan.nblocks;
     }
@@ -1127,7 +1133,7 @@ hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void
     if (m.n <= 0) return hipSuccess;
     MuonPlan plan = muon_plan(m.n, mats, m.steps, m.scale_mode);
     NsProgram P;
-    ns_program(m.steps, m.coeffs, P);
+    ns_program(m.steps, m.coeffs, kSegBf16, P);
     ProfScope ps(s, [&] { return "muon/" + std::to_string(m.n); });
     for (MuonPlan::Pass& p : plan.pass) {
         p.a.ws = static_cast<char*>(ws);
