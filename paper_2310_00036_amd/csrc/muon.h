@@ -14,11 +14,12 @@ constexpr int kNsMaxSteps = 16;
 struct NsGroup {
     int rows, cols, rp, cp, m, n, mp, np, tall;   // tall: rows > cols
     int batch, first;                 // first: index of its first matrix in the call
-    int bt, tiles, splits, kchunk;    // tile, tiles of a symmetric m x m product, the Gram product's k split
+    int bt, tiles, splits, kchunk;    // tile (64, 128 or 192), tiles of a symmetric m x m product, the Gram product's k split
     int table, nsum, part0;           // 1 + its first offset in NsArgs::off (0: b * rows * cols); its blocks of the sums
     float scale;                      // the update's factor (muon_step)
-    int64_t x[2], part, a, t, p, q[2];   // workspace byte offsets of the first matrix
-    int64_t xs, ms, ps;                  // bytes of one X plane, one m x m plane, one matrix's partials
+    int64_t x[2], xt[2], part, a, t, p, q[2];   // workspace byte offsets of the first matrix (xt: X transposed)
+    int ldx, ldt, ldm;                   // leading dimensions of X, its transpose and the m x m matrices
+    int64_t xs, ts, ms, ps;              // bytes of one plane of each, and of one matrix's partials
 };
 
 struct NsArgs {

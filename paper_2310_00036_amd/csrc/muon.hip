@@ -71,6 +71,21 @@ CB_DEV void ns_join(uint2 hi, uint2 lo, float (&v)[4]) {
     for (int r = 0; r < 4; ++r) v[r] = static_cast<float>(h[r]) + static_cast<float>(l[r]);
 }
 
+// Four neighbours of a row to both planes, or one below the other (`step` bytes apart).
+CB_DEV void ns_store(char* d, int64_t plane, int64_t o, uint2 hi, uint2 lo) {
+    *reinterpret_cast<uint2*>(d + o) = hi;
+    *reinterpret_cast<uint2*>(d + plane + o) = lo;
+}
+CB_DEV void ns_store_across(char* d, int64_t plane, int64_t o, int64_t step, uint2 hi, uint2 lo) {
+    const uint16_t h[4] = {uint16_t(hi.x), uint16_t(hi.x >> 16), uint16_t(hi.y), uint16_t(hi.y >> 16)};
+    const uint16_t l[4] = {uint16_t(lo.x), uint16_t(lo.x >> 16), uint16_t(lo.y), uint16_t(lo.y >> 16)};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        *reinterpret_cast<uint16_t*>(d + o + r * step) = h[r];
+        *reinterpret_cast<uint16_t*>(d + plane + o + r * step) = l[r];
+    }
+}
+
 // This workgroup's group; blk becomes its index within the group.
 CB_DEV int ns_group(const NsArgs& a, int& blk) {
     int g = 0;
@@ -90,9 +105,9 @@ CB_DEV void ns_tile(int t, int& ti, int& tj) {
 
 // ------------------------------------------------------------------ the tile product
 //
-// acc += A B^T over k in [k0, k1) for a BT x BT tile, four waves of BT/2 x BT/2. An operand is NP planes
-// (`plane` bytes apart) of a padded matrix, either [rows][k] or (KM) [k][rows], leading dimension ld
-// elements; padding is zero, so there are no edges. Tiles go from memory into an LDS ring of ST stages
+// acc += A B^T over k in [k0, k1) for a BT x BT tile, in NsWaves' waves. An operand is NP planes
+// (`plane` bytes apart) of a padded matrix [rows][k], leading dimension ld elements; padding is zero, so
+// there are no edges. Tiles go from memory into an LDS ring of ST stages
 // by direct loads that stay in flight across barriers (one wait per stage, counted), in the layout they
 // have in memory; 16-byte slots are permuted within a row so that a fragment read meets every bank.
 
@@ -114,57 +129,58 @@ CB_DEV ns_u32x4 ns_rsrc(const char* base, int64_t bytes) {
 }
 CB_DEV uint32_t ns_lds(const unsigned char* p) { return uint32_t(reinterpret_cast<uintptr_t>((lds_t*)(p))); }
 
-template <int BT, int BK, int KM>
+// Waves of a tile: WM x WN of them, FM x FN fragments of 16 each. What a wave reads of LDS per product
+// falls with its fragments: at 4 x 4 (tiles of 128) reads and the incoming loads take as long as the
+// products, at 6 x 6 (tiles of 192, one workgroup a CU) two thirds of that.
+template <int BT>
+struct NsWaves {
+    static constexpr int WM = 2, WN = 2, NW = WM * WN;
+    static constexpr int FM = BT / WM / 16, FN = BT / WN / 16;
+};
+
+template <int BT, int BK>
 struct NsOperand {
+    static constexpr int NW = NsWaves<BT>::NW;
     static constexpr int BYTES = BT * BK * 2;              // of a plane's tile
-    static constexpr int NI = BYTES / 4096;                // direct loads a wave and plane
-    static constexpr int SPR = (KM ? BT : BK) / 8;         // 16-byte slots per LDS row
-    static_assert(BYTES % 4096 == 0, "whole loads");
-    uint32_t base[NI], step;
+    static constexpr int NI = BYTES / (1024 * NW);         // direct loads a wave and plane
+    static constexpr int SPR = BK / 8;                     // 16-byte slots per LDS row
+    static_assert(BYTES % (1024 * NW) == 0, "whole loads");
+    uint32_t base[NI];
     // the slot that holds chunk c of row r (its own inverse)
-    static CB_DEV int swz(int r, int c) {
-        if (KM) return c ^ ((r & (SPR / 2 - 1)) << 1);
-        return BK == 64 ? c ^ (r & 7) : c ^ ((r >> 1) & 3);
-    }
+    static CB_DEV int swz(int r, int c) { return BK == 64 ? c ^ (r & 7) : c ^ ((r >> 1) & 3); }
     CB_DEV NsOperand(int ld, int row0, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int s = (wave + 4 * i) * 64 + lane, r = s / SPR, c = swz(r, s % SPR);
-            base[i] = KM ? (uint32_t(r) * uint32_t(ld) + uint32_t(row0 + c * 8)) * 2u
-                         : (uint32_t(row0 + r) * uint32_t(ld) + uint32_t(c * 8)) * 2u;
+            const int s = (wave + NW * i) * 64 + lane, r = s / SPR, c = swz(r, s % SPR);
+            base[i] = (uint32_t(row0 + r) * uint32_t(ld) + uint32_t(c * 8)) * 2u;
         }
-        step = KM ? uint32_t(ld) * 2u : 2u;
     }
-    CB_DEV void issue(ns_u32x4 rs, uint32_t lds, int k, bool live, int wave) const {
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-            ns_dma16(rs, lds + (wave + 4 * i) * 1024, live ? base[i] + uint32_t(k) * step : kOOB);
+    // this wave's load i of a tile at k
+    CB_DEV void issue(int i, ns_u32x4 rs, uint32_t lds, int k, bool live, int wave) const {
+        ns_dma16(rs, lds + (wave + NW * i) * 1024, live ? base[i] + uint32_t(k) * 2u : kOOB);
     }
     // 8 consecutive k (step ks of 32, lane group g) of tile row `row` (row % 16 == lane % 16)
     static CB_DEV uint4 frag(const unsigned char* t, int row, int ks, int lane) {
-        const int g = lane >> 4;
-        if (!KM) return *reinterpret_cast<const uint4*>(t + row * (BK * 2) + swz(row, ks * 4 + g) * 16);
-        // transpose read: lane 4j+q of the 16-lane group addresses k = base + j, rows 4q..4q+3
-        const int r16 = lane & 15, j = r16 >> 2, rb = row - r16 + 4 * (r16 & 3);
-        const int k = ks * 32 + g * 8 + j;
-        const uint2 lo = lds_read_tr16(t + k * (BT * 2) + swz(k, rb >> 3) * 16 + (rb & 7) * 2);
-        const uint2 hi = lds_read_tr16(t + (k + 4) * (BT * 2) + swz(k + 4, rb >> 3) * 16 + (rb & 7) * 2);
-        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        return *reinterpret_cast<const uint4*>(t + row * (BK * 2) + swz(row, ks * 4 + (lane >> 4)) * 16);
     }
 };
 
 template <int BT, int BK, int ST, int NA, int NB>
 constexpr int ns_lds_bytes() { return ST * (NA + NB) * BT * BK * 2; }
 
-template <int BT, int BK, int ST, int NA, int NB, int KMA, int KMB>
+template <int BT>
+using NsAcc = cb_f32x4[NsWaves<BT>::FM][NsWaves<BT>::FN];
+
+template <int BT, int BK, int ST, int NA, int NB>
 CB_DEV void ns_gemm(const char* A, int64_t aplane, int lda, int arow, const char* B, int64_t bplane, int ldb, int brow,
-                    int k0, int k1, unsigned char* smem, cb_f32x4 (&acc)[BT / 32][BT / 32]) {
-    constexpr int F = BT / 32;
-    using OA = NsOperand<BT, BK, KMA>;
-    using OB = NsOperand<BT, BK, KMB>;
+                    int k0, int k1, unsigned char* smem, NsAcc<BT>& acc) {
+    using W = NsWaves<BT>;
+    constexpr int FM = W::FM, FN = W::FN, KS = BK / 32;
+    using OA = NsOperand<BT, BK>;
+    using OB = OA;
     constexpr int STAGE = NA * OA::BYTES + NB * OB::BYTES, LPS = NA * OA::NI + NB * OB::NI;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r16 = lane & 15, wm = wave >> 1, wn = wave & 1;
+    const int r16 = lane & 15, wm = wave / W::WN, wn = wave % W::WN;
     const OA oa(lda, arow, wave, lane);
     const OB ob(ldb, brow, wave, lane);
     ns_u32x4 ra[NA], rb[NB];
@@ -174,87 +190,126 @@ CB_DEV void ns_gemm(const char* A, int64_t aplane, int lda, int arow, const char
     for (int p = 0; p < NB; ++p) rb[p] = ns_rsrc(B + p * bplane, bplane);
     const uint32_t lds0 = ns_lds(smem);
     const int nb = (k1 - k0) / BK;
-    // past the end the loads are out of range (zeros), so every stage counts the same loads
-    auto issue = [&](int it) CB_INLINE_LAMBDA {
-        const uint32_t l = lds0 + uint32_t(it % ST) * STAGE;
-#pragma unroll
-        for (int p = 0; p < NA; ++p) oa.issue(ra[p], l + p * OA::BYTES, k0 + it * BK, it < nb, wave);
-#pragma unroll
-        for (int p = 0; p < NB; ++p) ob.issue(rb[p], l + NA * OA::BYTES + p * OB::BYTES, k0 + it * BK, it < nb, wave);
+    // this wave's load d of stage `it`; past the end it is out of range (zeros), so every stage counts the same
+    auto issue = [&](int it, int d) CB_INLINE_LAMBDA {
+        const int p = d / OA::NI, i = d % OA::NI;
+        const uint32_t l = lds0 + uint32_t(it % ST) * STAGE + uint32_t(p) * OA::BYTES;
+        if (p < NA) oa.issue(i, ra[p < NA ? p : 0], l, k0 + it * BK, it < nb, wave);
+        else ob.issue(i, rb[p < NA ? 0 : p - NA], l, k0 + it * BK, it < nb, wave);
     };
-    for (int s = 0; s < ST - 1; ++s) issue(s);
+    auto read_a = [&](int st, int p, int ks, int i) CB_INLINE_LAMBDA {
+        return OA::frag(smem + (st % ST) * STAGE + p * OA::BYTES, wm * (FM * 16) + i * 16 + r16, ks, lane);
+    };
+    auto read_b = [&](int st, int p, int ks, int j) CB_INLINE_LAMBDA {
+        return OA::frag(smem + (st % ST) * STAGE + (NA + p) * OA::BYTES, wn * (FN * 16) + j * 16 + r16, ks, lane);
+    };
+    // x y row by row; with(ks, i) before row i of step ks: reads and loads go between the products, for
+    // one block of either would hold the matrix core up
+    auto mul = [&](const uint4 (&x)[KS][FM], const uint4 (&y)[KS][FN], auto&& with) CB_INLINE_LAMBDA {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                with(ks, i);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = ns_mma(x[ks][i], y[ks][j], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    static_assert(FM == FN, "a row's reads are one fragment of each operand");
+    // The barrier stands before a stage's last product, whose operands are in registers by then: after it
+    // the stage's buffer is free, the next stage is in LDS, and its first fragments are read in the first
+    // half of that product; the others are read during the products before. No product waits for LDS. The
+    // freed buffer's loads are issued half in that product and half in the next stage's first one.
+    constexpr int R = KS * FM, HALF = NA > 1 || NB > 1 ? LPS / 2 : LPS;
+    uint4 a0[KS][FM], b0[KS][FN], a1[KS][FM], b1[KS][FN], na[KS][FM], nbf[KS][FN];
+    for (int s = 0; s < ST - 1; ++s)
+#pragma unroll
+        for (int d = 0; d < LPS; ++d) issue(s, d);
+#pragma unroll
+    for (int d = 0; d < HALF; ++d) issue(ST - 1, d);
+    ns_wait<(ST - 2) * LPS + HALF>();   // this wave's loads of stage 0 are in LDS
+    lds_barrier();                      // all waves' are
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        a0[q / FM][q % FM] = read_a(0, 0, q / FM, q % FM);
+        b0[q / FM][q % FM] = read_b(0, 0, q / FM, q % FM);
+    }
     for (int it = 0; it < nb; ++it) {
-        ns_wait<(ST - 2) * LPS>();   // this stage's loads (this wave's) are in LDS
-        lds_barrier();               // all waves' are, and the stage before is read
-        issue(it + ST - 1);
-        const unsigned char* cur = smem + (it % ST) * STAGE;
+        if constexpr (NA > 1 || NB > 1)
+            mul(a0, b0, [&](int ks, int i) CB_INLINE_LAMBDA {
+                if constexpr (NB > 1) b1[ks][i] = read_b(it, 1, ks, i);
+                else a1[ks][i] = read_a(it, 1, ks, i);
+                const int at = ks * FM + i;
 #pragma unroll
-        for (int ks = 0; ks < BK / 32; ++ks) {
-            uint4 af[NA][F], bf[NB][F];
+                for (int d = HALF + at * (LPS - HALF) / R; d < HALF + (at + 1) * (LPS - HALF) / R; ++d) issue(it + ST - 1, d);
+            });
+        if constexpr (NA > 1 && NB > 1)
+            mul(a0, b1, [&](int ks, int i) CB_INLINE_LAMBDA { a1[ks][i] = read_a(it, 1, ks, i); });
+        ns_wait<(ST - 2) * LPS>();
+        lds_barrier();
+        mul(NA > 1 ? a1 : a0, NA > 1 ? b0 : NB > 1 ? b1 : b0, [&](int ks, int i) CB_INLINE_LAMBDA {
+            const int at = ks * FM + i;
 #pragma unroll
-            for (int p = 0; p < NA; ++p)
+            for (int q = 2 * at; q < 2 * at + 2; ++q)
+                if (q < R) {
+                    na[q / FM][q % FM] = read_a(it + 1, 0, q / FM, q % FM);
+                    nbf[q / FM][q % FM] = read_b(it + 1, 0, q / FM, q % FM);
+                }
 #pragma unroll
-                for (int i = 0; i < F; ++i)
-                    af[p][i] = OA::frag(cur + p * OA::BYTES, wm * (BT / 2) + i * 16 + r16, ks, lane);
+            for (int d = at * HALF / R; d < (at + 1) * HALF / R; ++d) issue(it + ST, d);
+        });
 #pragma unroll
-            for (int p = 0; p < NB; ++p)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int j = 0; j < F; ++j)
-                    bf[p][j] = OB::frag(cur + NA * OA::BYTES + p * OB::BYTES, wn * (BT / 2) + j * 16 + r16, ks, lane);
-#pragma unroll
-            for (int q = 0; q < NA + NB - 1; ++q)   // hi hi, then lo hi and hi lo where there are planes for them
-#pragma unroll
-                for (int i = 0; i < F; ++i)
-#pragma unroll
-                    for (int j = 0; j < F; ++j) {
-                        const int pa = q > 0 && q < NA ? q : 0, pb = q >= NA ? q - NA + 1 : 0;
-                        acc[i][j] = ns_mma(af[pa][i], bf[pb][j], acc[i][j]);
-                    }
-        }
+            for (int i = 0; i < FM; ++i) {
+                a0[ks][i] = na[ks][i];
+                b0[ks][i] = nbf[ks][i];
+            }
     }
     ns_wait<0>();
     lds_barrier();
 }
 
-template <int F>
-CB_DEV void ns_clear(cb_f32x4 (&acc)[F][F]) {
+template <int BT>
+CB_DEV void ns_clear(NsAcc<BT>& acc) {
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < NsWaves<BT>::FM; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j) acc[i][j] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NsWaves<BT>::FN; ++j) acc[i][j] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
 // f(M, N, acc[i][j]) for every group of four rows M .. M+3 of column N that this lane holds (local).
 template <int BT, class Fn>
-CB_DEV void ns_each(cb_f32x4 (&acc)[BT / 32][BT / 32], Fn&& f) {
+CB_DEV void ns_each(NsAcc<BT>& acc, Fn&& f) {
+    using W = NsWaves<BT>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int g = lane >> 4, r16 = lane & 15, wm = wave >> 1, wn = wave & 1;
+    const int g = lane >> 4, r16 = lane & 15, wm = wave / W::WN, wn = wave % W::WN;
 #pragma unroll
-    for (int i = 0; i < BT / 32; ++i)
+    for (int i = 0; i < W::FM; ++i)
 #pragma unroll
-        for (int j = 0; j < BT / 32; ++j)
-            f(wm * (BT / 2) + i * 16 + 4 * g, wn * (BT / 2) + j * 16 + r16, acc[i][j]);
+        for (int j = 0; j < W::FN; ++j)
+            f(wm * (W::FM * 16) + i * 16 + 4 * g, wn * (W::FN * 16) + j * 16 + r16, acc[i][j]);
 }
 
 // ------------------------------------------------------------------ Gram product
 
 // part [split][tile][N][M] float32: the k range of one split of one tile of X X^T (smaller side).
 template <int BT, int BK, int ST, int NP>
-__global__ __launch_bounds__(256) void ns_gram_kernel(NsArgs a, int src) {
+__global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a, int src) {
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
     const int z = blk % G.splits, t = blk / G.splits % G.tiles, b = blk / (G.splits * G.tiles);
     int ti, tj;
     ns_tile(t, ti, tj);
-    const char* X = a.ws + G.x[src] + int64_t(b) * NP * G.xs;
+    const char* X = a.ws + (G.tall ? G.xt : G.x)[src] + int64_t(b) * NP * (G.tall ? G.ts : G.xs);   // [m][n]
     const int k0 = z * G.kchunk, k1 = min(G.np, k0 + G.kchunk);
-    cb_f32x4 acc[BT / 32][BT / 32];
-    ns_clear(acc);
-    if (G.tall)
-        ns_gemm<BT, BK, ST, NP, NP, 1, 1>(X, G.xs, G.cp, ti * BT, X, G.xs, G.cp, tj * BT, k0, k1, smem, acc);
-    else
-        ns_gemm<BT, BK, ST, NP, NP, 0, 0>(X, G.xs, G.cp, ti * BT, X, G.xs, G.cp, tj * BT, k0, k1, smem, acc);
+    NsAcc<BT> acc;
+    ns_clear<BT>(acc);
+    const int ld = G.tall ? G.ldt : G.ldx;
+    const int64_t xs = G.tall ? G.ts : G.xs;
+    ns_gemm<BT, BK, ST, NP, NP>(X, xs, ld, ti * BT, X, xs, ld, tj * BT, k0, k1, smem, acc);
     float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.tiles + t) * (BT * BT);
     ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
         *reinterpret_cast<float4*>(part + N * BT + M) = make_float4(v[0], v[1], v[2], v[3]);
@@ -348,8 +403,7 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
         for (int r = 0; r < 4; ++r) v[r] = N < G.m && M + r < G.m ? Q[N * kSmPitch + M + r] * s.sq : 0.f;
         uint2 hi, lo;
         ns_split(v, hi, lo);
-        *reinterpret_cast<uint2*>(q + e * 2) = hi;
-        *reinterpret_cast<uint2*>(q + G.ms + e * 2) = lo;
+        ns_store(q, G.ms, (N * G.ldm + M) * 2, hi, lo);
     }
 }
 
@@ -385,9 +439,8 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
         }
         uint2 hi, lo;
         ns_split(v, hi, lo);
-        const int64_t o = (int64_t(tj * bt + N) * G.mp + ti * bt + M) * 2;
-        *reinterpret_cast<uint2*>(A + o) = hi;
-        *reinterpret_cast<uint2*>(A + G.ms + o) = lo;
+        const int64_t o = (int64_t(tj * bt + N) * G.ldm + ti * bt + M) * 2;
+        ns_store(A, G.ms, o, hi, lo);
     }
     if (ti == tj) return;
     __syncthreads();
@@ -396,9 +449,8 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
         const float v[4] = {sh[M * 17 + q], sh[M * 17 + q + 1], sh[M * 17 + q + 2], sh[M * 17 + q + 3]};
         uint2 hi, lo;
         ns_split(v, hi, lo);
-        const int64_t o = (int64_t(ti * bt + M) * G.mp + tj * bt + n0 + q) * 2;
-        *reinterpret_cast<uint2*>(A + o) = hi;
-        *reinterpret_cast<uint2*>(A + G.ms + o) = lo;
+        const int64_t o = (int64_t(ti * bt + M) * G.ldm + tj * bt + n0 + q) * 2;
+        ns_store(A, G.ms, o, hi, lo);
     }
 }
 
@@ -416,7 +468,7 @@ CB_DEV char* ns_buf(const NsArgs& a, const NsGroup& G, int id, int b) {
 
 // Products of symmetric matrices that commute: the lower triangle's tiles, and their mirror images.
 template <int BT, int BK, int ST>
-__global__ __launch_bounds__(256) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
+__global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
@@ -424,17 +476,17 @@ __global__ __launch_bounds__(256) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
     const int t = blk / jobs.n % G.tiles, b = blk / (jobs.n * G.tiles);
     int ti, tj;
     ns_tile(t, ti, tj);
-    cb_f32x4 acc[BT / 32][BT / 32];
-    ns_clear(acc);
-    ns_gemm<BT, BK, ST, 2, 2, 0, 0>(ns_buf(a, G, J.lhs, b), G.ms, G.mp, ti * BT, ns_buf(a, G, J.rhs, b), G.ms, G.mp,
-                                    tj * BT, 0, G.mp, smem, acc);
+    NsAcc<BT> acc;
+    ns_clear<BT>(acc);
+    ns_gemm<BT, BK, ST, 2, 2>(ns_buf(a, G, J.lhs, b), G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), G.ms, G.ldm, tj * BT, 0,
+                              G.mp, smem, acc);
     char* D = ns_buf(a, G, J.dst, b);
     const char* A = ns_buf(a, G, NS_A, b);
     const float f = J.f, fa = J.fa, diag = J.diag;
     const int poly = J.poly;
     ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
         const int m = ti * BT + M, n = tj * BT + N;
-        const int64_t o = (int64_t(n) * G.mp + m) * 2;
+        const int64_t o = (int64_t(n) * G.ldm + m) * 2;
         float w[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[r] = f * v[r];
@@ -446,18 +498,8 @@ __global__ __launch_bounds__(256) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
         }
         uint2 hi, lo;
         ns_split(w, hi, lo);
-        *reinterpret_cast<uint2*>(D + o) = hi;
-        *reinterpret_cast<uint2*>(D + G.ms + o) = lo;
-        if (ti != tj) {
-            const uint16_t h[4] = {uint16_t(hi.x), uint16_t(hi.x >> 16), uint16_t(hi.y), uint16_t(hi.y >> 16)};
-            const uint16_t l[4] = {uint16_t(lo.x), uint16_t(lo.x >> 16), uint16_t(lo.y), uint16_t(lo.y >> 16)};
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t m2 = (int64_t(m + r) * G.mp + n) * 2;
-                *reinterpret_cast<uint16_t*>(D + m2) = h[r];
-                *reinterpret_cast<uint16_t*>(D + G.ms + m2) = l[r];
-            }
-        }
+        ns_store(D, G.ms, o, hi, lo);
+        if (ti != tj) ns_store_across(D, G.ms, (int64_t(m) * G.ldm + n) * 2, int64_t(G.ldm) * 2, hi, lo);
     });
 }
 
@@ -475,33 +517,42 @@ struct NsApply {
 };
 
 template <int BT, int BK, int ST, int NP>
-__global__ __launch_bounds__(256) void ns_apply_kernel(NsArgs a, NsApply ap) {
+__global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a, NsApply ap) {
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
     const int tn = G.rp / BT, tm = G.cp / BT;   // N over the rows, M over the columns
     const int jt = blk % tn, it = blk / tn % tm, b = blk / (tn * tm);
-    const char* X = a.ws + G.x[ap.src] + int64_t(b) * NP * G.xs;
+    const int ld = G.tall ? G.ldx : G.ldt;
+    const int64_t xs = G.tall ? G.xs : G.ts;
+    const char* X = a.ws + (G.tall ? G.x : G.xt)[ap.src] + int64_t(b) * NP * xs;   // [n][m]
     const char* Q = a.ws + (G.mp == 64 ? G.q[0] : G.q[ap.q]) + int64_t(b) * 2 * G.ms;
-    cb_f32x4 acc[BT / 32][BT / 32];
-    ns_clear(acc);
-    if (G.tall)   // rows of X by Q: both k-contiguous
-        ns_gemm<BT, BK, ST, 2, NP, 0, 0>(Q, G.ms, G.mp, it * BT, X, G.xs, G.cp, jt * BT, 0, G.mp, smem, acc);
-    else          // columns of X by Q
-        ns_gemm<BT, BK, ST, NP, 2, 1, 0>(X, G.xs, G.cp, it * BT, Q, G.ms, G.mp, jt * BT, 0, G.mp, smem, acc);
+    NsAcc<BT> acc;
+    ns_clear<BT>(acc);
+    // the result's rows are X's where it is tall (M, the contiguous index, over Q's) and Q's where it is wide
+    if constexpr (NP == 2) {
+        const bool tall = G.tall;
+        ns_gemm<BT, BK, ST, 2, 2>(tall ? Q : X, tall ? G.ms : xs, tall ? G.ldm : ld, it * BT, tall ? X : Q,
+                                  tall ? xs : G.ms, tall ? ld : G.ldm, jt * BT, 0, G.mp, smem, acc);
+    } else if (G.tall) {
+        ns_gemm<BT, BK, ST, 2, NP>(Q, G.ms, G.ldm, it * BT, X, xs, ld, jt * BT, 0, G.mp, smem, acc);
+    } else {
+        ns_gemm<BT, BK, ST, NP, 2>(X, xs, ld, it * BT, Q, G.ms, G.ldm, jt * BT, 0, G.mp, smem, acc);
+    }
     float f = ap.f;
     const float2 info = ns_info(a, G.first + b);
     if (ap.use_inv) f *= info.x;
     if (ap.out != NS_OUT_MID) f *= info.y;
     if (ap.out == NS_OUT_MID) {
         char* D = a.ws + G.x[ap.dst] + int64_t(b) * 2 * G.xs;
+        char* T = a.ws + G.xt[ap.dst] + int64_t(b) * 2 * G.ts;
         ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
             const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
             uint2 hi, lo;
             ns_split(w, hi, lo);
-            const int64_t o = (int64_t(jt * BT + N) * G.cp + it * BT + M) * 2;
-            *reinterpret_cast<uint2*>(D + o) = hi;
-            *reinterpret_cast<uint2*>(D + G.xs + o) = lo;
+            const int r = jt * BT + N, c = it * BT + M;
+            ns_store(D, G.xs, (int64_t(r) * G.ldx + c) * 2, hi, lo);
+            ns_store_across(T, G.ts, (int64_t(c) * G.ldt + r) * 2, int64_t(G.ldt) * 2, hi, lo);
         });
         return;
     }
@@ -645,7 +696,8 @@ __global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, cons
     }
 }
 
-constexpr int kPrepElems = 8192;   // padded elements a workgroup of the planes
+// Workgroups of the planes: tiles of 64 x 64 of the padded shape.
+__host__ __device__ inline int ns_plane_blocks(const NsGroup& G) { return (G.rp / 64) * (G.cp / 64); }
 
 // The power of two that brings a matrix of this norm to a root mean square near one; info as ns_info.
 // A zero matrix: (1, 0).
@@ -698,10 +750,9 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         }
         return;
     }
+    __shared__ float tile[64 * 65];
     const NsGroup& G = a.g[ns_group(a, blk)];
-    const int64_t padded = int64_t(G.rp) * G.cp;
-    const int per = int((padded + kPrepElems - 1) / kPrepElems);
-    const int b = blk / per, k = blk % per;
+    const int per = ns_plane_blocks(G), b = blk / per, k = blk % per;
     const double* ms = sums + int64_t(3) * (G.part0 + b * G.nsum);
     double gg = 0.0, gm = 0.0, mm = 0.0;
     for (int i = threadIdx.x; i < G.nsum; i += 256) {
@@ -724,10 +775,11 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
     const float f = ns_scale(norm, double(G.rows) * G.cols, eps, info);
     if (k == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.ws + a.info)[G.first + b] = info;
     char* X = a.ws + G.x[0] + int64_t(b) * NP * G.xs;
+    char* T = a.ws + G.xt[0] + int64_t(b) * NP * G.ts;
     const int64_t off = ns_offset(a, G, b);
-    const int64_t end = min(padded, int64_t(k + 1) * kPrepElems);
-    for (int64_t q = int64_t(k) * kPrepElems + threadIdx.x * 4; q < end; q += 1024) {
-        const int r = int(q / G.cp), c = int(q - int64_t(r) * G.cp);
+    const int r0 = k / (G.cp / 64) * 64, q0 = k % (G.cp / 64) * 64;
+    for (int q = threadIdx.x; q < 1024; q += 256) {
+        const int lr = q >> 4, lc = (q & 15) * 4, r = r0 + lr, c = q0 + lc;
         float w[4] = {0.f, 0.f, 0.f, 0.f};
         if (r < G.rows && c < G.cols) {
             const int64_t o = off + int64_t(r) * G.cols + c;
@@ -782,8 +834,21 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         }
         uint2 hi, lo;
         ns_split(w, hi, lo);
-        *reinterpret_cast<uint2*>(X + q * 2) = hi;
-        if (NP > 1) *reinterpret_cast<uint2*>(X + G.xs + q * 2) = lo;
+        const int64_t o = (int64_t(r) * G.ldx + c) * 2;
+        *reinterpret_cast<uint2*>(X + o) = hi;
+        if (NP > 1) *reinterpret_cast<uint2*>(X + G.xs + o) = lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tile[(lc + i) * 65 + lr] = w[i];
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < 1024; q += 256) {   // the transpose
+        const int lc = q >> 4, lr = (q & 15) * 4;
+        const float w[4] = {tile[lc * 65 + lr], tile[lc * 65 + lr + 1], tile[lc * 65 + lr + 2], tile[lc * 65 + lr + 3]};
+        uint2 hi, lo;
+        ns_split(w, hi, lo);
+        const int64_t o = (int64_t(q0 + lc) * G.ldt + r0 + lr) * 2;
+        *reinterpret_cast<uint2*>(T + o) = hi;
+        if (NP > 1) *reinterpret_cast<uint2*>(T + G.ts + o) = lo;
     }
 }
 
@@ -792,10 +857,11 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
 int64_t up(int64_t v, int64_t k) { return (v + k - 1) / k * k; }
 int64_t a256(int64_t v) { return up(v, 256); }
 
-// Tiles of 128 where they fill the chip (256 CUs), else of 64: more workgroups, each a quarter of the work.
+// The smallest tile whose workgroups do not outnumber the CUs (one a CU): a tile of 128 takes 1.2 times as
+// long as one of 64 for four times the work, one of 192 twice as long for nine times.
 int ns_bt(int m, int64_t batch) {
-    const int64_t t = (m + 127) / 128;
-    return m > 64 && batch * t * (t + 1) / 2 >= 192 ? 128 : 64;
+    auto tiles = [&](int bt) { const int64_t t = (m + bt - 1) / bt; return batch * t * (t + 1) / 2; };
+    return m <= 64 || tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
 }
 
 void ns_shape(NsGroup& G, int rows, int cols, int batch) {
@@ -807,16 +873,19 @@ void ns_shape(NsGroup& G, int rows, int cols, int batch) {
     G.mp = std::min(G.rp, G.cp); G.np = std::max(G.rp, G.cp);
     const int t = G.mp / G.bt;
     G.tiles = t * (t + 1) / 2;
-    // the Gram product's k in splits of at least two 64-blocks, towards two workgroups per CU
+    // the Gram product's k in splits of at least two 64-blocks, towards what the CUs hold
     const int nb = G.np / 64;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::max(1, nb / 2), 512 / (int64_t(batch) * G.tiles)));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::max(1, nb / 2),
+                                                                256 / (int64_t(batch) * G.tiles)));
     const int each = int((nb + want - 1) / want);
     G.kchunk = each * 64;
     G.splits = (nb + each - 1) / each;
-    // blocks of the sums: 16384 elements each, at most 64 a matrix
-    G.nsum = int(std::max<int64_t>(1, std::min<int64_t>(64, int64_t(rows) * cols / 16384)));
-    G.xs = int64_t(G.rp) * G.cp * 2;
-    G.ms = int64_t(G.mp) * G.mp * 2;
+    // blocks of the sums: 8192 elements each, at most 1024 in all and 4 a thread of what adds them up
+    G.nsum = int(std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(1, 1024 / batch), int64_t(rows) * cols / 8192)));
+    G.ldx = G.cp; G.ldt = G.rp; G.ldm = G.mp;
+    G.xs = int64_t(G.rp) * G.ldx * 2;
+    G.ts = int64_t(G.cp) * G.ldt * 2;
+    G.ms = int64_t(G.mp) * G.ldm * 2;
     G.ps = int64_t(G.splits) * G.tiles * G.bt * G.bt * 4;
     G.scale = 1.f;
 }
@@ -828,8 +897,12 @@ int ns_most(int prec) { return prec == BF16 ? kSegBf16 : kSegF32; }
 int64_t ns_layout(NsGroup& G, int64_t at, int np0, bool two) {
     auto take = [&](int64_t bytes) { const int64_t o = at; at += a256(bytes); return o; };
     const bool big = G.mp > 64;
-    G.x[0] = take(G.batch * G.xs * (two ? 2 : np0));   // a later segment may write it with both planes
-    G.x[1] = take(two ? G.batch * G.xs * 2 : 0);
+    for (int k = 0; k < 2; ++k) {
+        int64_t* x = k ? G.xt : G.x;
+        const int64_t plane = G.batch * (k ? G.ts : G.xs);
+        x[0] = take(plane * (two ? 2 : np0));   // a later segment may write it with both planes
+        x[1] = take(two ? plane * 2 : 0);
+    }
     G.part = take(G.batch * G.ps);
     const int64_t mm = G.batch * G.ms * 2;
     G.q[0] = take(mm);
@@ -917,6 +990,7 @@ NsArgs ns_select(const NsArgs& a, Take&& take, Blocks&& blocks, int& total) {
 }
 
 #define NS_LAUNCH(K, N, LDS, ...) hipLaunchKernelGGL(K, dim3(unsigned(N)), dim3(256), LDS, s, __VA_ARGS__)
+#define NS_TILES(K, N, LDS, ...) hipLaunchKernelGGL(K, dim3(unsigned(N)), dim3(64 * NsWaves<BT>::NW), LDS, s, __VA_ARGS__)
 
 template <int BT, int BK, int ST>
 void ns_gram(const NsArgs& a, int src, int np, hipStream_t s) {
@@ -924,8 +998,8 @@ void ns_gram(const NsArgs& a, int src, int np, hipStream_t s) {
     const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
                                [](const NsGroup& G) { return G.batch * G.tiles * G.splits; }, n);
     if (!n) return;
-    if (np == 1) NS_LAUNCH((ns_gram_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 1, 1>()), r, src);
-    else NS_LAUNCH((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, src);
+    if (np == 1) NS_TILES((ns_gram_kernel<BT, 64, ST, 1>), n, (ns_lds_bytes<BT, 64, ST, 1, 1>()), r, src);
+    else NS_TILES((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, src);
 }
 
 template <int BT, int BK, int ST>
@@ -933,7 +1007,7 @@ void ns_prod(const NsArgs& a, const NsJobs& jobs, hipStream_t s) {
     int n;
     const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT && G.mp > 64; },
                                [&](const NsGroup& G) { return G.batch * G.tiles * jobs.n; }, n);
-    if (n) NS_LAUNCH((ns_prod_kernel<BT, BK, ST>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, jobs);
+    if (n) NS_TILES((ns_prod_kernel<BT, BK, ST>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, jobs);
 }
 
 template <int BT, int BK, int ST>
@@ -942,8 +1016,8 @@ void ns_apply(const NsArgs& a, const NsApply& ap, int np, hipStream_t s) {
     const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
                                [](const NsGroup& G) { return G.batch * (G.rp / BT) * (G.cp / BT); }, n);
     if (!n) return;
-    if (np == 1) NS_LAUNCH((ns_apply_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 2, 1>()), r, ap);
-    else NS_LAUNCH((ns_apply_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, ap);
+    if (np == 1) NS_TILES((ns_apply_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 2, 1>()), r, ap);
+    else NS_TILES((ns_apply_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, ap);
 }
 
 // All segments of one pass, X's planes (np of them) in place; `last` describes the final output.
@@ -952,18 +1026,20 @@ hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hip
     for (int k = 0; k < P.nseg; ++k) {
         const NsSeg& g = P.seg[k];
         ns_gram<64, 64, 4>(a, src, np, s);
-        ns_gram<128, 32, 2>(a, src, np, s);
+        ns_gram<128, 32, 4>(a, src, np, s);
+        ns_gram<192, 32, 3>(a, src, np, s);
         int n;
         const NsArgs r = ns_select(a, [](const NsGroup&) { return true; }, [](const NsGroup& G) {
             return G.mp == 64 ? G.batch : G.batch * G.tiles * (G.bt / 16);
         }, n);
         bool small = false;
         for (int i = 0; i < a.ng; ++i) small = small || a.g[i].mp == 64;
-        NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 128 * 17 * int(sizeof(float)), r, g);
+        NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 256 * 17 * int(sizeof(float)), r, g);
         int q = 0;   // the buffer that holds Q
         auto prod = [&](NsJobs j) {
             ns_prod<64, 64, 4>(a, j, s);
-            ns_prod<128, 32, 2>(a, j, s);
+            ns_prod<128, 32, 4>(a, j, s);
+            ns_prod<192, 32, 3>(a, j, s);
         };
         for (int t = 0; t < g.len; ++t) {
             const float sd = t == 0 ? g.sq : g.sp;        // the first P is Q
@@ -985,7 +1061,8 @@ hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hip
         ap.use_inv = k == 0;
         ap.f = float((end ? 1.0 : P.xscale[k]) / (double(g.sq) * (k == 0 ? 1.0 : P.xscale[k - 1])));
         ns_apply<64, 64, 4>(a, ap, np, s);
-        ns_apply<128, 32, 2>(a, ap, np, s);
+        ns_apply<128, 32, 4>(a, ap, np, s);
+        ns_apply<192, 32, 3>(a, ap, np, s);
         src ^= 1;
         np = 2;
     }
@@ -1024,7 +1101,7 @@ hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x,
     const NsGroup& G = a.g[0];
     ProfScope ps(s, [&] { return cb_key("muon_orthogonalize", prec, cb_dims(rows, cols) + "x" + std::to_string(batch)); });
     MuonElem e{};
-    const int64_t sums = batch * G.nsum, planes = batch * ((int64_t(G.rp) * G.cp + kPrepElems - 1) / kPrepElems);
+    const int64_t sums = batch * G.nsum, planes = batch * int64_t(ns_plane_blocks(G));
     if (prec == BF16) {
         NS_LAUNCH((ns_sums_kernel<NS_SRC_BF16>), sums, 0, a, e, x, 0);
         NS_LAUNCH((ns_planes_kernel<NS_SRC_BF16, 1>), planes, 0, a, e, x, eps, 0);
@@ -1098,7 +1175,7 @@ MuonPlan muon_plan(int64_t n_params, const std::vector<MuonMat>& mats, int steps
             P.a.start[P.a.ng++] = P.sums;
             G.part0 = P.block0 + P.sums;
             P.sums += G.batch * G.nsum;
-            P.planes += G.batch * int((int64_t(G.rp) * G.cp + kPrepElems - 1) / kPrepElems);
+            P.planes += G.batch * ns_plane_blocks(G);
         }
         P.a.start[P.a.ng] = P.sums;
         first += o;
@@ -1152,7 +1229,7 @@ hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void
         // the planes' blocks by group, then the gaps' (counted from start[ng])
         int n;
         const NsArgs r = ns_select(p.a, [](const NsGroup&) { return true; }, [](const NsGroup& G) {
-            return G.batch * int((int64_t(G.rp) * G.cp + kPrepElems - 1) / kPrepElems);
+            return G.batch * ns_plane_blocks(G);
         }, n);
         NS_LAUNCH((ns_planes_kernel<NS_SRC_STEP, 2>), p.planes, 0, r, p.e, nullptr, 0.f, p.block0);
         if (p.a.ng == 0) continue;

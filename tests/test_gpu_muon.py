@@ -97,6 +97,14 @@ def test_orthogonalize(prec, shape):
 
 
 @PREC
+@pytest.mark.parametrize("shape", [(8, 1030, 1100), (9, 1100, 1030), (30, 1024, 516)], ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_more_tiles_than_compute_units(prec, shape):
+    """Batches whose products fill the chip; the last matrix of each against the formula."""
+    x = G.q(_gradient(14, *shape), prec)
+    _close(_orth(prec, x)[-1:], ns(x[-1:]), prec, WORST[prec])
+
+
+@PREC
 def test_spread_singular_values_and_low_rank(prec):
     """Singular values from 1 to 1e-6 and to exactly 0: directions far below the matrix's rounding stay below 1.3."""
     rng = np.random.default_rng(3)
