@@ -71,18 +71,25 @@ CB_DEV void ns_join(uint2 hi, uint2 lo, float (&v)[4]) {
     for (int r = 0; r < 4; ++r) v[r] = static_cast<float>(h[r]) + static_cast<float>(l[r]);
 }
 
-// Four neighbours of a row to both planes, or one below the other (`step` bytes apart).
-CB_DEV void ns_store(char* d, int64_t plane, int64_t o, uint2 hi, uint2 lo) {
-    *reinterpret_cast<uint2*>(d + o) = hi;
-    *reinterpret_cast<uint2*>(d + plane + o) = lo;
+// A matrix of two planes is stored in blocks of 32 columns: a row's 32 hi, then its 32 lo, so that what a
+// tile loads of a row for one step of the products is one 128-byte line. ns_at: the byte offset of (row,
+// col)'s hi; its lo is 64 bytes on. A matrix of one plane is row-major.
+constexpr int kLo = 64;
+CB_DEV int64_t ns_at(int row, int col, int ld) { return (int64_t(row) * ld + (col & ~31)) * 4 + (col & 31) * 2; }
+// Four neighbours of a row (four-aligned), or one below the other.
+CB_DEV void ns_store(char* d, int row, int col, int ld, uint2 hi, uint2 lo) {
+    char* p = d + ns_at(row, col, ld);
+    *reinterpret_cast<uint2*>(p) = hi;
+    *reinterpret_cast<uint2*>(p + kLo) = lo;
 }
-CB_DEV void ns_store_across(char* d, int64_t plane, int64_t o, int64_t step, uint2 hi, uint2 lo) {
+CB_DEV void ns_store_across(char* d, int row, int col, int ld, uint2 hi, uint2 lo) {
     const uint16_t h[4] = {uint16_t(hi.x), uint16_t(hi.x >> 16), uint16_t(hi.y), uint16_t(hi.y >> 16)};
     const uint16_t l[4] = {uint16_t(lo.x), uint16_t(lo.x >> 16), uint16_t(lo.y), uint16_t(lo.y >> 16)};
+    char* p = d + ns_at(row, col, ld);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        *reinterpret_cast<uint16_t*>(d + o + r * step) = h[r];
-        *reinterpret_cast<uint16_t*>(d + plane + o + r * step) = l[r];
+    for (int r = 0; r < 4; ++r, p += int64_t(ld) * 4) {
+        *reinterpret_cast<uint16_t*>(p) = h[r];
+        *reinterpret_cast<uint16_t*>(p + kLo) = l[r];
     }
 }
 
@@ -105,11 +112,11 @@ CB_DEV void ns_tile(int t, int& ti, int& tj) {
 
 // ------------------------------------------------------------------ the tile product
 //
-// acc += A B^T over k in [k0, k1) for a BT x BT tile, in NsWaves' waves. An operand is NP planes
-// (`plane` bytes apart) of a padded matrix [rows][k], leading dimension ld elements; padding is zero, so
-// there are no edges. Tiles go from memory into an LDS ring of ST stages
-// by direct loads that stay in flight across barriers (one wait per stage, counted), in the layout they
-// have in memory; 16-byte slots are permuted within a row so that a fragment read meets every bank.
+// acc += A B^T over k in [k0, k1) for a BT x BT tile, in NsWaves' waves. An operand is a padded matrix
+// [rows][k] of NP planes, leading dimension ld elements; padding is zero, so there are no edges. Tiles go
+// from memory into an LDS ring of ST stages by direct loads that stay in flight across barriers (one wait
+// per stage, counted), in the layout they have in memory; 16-byte slots are permuted within a row so that
+// a fragment read meets every bank.
 
 // 16 bytes a lane to LDS at lds + 16 lane. Inline so that the compiler, which cannot tell a ring's
 // stages apart, does not wait for every load in flight before an LDS read; the waits are written out.
@@ -125,7 +132,10 @@ CB_DEV void ns_wait() {
 }
 CB_DEV ns_u32x4 ns_rsrc(const char* base, int64_t bytes) {
     const uint64_t p = reinterpret_cast<uint64_t>(base);
-    return ns_u32x4{uint32_t(p), uint32_t(p >> 32), uint32_t(bytes), 0x00020000u};
+    // (uniform, and said to be: it goes into scalar registers)
+    return ns_u32x4{uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(p)))),
+                    uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(p >> 32)))),
+                    uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(bytes)))), 0x00020000u};
 }
 CB_DEV uint32_t ns_lds(const unsigned char* p) { return uint32_t(reinterpret_cast<uintptr_t>((lds_t*)(p))); }
 
@@ -138,30 +148,31 @@ struct NsWaves {
     static constexpr int FM = BT / WM / 16, FN = BT / WN / 16;
 };
 
-template <int BT, int BK>
+template <int BT, int BK, int NP>
 struct NsOperand {
     static constexpr int NW = NsWaves<BT>::NW;
-    static constexpr int BYTES = BT * BK * 2;              // of a plane's tile
-    static constexpr int NI = BYTES / (1024 * NW);         // direct loads a wave and plane
-    static constexpr int SPR = BK / 8;                     // 16-byte slots per LDS row
+    static constexpr int RB = BK * NP * 2;                 // bytes of a tile row
+    static constexpr int BYTES = BT * RB;
+    static constexpr int NI = BYTES / (1024 * NW);         // direct loads a wave
+    static constexpr int SPR = RB / 16;                    // 16-byte slots per row
     static_assert(BYTES % (1024 * NW) == 0, "whole loads");
     uint32_t base[NI];
     // the slot that holds chunk c of row r (its own inverse)
-    static CB_DEV int swz(int r, int c) { return BK == 64 ? c ^ (r & 7) : c ^ ((r >> 1) & 3); }
+    static CB_DEV int swz(int r, int c) { return RB == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7); }
     CB_DEV NsOperand(int ld, int row0, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int s = (wave + NW * i) * 64 + lane, r = s / SPR, c = swz(r, s % SPR);
-            base[i] = (uint32_t(row0 + r) * uint32_t(ld) + uint32_t(c * 8)) * 2u;
+            base[i] = uint32_t(row0 + r) * uint32_t(ld) * (NP * 2u) + uint32_t(c * 16);
         }
     }
     // this wave's load i of a tile at k
     CB_DEV void issue(int i, ns_u32x4 rs, uint32_t lds, int k, bool live, int wave) const {
-        ns_dma16(rs, lds + (wave + NW * i) * 1024, live ? base[i] + uint32_t(k) * 2u : kOOB);
+        ns_dma16(rs, lds + (wave + NW * i) * 1024, live ? base[i] + uint32_t(k) * (NP * 2u) : kOOB);
     }
-    // 8 consecutive k (step ks of 32, lane group g) of tile row `row` (row % 16 == lane % 16)
-    static CB_DEV uint4 frag(const unsigned char* t, int row, int ks, int lane) {
-        return *reinterpret_cast<const uint4*>(t + row * (BK * 2) + swz(row, ks * 4 + (lane >> 4)) * 16);
+    // plane p's 8 consecutive k (step ks of 32, lane group g) of tile row `row` (row % 16 == lane % 16)
+    static CB_DEV uint4 frag(const unsigned char* t, int p, int row, int ks, int lane) {
+        return *reinterpret_cast<const uint4*>(t + row * RB + swz(row, (ks * NP + p) * 4 + (lane >> 4)) * 16);
     }
 };
 
@@ -172,36 +183,31 @@ template <int BT>
 using NsAcc = cb_f32x4[NsWaves<BT>::FM][NsWaves<BT>::FN];
 
 template <int BT, int BK, int ST, int NA, int NB>
-CB_DEV void ns_gemm(const char* A, int64_t aplane, int lda, int arow, const char* B, int64_t bplane, int ldb, int brow,
+CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char* B, int64_t bbytes, int ldb, int brow,
                     int k0, int k1, unsigned char* smem, NsAcc<BT>& acc) {
     using W = NsWaves<BT>;
     constexpr int FM = W::FM, FN = W::FN, KS = BK / 32;
-    using OA = NsOperand<BT, BK>;
-    using OB = OA;
-    constexpr int STAGE = NA * OA::BYTES + NB * OB::BYTES, LPS = NA * OA::NI + NB * OB::NI;
+    using OA = NsOperand<BT, BK, NA>;
+    using OB = NsOperand<BT, BK, NB>;
+    constexpr int STAGE = OA::BYTES + OB::BYTES, LPS = OA::NI + OB::NI;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, wm = wave / W::WN, wn = wave % W::WN;
     const OA oa(lda, arow, wave, lane);
     const OB ob(ldb, brow, wave, lane);
-    ns_u32x4 ra[NA], rb[NB];
-#pragma unroll
-    for (int p = 0; p < NA; ++p) ra[p] = ns_rsrc(A + p * aplane, aplane);
-#pragma unroll
-    for (int p = 0; p < NB; ++p) rb[p] = ns_rsrc(B + p * bplane, bplane);
+    const ns_u32x4 ra = ns_rsrc(A, abytes), rb = ns_rsrc(B, bbytes);
     const uint32_t lds0 = ns_lds(smem);
     const int nb = (k1 - k0) / BK;
     // this wave's load d of stage `it`; past the end it is out of range (zeros), so every stage counts the same
     auto issue = [&](int it, int d) CB_INLINE_LAMBDA {
-        const int p = d / OA::NI, i = d % OA::NI;
-        const uint32_t l = lds0 + uint32_t(it % ST) * STAGE + uint32_t(p) * OA::BYTES;
-        if (p < NA) oa.issue(i, ra[p < NA ? p : 0], l, k0 + it * BK, it < nb, wave);
-        else ob.issue(i, rb[p < NA ? 0 : p - NA], l, k0 + it * BK, it < nb, wave);
+        const uint32_t l = lds0 + uint32_t(it % ST) * STAGE;
+        if (d < OA::NI) oa.issue(d < OA::NI ? d : 0, ra, l, k0 + it * BK, it < nb, wave);
+        else ob.issue(d < OA::NI ? 0 : d - OA::NI, rb, l + OA::BYTES, k0 + it * BK, it < nb, wave);
     };
     auto read_a = [&](int st, int p, int ks, int i) CB_INLINE_LAMBDA {
-        return OA::frag(smem + (st % ST) * STAGE + p * OA::BYTES, wm * (FM * 16) + i * 16 + r16, ks, lane);
+        return OA::frag(smem + (st % ST) * STAGE, p, wm * (FM * 16) + i * 16 + r16, ks, lane);
     };
     auto read_b = [&](int st, int p, int ks, int j) CB_INLINE_LAMBDA {
-        return OA::frag(smem + (st % ST) * STAGE + (NA + p) * OA::BYTES, wn * (FN * 16) + j * 16 + r16, ks, lane);
+        return OB::frag(smem + (st % ST) * STAGE + OA::BYTES, p, wn * (FN * 16) + j * 16 + r16, ks, lane);
     };
     // x y row by row; with(ks, i) before row i of step ks: reads and loads go between the products, for
     // one block of either would hold the matrix core up
@@ -294,30 +300,6 @@ CB_DEV void ns_each(NsAcc<BT>& acc, Fn&& f) {
 
 // ------------------------------------------------------------------ Gram product
 
-// part [split][tile][N][M] float32: the k range of one split of one tile of X X^T (smaller side).
-template <int BT, int BK, int ST, int NP>
-__global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a, int src) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    int blk = blockIdx.x;
-    const NsGroup& G = a.g[ns_group(a, blk)];
-    const int z = blk % G.splits, t = blk / G.splits % G.tiles, b = blk / (G.splits * G.tiles);
-    int ti, tj;
-    ns_tile(t, ti, tj);
-    const char* X = a.ws + (G.tall ? G.xt : G.x)[src] + int64_t(b) * NP * (G.tall ? G.ts : G.xs);   // [m][n]
-    const int k0 = z * G.kchunk, k1 = min(G.np, k0 + G.kchunk);
-    NsAcc<BT> acc;
-    ns_clear<BT>(acc);
-    const int ld = G.tall ? G.ldt : G.ldx;
-    const int64_t xs = G.tall ? G.ts : G.xs;
-    ns_gemm<BT, BK, ST, NP, NP>(X, xs, ld, ti * BT, X, xs, ld, tj * BT, k0, k1, smem, acc);
-    float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.tiles + t) * (BT * BT);
-    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
-        *reinterpret_cast<float4*>(part + N * BT + M) = make_float4(v[0], v[1], v[2], v[3]);
-    });
-}
-
-// ------------------------------------------------------------------ the m x m products
-
 struct NsSeg {                 // one segment's polynomials and scales (host constants)
     int len;
     float c[kSegBf16][3];
@@ -334,23 +316,101 @@ CB_DEV float ns_alpha(const NsArgs& a, const NsSeg& s, int mat) {
     return s.alpha > 0.f ? s.alpha * f * f : f * f;
 }
 
+// One tile of A = X X^T (smaller side), scaled; or, where k is split or the m x m part is done in LDS, the
+// k range of one split of it to part [split][tile][N][M] float32.
+template <int BT, int BK, int ST, int NP>
+__global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a, NsSeg s, int src) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    int blk = blockIdx.x;
+    const NsGroup& G = a.g[ns_group(a, blk)];
+    const int z = blk % G.splits, t = blk / G.splits % G.tiles, b = blk / (G.splits * G.tiles);
+    int ti, tj;
+    ns_tile(t, ti, tj);
+    const char* X = a.ws + (G.tall ? G.xt : G.x)[src] + int64_t(b) * NP * (G.tall ? G.ts : G.xs);   // [m][n]
+    const int k0 = z * G.kchunk, k1 = min(G.np, k0 + G.kchunk);
+    NsAcc<BT> acc;
+    ns_clear<BT>(acc);
+    const int ld = G.tall ? G.ldt : G.ldx;
+    const int64_t xs = NP * (G.tall ? G.ts : G.xs);
+    ns_gemm<BT, BK, ST, NP, NP>(X, xs, ld, ti * BT, X, xs, ld, tj * BT, k0, k1, smem, acc);
+    if (G.splits == 1 && G.mp > 64) {
+        char* D = a.ws + G.a + int64_t(b) * 2 * G.ms;
+        const float f = ns_alpha(a, s, G.first + b) * s.sa;
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+            const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+            uint2 hi, lo;
+            ns_split(w, hi, lo);
+            ns_store(D, tj * BT + N, ti * BT + M, G.ldm, hi, lo);
+            if (ti != tj) ns_store_across(D, ti * BT + M, tj * BT + N, G.ldm, hi, lo);
+        });
+        return;
+    }
+    float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.tiles + t) * (BT * BT);
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        *reinterpret_cast<float4*>(part + N * BT + M) = make_float4(v[0], v[1], v[2], v[3]);
+    });
+}
+
+// ------------------------------------------------------------------ the m x m products
+
 // A whole segment's m x m part of one matrix with m <= 64 in LDS, float32: five m x m buffers of pitch
-// 68 (the fragment reads of 16 rows by 4 k meet 64 different banks).
+// 68, which a fragment read of 16 bytes from each of 16 rows crosses without bank conflicts.
 constexpr int kSmPitch = 68, kSmBuf = 64 * kSmPitch;
 constexpr int kSmLds = 5 * kSmBuf * int(sizeof(float));
 
-// f(N, M, v): four rows M .. M+3 of column N of L R^T, tiles of 16 in turn over the waves.
+// f(N, M, v, mirror): four rows M .. M+3 of column N of L R^T for symmetric L, R that commute: the lower
+// triangle's tiles of 16 in turn over the waves, the others their mirror images. A lane group takes four
+// neighbouring k of each 16 (any order of k is the same sum), so four products share a 16-byte read.
 template <class Fn>
 CB_DEV void ns_small_mul(const float* L, const float* R, int mt, Fn&& f) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r16 = lane & 15;
-    for (int t = wave; t < mt * mt; t += 4) {
-        const int i = t / mt, j = t - i * mt;
-        const float* l = L + (i * 16 + r16) * kSmPitch + g;
-        const float* r = R + (j * 16 + r16) * kSmPitch + g;
-        cb_f32x4 acc{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < mt * 16; k += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(l[k], r[k], acc, 0, 0, 0);
-        f(j * 16 + r16, i * 16 + 4 * g, acc);
+    for (int t = wave; t < mt * (mt + 1) / 2; t += 4) {
+        int i, j;
+        ns_tile(t, i, j);
+        const float* l = L + (i * 16 + r16) * kSmPitch + 4 * g;
+        const float* r = R + (j * 16 + r16) * kSmPitch + 4 * g;
+        float4 x[4], y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < mt) {
+                x[k] = *reinterpret_cast<const float4*>(l + 16 * k);
+                y[k] = *reinterpret_cast<const float4*>(r + 16 * k);
+            }
+        // two sums, so that a product does not wait for the one before
+        cb_f32x4 acc{0.f, 0.f, 0.f, 0.f}, acc2{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < mt) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[k].x, y[k].x, acc, 0, 0, 0);
+                acc2 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[k].y, y[k].y, acc2, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[k].z, y[k].z, acc, 0, 0, 0);
+                acc2 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[k].w, y[k].w, acc2, 0, 0, 0);
+            }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += acc2[e];
+        f(j * 16 + r16, i * 16 + 4 * g, acc, i != j);
     }
+}
+CB_DEV void ns_small_put(float* D, int N, int M, float4 v, bool mirror) {
+    *reinterpret_cast<float4*>(D + N * kSmPitch + M) = v;
+    if (mirror) {
+        D[M * kSmPitch + N] = v.x; D[(M + 1) * kSmPitch + N] = v.y;
+        D[(M + 2) * kSmPitch + N] = v.z; D[(M + 3) * kSmPitch + N] = v.w;
+    }
+}
+
+// The sum of n float4, `step` floats apart, in order; eight loads in flight.
+CB_DEV float4 ns_sum(const float* p, int n, int64_t step) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z = 0; z < n; z += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const float4*>(p + min(z + u, n - 1) * step);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (z + u < n) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+    }
+    return s;
 }
 
 CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, float* sm) {
@@ -359,28 +419,25 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
     const float alpha = ns_alpha(a, s, G.first + b);
     const float* part = reinterpret_cast<const float*>(a.ws + G.part + int64_t(b) * G.ps);
     for (int e = threadIdx.x * 4; e < 64 * 64; e += 1024) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int z = 0; z < G.splits; ++z) {
-            const float4 q = *reinterpret_cast<const float4*>(part + z * 4096 + e);
-            v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
-        }
+        const float4 v = ns_sum(part + e, G.splits, 4096);
         *reinterpret_cast<float4*>(A + (e >> 6) * kSmPitch + (e & 63)) =
             make_float4(v.x * alpha, v.y * alpha, v.z * alpha, v.w * alpha);
     }
     __syncthreads();
     auto put = [&](float* D) {
-        return [=](int N, int M, cb_f32x4 v) CB_INLINE_LAMBDA {
-            *reinterpret_cast<float4*>(D + N * kSmPitch + M) = make_float4(v[0], v[1], v[2], v[3]);
+        return [=](int N, int M, cb_f32x4 v, bool mirror) CB_INLINE_LAMBDA {
+            ns_small_put(D, N, M, make_float4(v[0], v[1], v[2], v[3]), mirror);
         };
     };
     for (int t = 0; t < s.len; ++t) {
         float* D = t == 0 ? Q : P;
         const float ca = s.c[t][0], cb = s.c[t][1], cc = s.c[t][2];
-        ns_small_mul(A, A, mt, [&](int N, int M, cb_f32x4 v) CB_INLINE_LAMBDA {
+        ns_small_mul(A, A, mt, [&](int N, int M, cb_f32x4 v, bool mirror) CB_INLINE_LAMBDA {
             const float4 q = *reinterpret_cast<const float4*>(A + N * kSmPitch + M);
-            *reinterpret_cast<float4*>(D + N * kSmPitch + M) =
-                make_float4(cb * q.x + cc * v[0] + (N == M ? ca : 0.f), cb * q.y + cc * v[1] + (N == M + 1 ? ca : 0.f),
-                            cb * q.z + cc * v[2] + (N == M + 2 ? ca : 0.f), cb * q.w + cc * v[3] + (N == M + 3 ? ca : 0.f));
+            ns_small_put(D, N, M,
+                         make_float4(cb * q.x + cc * v[0] + (N == M ? ca : 0.f), cb * q.y + cc * v[1] + (N == M + 1 ? ca : 0.f),
+                                     cb * q.z + cc * v[2] + (N == M + 2 ? ca : 0.f), cb * q.w + cc * v[3] + (N == M + 3 ? ca : 0.f)),
+                         mirror);
         });
         __syncthreads();
         if (t > 0) {
@@ -403,7 +460,7 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
         for (int r = 0; r < 4; ++r) v[r] = N < G.m && M + r < G.m ? Q[N * kSmPitch + M + r] * s.sq : 0.f;
         uint2 hi, lo;
         ns_split(v, hi, lo);
-        ns_store(q, G.ms, (N * G.ldm + M) * 2, hi, lo);
+        ns_store(q, N, M, G.ldm, hi, lo);
     }
 }
 
@@ -427,11 +484,8 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     char* A = a.ws + G.a + int64_t(b) * 2 * G.ms;
     for (int e = threadIdx.x * 4; e < 16 * bt; e += 1024) {
         const int N = n0 + e / bt, M = e % bt;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int z = 0; z < G.splits; ++z) {
-            const float4 q = *reinterpret_cast<const float4*>(part + int64_t(z) * G.tiles * bt * bt + N * bt + M);
-            v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
-        }
+        const float4 q = ns_sum(part + N * bt + M, G.splits, int64_t(G.tiles) * bt * bt);
+        float v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             v[r] *= alpha;
@@ -439,8 +493,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
         }
         uint2 hi, lo;
         ns_split(v, hi, lo);
-        const int64_t o = (int64_t(tj * bt + N) * G.ldm + ti * bt + M) * 2;
-        ns_store(A, G.ms, o, hi, lo);
+        ns_store(A, tj * bt + N, ti * bt + M, G.ldm, hi, lo);
     }
     if (ti == tj) return;
     __syncthreads();
@@ -449,8 +502,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
         const float v[4] = {sh[M * 17 + q], sh[M * 17 + q + 1], sh[M * 17 + q + 2], sh[M * 17 + q + 3]};
         uint2 hi, lo;
         ns_split(v, hi, lo);
-        const int64_t o = (int64_t(ti * bt + M) * G.ldm + tj * bt + n0 + q) * 2;
-        ns_store(A, G.ms, o, hi, lo);
+        ns_store(A, ti * bt + M, tj * bt + n0 + q, G.ldm, hi, lo);
     }
 }
 
@@ -478,7 +530,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
     ns_tile(t, ti, tj);
     NsAcc<BT> acc;
     ns_clear<BT>(acc);
-    ns_gemm<BT, BK, ST, 2, 2>(ns_buf(a, G, J.lhs, b), G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), G.ms, G.ldm, tj * BT, 0,
+    ns_gemm<BT, BK, ST, 2, 2>(ns_buf(a, G, J.lhs, b), 2 * G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), 2 * G.ms, G.ldm, tj * BT, 0,
                               G.mp, smem, acc);
     char* D = ns_buf(a, G, J.dst, b);
     const char* A = ns_buf(a, G, NS_A, b);
@@ -486,20 +538,20 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
     const int poly = J.poly;
     ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
         const int m = ti * BT + M, n = tj * BT + N;
-        const int64_t o = (int64_t(n) * G.ldm + m) * 2;
         float w[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[r] = f * v[r];
         if (poly) {
+            const char* p = A + ns_at(n, m, G.ldm);
             float q[4];
-            ns_join(*reinterpret_cast<const uint2*>(A + o), *reinterpret_cast<const uint2*>(A + G.ms + o), q);
+            ns_join(*reinterpret_cast<const uint2*>(p), *reinterpret_cast<const uint2*>(p + kLo), q);
 #pragma unroll
             for (int r = 0; r < 4; ++r) w[r] += fa * q[r] + (m + r == n ? diag : 0.f);
         }
         uint2 hi, lo;
         ns_split(w, hi, lo);
-        ns_store(D, G.ms, o, hi, lo);
-        if (ti != tj) ns_store_across(D, G.ms, (int64_t(m) * G.ldm + n) * 2, int64_t(G.ldm) * 2, hi, lo);
+        ns_store(D, n, m, G.ldm, hi, lo);
+        if (ti != tj) ns_store_across(D, m, n, G.ldm, hi, lo);
     });
 }
 
@@ -524,20 +576,20 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     const int tn = G.rp / BT, tm = G.cp / BT;   // N over the rows, M over the columns
     const int jt = blk % tn, it = blk / tn % tm, b = blk / (tn * tm);
     const int ld = G.tall ? G.ldx : G.ldt;
-    const int64_t xs = G.tall ? G.xs : G.ts;
-    const char* X = a.ws + (G.tall ? G.x : G.xt)[ap.src] + int64_t(b) * NP * xs;   // [n][m]
+    const int64_t xs = NP * (G.tall ? G.xs : G.ts);
+    const char* X = a.ws + (G.tall ? G.x : G.xt)[ap.src] + b * xs;   // [n][m]
     const char* Q = a.ws + (G.mp == 64 ? G.q[0] : G.q[ap.q]) + int64_t(b) * 2 * G.ms;
     NsAcc<BT> acc;
     ns_clear<BT>(acc);
     // the result's rows are X's where it is tall (M, the contiguous index, over Q's) and Q's where it is wide
     if constexpr (NP == 2) {
         const bool tall = G.tall;
-        ns_gemm<BT, BK, ST, 2, 2>(tall ? Q : X, tall ? G.ms : xs, tall ? G.ldm : ld, it * BT, tall ? X : Q,
-                                  tall ? xs : G.ms, tall ? ld : G.ldm, jt * BT, 0, G.mp, smem, acc);
+        ns_gemm<BT, BK, ST, 2, 2>(tall ? Q : X, tall ? 2 * G.ms : xs, tall ? G.ldm : ld, it * BT, tall ? X : Q,
+                                  tall ? xs : 2 * G.ms, tall ? ld : G.ldm, jt * BT, 0, G.mp, smem, acc);
     } else if (G.tall) {
-        ns_gemm<BT, BK, ST, 2, NP>(Q, G.ms, G.ldm, it * BT, X, xs, ld, jt * BT, 0, G.mp, smem, acc);
+        ns_gemm<BT, BK, ST, 2, NP>(Q, 2 * G.ms, G.ldm, it * BT, X, xs, ld, jt * BT, 0, G.mp, smem, acc);
     } else {
-        ns_gemm<BT, BK, ST, NP, 2>(X, xs, ld, it * BT, Q, G.ms, G.ldm, jt * BT, 0, G.mp, smem, acc);
+        ns_gemm<BT, BK, ST, NP, 2>(X, xs, ld, it * BT, Q, 2 * G.ms, G.ldm, jt * BT, 0, G.mp, smem, acc);
     }
     float f = ap.f;
     const float2 info = ns_info(a, G.first + b);
@@ -551,8 +603,8 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
             uint2 hi, lo;
             ns_split(w, hi, lo);
             const int r = jt * BT + N, c = it * BT + M;
-            ns_store(D, G.xs, (int64_t(r) * G.ldx + c) * 2, hi, lo);
-            ns_store_across(T, G.ts, (int64_t(c) * G.ldt + r) * 2, int64_t(G.ldt) * 2, hi, lo);
+            ns_store(D, r, c, G.ldx, hi, lo);
+            ns_store_across(T, c, r, G.ldt, hi, lo);
         });
         return;
     }
@@ -834,9 +886,8 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         }
         uint2 hi, lo;
         ns_split(w, hi, lo);
-        const int64_t o = (int64_t(r) * G.ldx + c) * 2;
-        *reinterpret_cast<uint2*>(X + o) = hi;
-        if (NP > 1) *reinterpret_cast<uint2*>(X + G.xs + o) = lo;
+        if (NP > 1) ns_store(X, r, c, G.ldx, hi, lo);
+        else *reinterpret_cast<uint2*>(X + (int64_t(r) * G.ldx + c) * 2) = hi;
 #pragma unroll
         for (int i = 0; i < 4; ++i) tile[(lc + i) * 65 + lr] = w[i];
     }
@@ -846,9 +897,8 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         const float w[4] = {tile[lc * 65 + lr], tile[lc * 65 + lr + 1], tile[lc * 65 + lr + 2], tile[lc * 65 + lr + 3]};
         uint2 hi, lo;
         ns_split(w, hi, lo);
-        const int64_t o = (int64_t(q0 + lc) * G.ldt + r0 + lr) * 2;
-        *reinterpret_cast<uint2*>(T + o) = hi;
-        if (NP > 1) *reinterpret_cast<uint2*>(T + G.ts + o) = lo;
+        if (NP > 1) ns_store(T, q0 + lc, r0 + lr, G.ldt, hi, lo);
+        else *reinterpret_cast<uint2*>(T + (int64_t(q0 + lc) * G.ldt + r0 + lr) * 2) = hi;
     }
 }
 
@@ -993,13 +1043,13 @@ NsArgs ns_select(const NsArgs& a, Take&& take, Blocks&& blocks, int& total) {
 #define NS_TILES(K, N, LDS, ...) hipLaunchKernelGGL(K, dim3(unsigned(N)), dim3(64 * NsWaves<BT>::NW), LDS, s, __VA_ARGS__)
 
 template <int BT, int BK, int ST>
-void ns_gram(const NsArgs& a, int src, int np, hipStream_t s) {
+void ns_gram(const NsArgs& a, const NsSeg& g, int src, int np, hipStream_t s) {
     int n;
     const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
                                [](const NsGroup& G) { return G.batch * G.tiles * G.splits; }, n);
     if (!n) return;
-    if (np == 1) NS_TILES((ns_gram_kernel<BT, 64, ST, 1>), n, (ns_lds_bytes<BT, 64, ST, 1, 1>()), r, src);
-    else NS_TILES((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, src);
+    if (np == 1) NS_TILES((ns_gram_kernel<BT, 64, ST, 1>), n, (ns_lds_bytes<BT, 64, ST, 1, 1>()), r, g, src);
+    else NS_TILES((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, g, src);
 }
 
 template <int BT, int BK, int ST>
@@ -1025,16 +1075,16 @@ hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hip
     int src = 0;
     for (int k = 0; k < P.nseg; ++k) {
         const NsSeg& g = P.seg[k];
-        ns_gram<64, 64, 4>(a, src, np, s);
-        ns_gram<128, 32, 4>(a, src, np, s);
-        ns_gram<192, 32, 3>(a, src, np, s);
+        ns_gram<64, 64, 4>(a, g, src, np, s);
+        ns_gram<128, 32, 4>(a, g, src, np, s);
+        ns_gram<192, 32, 3>(a, g, src, np, s);
         int n;
-        const NsArgs r = ns_select(a, [](const NsGroup&) { return true; }, [](const NsGroup& G) {
+        const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.mp == 64 || G.splits > 1; }, [](const NsGroup& G) {
             return G.mp == 64 ? G.batch : G.batch * G.tiles * (G.bt / 16);
         }, n);
         bool small = false;
         for (int i = 0; i < a.ng; ++i) small = small || a.g[i].mp == 64;
-        NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 256 * 17 * int(sizeof(float)), r, g);
+        if (n) NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 256 * 17 * int(sizeof(float)), r, g);
         int q = 0;   // the buffer that holds Q
         auto prod = [&](NsJobs j) {
             ns_prod<64, 64, 4>(a, j, s);
