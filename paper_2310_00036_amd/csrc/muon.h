@@ -14,7 +14,9 @@ constexpr int kNsMaxSteps = 16;
 struct NsGroup {
     int rows, cols, rp, cp, m, n, mp, np, tall;   // tall: rows > cols
     int batch, first;                 // first: index of its first matrix in the call
-    int bt, tiles, splits, kchunk;    // tile (64, 128 or 192), tiles of a symmetric m x m product, the Gram product's k split
+    int small;                        // m <= 64: the m x m part in one workgroup
+    int bt, bg, ba;                   // tiles of the m x m products (32 to 192), of the Gram product, of Q X
+    int tiles, gtiles, splits, kchunk;   // tiles of symmetric m x m products; the Gram product's k split
     int table, nsum, part0;           // 1 + its first offset in NsArgs::off (0: b * rows * cols); its blocks of the sums
     float scale;                      // the update's factor (muon_step)
     int64_t x[2], xt[2], part, a, t, p, q[2];   // workspace byte offsets of the first matrix (xt: X transposed)

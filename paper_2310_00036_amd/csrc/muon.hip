@@ -285,7 +285,7 @@ CB_DEV void ns_clear(NsAcc<BT>& acc) {
         for (int j = 0; j < NsWaves<BT>::FN; ++j) acc[i][j] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// f(M, N, acc[i][j]) for every group of four rows M .. M+3 of column N that this lane holds (local).
+// f(M, N, acc[i][j], i, j) for every group of four rows M .. M+3 of column N that this lane holds (local).
 template <int BT, class Fn>
 CB_DEV void ns_each(NsAcc<BT>& acc, Fn&& f) {
     using W = NsWaves<BT>;
@@ -295,7 +295,7 @@ CB_DEV void ns_each(NsAcc<BT>& acc, Fn&& f) {
     for (int i = 0; i < W::FM; ++i)
 #pragma unroll
         for (int j = 0; j < W::FN; ++j)
-            f(wm * (W::FM * 16) + i * 16 + 4 * g, wn * (W::FN * 16) + j * 16 + r16, acc[i][j]);
+            f(wm * (W::FM * 16) + i * 16 + 4 * g, wn * (W::FN * 16) + j * 16 + r16, acc[i][j], i, j);
 }
 
 // ------------------------------------------------------------------ Gram product
@@ -304,6 +304,7 @@ struct NsSeg {                 // one segment's polynomials and scales (host con
     int len;
     float c[kSegBf16][3];
     float sa, sp, st, sq;      // power-of-two scales of A, P, P A and Q
+    float ss, sv;              // and of P P and b P + c A' P
     float alpha;               // the Gram matrix's scale where X's planes have a static one, else 0
 };
 
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a,
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
-    const int z = blk % G.splits, t = blk / G.splits % G.tiles, b = blk / (G.splits * G.tiles);
+    const int z = blk % G.splits, t = blk / G.splits % G.gtiles, b = blk / (G.splits * G.gtiles);
     int ti, tj;
     ns_tile(t, ti, tj);
     const char* X = a.ws + (G.tall ? G.xt : G.x)[src] + int64_t(b) * NP * (G.tall ? G.ts : G.xs);   // [m][n]
@@ -333,10 +334,10 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a,
     const int ld = G.tall ? G.ldt : G.ldx;
     const int64_t xs = NP * (G.tall ? G.ts : G.xs);
     ns_gemm<BT, BK, ST, NP, NP>(X, xs, ld, ti * BT, X, xs, ld, tj * BT, k0, k1, smem, acc);
-    if (G.splits == 1 && G.mp > 64) {
+    if (G.splits == 1 && !G.small) {
         char* D = a.ws + G.a + int64_t(b) * 2 * G.ms;
         const float f = ns_alpha(a, s, G.first + b) * s.sa;
-        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
             const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
             uint2 hi, lo;
             ns_split(w, hi, lo);
@@ -345,8 +346,8 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a,
         });
         return;
     }
-    float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.tiles + t) * (BT * BT);
-    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+    float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.gtiles + t) * (BT * BT);
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
         *reinterpret_cast<float4*>(part + N * BT + M) = make_float4(v[0], v[1], v[2], v[3]);
     });
 }
@@ -470,13 +471,13 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
-    if (G.mp == 64) {
+    if (G.small) {
         ns_small(a, G, s, blk, reinterpret_cast<float*>(smem));
         return;
     }
     float* sh = reinterpret_cast<float*>(smem);   // [BT][17]
-    const int bt = G.bt, strips = bt / 16;
-    const int n0 = (blk % strips) * 16, t = blk / strips % G.tiles, b = blk / (strips * G.tiles);
+    const int bt = G.bg, strips = bt / 16;
+    const int n0 = (blk % strips) * 16, t = blk / strips % G.gtiles, b = blk / (strips * G.gtiles);
     int ti, tj;
     ns_tile(t, ti, tj);
     const float alpha = ns_alpha(a, s, G.first + b) * s.sa;
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     char* A = a.ws + G.a + int64_t(b) * 2 * G.ms;
     for (int e = threadIdx.x * 4; e < 16 * bt; e += 1024) {
         const int N = n0 + e / bt, M = e % bt;
-        const float4 q = ns_sum(part + N * bt + M, G.splits, int64_t(G.tiles) * bt * bt);
+        const float4 q = ns_sum(part + N * bt + M, G.splits, int64_t(G.gtiles) * bt * bt);
         float v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -507,8 +508,8 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
 }
 
 enum { NS_A = 0, NS_T, NS_P, NS_Q0, NS_Q1 };
-struct NsJob {                 // dst = lhs rhs (scaled), or with poly diag I + fa A + f lhs rhs
-    int lhs, rhs, dst, poly;
+struct NsJob {                 // dst = diag I + fa add + f lhs rhs (scales included)
+    int lhs, rhs, dst, add;
     float f, fa, diag;
 };
 struct NsJobs { int n; NsJob j[2]; };
@@ -518,33 +519,49 @@ CB_DEV char* ns_buf(const NsArgs& a, const NsGroup& G, int id, int b) {
     return a.ws + o + int64_t(b) * 2 * G.ms;
 }
 
-// Products of symmetric matrices that commute: the lower triangle's tiles, and their mirror images.
+// Products of symmetric matrices that commute: the lower triangle's tiles, and their mirror images. With
+// tiles of 32 and 64, where a launch is a row of latencies, `add` is read before the product.
 template <int BT, int BK, int ST>
 __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
     extern __shared__ __align__(16) unsigned char smem[];
+    constexpr bool EARLY = BT <= 64;
+    using W = NsWaves<BT>;
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
     const NsJob& J = jobs.j[blk % jobs.n];
     const int t = blk / jobs.n % G.tiles, b = blk / (jobs.n * G.tiles);
     int ti, tj;
     ns_tile(t, ti, tj);
+    const char* add = ns_buf(a, G, J.add, b);
+    uint4 early[EARLY ? W::FM : 1][EARLY ? W::FN : 1];
     NsAcc<BT> acc;
     ns_clear<BT>(acc);
-    ns_gemm<BT, BK, ST, 2, 2>(ns_buf(a, G, J.lhs, b), 2 * G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), 2 * G.ms, G.ldm, tj * BT, 0,
-                              G.mp, smem, acc);
+    if (EARLY && (J.fa != 0.f || J.diag != 0.f))
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4, int i, int j) CB_INLINE_LAMBDA {
+            const char* p = add + ns_at(tj * BT + N, ti * BT + M, G.ldm);
+            const uint2 h = *reinterpret_cast<const uint2*>(p), l = *reinterpret_cast<const uint2*>(p + kLo);
+            early[i][j] = make_uint4(h.x, h.y, l.x, l.y);
+        });
+    ns_gemm<BT, BK, ST, 2, 2>(ns_buf(a, G, J.lhs, b), 2 * G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), 2 * G.ms, G.ldm,
+                              tj * BT, 0, G.mp, smem, acc);
     char* D = ns_buf(a, G, J.dst, b);
-    const char* A = ns_buf(a, G, NS_A, b);
     const float f = J.f, fa = J.fa, diag = J.diag;
-    const int poly = J.poly;
-    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int i, int j) CB_INLINE_LAMBDA {
         const int m = ti * BT + M, n = tj * BT + N;
         float w[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[r] = f * v[r];
-        if (poly) {
-            const char* p = A + ns_at(n, m, G.ldm);
+        if (fa != 0.f || diag != 0.f) {
+            uint4 e;
+            if constexpr (EARLY) {
+                e = early[i][j];
+            } else {
+                const char* p = add + ns_at(n, m, G.ldm);
+                const uint2 h = *reinterpret_cast<const uint2*>(p), l = *reinterpret_cast<const uint2*>(p + kLo);
+                e = make_uint4(h.x, h.y, l.x, l.y);
+            }
             float q[4];
-            ns_join(*reinterpret_cast<const uint2*>(p), *reinterpret_cast<const uint2*>(p + kLo), q);
+            ns_join(make_uint2(e.x, e.y), make_uint2(e.z, e.w), q);
 #pragma unroll
             for (int r = 0; r < 4; ++r) w[r] += fa * q[r] + (m + r == n ? diag : 0.f);
         }
@@ -578,7 +595,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     const int ld = G.tall ? G.ldx : G.ldt;
     const int64_t xs = NP * (G.tall ? G.xs : G.ts);
     const char* X = a.ws + (G.tall ? G.x : G.xt)[ap.src] + b * xs;   // [n][m]
-    const char* Q = a.ws + (G.mp == 64 ? G.q[0] : G.q[ap.q]) + int64_t(b) * 2 * G.ms;
+    const char* Q = a.ws + (G.small ? G.q[0] : G.q[ap.q]) + int64_t(b) * 2 * G.ms;
     NsAcc<BT> acc;
     ns_clear<BT>(acc);
     // the result's rows are X's where it is tall (M, the contiguous index, over Q's) and Q's where it is wide
@@ -598,7 +615,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     if (ap.out == NS_OUT_MID) {
         char* D = a.ws + G.x[ap.dst] + int64_t(b) * 2 * G.xs;
         char* T = a.ws + G.xt[ap.dst] + int64_t(b) * 2 * G.ts;
-        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
             const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
             uint2 hi, lo;
             ns_split(w, hi, lo);
@@ -613,7 +630,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     if (ap.out == NS_OUT_BF16) {
         uint16_t* y = static_cast<uint16_t*>(ap.y) + off;
         const bool vec = cols % 4 == 0 && (reinterpret_cast<uintptr_t>(y) & 7) == 0;
-        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
             const int r = jt * BT + N, c = it * BT + M;
             if (r >= rows) return;
             uint16_t* o = y + int64_t(r) * cols + c;
@@ -627,7 +644,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     }
     if (ap.out == NS_OUT_F32) {
         float* y = static_cast<float*>(ap.y) + off;
-        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
             const int r = jt * BT + N, c = it * BT + M;
             if (r >= rows) return;
             float* o = y + int64_t(r) * cols + c;
@@ -643,7 +660,7 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     }
     // the parameters: p <- decay p - lr scale O
     f *= ap.lr * G.scale;
-    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v) CB_INLINE_LAMBDA {
+    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
         const int r = jt * BT + N, c = it * BT + M;
         if (r >= rows || c >= cols) return;
         const int64_t o = off + int64_t(r) * cols + c;
@@ -907,26 +924,34 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
 int64_t up(int64_t v, int64_t k) { return (v + k - 1) / k * k; }
 int64_t a256(int64_t v) { return up(v, 256); }
 
-// The smallest tile whose workgroups do not outnumber the CUs (one a CU): a tile of 128 takes 1.2 times as
-// long as one of 64 for four times the work, one of 192 twice as long for nine times.
+// Tiles of the m x m products: the smallest whose workgroups do not outnumber the CUs (one a CU). A tile of
+// 128 takes 1.2 times as long as one of 64 for four times the work, one of 192 twice as long for nine
+// times; of 32, where a launch is mostly latency, (m = 256) a third less than one of 64.
 int ns_bt(int m, int64_t batch) {
     auto tiles = [&](int bt) { const int64_t t = (m + bt - 1) / bt; return batch * t * (t + 1) / 2; };
-    return m <= 64 || tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
+    return tiles(32) <= 256 ? 32 : tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
 }
 
 void ns_shape(NsGroup& G, int rows, int cols, int batch) {
     G.rows = rows; G.cols = cols; G.batch = batch;
     G.tall = rows > cols;
     G.m = std::min(rows, cols); G.n = std::max(rows, cols);
-    G.bt = ns_bt(G.m, batch);
-    G.rp = int(up(rows, G.bt)); G.cp = int(up(cols, G.bt));
+    G.small = G.m <= 64;
+    G.bt = G.small ? 64 : ns_bt(G.m, batch);
+    G.bg = std::max(G.bt, 64);
+    // tiles of Q X: the same rule on their own number
+    const int64_t wide = int64_t(batch) * ((rows + 63) / 64) * ((cols + 63) / 64);
+    G.ba = G.bt == 192 ? 192 : G.small || (wide <= 256 && G.bt <= 64) ? 64 : 128;
+    const int pad = std::max(G.bg, G.ba);
+    G.rp = int(up(rows, pad)); G.cp = int(up(cols, pad));
     G.mp = std::min(G.rp, G.cp); G.np = std::max(G.rp, G.cp);
-    const int t = G.mp / G.bt;
-    G.tiles = t * (t + 1) / 2;
+    auto triangle = [](int t) { return t * (t + 1) / 2; };
+    G.tiles = triangle(G.mp / G.bt);
+    G.gtiles = triangle(G.mp / G.bg);
     // the Gram product's k in splits of at least two 64-blocks, towards what the CUs hold
     const int nb = G.np / 64;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::max(1, nb / 2),
-                                                                256 / (int64_t(batch) * G.tiles)));
+                                                                256 / (int64_t(batch) * G.gtiles)));
     const int each = int((nb + want - 1) / want);
     G.kchunk = each * 64;
     G.splits = (nb + each - 1) / each;
@@ -936,7 +961,7 @@ void ns_shape(NsGroup& G, int rows, int cols, int batch) {
     G.xs = int64_t(G.rp) * G.ldx * 2;
     G.ts = int64_t(G.cp) * G.ldt * 2;
     G.ms = int64_t(G.mp) * G.ldm * 2;
-    G.ps = int64_t(G.splits) * G.tiles * G.bt * G.bt * 4;
+    G.ps = int64_t(G.splits) * G.gtiles * G.bg * G.bg * 4;
     G.scale = 1.f;
 }
 
@@ -946,7 +971,7 @@ int ns_most(int prec) { return prec == BF16 ? kSegBf16 : kSegF32; }
 // Lays the group's buffers out from `at`; np0: planes of X as it comes; two: a second X buffer.
 int64_t ns_layout(NsGroup& G, int64_t at, int np0, bool two) {
     auto take = [&](int64_t bytes) { const int64_t o = at; at += a256(bytes); return o; };
-    const bool big = G.mp > 64;
+    const bool big = !G.small;
     for (int k = 0; k < 2; ++k) {
         int64_t* x = k ? G.xt : G.x;
         const int64_t plane = G.batch * (k ? G.ts : G.xs);
@@ -1017,6 +1042,8 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
         g.sp = float(pow2_scale(pmax, 14));
         g.st = float(pow2_scale(tmax, 14));
         g.sq = float(pow2_scale(qmax, 14));
+        g.ss = float(pow2_scale(pmax * pmax, 14));
+        g.sv = g.len < 2 ? 1.f : float(pow2_scale(pmax * (std::fabs(g.c[1][1]) + std::fabs(g.c[1][2]) * amax), 14));
         P.xscale[k] = pow2_scale(s, 12);
         g.alpha = k == 0 ? 0.f : float(1.0 / (P.xscale[k - 1] * P.xscale[k - 1]));
     }
@@ -1045,8 +1072,8 @@ NsArgs ns_select(const NsArgs& a, Take&& take, Blocks&& blocks, int& total) {
 template <int BT, int BK, int ST>
 void ns_gram(const NsArgs& a, const NsSeg& g, int src, int np, hipStream_t s) {
     int n;
-    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
-                               [](const NsGroup& G) { return G.batch * G.tiles * G.splits; }, n);
+    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bg == BT; },
+                               [](const NsGroup& G) { return G.batch * G.gtiles * G.splits; }, n);
     if (!n) return;
     if (np == 1) NS_TILES((ns_gram_kernel<BT, 64, ST, 1>), n, (ns_lds_bytes<BT, 64, ST, 1, 1>()), r, g, src);
     else NS_TILES((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, g, src);
@@ -1055,7 +1082,7 @@ void ns_gram(const NsArgs& a, const NsSeg& g, int src, int np, hipStream_t s) {
 template <int BT, int BK, int ST>
 void ns_prod(const NsArgs& a, const NsJobs& jobs, hipStream_t s) {
     int n;
-    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT && G.mp > 64; },
+    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT && !G.small; },
                                [&](const NsGroup& G) { return G.batch * G.tiles * jobs.n; }, n);
     if (n) NS_TILES((ns_prod_kernel<BT, BK, ST>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, jobs);
 }
@@ -1063,11 +1090,52 @@ void ns_prod(const NsArgs& a, const NsJobs& jobs, hipStream_t s) {
 template <int BT, int BK, int ST>
 void ns_apply(const NsArgs& a, const NsApply& ap, int np, hipStream_t s) {
     int n;
-    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT; },
+    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.ba == BT; },
                                [](const NsGroup& G) { return G.batch * (G.rp / BT) * (G.cp / BT); }, n);
     if (!n) return;
     if (np == 1) NS_TILES((ns_apply_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 2, 1>()), r, ap);
     else NS_TILES((ns_apply_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, ap);
+}
+
+// The m x m products of a segment; returns which Q buffer holds Q.
+int ns_chain(const NsArgs& a, const NsSeg& g, hipStream_t s) {
+    auto run = [&](const NsJobs& j) {
+        ns_prod<32, 64, 4>(a, j, s);
+        ns_prod<64, 64, 4>(a, j, s);
+        ns_prod<128, 32, 4>(a, j, s);
+        ns_prod<192, 32, 3>(a, j, s);
+    };
+    // the first P is Q
+    run({1, {{NS_A, NS_A, NS_Q0, NS_A, g.sq * g.c[0][2] / (g.sa * g.sa), g.sq * g.c[0][1] / g.sa, g.sq * g.c[0][0]}}});
+    bool wide = true;   // the chip holds two products at once
+    for (int i = 0; i < a.ng; ++i) wide = wide && (a.g[i].small || 2 * int64_t(a.g[i].batch) * a.g[i].tiles <= 256);
+    if (g.len == 2 && wide) {
+        // Two steps in four launches of six products, where the other way takes five of five: with S = P P
+        // and R = P A, the second step's A is A' = R P, and Q = P' P = a P + A' (b P + c A' P), A' P = R S.
+        const float b = g.c[1][1], c = g.c[1][2];
+        run({2, {{NS_Q0, NS_Q0, NS_T, NS_A, g.ss / (g.sq * g.sq), 0.f, 0.f},
+                 {NS_Q0, NS_A, NS_Q1, NS_A, g.st / (g.sq * g.sa), 0.f, 0.f}}});
+        run({2, {{NS_Q1, NS_Q0, NS_A, NS_A, g.sa / (g.st * g.sq), 0.f, 0.f},
+                 {NS_Q1, NS_T, NS_P, NS_Q0, c * g.sv / (g.st * g.ss), b * g.sv / g.sq, 0.f}}});
+        run({1, {{NS_A, NS_P, NS_Q1, NS_Q0, g.sq / (g.sa * g.sv), g.c[1][0], 0.f}}});
+        return 1;
+    }
+    int q = 0;
+    for (int t = 0; t < g.len; ++t) {
+        const float sd = t == 0 ? g.sq : g.sp;
+        const int p = t == 0 ? NS_Q0 : NS_P;
+        if (t > 0)
+            run({1, {{NS_A, NS_A, p, NS_A, sd * g.c[t][2] / (g.sa * g.sa), sd * g.c[t][1] / g.sa, sd * g.c[t][0]}}});
+        NsJobs j{};
+        if (t > 0) {
+            j.j[j.n++] = {NS_P, q ? NS_Q1 : NS_Q0, q ? NS_Q0 : NS_Q1, NS_A, 1.f / g.sp, 0.f, 0.f};
+            q ^= 1;
+        }
+        if (t + 1 < g.len) j.j[j.n++] = {p, NS_A, NS_T, NS_A, g.st / (sd * g.sa), 0.f, 0.f};
+        if (j.n) run(j);
+        if (t + 1 < g.len) run({1, {{NS_T, p, NS_A, NS_A, g.sa / (g.st * sd), 0.f, 0.f}}});
+    }
+    return q;
 }
 
 // All segments of one pass, X's planes (np of them) in place; `last` describes the final output.
@@ -1079,31 +1147,13 @@ hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hip
         ns_gram<128, 32, 4>(a, g, src, np, s);
         ns_gram<192, 32, 3>(a, g, src, np, s);
         int n;
-        const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.mp == 64 || G.splits > 1; }, [](const NsGroup& G) {
-            return G.mp == 64 ? G.batch : G.batch * G.tiles * (G.bt / 16);
+        const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.small || G.splits > 1; }, [](const NsGroup& G) {
+            return G.small ? G.batch : G.batch * G.gtiles * (G.bg / 16);
         }, n);
         bool small = false;
-        for (int i = 0; i < a.ng; ++i) small = small || a.g[i].mp == 64;
+        for (int i = 0; i < a.ng; ++i) small = small || a.g[i].small;
         if (n) NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 256 * 17 * int(sizeof(float)), r, g);
-        int q = 0;   // the buffer that holds Q
-        auto prod = [&](NsJobs j) {
-            ns_prod<64, 64, 4>(a, j, s);
-            ns_prod<128, 32, 4>(a, j, s);
-            ns_prod<192, 32, 3>(a, j, s);
-        };
-        for (int t = 0; t < g.len; ++t) {
-            const float sd = t == 0 ? g.sq : g.sp;        // the first P is Q
-            const int p = t == 0 ? NS_Q0 : NS_P;
-            prod({1, {{NS_A, NS_A, p, 1, sd * g.c[t][2] / (g.sa * g.sa), sd * g.c[t][1] / g.sa, sd * g.c[t][0]}}});
-            NsJobs j{};
-            if (t > 0) {
-                j.j[j.n++] = {NS_P, q ? NS_Q1 : NS_Q0, q ? NS_Q0 : NS_Q1, 0, 1.f / g.sp, 0.f, 0.f};
-                q ^= 1;
-            }
-            if (t + 1 < g.len) j.j[j.n++] = {p, NS_A, NS_T, 0, g.st / (sd * g.sa), 0.f, 0.f};
-            if (j.n) prod(j);
-            if (t + 1 < g.len) prod({1, {{NS_T, p, NS_A, 0, g.sa / (g.st * sd), 0.f, 0.f}}});
-        }
+        const int q = ns_chain(a, g, s);
         const bool end = k + 1 == P.nseg;
         NsApply ap = last;
         if (!end) ap.out = NS_OUT_MID;
