@@ -217,10 +217,12 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * coeffs: HOST float [steps][3], row k = (a_k, b_k, c_k), or NULL for (3.4445, -4.7750, 2.0315) in
  * every step. 1 <= steps <= 16. Coefficients that let a singular value of [0, 1] grow past 2^10, or
  * the product of the steps' polynomials past 10^15, are IMPALA_EUNSUPPORTED.
- * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included;
- * batch * rows * cols <= 2^34.
+ * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included; batch
+ * <= 2^21, and, but for small matrices that fit one CU, batch times both sides rounded up to 192
+ * <= 2^34 (more: IMPALA_EUNSUPPORTED).
  * Precision: the products run on f16 matrix cores, each operand as the sum of two f16 numbers, with
- * float32 accumulation; ||x|| is a 64-bit sum. IMPALA_PREC_FP32 results differ from the exact ones
+ * float32 accumulation (small matrices: on float32 matrix cores); ||x|| is a 64-bit
+ * sum. IMPALA_PREC_FP32 results differ from the exact ones
  * by about what a float32 evaluation does; IMPALA_PREC_BF16 results by about their own rounding. A
  * zero matrix gives zeros; one with an element that is not finite gives NaN in all of its own.
  * ws: device scratch of muon_orthogonalize_workspace_bytes() bytes. */
@@ -259,7 +261,7 @@ typedef struct muon_cfg {
  * and one Adam step (step 1-based, adam_lr, no weight decay) on every parameter that no matrix
  * covers. params, m, v are updated in place; v is left alone inside the matrices; grads is read
  * only. mats: HOST array of n_mats matrices in any order, disjoint, inside the buffer; at most 512,
- * sides as muon_orthogonalize. cfg is HOST memory and, like mats, not kept after the call returns.
+ * sides as muon_orthogonalize, their sides rounded up to 192 multiplying to 2^34 in all at most. cfg is HOST memory and, like mats, not kept after the call returns.
  * stats as adam_step. ws: device scratch of muon_workspace_bytes() bytes. */
 size_t muon_workspace_bytes(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
                             const muon_cfg_t* cfg);

@@ -71,6 +71,11 @@ size_t a256(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int64_t kMuonMaxSize = int64_t(1) << 28;   // elements of one matrix
 constexpr int kMuonMaxSide = 16384, kMuonMaxMats = 512, kMuonMaxSteps = 16;
 
+// What a shape takes in whole tiles, at most. The launches have at most 512 threads for 64 x 64 of it, so this
+// many elements in a call keep them under 2^32 threads.
+constexpr int64_t kMuonMaxPadded = int64_t(1) << 34;
+int64_t muon_padded(int64_t rows, int64_t cols) { return (rows + 191) / 192 * 192 * ((cols + 191) / 192 * 192); }
+
 bool muon_shape_ok(int64_t rows, int64_t cols) {
     return rows >= 1 && cols >= 1 && rows * cols <= kMuonMaxSize && std::min(rows, cols) <= kMuonMaxSide;
 }
@@ -101,11 +106,13 @@ std::string muon_mats(int64_t n_params, const muon_matrix_t* mats, int n_mats, s
     if (n_mats < 0 || n_mats > kMuonMaxMats) return "between 0 and 512 matrices";
     if (n_mats > 0 && !mats) return "mats is NULL";
     out.clear();
+    int64_t padded = 0;
     for (int i = 0; i < n_mats; ++i) {
         const muon_matrix_t& m = mats[i];
         if (!muon_shape_ok(m.rows, m.cols)) return "matrix " + std::to_string(i) + " has unsupported sides";
         if (m.offset < 0 || m.offset > n_params || int64_t(m.rows) * m.cols > n_params - m.offset)
             return "matrix " + std::to_string(i) + " lies outside the buffer";
+        if ((padded += muon_padded(m.rows, m.cols)) > kMuonMaxPadded) return "the matrices are too large for one call";
         out.push_back({m.offset, m.rows, m.cols});
     }
     std::sort(out.begin(), out.end(), [](const MuonMat& a, const MuonMat& b) { return a.offset < b.offset; });
@@ -564,8 +571,10 @@ static std::string check_orth(int prec, int64_t batch, int rows, int cols, int s
     if (steps < 1 || steps > kMuonMaxSteps) return "steps must be in [1, 16]";
     return "";
 }
+// One workgroup of 1024 threads a matrix: fewer than 2^32 threads.
 static bool orth_supported(int64_t batch, int rows, int cols) {
-    return muon_shape_ok(rows, cols) && batch <= (int64_t(1) << 24) && batch * rows * cols <= (int64_t(1) << 34);
+    return muon_shape_ok(rows, cols) && batch <= (int64_t(1) << 21) &&
+           (muon_orth_small(batch, rows, cols) || batch * muon_padded(rows, cols) <= kMuonMaxPadded);
 }
 
 size_t muon_orthogonalize_workspace_bytes(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
@@ -1005,7 +1014,7 @@ static impala_status_t check_groupnorm(const char* fn, int prec, int64_t n, int 
     if (C < 1 || G < 1 || C % G) return fail(IMPALA_EINVAL, "%s: groups must divide C (got C=%d groups=%d)", fn, C, G);
     if (C > kGnMaxC) return fail(IMPALA_EUNSUPPORTED, "%s: at most %d channels (got %d)", fn, kGnMaxC, C);
     if (act < IMPALA_ACT_NONE || act > IMPALA_ACT_SILU) return fail(IMPALA_EINVAL, "%s: bad act %d", fn, act);
-    if (groupnorm_blocks(prec, n, H, W, C, G) > (int64_t(1) << 31) - 1)
+    if (groupnorm_threads(prec, n, H, W, C, G) >= (int64_t(1) << 32))   // of one launch
         return fail(IMPALA_EUNSUPPORTED, "%s: too many elements for one call", fn);
     return IMPALA_OK;
 }

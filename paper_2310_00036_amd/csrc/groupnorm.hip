@@ -642,6 +642,15 @@ void gn_fwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
 #undef GN_C
 }
 
+// Each frame's column sums over its chunks; a launch holds fewer than 2^32 threads.
+void gn_frame_sums(const GnArgs& a, hipStream_t s) {
+    const int64_t cols = 2 * int64_t(a.C), blocks = (cols + 3) / 4, most = (int64_t(1) << 21) / blocks;
+    for (int64_t f = 0; f < a.n; f += most)
+        hipLaunchKernelGGL(gn_columns_kernel, dim3(unsigned(std::min(most, a.n - f) * blocks)), dim3(1024), 0, s,
+                           a.part + f * a.chunks * cols, int64_t(a.chunks), int(cols), int(cols), a.fsum + f * cols,
+                           static_cast<float*>(nullptr));
+}
+
 template <class P, int V, int ACT>
 void gn_bwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
     const dim3 grid(unsigned(a.n * a.chunks));
@@ -653,8 +662,7 @@ void gn_bwd_launch(const GnPlan& p, const GnArgs& a, hipStream_t s) {
 #define GN_C(K, NT, NV)                                                                                  \
     if (p.shape == K) {                                                                                  \
         hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 1, ACT>), grid, dim3(NT), 0, s, a);              \
-        hipLaunchKernelGGL(gn_columns_kernel, dim3(unsigned(a.n * ((2 * a.C + 3) / 4))), dim3(1024), 0, s, a.part, \
-                           int64_t(a.chunks), 2 * a.C, 2 * a.C, a.fsum, static_cast<float*>(nullptr));  \
+        gn_frame_sums(a, s);                                                                             \
         hipLaunchKernelGGL((gn_bwd_kernel<P, V, NV, NT, 2, ACT>), grid, dim3(NT), 0, s, a);              \
     }
     GN_C(1, 256, 8)
@@ -684,9 +692,9 @@ std::string gn_key(const char* name, int prec, int H, int W, int C) {
 
 }  // namespace
 
-int64_t groupnorm_blocks(int prec, int64_t n, int H, int W, int C, int G) {
-    // one-channel columns: the most chunks; the column sums take 4 columns of a frame each
-    return std::max(n * gn_plan(prec, n, H, W, C, G, 0, 0, nullptr).chunks, n * ((2 * C + 3) / 4));
+int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G) {
+    const GnPlan p = gn_plan(prec, n, H, W, C, G, 0, 0, nullptr);   // one-channel columns: the most chunks
+    return n * std::max(256, p.chunks * kGnShapes[p.shape].nt);
 }
 
 size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd) {

@@ -187,7 +187,7 @@ struct GnArgs {
     float* part; float* fsum; float* smean; float* srstd;
 };
 size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd);
-int64_t groupnorm_blocks(int prec, int64_t n, int H, int W, int C, int G);   // workgroups at most
+int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G);   // workgroups at most
 hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t s);
 // n == 0: dgamma and dbeta are cleared. Either may be NULL.
 hipError_t groupnorm_bwd(int prec, int H, int W, GnArgs a, float* dgamma, float* dbeta, void* ws, hipStream_t s);
@@ -308,6 +308,7 @@ hipError_t clip_opt_step(int opt, const OptArgs& a, float* stats, float* partial
 // ---- orthogonalised updates (Newton-Schulz products) and the Muon step
 // steps in [1, 16]; coeffs: host [steps][3] or NULL (the default quintic in every step)
 bool muon_coeffs_ok(int steps, const float* coeffs);   // singular values stay bounded
+bool muon_orth_small(int64_t batch, int rows, int cols);   // one launch, no workspace
 size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps);
 hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,
                      float eps, void* y, void* ws, hipStream_t s);

@@ -40,6 +40,7 @@ namespace cb {
 namespace {
 
 constexpr int kSegF32 = 2, kSegBf16 = 3, kMaxSegs = kNsMaxSteps / 2;
+constexpr float kNsDefault[3] = {3.4445f, -4.7750f, 2.0315f};
 
 typedef _Float16 ns_f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 ns_f16x4 __attribute__((ext_vector_type(4)));
@@ -356,20 +357,22 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a,
 
 // A whole segment's m x m part of one matrix with m <= 64 in LDS, float32: five m x m buffers of pitch
 // 68, which a fragment read of 16 bytes from each of 16 rows crosses without bank conflicts.
-constexpr int kSmPitch = 68, kSmBuf = 64 * kSmPitch;
+constexpr int kSmPitch = 68, kSmBuf = 64 * kSmPitch, kSmThreads = 1024;
 constexpr int kSmLds = 5 * kSmBuf * int(sizeof(float));
 
 // f(N, M, v, mirror): four rows M .. M+3 of column N of L R^T for symmetric L, R that commute: the lower
 // triangle's tiles of 16 in turn over the waves, the others their mirror images. A lane group takes four
 // neighbouring k of each 16 (any order of k is the same sum), so four products share a 16-byte read.
+// back: from the last wave on, for the second of two products between the same barriers.
 template <class Fn>
-CB_DEV void ns_small_mul(const float* L, const float* R, int mt, Fn&& f) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r16 = lane & 15;
-    for (int t = wave; t < mt * (mt + 1) / 2; t += 4) {
+CB_DEV void ns_small_mul(const float* L, const float* R, int mt, int pitch, bool back, Fn&& f) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
+    const int wave = back ? kSmThreads / 64 - 1 - (threadIdx.x >> 6) : threadIdx.x >> 6;
+    for (int t = wave; t < mt * (mt + 1) / 2; t += kSmThreads / 64) {
         int i, j;
         ns_tile(t, i, j);
-        const float* l = L + (i * 16 + r16) * kSmPitch + 4 * g;
-        const float* r = R + (j * 16 + r16) * kSmPitch + 4 * g;
+        const float* l = L + (i * 16 + r16) * pitch + 4 * g;
+        const float* r = R + (j * 16 + r16) * pitch + 4 * g;
         float4 x[4], y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -392,12 +395,22 @@ CB_DEV void ns_small_mul(const float* L, const float* R, int mt, Fn&& f) {
         f(j * 16 + r16, i * 16 + 4 * g, acc, i != j);
     }
 }
-CB_DEV void ns_small_put(float* D, int N, int M, float4 v, bool mirror) {
-    *reinterpret_cast<float4*>(D + N * kSmPitch + M) = v;
+CB_DEV void ns_small_put(float* D, int pitch, int N, int M, float4 v, bool mirror) {
+    *reinterpret_cast<float4*>(D + N * pitch + M) = v;
     if (mirror) {
-        D[M * kSmPitch + N] = v.x; D[(M + 1) * kSmPitch + N] = v.y;
-        D[(M + 2) * kSmPitch + N] = v.z; D[(M + 3) * kSmPitch + N] = v.w;
+        D[M * pitch + N] = v.x; D[(M + 1) * pitch + N] = v.y;
+        D[(M + 2) * pitch + N] = v.z; D[(M + 3) * pitch + N] = v.w;
     }
+}
+// D = a I + b A + c A^2.
+CB_DEV void ns_small_poly(const float* A, float* D, int mt, int pitch, float a, float b, float c) {
+    ns_small_mul(A, A, mt, pitch, false, [&](int N, int M, cb_f32x4 v, bool mirror) CB_INLINE_LAMBDA {
+        const float4 q = *reinterpret_cast<const float4*>(A + N * pitch + M);
+        ns_small_put(D, pitch, N, M,
+                     make_float4(b * q.x + c * v[0] + (N == M ? a : 0.f), b * q.y + c * v[1] + (N == M + 1 ? a : 0.f),
+                                 b * q.z + c * v[2] + (N == M + 2 ? a : 0.f), b * q.w + c * v[3] + (N == M + 3 ? a : 0.f)),
+                     mirror);
+    });
 }
 
 // The sum of n float4, `step` floats apart, in order; eight loads in flight.
@@ -419,7 +432,7 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
     const int mt = (G.m + 15) / 16;
     const float alpha = ns_alpha(a, s, G.first + b);
     const float* part = reinterpret_cast<const float*>(a.ws + G.part + int64_t(b) * G.ps);
-    for (int e = threadIdx.x * 4; e < 64 * 64; e += 1024) {
+    for (int e = threadIdx.x * 4; e < 64 * 64; e += 4 * kSmThreads) {
         const float4 v = ns_sum(part + e, G.splits, 4096);
         *reinterpret_cast<float4*>(A + (e >> 6) * kSmPitch + (e & 63)) =
             make_float4(v.x * alpha, v.y * alpha, v.z * alpha, v.w * alpha);
@@ -427,34 +440,27 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
     __syncthreads();
     auto put = [&](float* D) {
         return [=](int N, int M, cb_f32x4 v, bool mirror) CB_INLINE_LAMBDA {
-            ns_small_put(D, N, M, make_float4(v[0], v[1], v[2], v[3]), mirror);
+            ns_small_put(D, kSmPitch, N, M, make_float4(v[0], v[1], v[2], v[3]), mirror);
         };
     };
     for (int t = 0; t < s.len; ++t) {
         float* D = t == 0 ? Q : P;
-        const float ca = s.c[t][0], cb = s.c[t][1], cc = s.c[t][2];
-        ns_small_mul(A, A, mt, [&](int N, int M, cb_f32x4 v, bool mirror) CB_INLINE_LAMBDA {
-            const float4 q = *reinterpret_cast<const float4*>(A + N * kSmPitch + M);
-            ns_small_put(D, N, M,
-                         make_float4(cb * q.x + cc * v[0] + (N == M ? ca : 0.f), cb * q.y + cc * v[1] + (N == M + 1 ? ca : 0.f),
-                                     cb * q.z + cc * v[2] + (N == M + 2 ? ca : 0.f), cb * q.w + cc * v[3] + (N == M + 3 ? ca : 0.f)),
-                         mirror);
-        });
+        ns_small_poly(A, D, mt, kSmPitch, s.c[t][0], s.c[t][1], s.c[t][2]);
         __syncthreads();
         if (t > 0) {
-            ns_small_mul(P, Q, mt, put(Q2));
+            ns_small_mul(P, Q, mt, kSmPitch, false, put(Q2));
             float* w = Q; Q = Q2; Q2 = w;
         }
         if (t + 1 < s.len) {
             const float* F = t == 0 ? Q : P;   // the first P is Q
-            ns_small_mul(F, A, mt, put(T));
+            ns_small_mul(F, A, mt, kSmPitch, t > 0, put(T));
             __syncthreads();
-            ns_small_mul(T, F, mt, put(A));
+            ns_small_mul(T, F, mt, kSmPitch, false, put(A));
         }
         __syncthreads();
     }
     char* q = a.ws + G.q[0] + int64_t(b) * 2 * G.ms;
-    for (int e = threadIdx.x * 4; e < 64 * 64; e += 1024) {
+    for (int e = threadIdx.x * 4; e < 64 * 64; e += 4 * kSmThreads) {
         const int N = e >> 6, M = e & 63;
         float v[4];
 #pragma unroll
@@ -467,14 +473,16 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
 
 // Sums the Gram partials in split order. m <= 64: and goes on to Q. Else A's planes, 16 columns of a
 // tile a workgroup, with the mirror image of an off-diagonal tile.
-__global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
+template <int NT>
+__global__ __launch_bounds__(NT) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
-    if (G.small) {
-        ns_small(a, G, s, blk, reinterpret_cast<float*>(smem));
-        return;
-    }
+    if constexpr (NT == kSmThreads)
+        if (G.small) {
+            ns_small(a, G, s, blk, reinterpret_cast<float*>(smem));
+            return;
+        }
     float* sh = reinterpret_cast<float*>(smem);   // [BT][17]
     const int bt = G.bg, strips = bt / 16;
     const int n0 = (blk % strips) * 16, t = blk / strips % G.gtiles, b = blk / (strips * G.gtiles);
@@ -483,7 +491,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     const float alpha = ns_alpha(a, s, G.first + b) * s.sa;
     const float* part = reinterpret_cast<const float*>(a.ws + G.part + int64_t(b) * G.ps) + int64_t(t) * bt * bt;
     char* A = a.ws + G.a + int64_t(b) * 2 * G.ms;
-    for (int e = threadIdx.x * 4; e < 16 * bt; e += 1024) {
+    for (int e = threadIdx.x * 4; e < 16 * bt; e += 4 * NT) {
         const int N = n0 + e / bt, M = e % bt;
         const float4 q = ns_sum(part + N * bt + M, G.splits, int64_t(G.gtiles) * bt * bt);
         float v[4] = {q.x, q.y, q.z, q.w};
@@ -498,7 +506,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     }
     if (ti == tj) return;
     __syncthreads();
-    for (int e = threadIdx.x * 4; e < 16 * bt; e += 1024) {
+    for (int e = threadIdx.x * 4; e < 16 * bt; e += 4 * NT) {
         const int M = e / 16, q = e % 16;
         const float v[4] = {sh[M * 17 + q], sh[M * 17 + q + 1], sh[M * 17 + q + 2], sh[M * 17 + q + 3]};
         uint2 hi, lo;
@@ -919,17 +927,156 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
     }
 }
 
+// ------------------------------------------------------------------ small matrices: all of it in one launch
+//
+// A matrix of at most 64 on its smaller side that fits one CU's LDS in float32 takes one workgroup and no
+// workspace: its steps one by one, as they are written, from LDS in float32 MFMAs. What bounds it is the
+// latency of each of its products and, at m = 64, the float32 matrix rate of one CU; the launches of the
+// other way are 5 us each.
+
+struct NsOne { int rows, cols, steps; float eps; float c[kNsMaxSteps][3]; };
+
+constexpr int kOnePart = 16 * 256;   // the Gram product's shares, and the doubles of the norm's sum
+__host__ __device__ inline int ns_one_pitch(int v) { return (v + 15) / 16 * 16 + 4; }   // 4 x odd: rows meet all banks
+__host__ __device__ inline int64_t ns_one_lds(int rows, int cols) {
+    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, mp = (m + 15) / 16 * 16;
+    return (int64_t(mp) * ns_one_pitch(n) + 2 * int64_t(mp) * ns_one_pitch(m) + kOnePart) * 4;
+}
+
+// f(row, col, element) over a rows x cols matrix: a group of lanes along a row, so that memory is read
+// and written in order.
+template <class Fn>
+CB_DEV void ns_one_each(int rows, int cols, Fn&& f) {
+    const int sh = cols <= 8 ? 3 : cols <= 16 ? 4 : cols <= 32 ? 5 : 6;
+#pragma unroll 4
+    for (int r = threadIdx.x >> sh; r < rows; r += kSmThreads >> sh)
+#pragma unroll 2
+        for (int c = threadIdx.x & ((1 << sh) - 1); c < cols; c += 1 << sh) f(r, c, r * cols + c);
+}
+
+template <bool BF>
+__global__ __launch_bounds__(kSmThreads) void ns_one_kernel(const void* src, void* dst, NsOne o) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int rows = o.rows, cols = o.cols;
+    const bool tall = rows > cols;
+    const int m = tall ? cols : rows, n = tall ? rows : cols;
+    const int mt = (m + 15) / 16, nt = (n + 15) / 16, pm = mt * 16 + 4, pn = nt * 16 + 4;
+    float* part = reinterpret_cast<float*>(smem);
+    float* A = part + kOnePart;
+    float* P = A + mt * 16 * pm;
+    float* X = P + mt * 16 * pm;   // [m][n]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r16 = lane & 15;
+    constexpr int NW = kSmThreads / 64;
+    const int64_t base = int64_t(blockIdx.x) * rows * cols;
+
+    for (int i = threadIdx.x; i < mt * 16 * pn; i += kSmThreads) X[i] = 0.f;
+    __syncthreads();
+    double gg = 0.0;
+    ns_one_each(rows, cols, [&](int r, int c, int e) CB_INLINE_LAMBDA {
+        const float v = BF ? bf2f(static_cast<const uint16_t*>(src)[base + e]) : static_cast<const float*>(src)[base + e];
+        X[tall ? c * pn + r : r * pn + c] = v;
+        gg += double(v) * v;
+    });
+    const double norm = sqrt(block_sum<kSmThreads>(gg, reinterpret_cast<double*>(smem)));
+    // X = rho x / norm with the factor rho beside it: an eps far above the norm does not underflow X
+    const double inv = norm == 0.0 ? 1.0 : 1.0 / norm;
+    float rho = norm == 0.0 ? 0.f : float(norm / (norm > double(o.eps) || norm != norm ? norm : double(o.eps)));
+    for (int i = threadIdx.x; i < mt * 16 * pn; i += kSmThreads) X[i] = float(X[i] * inv);
+    __syncthreads();
+
+    const int tiles = mt * (mt + 1) / 2, split = NW / tiles;
+    for (int t = 0; t < o.steps; ++t) {
+        // A = X X^T: the lower triangle's tiles over the waves, k in `split` shares; the sum in their order
+        if (wave < tiles * split) {
+            const int z = wave / tiles;
+            int i, j;
+            ns_tile(wave - z * tiles, i, j);
+            const float* l = X + (i * 16 + r16) * pn + 4 * g;
+            const float* r = X + (j * 16 + r16) * pn + 4 * g;
+            cb_f32x4 acc{0.f, 0.f, 0.f, 0.f}, acc2{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int k = z; k < nt; k += split) {
+                const float4 x = *reinterpret_cast<const float4*>(l + 16 * k), y = *reinterpret_cast<const float4*>(r + 16 * k);
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.x, y.x, acc, 0, 0, 0);
+                acc2 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.y, y.y, acc2, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, y.z, acc, 0, 0, 0);
+                acc2 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, y.w, acc2, 0, 0, 0);
+            }
+            *reinterpret_cast<float4*>(part + wave * 256 + r16 * 16 + 4 * g) =
+                make_float4(acc[0] + acc2[0], acc[1] + acc2[1], acc[2] + acc2[2], acc[3] + acc2[3]);
+        }
+        __syncthreads();
+        for (int e = threadIdx.x * 4; e < tiles * 256; e += 4 * kSmThreads) {
+            const int q = e >> 8, N = (e >> 4) & 15, M = e & 15;
+            int i, j;
+            ns_tile(q, i, j);
+            float4 v = *reinterpret_cast<const float4*>(part + e);
+            for (int z = 1; z < split; ++z) {
+                const float4 w = *reinterpret_cast<const float4*>(part + z * tiles * 256 + e);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+            const float f = t == 0 ? rho * rho : 1.f;
+            v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+            ns_small_put(A, pm, j * 16 + N, i * 16 + M, v, i != j);
+        }
+        __syncthreads();
+        ns_small_poly(A, P, mt, pm, o.c[t][0], o.c[t][1], o.c[t][2]);
+        __syncthreads();
+        // X <- P X in place: a wave owns 16 columns, and has read them before it writes
+        const float f = t == 0 ? rho : 1.f;
+        for (int cb = wave; cb < nt; cb += NW) {
+            float x[16];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[k * 4 + r] = X[(16 * k + 4 * g + r) * pn + cb * 16 + r16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < mt) {
+                    cb_f32x4 acc{0.f, 0.f, 0.f, 0.f}, acc2{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < mt) {
+                            const float4 p = *reinterpret_cast<const float4*>(P + (i * 16 + r16) * pm + 16 * k + 4 * g);
+                            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p.x, x[k * 4], acc, 0, 0, 0);
+                            acc2 = __builtin_amdgcn_mfma_f32_16x16x4f32(p.y, x[k * 4 + 1], acc2, 0, 0, 0);
+                            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p.z, x[k * 4 + 2], acc, 0, 0, 0);
+                            acc2 = __builtin_amdgcn_mfma_f32_16x16x4f32(p.w, x[k * 4 + 3], acc2, 0, 0, 0);
+                        }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) X[(i * 16 + 4 * g + r) * pn + cb * 16 + r16] = f * (acc[r] + acc2[r]);
+                }
+        }
+        __syncthreads();
+    }
+    ns_one_each(rows, cols, [&](int r, int c, int e) CB_INLINE_LAMBDA {
+        const float v = X[tall ? c * pn + r : r * pn + c];
+        if (BF) static_cast<uint16_t*>(dst)[base + e] = f2bf(v);
+        else static_cast<float*>(dst)[base + e] = v;
+    });
+}
+
 // ------------------------------------------------------------------ host: shapes, layout, launches
+
 
 int64_t up(int64_t v, int64_t k) { return (v + k - 1) / k * k; }
 int64_t a256(int64_t v) { return up(v, 256); }
+
+// Which way a batch goes: the one launch where it fits, unless few matrices have so much work that the other
+// way, which spreads one over several CUs, is the faster (8 x 320x64: 69 against 73 us, 8 x 432x64: 88 against
+// 73, 64 x 432x64: 90 against 95; 4 x 144x16: 15 against 61).
+bool ns_one(int64_t batch, int rows, int cols) {
+    const int64_t m = up(std::min(rows, cols), 16), n = up(std::max(rows, cols), 16);
+    return m <= 64 && ns_one_lds(rows, cols) <= 160 * 1024 && (batch >= 64 || m * m * n <= 64 * 64 * 320);
+}
 
 // Tiles of the m x m products: the smallest whose workgroups do not outnumber the CUs (one a CU). A tile of
 // 128 takes 1.2 times as long as one of 64 for four times the work, one of 192 twice as long for nine
 // times; of 32, where a launch is mostly latency, (m = 256) a third less than one of 64.
 int ns_bt(int m, int64_t batch) {
     auto tiles = [&](int bt) { const int64_t t = (m + bt - 1) / bt; return batch * t * (t + 1) / 2; };
-    return tiles(32) <= 256 ? 32 : tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
+    return tiles(32) <= 512 ? 32 : tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
 }
 
 void ns_shape(NsGroup& G, int rows, int cols, int batch) {
@@ -1003,7 +1150,6 @@ double pow2_scale(double bound, int most) {   // the largest power of two (at mo
 // they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False where they
 // could grow past 2^10 (planes would no longer resolve them).
 bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
-    static const float kDefault[3] = {3.4445f, -4.7750f, 2.0315f};
     P.nseg = (steps + most - 1) / most;
     double s = 1.0 + 0x1p-10;
     int at = 0;
@@ -1013,7 +1159,7 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
         g.len = (steps - at + P.nseg - k - 1) / (P.nseg - k);
         double amax = s * s, pmax = 0, tmax = 0, q = 1, qmax = 0;
         for (int t = 0; t < g.len; ++t, ++at) {
-            const float* c = coeffs ? coeffs + 3 * at : kDefault;
+            const float* c = coeffs ? coeffs + 3 * at : kNsDefault;
             const double a = c[0], b = c[1], cc = c[2], lam = s * s;
             for (int i = 0; i < 3; ++i) g.c[t][i] = c[i];
             auto poly = [&](double l) { return std::fabs(a + b * l + cc * l * l); };
@@ -1152,7 +1298,8 @@ hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hip
         }, n);
         bool small = false;
         for (int i = 0; i < a.ng; ++i) small = small || a.g[i].small;
-        if (n) NS_LAUNCH(ns_reduce_kernel, n, small ? kSmLds : 256 * 17 * int(sizeof(float)), r, g);
+        if (n && small) hipLaunchKernelGGL(ns_reduce_kernel<kSmThreads>, dim3(unsigned(n)), dim3(kSmThreads), kSmLds, s, r, g);
+        else if (n) NS_LAUNCH(ns_reduce_kernel<256>, n, 256 * 17 * int(sizeof(float)), r, g);
         const int q = ns_chain(a, g, s);
         const bool end = k + 1 == P.nseg;
         NsApply ap = last;
@@ -1186,20 +1333,32 @@ bool muon_coeffs_ok(int steps, const float* coeffs) {
     return ns_program(steps, coeffs, kSegBf16, P);   // (shorter segments have smaller products)
 }
 
+bool muon_orth_small(int64_t batch, int rows, int cols) { return ns_one(batch, rows, cols); }
+
 size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps) {
+    if (ns_one(batch, rows, cols)) return 256;   // nothing; but zero stands for a refusal
     NsArgs a;
     return size_t(orth_layout(prec, batch, rows, cols, steps, a));
 }
 
 hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,
                      float eps, void* y, void* ws, hipStream_t s) {
+    ProfScope ps(s, [&] { return cb_key("muon_orthogonalize", prec, cb_dims(rows, cols) + "x" + std::to_string(batch)); });
+    if (ns_one(batch, rows, cols)) {
+        NsOne o{rows, cols, steps, eps, {}};
+        for (int t = 0; t < steps; ++t)
+            for (int i = 0; i < 3; ++i) o.c[t][i] = coeffs ? coeffs[3 * t + i] : kNsDefault[i];
+        const unsigned lds = unsigned(ns_one_lds(rows, cols));
+        if (prec == BF16) hipLaunchKernelGGL(ns_one_kernel<true>, dim3(unsigned(batch)), dim3(kSmThreads), lds, s, x, y, o);
+        else hipLaunchKernelGGL(ns_one_kernel<false>, dim3(unsigned(batch)), dim3(kSmThreads), lds, s, x, y, o);
+        return hipGetLastError();
+    }
     NsArgs a;
     orth_layout(prec, batch, rows, cols, steps, a);
     a.ws = static_cast<char*>(ws);
     NsProgram P;
     ns_program(steps, coeffs, ns_most(prec), P);
     const NsGroup& G = a.g[0];
-    ProfScope ps(s, [&] { return cb_key("muon_orthogonalize", prec, cb_dims(rows, cols) + "x" + std::to_string(batch)); });
     MuonElem e{};
     const int64_t sums = batch * G.nsum, planes = batch * int64_t(ns_plane_blocks(G));
     if (prec == BF16) {

@@ -81,6 +81,10 @@ PREC = pytest.mark.parametrize("prec", [G.BF16, G.FP32], ids=["bf16", "fp32"])
 SHAPES = [(1, 1, 1), (3, 1, 40), (2, 40, 1), (2, 7, 5), (5, 36, 16), (4, 144, 16), (2, 16, 17), (1, 64, 64), (2, 65, 64),
           (2, 63, 130), (2, 576, 64), (1, 65, 65), (2, 128, 127), (2, 129, 200), (1, 300, 129), (1, 257, 256), (2, 100, 1000),
           (1, 1000, 100), (1, 512, 600), (200, 96, 130), (70, 200, 260), (70, 261, 200), (1, 3872, 256), (1, 33, 5000)]
+# what one workgroup does by itself, at the edges of its tiles of 16, of its lanes and of its memory
+SMALL = [(3, 2, 3), (2, 16, 16), (2, 15, 33), (3, 48, 49), (5, 288, 32), (2, 432, 27), (2, 320, 64), (2, 321, 64), (1, 64, 336),
+         (64, 432, 64), (64, 64, 448), (64, 449, 64), (1, 2000, 16), (1, 8, 2100), (1, 2300, 16), (1, 1, 2048), (1, 2048, 1),
+         (300, 9, 4)]
 
 
 @PREC
@@ -94,6 +98,29 @@ def test_orthogonalize(prec, shape):
         # a square Gaussian matrix or a gradient with many small directions is not well conditioned
         tol = TYPICAL[prec] if max(shape[1:]) >= 4 * min(shape[1:]) and make is _gauss else WORST[prec]
         _close(got[pick], ns(x[pick]), prec, tol, make.__name__)
+
+
+@PREC
+@pytest.mark.parametrize("shape", SMALL, ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_small(prec, shape):
+    # One rounding to bf16 is off by 2^-8 of the value at most, and so is a matrix of roundings in norm;
+    # half of that, which WORST has, is where the errors of many elements average.
+    tol = 2.0 ** -8 + 2.0 ** -14 if prec == G.BF16 and shape[1] * shape[2] < 64 else WORST[prec]
+    for k, make in enumerate((_gauss, _gradient)):
+        x = G.q(make(k, *shape), prec)
+        got = _orth(prec, x)
+        pick = np.unique(np.linspace(0, shape[0] - 1, 3).astype(int))
+        _close(got[pick], ns(x[pick]), prec, tol, make.__name__)
+
+
+@PREC
+def test_small_step_counts_and_coefficients(prec):
+    co = np.array([[3.0, -3.2, 1.2], [1.5, -0.5, 0.0], [2.0, -1.5, 0.5]], np.float32)
+    for shape in ((2, 70, 16), (2, 30, 200), (3, 50, 60)):
+        x = G.q(_gradient(15, *shape), prec)
+        for steps in (1, 2, 3, 8, 16):
+            _close(_orth(prec, x, steps), ns(x, steps), prec, WORST[prec])
+        _close(_orth(prec, x, 3, co), ns(x, 3, co), prec, WORST[prec])
 
 
 @PREC

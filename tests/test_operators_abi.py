@@ -26,6 +26,9 @@ def test_groupnorm_refusals():
     # ranges that overlap in part: 2 x 9 x 9 x 32 bf16 are 10368 bytes
     assert fwd(y=(1 << 20) + 10366) == EINVAL and fwd(y=(1 << 20) - 10366) == EINVAL
     assert b"overlap" in lib.impala_last_error()
+    # a launch of 2^32 threads
+    assert fwd(n=1 << 24, H=1, W=1, C_=8) == EUNSUPPORTED and fwd(n=1 << 13, H=4096, W=4096, C_=64) == EUNSUPPORTED
+    assert fwd(n=(1 << 24) - 1, H=1, W=1, C_=8, x=None) == EINVAL
     need = P.impala_groupnorm_fwd_workspace_bytes(P.PREC_BF16, 2, 200, 200, 64, 4)
     assert need > 0 and fwd(H=200, W=200, C_=64, wsb=need - 1) == EWORKSPACE
     assert fwd(H=200, W=200, C_=64, ws=None, wsb=0) == EINVAL
@@ -50,12 +53,14 @@ def test_orthogonalize_refusals():
                 dict(eps=float("nan")), dict(x=None), dict(y=None), dict(ws=None), dict(y=(1 << 20) + 4)):
         assert orth(**bad) == EINVAL, bad
     assert b"overlap" in lib.impala_last_error()
-    for bad in (dict(r=1 << 15, c=1 << 15), dict(r=20000, c=20000), dict(b=1 << 20, r=1000, c=1000)):
+    for bad in (dict(r=1 << 15, c=1 << 15), dict(r=20000, c=20000), dict(b=1 << 20, r=1000, c=1000),
+                dict(b=(1 << 21) + 1, r=1, c=1), dict(b=1 << 17, r=400, c=200)):
         assert orth(**bad) == EUNSUPPORTED, bad
     grow = (C.c_float * 15)(*([5.0, 5.0, 5.0] * 5))
     assert orth(co=grow) == EUNSUPPORTED and b"grow" in lib.impala_last_error()
     nan = (C.c_float * 15)(*([float("nan")] * 15))
     assert orth(co=nan) == EUNSUPPORTED
+    assert P.muon_orthogonalize_workspace_bytes(P.PREC_FP32, 1 << 21, 3, 5, 5) > 0
     need = P.muon_orthogonalize_workspace_bytes(P.PREC_FP32, 2, 40, 30, 5)
     assert need > 0 and orth(wsb=need - 1) == EWORKSPACE
     assert orth(b=0, x=None, y=None, ws=None, wsb=0) == 0
