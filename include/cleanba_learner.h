@@ -217,9 +217,9 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * coeffs: HOST float [steps][3], row k = (a_k, b_k, c_k), or NULL for (3.4445, -4.7750, 2.0315) in
  * every step. 1 <= steps <= 16. Coefficients that let a singular value of [0, 1] grow past 2^10, or
  * the product of the steps' polynomials past 10^15, are IMPALA_EUNSUPPORTED.
- * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included; batch
- * <= 2^21, and, but for small matrices that fit one CU, batch times both sides rounded up to 192
- * <= 2^34 (more: IMPALA_EUNSUPPORTED).
+ * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included, whose
+ * product rounded up to multiples of 192 is <= 2^29; batch <= 2^21, and, but for small matrices that
+ * fit one CU, batch times that product <= 2^34 (more: IMPALA_EUNSUPPORTED).
  * Precision: the products run on f16 matrix cores, each operand as the sum of two f16 numbers, with
  * float32 accumulation (small matrices: on float32 matrix cores); ||x|| is a 64-bit
  * sum. IMPALA_PREC_FP32 results differ from the exact ones

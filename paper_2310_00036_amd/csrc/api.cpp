@@ -68,7 +68,9 @@ size_t a256(size_t x) { return (x + 255) / 256 * 256; }
 
 // ---- the Muon step's arguments
 
-constexpr int64_t kMuonMaxSize = int64_t(1) << 28;   // elements of one matrix
+// Elements of one matrix, and with its sides in whole tiles: its planes (4 bytes) are within 2^31 bytes, which
+// the tile product's 32-bit offsets and its out-of-range offset need.
+constexpr int64_t kMuonMaxSize = int64_t(1) << 28, kMuonMaxTiled = int64_t(1) << 29;
 constexpr int kMuonMaxSide = 16384, kMuonMaxMats = 512, kMuonMaxSteps = 16;
 
 // What a shape takes in whole tiles, at most. The launches have at most 512 threads for 64 x 64 of it, so this
@@ -77,7 +79,8 @@ constexpr int64_t kMuonMaxPadded = int64_t(1) << 34;
 int64_t muon_padded(int64_t rows, int64_t cols) { return (rows + 191) / 192 * 192 * ((cols + 191) / 192 * 192); }
 
 bool muon_shape_ok(int64_t rows, int64_t cols) {
-    return rows >= 1 && cols >= 1 && rows * cols <= kMuonMaxSize && std::min(rows, cols) <= kMuonMaxSide;
+    return rows >= 1 && cols >= 1 && rows * cols <= kMuonMaxSize && muon_padded(rows, cols) <= kMuonMaxTiled &&
+           std::min(rows, cols) <= kMuonMaxSide;
 }
 
 muon_cfg_t muon_of(const learner_cfg_t& c) {

@@ -54,13 +54,15 @@ def test_orthogonalize_refusals():
         assert orth(**bad) == EINVAL, bad
     assert b"overlap" in lib.impala_last_error()
     for bad in (dict(r=1 << 15, c=1 << 15), dict(r=20000, c=20000), dict(b=1 << 20, r=1000, c=1000),
-                dict(b=(1 << 21) + 1, r=1, c=1), dict(b=1 << 17, r=400, c=200)):
+                dict(r=1, c=1 << 28), dict(r=1 << 22, c=3), dict(b=(1 << 21) + 1, r=1, c=1), dict(b=1 << 17, r=400, c=200)):
         assert orth(**bad) == EUNSUPPORTED, bad
     grow = (C.c_float * 15)(*([5.0, 5.0, 5.0] * 5))
     assert orth(co=grow) == EUNSUPPORTED and b"grow" in lib.impala_last_error()
     nan = (C.c_float * 15)(*([float("nan")] * 15))
     assert orth(co=nan) == EUNSUPPORTED
     assert P.muon_orthogonalize_workspace_bytes(P.PREC_FP32, 1 << 21, 3, 5, 5) > 0
+    assert P.muon_orthogonalize_workspace_bytes(P.PREC_FP32, 1, 1, 1 << 21, 5) > 0
+    assert P.muon_orthogonalize_workspace_bytes(P.PREC_FP32, 1, 1 << 14, 1 << 14, 5) > 0
     need = P.muon_orthogonalize_workspace_bytes(P.PREC_FP32, 2, 40, 30, 5)
     assert need > 0 and orth(wsb=need - 1) == EWORKSPACE
     assert orth(b=0, x=None, y=None, ws=None, wsb=0) == 0
@@ -82,6 +84,10 @@ def test_muon_step_refusals():
                 dict(mats=[(k, 1, 1) for k in range(513)]), dict(mats=[(2000, 1, 1)]), dict(t=0), dict(p=None),
                 dict(g=None), dict(m=None), dict(v=None), dict(ws=None)):
         assert step(**bad) == EINVAL, bad
+    # 32-bit offsets in a matrix's planes; the threads of a launch
+    assert step(n=1 << 28, mats=[(0, 1, 1 << 28)]) == EINVAL
+    assert step(n=64 << 28, mats=[(k << 28, 1 << 14, 1 << 14) for k in range(64)]) == EINVAL
+    assert b"too large" in lib.impala_last_error()
     for kw in (dict(lr=-1.0), dict(momentum=1.0), dict(momentum=-0.1), dict(weight_decay=-1.0), dict(steps=0),
                dict(steps=17), dict(scale=2), dict(eps=-1.0), dict(adam_lr=-1.0), dict(beta1=1.0), dict(beta2=1.5),
                dict(adam_eps=-1.0), dict(lr=float("nan"))):
