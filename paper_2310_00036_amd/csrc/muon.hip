@@ -33,6 +33,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 #include <vector>
 
 namespace cb {
@@ -700,11 +701,30 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
 
 enum { NS_SRC_F32 = 0, NS_SRC_BF16, NS_SRC_STEP };
 
+// The workgroup's sums of N values of each of 256 threads, in a fixed order. Ends with a barrier.
+template <int N>
+CB_DEV void ns_sum256(double (&v)[N], double* sh) {
+    for (int m = 1; m < 64; m <<= 1) {
+        double o[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] = __shfl_xor(v[k], m);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += o[k];
+    }
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sh[(threadIdx.x >> 6) * N + k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = (sh[k] + sh[N + k]) + (sh[2 * N + k] + sh[3 * N + k]);
+    __syncthreads();
+}
+
 // Blocks [0, start[ng]) sum a matrix's elements in G.nsum shares; (STEP) those after them the gaps'.
 // Three doubles a block: sum g^2, sum g m, sum m^2 (others: sum x^2, 0, 0).
 template <int SRC>
 __global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, const void* src, int block0) {
-    __shared__ double sh[256];
+    __shared__ double sh[12];
     int64_t at, len;
     int blk = blockIdx.x;
     bool both = SRC == NS_SRC_STEP;
@@ -762,14 +782,11 @@ __global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, cons
             }
         }
     }
-    gg = block_sum<256>(gg, sh);
-    if (SRC == NS_SRC_STEP) {
-        gm = block_sum<256>(gm, sh);
-        mm = block_sum<256>(mm, sh);
-    }
+    double t[3] = {gg, gm, mm};
+    ns_sum256(t, sh);
     if (threadIdx.x == 0) {
         double* o = reinterpret_cast<double*>(a.ws + a.sums) + int64_t(3) * (block0 + blockIdx.x);
-        o[0] = gg; o[1] = gm; o[2] = mm;
+        o[0] = t[0]; o[1] = t[1]; o[2] = t[2];
     }
 }
 
@@ -795,30 +812,75 @@ CB_DEV float ns_adam(float p, float g, float& m, float& v, const MuonElem& e) {
     return p - e.alr * mh / (sqrtf(vh) + e.aeps);
 }
 
+// Four neighbours of a row as they are in memory, n of them inside.
+template <class T>
+CB_DEV void ns_load4(const T* x, int n, float (&w)[4]) {
+    if (sizeof(T) == 4) {
+        if (n == 4) {
+            const float4 v = load_f4(reinterpret_cast<const float*>(x));
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            return;
+        }
+    } else if (n == 4 && (reinterpret_cast<uintptr_t>(x) & 7) == 0) {
+        load4(reinterpret_cast<const uint16_t*>(x), w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = i >= n ? 0.f : sizeof(T) == 4 ? reinterpret_cast<const float*>(x)[i] : bf2f(reinterpret_cast<const uint16_t*>(x)[i]);
+}
+
 // X's planes from the source (STEP: u from the clipped gradient and the momentum, which is updated),
-// padded with zeros; blocks after the matrices' (STEP): Adam on what no matrix covers.
+// padded with zeros; blocks after the matrices' (STEP): Adam on what no matrix covers. The elements are
+// loaded before the norms are formed, which takes as long as they do to arrive.
 template <int SRC, int NP>
 __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, const void* src, float eps, int block0) {
-    __shared__ double sh[256];
+    using T = std::conditional_t<SRC == NS_SRC_BF16, uint16_t, float>;
+    __shared__ double sh[16];
+    __shared__ float tile[64 * 65];
     const double* sums = reinterpret_cast<const double*>(a.ws + a.sums);
+    int blk = blockIdx.x;
+    const bool gap = SRC == NS_SRC_STEP && blk >= a.start[a.ng];
+    const int gi = gap ? 0 : ns_group(a, blk);
+    const NsGroup& G = a.g[gi];
+    const int per = ns_plane_blocks(G), b = gap ? 0 : blk / per, k = gap ? 0 : blk % per;
+    const int64_t off = ns_offset(a, G, b);
+    const int tc = max(1, G.cp / 64), r0 = k / tc * 64, q0 = k % tc * 64;   // (no group at all: gaps only)
+    float x[4][4], mv[4][4];
+    if (!gap)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int q = threadIdx.x + 256 * i, r = r0 + (q >> 4), c = q0 + (q & 15) * 4;
+            const int n = r < G.rows ? min(4, G.cols - c) : 0;
+            const int64_t o = off + int64_t(r) * G.cols + c;
+            ns_load4((SRC == NS_SRC_STEP ? reinterpret_cast<const T*>(e.g) : static_cast<const T*>(src)) + o, n, x[i]);
+            if (SRC == NS_SRC_STEP) ns_load4(reinterpret_cast<const T*>(e.m) + o, n, mv[i]);
+        }
+    double t[4] = {0.0, 0.0, 0.0, 0.0};   // the call's g^2; the matrix's g^2, g m, m^2
+    if (SRC == NS_SRC_STEP)
+        for (int i = threadIdx.x; i < e.nblocks; i += 256) t[0] += sums[3 * i];
+    if (!gap) {
+        const double* ms = sums + int64_t(3) * (G.part0 + b * G.nsum);
+        for (int i = threadIdx.x; i < G.nsum; i += 256) {
+            t[1] += ms[3 * i]; t[2] += ms[3 * i + 1]; t[3] += ms[3 * i + 2];
+        }
+    }
+    ns_sum256(t, sh);
     float clip = 1.f;
     if (SRC == NS_SRC_STEP) {
-        double s = 0.0;
-        for (int i = threadIdx.x; i < e.nblocks; i += 256) s += sums[3 * i];
-        const double norm = sqrt(block_sum<256>(s, sh));
+        const double norm = sqrt(t[0]);
         if (blockIdx.x == 0 && block0 == 0 && threadIdx.x == 0 && e.stats) {
             e.stats[0] = float(norm);
             e.stats[1] = isfinite(norm) ? 0.f : 1.f;
         }
         clip = (e.max_norm > 0.f && norm > double(e.max_norm)) ? float(double(e.max_norm) / norm) : 1.f;
     }
-    int blk = blockIdx.x;
-    if (SRC == NS_SRC_STEP && blk >= a.start[a.ng]) {
+    if (gap) {
         blk -= a.start[a.ng];
         int i = 0;
         while (i + 1 < e.ngaps && blk >= e.gap_start[i + 1]) ++i;
-        const int nb = e.gap_start[i + 1] - e.gap_start[i], k = blk - e.gap_start[i];
-        for (int64_t q = int64_t(k) * 256 + threadIdx.x; q < e.gap_len[i]; q += int64_t(nb) * 256) {
+        const int nb = e.gap_start[i + 1] - e.gap_start[i], z = blk - e.gap_start[i];
+        for (int64_t q = int64_t(z) * 256 + threadIdx.x; q < e.gap_len[i]; q += int64_t(nb) * 256) {
             const int64_t o = e.gap[i] + q;
             float m = e.m[o], v = e.v[o];
             const float p = ns_adam(e.p[o], e.g[o] * clip, m, v, e);
@@ -827,24 +889,13 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         }
         return;
     }
-    __shared__ float tile[64 * 65];
-    const NsGroup& G = a.g[ns_group(a, blk)];
-    const int per = ns_plane_blocks(G), b = blk / per, k = blk % per;
-    const double* ms = sums + int64_t(3) * (G.part0 + b * G.nsum);
-    double gg = 0.0, gm = 0.0, mm = 0.0;
-    for (int i = threadIdx.x; i < G.nsum; i += 256) {
-        gg += ms[3 * i]; gm += ms[3 * i + 1]; mm += ms[3 * i + 2];
-    }
-    gg = block_sum<256>(gg, sh);
-    double norm = sqrt(gg);
+    double norm = sqrt(t[1]);
     if (SRC == NS_SRC_STEP) {
-        gm = block_sum<256>(gm, sh);
-        mm = block_sum<256>(mm, sh);
         // ||c1 g + c2 m|| from the three sums; where the two all but cancel what is left of it is
         // their rounding, and a norm no smaller than that keeps the singular values below one
         const double c1 = double(e.c1) * clip, c2 = e.c2;
-        const double est = c1 * c1 * gg + 2.0 * c1 * c2 * gm + c2 * c2 * mm;
-        const double least = 0x1p-21 * (fabs(c1) * sqrt(gg) + fabs(c2) * sqrt(mm));
+        const double est = c1 * c1 * t[1] + 2.0 * c1 * c2 * t[2] + c2 * c2 * t[3];
+        const double least = 0x1p-21 * (fabs(c1) * sqrt(t[1]) + fabs(c2) * sqrt(t[3]));
         norm = est < least * least ? least : sqrt(est);
         eps = e.eps;
     }
@@ -852,69 +903,36 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
     const float f = ns_scale(norm, double(G.rows) * G.cols, eps, info);
     if (k == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.ws + a.info)[G.first + b] = info;
     char* X = a.ws + G.x[0] + int64_t(b) * NP * G.xs;
-    char* T = a.ws + G.xt[0] + int64_t(b) * NP * G.ts;
-    const int64_t off = ns_offset(a, G, b);
-    const int r0 = k / (G.cp / 64) * 64, q0 = k % (G.cp / 64) * 64;
-    for (int q = threadIdx.x; q < 1024; q += 256) {
-        const int lr = q >> 4, lc = (q & 15) * 4, r = r0 + lr, c = q0 + lc;
-        float w[4] = {0.f, 0.f, 0.f, 0.f};
-        if (r < G.rows && c < G.cols) {
-            const int64_t o = off + int64_t(r) * G.cols + c;
-            const int n = min(4, G.cols - c);
-            if (SRC == NS_SRC_BF16) {
-                const uint16_t* x = static_cast<const uint16_t*>(src) + o;
-                if (n == 4 && (reinterpret_cast<uintptr_t>(x) & 7) == 0) load4(x, w);
-                else
+    char* Xt = a.ws + G.xt[0] + int64_t(b) * NP * G.ts;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (i < n) w[i] = bf2f(x[i]);
-            } else if (SRC == NS_SRC_F32) {
-                const float* x = static_cast<const float*>(src) + o;
-                if (n == 4) {
-                    const float4 v = load_f4(x);
-                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                } else {
+    for (int i = 0; i < 4; ++i) {
+        const int q = threadIdx.x + 256 * i, lr = q >> 4, lc = (q & 15) * 4, r = r0 + lr, c = q0 + lc;
+        const int n = r < G.rows ? min(4, G.cols - c) : 0;
+        float (&w)[4] = x[i];
+        if (SRC == NS_SRC_STEP) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (i < n) w[i] = x[i];
-                }
-            } else {
-                float gv[4], mv[4];
-                if (n == 4) {
-                    const float4 g = load_f4(e.g + o), m = load_f4(e.m + o);
-                    gv[0] = g.x; gv[1] = g.y; gv[2] = g.z; gv[3] = g.w;
-                    mv[0] = m.x; mv[1] = m.y; mv[2] = m.z; mv[3] = m.w;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        gv[i] = i < n ? e.g[o + i] : 0.f;
-                        mv[i] = i < n ? e.m[o + i] : 0.f;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < n) {
-                        const float gs = e.omu * (gv[i] * clip);
-                        mv[i] = e.mu * mv[i] + gs;
-                        w[i] = e.nesterov ? e.mu * mv[i] + gs : mv[i];
-                    }
-                if (n == 4) {
-                    *reinterpret_cast<cb_f32x4_a4*>(e.m + o) = cb_f32x4_a4{mv[0], mv[1], mv[2], mv[3]};
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (i < n) e.m[o + i] = mv[i];
-                }
+            for (int u = 0; u < 4; ++u) {
+                const float gs = e.omu * (w[u] * clip);
+                mv[i][u] = e.mu * mv[i][u] + gs;
+                w[u] = e.nesterov ? e.mu * mv[i][u] + gs : mv[i][u];
             }
+            float* m = e.m + off + int64_t(r) * G.cols + c;
+            if (n == 4) {
+                *reinterpret_cast<cb_f32x4_a4*>(m) = cb_f32x4_a4{mv[i][0], mv[i][1], mv[i][2], mv[i][3]};
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = i < n ? w[i] * f : 0.f;
+                for (int u = 0; u < 4; ++u)
+                    if (u < n) m[u] = mv[i][u];
+            }
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[u] = u < n ? w[u] * f : 0.f;
         uint2 hi, lo;
         ns_split(w, hi, lo);
         if (NP > 1) ns_store(X, r, c, G.ldx, hi, lo);
         else *reinterpret_cast<uint2*>(X + (int64_t(r) * G.ldx + c) * 2) = hi;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tile[(lc + i) * 65 + lr] = w[i];
+        for (int u = 0; u < 4; ++u) tile[(lc + u) * 65 + lr] = w[u];
     }
     __syncthreads();
     for (int q = threadIdx.x; q < 1024; q += 256) {   // the transpose
@@ -922,8 +940,8 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         const float w[4] = {tile[lc * 65 + lr], tile[lc * 65 + lr + 1], tile[lc * 65 + lr + 2], tile[lc * 65 + lr + 3]};
         uint2 hi, lo;
         ns_split(w, hi, lo);
-        if (NP > 1) ns_store(T, q0 + lc, r0 + lr, G.ldt, hi, lo);
-        else *reinterpret_cast<uint2*>(T + (int64_t(q0 + lc) * G.ldt + r0 + lr) * 2) = hi;
+        if (NP > 1) ns_store(Xt, q0 + lc, r0 + lr, G.ldt, hi, lo);
+        else *reinterpret_cast<uint2*>(Xt + (int64_t(q0 + lc) * G.ldt + r0 + lr) * 2) = hi;
     }
 }
 
