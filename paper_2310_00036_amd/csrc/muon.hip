@@ -793,16 +793,18 @@ __global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, cons
 // Workgroups of the planes: tiles of 64 x 64 of the padded shape.
 __host__ __device__ inline int ns_plane_blocks(const NsGroup& G) { return (G.rp / 64) * (G.cp / 64); }
 
-// The power of two that brings a matrix of this norm to a root mean square near one; info as ns_info.
-// A zero matrix: (1, 0).
-CB_DEV float ns_scale(double norm, double elems, float eps, float2& info) {
+// The power of two that brings a matrix of this norm to a root mean square in [1, 2): elements stay below
+// 2 sqrt(2^28) in f16's range. By exponents: the double logarithm and power of a few threads would be most of
+// the launch's time where it is short.
+CB_DEV float ns_scale(double norm, double elems) {
     int k = 0;
-    if (norm > 0.0 && isfinite(norm)) k = -int(rint(log2(norm / sqrt(elems))));
-    k = k < -126 ? -126 : k > 126 ? 126 : k;
-    const double f = exp2(double(k));
-    info.x = norm == 0.0 ? 1.f : float(1.0 / (norm * f));
-    info.y = norm == 0.0 ? 0.f : float(norm / (norm > double(eps) || norm != norm ? norm : double(eps)));
-    return float(f);
+    if (norm > 0.0 && isfinite(norm)) k = -(ilogb(norm * norm / elems) >> 1);
+    return ldexpf(1.f, k < -126 ? -126 : k > 126 ? 126 : k);
+}
+// ... and info as ns_info. A zero matrix: (1, 0).
+CB_DEV float2 ns_norms(double norm, double f, float eps) {
+    if (norm == 0.0) return make_float2(1.f, 0.f);
+    return make_float2(float(1.0 / (norm * f)), float(norm / (norm > double(eps) || norm != norm ? norm : double(eps))));
 }
 
 CB_DEV float ns_adam(float p, float g, float& m, float& v, const MuonElem& e) {
@@ -899,9 +901,8 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
         norm = est < least * least ? least : sqrt(est);
         eps = e.eps;
     }
-    float2 info;
-    const float f = ns_scale(norm, double(G.rows) * G.cols, eps, info);
-    if (k == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.ws + a.info)[G.first + b] = info;
+    const float f = ns_scale(norm, double(G.rows) * G.cols);
+    if (k == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.ws + a.info)[G.first + b] = ns_norms(norm, f, eps);
     char* X = a.ws + G.x[0] + int64_t(b) * NP * G.xs;
     char* Xt = a.ws + G.xt[0] + int64_t(b) * NP * G.ts;
 #pragma unroll
