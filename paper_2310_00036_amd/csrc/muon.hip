@@ -112,6 +112,34 @@ CB_DEV void ns_tile(int t, int& ti, int& tj) {
     tj = t;
 }
 
+// Workgroups go to the eight XCDs in turn. The one of n that works on item `blk` so that each XCD has its
+// items in one run, and (ns_tile_near) neighbouring items share panels of the operands in its L2.
+CB_DEV int ns_xcd(int blk, int n) {
+    const int x = blk & 7, q = n >> 3, r = n & 7;
+    return x * q + min(x, r) + (blk >> 3);
+}
+// Tile t of the lower triangle of T x T, in bands of kNear rows, column by column.
+constexpr int kNear = 6, kWide = 8;
+CB_DEV void ns_tile_near(int t, int T, int& ti, int& tj) {
+    int r = 0, h;
+    for (;; r += h) {
+        h = min(kNear, T - r);
+        const int count = h * r + h * (h + 1) / 2;
+        if (t < count) break;
+        t -= count;
+    }
+    if (t < h * r) {
+        tj = t / h;
+        ti = r + t % h;
+        return;
+    }
+    t -= h * r;
+    int d = 0;
+    while (t >= h - d) t -= h - d++;
+    tj = r + d;
+    ti = tj + t;
+}
+
 // ------------------------------------------------------------------ the tile product
 //
 // acc += A B^T over k in [k0, k1) for a BT x BT tile, in NsWaves' waves. An operand is a padded matrix
@@ -326,9 +354,11 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a,
     extern __shared__ __align__(16) unsigned char smem[];
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
-    const int z = blk % G.splits, t = blk / G.splits % G.gtiles, b = blk / (G.splits * G.gtiles);
+    if (BT >= 128) blk = ns_xcd(blk, G.batch * G.gtiles * G.splits);
+    const int t = blk % G.gtiles, z = blk / G.gtiles % G.splits, b = blk / (G.splits * G.gtiles);
     int ti, tj;
-    ns_tile(t, ti, tj);
+    ns_tile(t, ti, tj);   // (where partials are summed, in this order)
+    if (BT >= 128 && G.splits == 1) ns_tile_near(t, G.mp / BT, ti, tj);
     const char* X = a.ws + (G.tall ? G.xt : G.x)[src] + int64_t(b) * NP * (G.tall ? G.ts : G.xs);   // [m][n]
     const int k0 = z * G.kchunk, k1 = min(G.np, k0 + G.kchunk);
     NsAcc<BT> acc;
@@ -537,10 +567,12 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
     using W = NsWaves<BT>;
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
-    const NsJob& J = jobs.j[blk % jobs.n];
-    const int t = blk / jobs.n % G.tiles, b = blk / (jobs.n * G.tiles);
+    if (BT >= 128) blk = ns_xcd(blk, G.batch * G.tiles * jobs.n);
+    const NsJob& J = jobs.j[blk / G.tiles % jobs.n];
+    const int b = blk / (jobs.n * G.tiles);
     int ti, tj;
-    ns_tile(t, ti, tj);
+    if (BT >= 128) ns_tile_near(blk % G.tiles, G.mp / BT, ti, tj);
+    else ns_tile(blk % G.tiles, ti, tj);
     const char* add = ns_buf(a, G, J.add, b);
     uint4 early[EARLY ? W::FM : 1][EARLY ? W::FN : 1];
     NsAcc<BT> acc;
@@ -600,7 +632,16 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     int blk = blockIdx.x;
     const NsGroup& G = a.g[ns_group(a, blk)];
     const int tn = G.rp / BT, tm = G.cp / BT;   // N over the rows, M over the columns
-    const int jt = blk % tn, it = blk / tn % tm, b = blk / (tn * tm);
+    int jt = blk % tn, it = blk / tn % tm, b = blk / (tn * tm);
+    if (BT >= 128) {   // bands of kWide rows, column by column
+        blk = ns_xcd(blk, G.batch * tn * tm);
+        b = blk / (tn * tm);
+        blk %= tn * tm;
+        const int r = blk / (kWide * tm) * kWide, h = min(kWide, tn - r);
+        blk -= r * tm;
+        jt = r + blk % h;
+        it = blk / h;
+    }
     const int ld = G.tall ? G.ldx : G.ldt;
     const int64_t xs = NP * (G.tall ? G.xs : G.ts);
     const char* X = a.ws + (G.tall ? G.x : G.xt)[ap.src] + b * xs;   // [n][m]
