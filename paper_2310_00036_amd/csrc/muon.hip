@@ -178,6 +178,14 @@ struct NsWaves {
     static constexpr int FM = BT / WM / 16, FN = BT / WN / 16;
 };
 
+// The rows of a tile that fragment i, j of the two operands hold (r: 0 .. 15). Any order gives the same
+// products; with this one a lane's results of two neighbouring fragments are eight neighbours along M, and
+// two along N, so that it writes 16 bytes of a row at once and 4 of a mirrored one.
+template <int BT>
+CB_DEV int ns_row_a(int i, int r) { return BT == 32 ? r : i / 2 * 32 + (r >> 2) * 8 + (i & 1) * 4 + (r & 3); }
+template <int BT>
+CB_DEV int ns_row_b(int j, int r) { return BT == 32 ? r : j / 2 * 32 + r * 2 + (j & 1); }
+
 template <int BT, int BK, int NP>
 struct NsOperand {
     static constexpr int NW = NsWaves<BT>::NW;
@@ -186,13 +194,31 @@ struct NsOperand {
     static constexpr int NI = BYTES / (1024 * NW);         // direct loads a wave
     static constexpr int SPR = RB / 16;                    // 16-byte slots per row
     static_assert(BYTES % (1024 * NW) == 0, "whole loads");
+    static_assert(BT != 32 || RB != 64, "key would depend on r0");
     uint32_t base[NI];
-    // the slot that holds chunk c of row r (its own inverse)
-    static CB_DEV int swz(int r, int c) { return RB == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7); }
+    // Chunk c of row r is in slot c ^ key(r), or, where two rows share 128 bytes, half of them in the other's
+    // place. key: eight lanes of a fragment read meet eight slots, with the rows that ns_row_a and ns_row_b give
+    // them (of the bits r0 .. r4 of a row they vary r0, r1, r3 and r1, r2, r3; in tiles of 32 r0, r1, r2).
+    static CB_DEV int key(int r) {
+        const int hi = (RB == 64 ? 0 : r << 2) ^ r, lo = BT == 32 ? r >> 2 : r >> 3;
+        return BT == 32 ? r & 7 : (hi & 4) | (r & 2) | (lo & 1);
+    }
+    static CB_DEV int slot(int r, int c) {   // in 16 bytes from the tile's start
+        return RB == 64 ? (r >> 1) * 8 + ((((r & 1) << 2) | c) ^ key(r)) : r * SPR + (c ^ key(r));
+    }
     CB_DEV NsOperand(int ld, int row0, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int s = (wave + NW * i) * 64 + lane, r = s / SPR, c = swz(r, s % SPR);
+            const int s = (wave + NW * i) * 64 + lane;
+            int r, c;
+            if (RB == 64) {   // (key does not depend on r0)
+                const int e = (s & 7) ^ key(s >> 3 << 1);
+                r = (s >> 3 << 1) + (e >> 2);
+                c = e & 3;
+            } else {
+                r = s / SPR;
+                c = (s % SPR) ^ key(r);
+            }
             base[i] = uint32_t(row0 + r) * uint32_t(ld) * (NP * 2u) + uint32_t(c * 16);
         }
     }
@@ -200,9 +226,9 @@ struct NsOperand {
     CB_DEV void issue(int i, ns_u32x4 rs, uint32_t lds, int k, bool live, int wave) const {
         ns_dma16(rs, lds + (wave + NW * i) * 1024, live ? base[i] + uint32_t(k) * (NP * 2u) : kOOB);
     }
-    // plane p's 8 consecutive k (step ks of 32, lane group g) of tile row `row` (row % 16 == lane % 16)
+    // plane p's 8 consecutive k (step ks of 32, lane group g) of tile row `row`
     static CB_DEV uint4 frag(const unsigned char* t, int p, int row, int ks, int lane) {
-        return *reinterpret_cast<const uint4*>(t + row * RB + swz(row, (ks * NP + p) * 4 + (lane >> 4)) * 16);
+        return *reinterpret_cast<const uint4*>(t + slot(row, (ks * NP + p) * 4 + (lane >> 4)) * 16);
     }
 };
 
@@ -234,10 +260,10 @@ CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char
         else ob.issue(d < OA::NI ? 0 : d - OA::NI, rb, l + OA::BYTES, k0 + it * BK, it < nb, wave);
     };
     auto read_a = [&](int st, int p, int ks, int i) CB_INLINE_LAMBDA {
-        return OA::frag(smem + (st % ST) * STAGE, p, wm * (FM * 16) + i * 16 + r16, ks, lane);
+        return OA::frag(smem + (st % ST) * STAGE, p, wm * (FM * 16) + ns_row_a<BT>(i, r16), ks, lane);
     };
     auto read_b = [&](int st, int p, int ks, int j) CB_INLINE_LAMBDA {
-        return OB::frag(smem + (st % ST) * STAGE + OA::BYTES, p, wn * (FN * 16) + j * 16 + r16, ks, lane);
+        return OB::frag(smem + (st % ST) * STAGE + OA::BYTES, p, wn * (FN * 16) + ns_row_b<BT>(j, r16), ks, lane);
     };
     // x y row by row; with(ks, i) before row i of step ks: reads and loads go between the products, for
     // one block of either would hold the matrix core up
@@ -325,7 +351,59 @@ CB_DEV void ns_each(NsAcc<BT>& acc, Fn&& f) {
     for (int i = 0; i < W::FM; ++i)
 #pragma unroll
         for (int j = 0; j < W::FN; ++j)
-            f(wm * (W::FM * 16) + i * 16 + 4 * g, wn * (W::FN * 16) + j * 16 + r16, acc[i][j], i, j);
+            f(wm * (W::FM * 16) + ns_row_a<BT>(i, 4 * g), wn * (W::FN * 16) + ns_row_b<BT>(j, r16), acc[i][j], i, j);
+}
+
+// The planes of value(M, N, acc[i][j], i, j, w) (four rows M .. of column N), to d as the matrix [N][M] from
+// (n0, m0) on, and with `mirror` to e as [M][N] from (m0, n0) on. Blocks of two by two fragments together.
+template <int BT, class Fn>
+CB_DEV void ns_emit(NsAcc<BT>& acc, char* d, int ld, int n0, int m0, bool mirror, char* e, int lde, Fn&& value) {
+    using W = NsWaves<BT>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int g = lane >> 4, r16 = lane & 15, wm = wave / W::WN * (W::FM * 16), wn = wave % W::WN * (W::FN * 16);
+    if constexpr (BT == 32) {
+        const int M = wm + 4 * g, N = wn + r16;
+        float w[4];
+        value(M, N, acc[0][0], 0, 0, w);
+        uint2 hi, lo;
+        ns_split(w, hi, lo);
+        ns_store(d, n0 + N, m0 + M, ld, hi, lo);
+        if (mirror) ns_store_across(e, m0 + M, n0 + N, lde, hi, lo);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::FM; i += 2)
+#pragma unroll
+            for (int j = 0; j < W::FN; j += 2) {
+                const int M = wm + ns_row_a<BT>(i, 4 * g), N = wn + ns_row_b<BT>(j, r16);
+                uint2 hi[2][2], lo[2][2];   // [N][M / 4]
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float w[4];
+                        value(M + 4 * u, N + v, acc[i + u][j + v], i + u, j + v, w);
+                        ns_split(w, hi[v][u], lo[v][u]);
+                    }
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    char* p = d + ns_at(n0 + N + v, m0 + M, ld);
+                    *reinterpret_cast<uint4*>(p) = make_uint4(hi[v][0].x, hi[v][0].y, hi[v][1].x, hi[v][1].y);
+                    *reinterpret_cast<uint4*>(p + kLo) = make_uint4(lo[v][0].x, lo[v][0].y, lo[v][1].x, lo[v][1].y);
+                }
+                if (mirror) {
+                    char* p = e + ns_at(m0 + M, n0 + N, lde);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r, p += int64_t(lde) * 4) {
+                        auto two = [&](const uint2 (&x)[2][2]) CB_INLINE_LAMBDA {
+                            const uint32_t a = r & 2 ? x[0][r / 4].y : x[0][r / 4].x, b = r & 2 ? x[1][r / 4].y : x[1][r / 4].x;
+                            return r & 1 ? (a >> 16) | (b & 0xffff0000u) : (a & 0xffffu) | (b << 16);
+                        };
+                        *reinterpret_cast<uint32_t*>(p) = two(hi);
+                        *reinterpret_cast<uint32_t*>(p + kLo) = two(lo);
+                    }
+                }
+            }
+    }
 }
 
 // ------------------------------------------------------------------ Gram product
@@ -369,13 +447,11 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a,
     if (G.splits == 1 && !G.small) {
         char* D = a.ws + G.a + int64_t(b) * 2 * G.ms;
         const float f = ns_alpha(a, s, G.first + b) * s.sa;
-        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
-            const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
-            uint2 hi, lo;
-            ns_split(w, hi, lo);
-            ns_store(D, tj * BT + N, ti * BT + M, G.ldm, hi, lo);
-            if (ti != tj) ns_store_across(D, ti * BT + M, tj * BT + N, G.ldm, hi, lo);
-        });
+        ns_emit<BT>(acc, D, G.ldm, tj * BT, ti * BT, ti != tj, D, G.ldm,
+                    [&](int, int, cb_f32x4 v, int, int, float (&w)[4]) CB_INLINE_LAMBDA {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) w[r] = v[r] * f;
+                    });
         return;
     }
     float* part = reinterpret_cast<float*>(a.ws + G.part + int64_t(b) * G.ps) + (int64_t(z) * G.gtiles + t) * (BT * BT);
@@ -587,9 +663,9 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
                               tj * BT, 0, G.mp, smem, acc);
     char* D = ns_buf(a, G, J.dst, b);
     const float f = J.f, fa = J.fa, diag = J.diag;
-    ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int i, int j) CB_INLINE_LAMBDA {
+    ns_emit<BT>(acc, D, G.ldm, tj * BT, ti * BT, ti != tj, D, G.ldm,
+                [&](int M, int N, cb_f32x4 v, int i, int j, float (&w)[4]) CB_INLINE_LAMBDA {
         const int m = ti * BT + M, n = tj * BT + N;
-        float w[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[r] = f * v[r];
         if (fa != 0.f || diag != 0.f) {
@@ -606,10 +682,6 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
 #pragma unroll
             for (int r = 0; r < 4; ++r) w[r] += fa * q[r] + (m + r == n ? diag : 0.f);
         }
-        uint2 hi, lo;
-        ns_split(w, hi, lo);
-        ns_store(D, n, m, G.ldm, hi, lo);
-        if (ti != tj) ns_store_across(D, m, n, G.ldm, hi, lo);
     });
 }
 
@@ -665,14 +737,11 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_apply_kernel(NsArgs a
     if (ap.out == NS_OUT_MID) {
         char* D = a.ws + G.x[ap.dst] + int64_t(b) * 2 * G.xs;
         char* T = a.ws + G.xt[ap.dst] + int64_t(b) * 2 * G.ts;
-        ns_each<BT>(acc, [&](int M, int N, cb_f32x4 v, int, int) CB_INLINE_LAMBDA {
-            const float w[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
-            uint2 hi, lo;
-            ns_split(w, hi, lo);
-            const int r = jt * BT + N, c = it * BT + M;
-            ns_store(D, r, c, G.ldx, hi, lo);
-            ns_store_across(T, c, r, G.ldt, hi, lo);
-        });
+        ns_emit<BT>(acc, D, G.ldx, jt * BT, it * BT, true, T, G.ldt,
+                    [&](int, int, cb_f32x4 v, int, int, float (&w)[4]) CB_INLINE_LAMBDA {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) w[r] = v[r] * f;
+                    });
         return;
     }
     const int64_t off = ns_offset(a, G, b);
