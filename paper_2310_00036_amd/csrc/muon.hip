@@ -25,7 +25,13 @@
 // for the rest); and per segment the Gram product (split over k), its sum, the m x m products, and
 // Q X, whose last form writes the result or the updated parameters. Matrices of up to 64 on the
 // smaller side have their whole m x m part in one workgroup's LDS, in float32, inside the launch that
-// sums the others' Gram partials. All matrices of a call go through the same launches.
+// sums the others' Gram partials. All matrices of a call go through the same launches. Small matrices
+// of muon_orthogonalize do without all that: one launch, a workgroup each (ns_one_kernel).
+//
+// What bounds a call: up to m = 512 or so the latency of its 20 launches, 4 to 8 us each (3872 x 256
+// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the standard net's muon_step 132 us);
+// from there on the tile product (4096 x 4096 bf16 3.55 ms, 390 TFLOP/s of the result's operations,
+// 1.2 PFLOP/s of f16 products where a large library product of f16 matrices reaches 1.49).
 #include "common.h"
 #include "kernels.h"
 #include "muon.h"
@@ -146,7 +152,9 @@ CB_DEV void ns_tile_near(int t, int T, int& ti, int& tj) {
 // [rows][k] of NP planes, leading dimension ld elements; padding is zero, so there are no edges. Tiles go
 // from memory into an LDS ring of ST stages by direct loads that stay in flight across barriers (one wait
 // per stage, counted), in the layout they have in memory; 16-byte slots are permuted within a row so that
-// a fragment read meets every bank.
+// a fragment read meets every bank. A product of 4224 x 4224 planes (253 tiles of 192, one a CU) takes 195
+// us; on zeros, which draw less power, 160, and of these 142 without its loads, 139 without its matrix
+// instructions: both pipes are near their ends, and finer interleaving of the two brought nothing.
 
 // 16 bytes a lane to LDS at lds + 16 lane. Inline so that the compiler, which cannot tell a ring's
 // stages apart, does not wait for every load in flight before an LDS read; the waits are written out.
@@ -426,7 +434,9 @@ CB_DEV float ns_alpha(const NsArgs& a, const NsSeg& s, int mat) {
 }
 
 // One tile of A = X X^T (smaller side), scaled; or, where k is split or the m x m part is done in LDS, the
-// k range of one split of it to part [split][tile][N][M] float32.
+// k range of one split of it to part [split][tile][N][M] float32. Only the lower triangle's tiles, so half
+// the operations. Without the split 3872 x 256 would be 10 workgroups of 61 steps; with it 210 of 3, 8 us,
+// of which the start and the end of a workgroup are most. 4096 x 4096: 243 us, 114 in one plane.
 template <int BT, int BK, int ST, int NP>
 __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_gram_kernel(NsArgs a, NsSeg s, int src) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -579,7 +589,8 @@ CB_DEV void ns_small(const NsArgs& a, const NsGroup& G, const NsSeg& s, int b, f
 }
 
 // Sums the Gram partials in split order. m <= 64: and goes on to Q. Else A's planes, 16 columns of a
-// tile a workgroup, with the mirror image of an off-diagonal tile.
+// tile a workgroup, with the mirror image of an off-diagonal tile. Two steps at m = 64: 11 us on 16 waves
+// (17 on 4), a product of 64 x 64 taking 0.5 us of a CU's float32 matrix rate; 256 x 256 in 20 splits: 6 us.
 template <int NT>
 __global__ __launch_bounds__(NT) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -622,6 +633,10 @@ __global__ __launch_bounds__(NT) void ns_reduce_kernel(NsArgs a, NsSeg s) {
     }
 }
 
+// The products of symmetric matrices that commute: tiles of the lower triangle and their mirror images, one
+// or two products a launch. Tiles of up to 64 read what is added early, behind the product. m = 256: 5 us
+// (36 tiles of 32), a launch and eight trips to memory in turn; 1001 x 2: 30 us for one product or two (72 or
+// 144 tiles of 128; tiles of 64, 272 or 544, took 24 and 38); 4096: 195 us, 1.21 PFLOP/s.
 enum { NS_A = 0, NS_T, NS_P, NS_Q0, NS_Q1 };
 struct NsJob {                 // dst = diag I + fa add + f lhs rhs (scales included)
     int lhs, rhs, dst, add;
@@ -687,6 +702,9 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
 
 // ------------------------------------------------------------------ Q X
 
+// A tile of Q X: the next segment's planes of X and of its transpose, the result, or the parameters, so that
+// the result of muon_step is never written. 3872 x 256: 9 us (244 tiles of 64), where k = 256 is four steps of
+// the ring and the start, the writes and the launch are most; 7744 x 512: 19 us; 4096 x 4096: 360 us.
 enum { NS_OUT_MID = 0, NS_OUT_F32, NS_OUT_BF16, NS_OUT_STEP };
 struct NsApply {
     int out, src, dst, q;      // X buffer read, X buffer written (MID), Q buffer of the large groups
@@ -831,6 +849,7 @@ CB_DEV void ns_sum256(double (&v)[N], double* sh) {
 }
 
 // Blocks [0, start[ng]) sum a matrix's elements in G.nsum shares; (STEP) those after them the gaps'.
+// Memory-bound where it is long (the wide net's 35 MB of g and m: 10 us), else latency: 5 to 7 us.
 // Three doubles a block: sum g^2, sum g m, sum m^2 (others: sum x^2, 0, 0).
 template <int SRC>
 __global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, const void* src, int block0) {
@@ -944,7 +963,9 @@ CB_DEV void ns_load4(const T* x, int n, float (&w)[4]) {
 
 // X's planes from the source (STEP: u from the clipped gradient and the momentum, which is updated),
 // padded with zeros; blocks after the matrices' (STEP): Adam on what no matrix covers. The elements are
-// loaded before the norms are formed, which takes as long as they do to arrive.
+// loaded before the norms are formed, which takes as long as they do to arrive. A workgroup takes 64 x 64
+// through LDS, so that both forms are written by rows. 3872 x 256: 11 us for 12 MB, latency; the wide net's
+// 1101 tiles: 24 us, 87 MB at 3.6 TB/s.
 template <int SRC, int NP>
 __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, const void* src, float eps, int block0) {
     using T = std::conditional_t<SRC == NS_SRC_BF16, uint16_t, float>;
@@ -1061,7 +1082,8 @@ __global__ __launch_bounds__(256) void ns_planes_kernel(NsArgs a, MuonElem e, co
 // A matrix of at most 64 on its smaller side that fits one CU's LDS in float32 takes one workgroup and no
 // workspace: its steps one by one, as they are written, from LDS in float32 MFMAs. What bounds it is the
 // latency of each of its products and, at m = 64, the float32 matrix rate of one CU; the launches of the
-// other way are 5 us each.
+// other way are 5 us each. 4 x 144x16: 15 us (61 the other way), 4 x 288x32: 28, 8 x 288x64: 66, 300 x
+// 144x32: 40. Float32 products also keep it at half the error, 5e-7 of the norm where the planes have 1e-6.
 
 struct NsOne { int rows, cols, steps; float eps; float c[kNsMaxSteps][3]; };
 
@@ -1200,9 +1222,11 @@ bool ns_one(int64_t batch, int rows, int cols) {
     return m <= 64 && ns_one_lds(rows, cols) <= 160 * 1024 && (batch >= 64 || m * m * n <= 64 * 64 * 320);
 }
 
-// Tiles of the m x m products: the smallest whose workgroups do not outnumber the CUs (one a CU). A tile of
-// 128 takes 1.2 times as long as one of 64 for four times the work, one of 192 twice as long for nine
-// times; of 32, where a launch is mostly latency, (m = 256) a third less than one of 64.
+// Tiles of the m x m products: the smallest whose workgroups do not outnumber the CUs, one a CU (of 32: two).
+// Measured, one product: m = 256, tiles of 32 and 64: 4.9 and 7.3 us; 768 (300 and 78 tiles): 8.6 and 11.2,
+// two matrices (600 and 156): 15.3 and 13.1; 1024, tiles of 64 and 128: 13.7 and 24.9, two matrices (272 and
+// 72): 24 and 25; 2816, 128 and 192 (253 and 120): 66 and 106; 4096 (561 and 253): 192 a fifth faster. Sides
+// below 1024 would be padded too far by 192.
 int ns_bt(int m, int64_t batch) {
     auto tiles = [&](int bt) { const int64_t t = (m + bt - 1) / bt; return batch * t * (t + 1) / 2; };
     return tiles(32) <= 512 ? 32 : tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
