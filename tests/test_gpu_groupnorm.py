@@ -321,3 +321,28 @@ def test_captured_and_replayed_on_another_stream(dims):
         graph.replay()
         G.sync()
         assert all(t.equal(a, b) for a, b in zip(want, (y, mean, rstd, dx, dg, db))), k
+
+
+def test_more_frames_than_one_launch_of_their_sums():
+    """4100 frames of 65 x 1024 in chunks: their sums take two launches. dx as from two calls of 2050 frames, bit
+    for bit; the parameters' gradients, each rounded once from a 64-bit sum, as the two calls' sum."""
+    t = G.torch()
+    n, H, W, C, groups = 4100, 5, 13, 1024, 32
+    gen = t.Generator(device="cuda:0").manual_seed(5)
+    x, dy = (t.empty((n, H, W, C), dtype=t.bfloat16, device="cuda:0").normal_(generator=gen) for _ in range(2))
+    gamma, beta = (t.randn(C, generator=gen, device="cuda:0") for _ in range(2))
+    y, dx, part = (t.empty_like(x) for _ in range(3))
+    mean, rstd = (t.empty((n, groups), device="cuda:0") for _ in range(2))
+    ws = G.ws_bytes(max(f(G.BF16, n, H, W, C, groups) for f in (P.impala_groupnorm_fwd_workspace_bytes,
+                                                                P.impala_groupnorm_bwd_workspace_bytes)))
+    P.impala_groupnorm_fwd(G.BF16, n, H, W, C, groups, x, gamma, beta, EPS, P.ACT_RELU, y, mean, rstd, ws)
+    grads = [[t.empty(C, device="cuda:0") for _ in range(2)] for _ in range(3)]
+    P.impala_groupnorm_bwd(G.BF16, n, H, W, C, groups, dy, x, gamma, beta, mean, rstd, P.ACT_RELU, dx, *grads[0], ws)
+    for k, f in enumerate((0, n // 2)):
+        s = slice(f, f + n // 2)
+        P.impala_groupnorm_bwd(G.BF16, n // 2, H, W, C, groups, dy[s], x[s], gamma, beta, mean[s], rstd[s], P.ACT_RELU,
+                               part[s], *grads[k + 1], ws)
+    G.sync()
+    assert t.equal(dx, part)
+    for a, b, c in zip(*([v.double() for v in g] for g in grads)):
+        assert bool(((a - b - c).abs() <= U * (a.abs() + b.abs() + c.abs())).all())

@@ -500,3 +500,47 @@ def test_normalised_conv_trained_with_orthogonalised_updates():
              v=np.zeros(p0.size, np.float32))
     wp, _, _, _, tp, _ = _step_want(b, [(0, 9 * C, C)], step=1)
     assert np.all(np.abs(G.host(flat)[:N] - wp[:N]) <= tp[:N])
+
+
+@PREC
+def test_orthogonalize_captured_and_beside_another_stream(prec):
+    """Calls of every form on two streams at once, each with its own workspace, and the same captured into one
+    graph and replayed on new inputs with eager work between: the eager results, bit for bit."""
+    t = G.torch()
+    shapes = [(4, 144, 16), (3, 576, 64), (1, 300, 520), (1, 1100, 1200)]
+    xs = [[G.dev_act(G.q(_gauss(20 + r, *s), prec), prec) for s in shapes] for r in range(3)]
+    want = [[t.empty_like(x) for x in v] for v in xs]
+    ws = [[G.ws_bytes(P.muon_orthogonalize_workspace_bytes(prec, *s)) for s in shapes] for _ in range(2)]
+
+    def run(inputs, outputs, k):
+        for s, x, y, w in zip(shapes, inputs, outputs, ws[k]):
+            P.muon_orthogonalize(prec, *s, x, y, w)
+
+    for v, w in zip(xs, want):
+        run(v, w, 0)
+    G.sync()
+    got = [[t.empty_like(x) for x in v] for v in xs]
+    streams = [t.cuda.Stream() for _ in range(2)]
+    for st in streams:
+        st.wait_stream(t.cuda.current_stream())
+    for k, st in enumerate(streams):
+        with t.cuda.stream(st):
+            run(xs[k], got[k], k)
+            run(xs[k], got[k], k)
+    G.sync()
+    for k in range(2):
+        assert all(t.equal(a, b) for a, b in zip(got[k], want[k]))
+    held = [x.clone() for x in xs[0]]
+    with t.cuda.stream(streams[0]):
+        run(held, got[2], 0)
+    G.sync()
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        run(held, got[2], 0)
+    for r in (1, 2, 0):
+        for h, x in zip(held, xs[r]):
+            h.copy_(x)
+        graph.replay()
+        run(xs[r], got[1], 1)
+        G.sync()
+        assert all(t.equal(a, b) for a, b in zip(got[2], want[r])) and all(t.equal(a, b) for a, b in zip(got[1], want[r]))
