@@ -19,7 +19,7 @@ struct NsGroup {
     int tiles, gtiles, splits, kchunk;   // tiles of symmetric m x m products; the Gram product's k split
     int table, nsum, part0;           // 1 + its first offset in NsArgs::off (0: b * rows * cols); its blocks of the sums
     float scale;                      // the update's factor (muon_step)
-    int64_t x[2], xt[2], part, a, t, p, q[2];   // workspace byte offsets of the first matrix (xt: X transposed)
+    int64_t x[2], xt[2], part, a, t, p, v, q[2];   // workspace byte offsets of the first matrix (xt: X transposed)
     int ldx, ldt, ldm;                   // leading dimensions of X, its transpose and the m x m matrices
     int64_t xs, ts, ms, ps;              // bytes of one plane of each, and of one matrix's partials
 };

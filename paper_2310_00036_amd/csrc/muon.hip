@@ -29,7 +29,7 @@
 // of muon_orthogonalize do without all that: one launch, a workgroup each (ns_one_kernel).
 //
 // What bounds a call: up to m = 512 or so the latency of its 20 launches, 4 to 8 us each (3872 x 256
-// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the standard net's muon_step 132 us);
+// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 129 us);
 // from there on the tile product (4096 x 4096 bf16 3.55 ms, 390 TFLOP/s of the result's operations,
 // 1.2 PFLOP/s of f16 products where a large library product of f16 matrices reaches 1.49).
 #include "common.h"
@@ -420,7 +420,7 @@ struct NsSeg {                 // one segment's polynomials and scales (host con
     int len;
     float c[kSegBf16][3];
     float sa, sp, st, sq;      // power-of-two scales of A, P, P A and Q
-    float ss, sv;              // and of P P and b P + c A' P
+    float su, sv;              // and of P Q and b Q + c A' Q
     float alpha;               // the Gram matrix's scale where X's planes have a static one, else 0
 };
 
@@ -637,7 +637,7 @@ __global__ __launch_bounds__(NT) void ns_reduce_kernel(NsArgs a, NsSeg s) {
 // or two products a launch. Tiles of up to 64 read what is added early, behind the product. m = 256: 5 us
 // (36 tiles of 32), a launch and eight trips to memory in turn; 1001 x 2: 30 us for one product or two (72 or
 // 144 tiles of 128; tiles of 64, 272 or 544, took 24 and 38); 4096: 195 us, 1.21 PFLOP/s.
-enum { NS_A = 0, NS_T, NS_P, NS_Q0, NS_Q1 };
+enum { NS_A = 0, NS_T, NS_P, NS_V, NS_Q0, NS_Q1 };
 struct NsJob {                 // dst = diag I + fa add + f lhs rhs (scales included)
     int lhs, rhs, dst, add;
     float f, fa, diag;
@@ -645,7 +645,7 @@ struct NsJob {                 // dst = diag I + fa add + f lhs rhs (scales incl
 struct NsJobs { int n; NsJob j[2]; };
 
 CB_DEV char* ns_buf(const NsArgs& a, const NsGroup& G, int id, int b) {
-    const int64_t o = id == NS_A ? G.a : id == NS_T ? G.t : id == NS_P ? G.p : id == NS_Q0 ? G.q[0] : G.q[1];
+    const int64_t o = id == NS_A ? G.a : id == NS_T ? G.t : id == NS_P ? G.p : id == NS_V ? G.v : id == NS_Q0 ? G.q[0] : G.q[1];
     return a.ws + o + int64_t(b) * 2 * G.ms;
 }
 
@@ -1285,6 +1285,7 @@ int64_t ns_layout(NsGroup& G, int64_t at, int np0, bool two) {
     G.a = take(big ? mm : 0);
     G.t = take(big ? mm : 0);
     G.p = take(big ? mm : 0);
+    G.v = take(big ? mm : 0);
     return at;
 }
 
@@ -1341,8 +1342,10 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
         g.sp = float(pow2_scale(pmax, 14));
         g.st = float(pow2_scale(tmax, 14));
         g.sq = float(pow2_scale(qmax, 14));
-        g.ss = float(pow2_scale(pmax * pmax, 14));
-        g.sv = g.len < 2 ? 1.f : float(pow2_scale(pmax * (std::fabs(g.c[1][1]) + std::fabs(g.c[1][2]) * amax), 14));
+        double v = 0;
+        for (int t = 1; t < g.len; ++t) v = std::max(v, double(std::fabs(g.c[t][1])) + std::fabs(g.c[t][2]) * amax);
+        g.su = float(pow2_scale(pmax * qmax, 14));
+        g.sv = float(pow2_scale(qmax * v, 14));
         P.xscale[k] = pow2_scale(s, 12);
         g.alpha = k == 0 ? 0.f : float(1.0 / (P.xscale[k - 1] * P.xscale[k - 1]));
     }
@@ -1406,18 +1409,28 @@ int ns_chain(const NsArgs& a, const NsSeg& g, hipStream_t s) {
     };
     // the first P is Q
     run({1, {{NS_A, NS_A, NS_Q0, NS_A, g.sq * g.c[0][2] / (g.sa * g.sa), g.sq * g.c[0][1] / g.sa, g.sq * g.c[0][0]}}});
-    bool wide = true;   // the chip holds two products at once
+    // The chip holds two products at once (m = 256: two cost 5.2 us, one 5.1; at m = 512, 272 tiles, 8.1 and
+    // 6.4, and both ways take the same time).
+    bool wide = true;
     for (int i = 0; i < a.ng; ++i) wide = wide && (a.g[i].small || 2 * int64_t(a.g[i].batch) * a.g[i].tiles <= 256);
-    if (g.len == 2 && wide) {
-        // Two steps in four launches of six products, where the other way takes five of five: with S = P P
-        // and R = P A, the second step's A is A' = R P, and Q = P' P = a P + A' (b P + c A' P), A' P = R S.
-        const float b = g.c[1][1], c = g.c[1][2];
-        run({2, {{NS_Q0, NS_Q0, NS_T, NS_A, g.ss / (g.sq * g.sq), 0.f, 0.f},
-                 {NS_Q0, NS_A, NS_Q1, NS_A, g.st / (g.sq * g.sa), 0.f, 0.f}}});
-        run({2, {{NS_Q1, NS_Q0, NS_A, NS_A, g.sa / (g.st * g.sq), 0.f, 0.f},
-                 {NS_Q1, NS_T, NS_P, NS_Q0, c * g.sv / (g.st * g.ss), b * g.sv / g.sq, 0.f}}});
-        run({1, {{NS_A, NS_P, NS_Q1, NS_Q0, g.sq / (g.sa * g.sv), g.c[1][0], 0.f}}});
-        return 1;
+    if (wide) {
+        // A step more in three launches of two products each, where the other way takes four: with R = P A and
+        // U = P Q the next A is A' = R P, and the next Q = P' Q = a Q + A' (b Q + c A' Q), A' Q = R U; the P'
+        // of a step after that goes with it. What was read last is written next; A' takes A's place.
+        int q = NS_Q0, p = NS_Q0, r = NS_Q1, u = NS_T, v = NS_P;
+        float sp = g.sq;
+        for (int t = 1; t < g.len; ++t) {
+            const float ca = g.c[t][0], cb = g.c[t][1], cc = g.c[t][2];
+            run({2, {{p, q, u, NS_A, g.su / (sp * g.sq), 0.f, 0.f}, {p, NS_A, r, NS_A, g.st / (sp * g.sa), 0.f, 0.f}}});
+            run({2, {{r, p, NS_A, NS_A, g.sa / (g.st * sp), 0.f, 0.f},
+                     {r, u, v, q, cc * g.sv / (g.st * g.su), cb * g.sv / g.sq, 0.f}}});
+            run({t + 1 < g.len ? 2 : 1, {{NS_A, v, r, q, g.sq / (g.sa * g.sv), ca, 0.f},
+                                         {NS_A, NS_A, u, NS_A, g.sp * cc / (g.sa * g.sa), g.sp * cb / g.sa, g.sp * ca}}});
+            const int q0 = q, u0 = v;
+            q = r; p = u; r = q0; u = t == 1 ? u0 : u == NS_T ? NS_P : NS_T; v = NS_V;
+            sp = g.sp;
+        }
+        return q == NS_Q1;
     }
     int q = 0;
     for (int t = 0; t < g.len; ++t) {
