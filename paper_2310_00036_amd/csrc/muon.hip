@@ -29,7 +29,7 @@
 // of muon_orthogonalize do without all that: one launch, a workgroup each (ns_one_kernel).
 //
 // What bounds a call: up to m = 512 or so the latency of its 20 launches, 4 to 8 us each (3872 x 256
-// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 129 us);
+// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 124 us);
 // from there on the tile product (4096 x 4096 bf16 3.55 ms, 390 TFLOP/s of the result's operations,
 // 1.2 PFLOP/s of f16 products where a large library product of f16 matrices reaches 1.49).
 #include "common.h"
@@ -1395,6 +1395,13 @@ void ns_apply(const NsArgs& a, const NsApply& ap, int np, hipStream_t s) {
     const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.ba == BT; },
                                [](const NsGroup& G) { return G.batch * (G.rp / BT) * (G.cp / BT); }, n);
     if (!n) return;
+    if constexpr (BT == 64 && ST > 2)
+        // More tiles than CUs: two stages, so that a CU holds two of them and there is no second round (the base
+        // net's 305: 14 -> 11 us, muon_step 129 -> 124; the 244 of 3872 x 256 take 0.4 us longer with two).
+        if (n > 256) {
+            ns_apply<BT, BK, 2>(a, ap, np, s);
+            return;
+        }
     if (np == 1) NS_TILES((ns_apply_kernel<BT, BK, ST, 1>), n, (ns_lds_bytes<BT, BK, ST, 2, 1>()), r, ap);
     else NS_TILES((ns_apply_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, ap);
 }
