@@ -9,7 +9,7 @@
 // and P A P grows what is small by a^2 a step, the rounding of A along with it. A's error is 2^-24 of
 // its norm, so the next segment starts from a fresh Gram matrix. Five steps on gradient-like matrices
 // (a few strong directions over noise) come out as near the exact result as the steps one by one in
-// float32 do, 1e-6 of their norm, with segments of 2, 2 and 1 steps (kSegF32); with 3 and 2 (kSegBf16)
+// float32 do, 1e-6 to 3e-6 of their norm, with segments of 2, 2 and 1 steps (kSegF32); with 3 and 2 (kSegBf16)
 // they are off by 6e-6, which bf16 results and parameters that move by a few per cent do not see; one
 // segment of 5 is off by 2^-7 for singular values spread over six decades, more than bf16 resolves.
 // On square matrices the operations are the same either way; on 15 : 1 they are 1 : 1.4.
