@@ -173,7 +173,8 @@ impala_status_t impala_groupnorm_fwd(impala_prec_t prec, int64_t n, int32_t H, i
  *   dx = rstd (h - mean_group(h) - xh mean_group(h xh)).
  * dy, x, dx: [n, H, W, C]; dx may be dy itself; any other overlap of dx with dy or x is
  * IMPALA_EINVAL. dgamma, dbeta: float [C], overwritten (zero for n = 0), or NULL where not wanted.
- * ws: impala_groupnorm_bwd_workspace_bytes() bytes. Shapes and alignment as the forward. */
+ * ws: impala_groupnorm_bwd_workspace_bytes() bytes, 16-byte aligned. Shapes and alignment as the
+ * forward. */
 size_t impala_groupnorm_bwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
                                             int32_t groups);
 impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,

@@ -225,7 +225,7 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * sum. IMPALA_PREC_FP32 results differ from the exact ones
  * by about what a float32 evaluation does; IMPALA_PREC_BF16 results by about their own rounding. A
  * zero matrix gives zeros; one with an element that is not finite gives NaN in all of its own.
- * ws: device scratch of muon_orthogonalize_workspace_bytes() bytes. */
+ * ws: device scratch of muon_orthogonalize_workspace_bytes() bytes, 16-byte aligned. */
 size_t muon_orthogonalize_workspace_bytes(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
                                           int32_t steps);
 impala_status_t muon_orthogonalize(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
@@ -262,7 +262,7 @@ typedef struct muon_cfg {
  * covers. params, m, v are updated in place; v is left alone inside the matrices; grads is read
  * only. mats: HOST array of n_mats matrices in any order, disjoint, inside the buffer; at most 512,
  * sides as muon_orthogonalize, their sides rounded up to 192 multiplying to 2^34 in all at most. cfg is HOST memory and, like mats, not kept after the call returns.
- * stats as adam_step. ws: device scratch of muon_workspace_bytes() bytes. */
+ * stats as adam_step. ws: device scratch of muon_workspace_bytes() bytes, 16-byte aligned. */
 size_t muon_workspace_bytes(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
                             const muon_cfg_t* cfg);
 impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
