@@ -215,8 +215,10 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * Muon optimiser). x, y: [batch, rows, cols], row-major, in the storage type (bf16 or float32); y
  * may be x itself, any other overlap is IMPALA_EINVAL.
  * coeffs: HOST float [steps][3], row k = (a_k, b_k, c_k), or NULL for (3.4445, -4.7750, 2.0315) in
- * every step. 1 <= steps <= 16. Coefficients that let a singular value of [0, 1] grow past 2^10, or
- * the product of the steps' polynomials past 10^15, are IMPALA_EUNSUPPORTED.
+ * every step. 1 <= steps <= 16. The steps run in ceil(steps / L) segments of nearly equal length, the
+ * longer ones first, with L = 2 in float32 and 3 in bf16 (five steps: 2, 2, 1 and 3, 2). Coefficients
+ * that let a singular value of [0, 1] grow past 2^10, or the product of the polynomials of a segment's
+ * steps past 10^15, are IMPALA_EUNSUPPORTED, whatever the sides.
  * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included, whose
  * product rounded up to multiples of 192 is <= 2^29; batch <= 2^21, and, but for small matrices that
  * fit one CU, batch times that product <= 2^34 (more: IMPALA_EUNSUPPORTED).

@@ -599,7 +599,7 @@ impala_status_t muon_orthogonalize(impala_prec_t prec, int64_t batch, int32_t ro
     if (!e.empty()) return fail(IMPALA_EINVAL, "muon_orthogonalize: %s", e.c_str());
     if (!(eps >= 0.f)) return fail(IMPALA_EINVAL, "muon_orthogonalize: eps must be >= 0");
     if (!orth_supported(batch, rows, cols)) return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: too large");
-    if (!muon_coeffs_ok(steps, coeffs))
+    if (!muon_coeffs_ok(prec, steps, coeffs))
         return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: the coefficients let singular values grow without bound");
     if (batch == 0) return ok();
     CHECK_PTR(x); CHECK_PTR(y); CHECK_PTR(ws);
@@ -635,7 +635,7 @@ impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n
     const std::string e = check_muon_call(n_params, mats, n_mats, cfg, mv);
     if (!e.empty()) return fail(IMPALA_EINVAL, "muon_step: %s", e.c_str());
     if (step < 1) return fail(IMPALA_EINVAL, "muon_step: step is 1-based (got %d)", step);
-    if (!muon_coeffs_ok(cfg->steps, cfg->coeffs))
+    if (!muon_step_coeffs_ok(cfg->steps, cfg->coeffs))
         return fail(IMPALA_EUNSUPPORTED, "muon_step: the coefficients let singular values grow without bound");
     if (n_params == 0) return ok();
     CHECK_PTR(params); CHECK_PTR(grads); CHECK_PTR(m); CHECK_PTR(v); CHECK_PTR(ws);

@@ -47,6 +47,7 @@ namespace cb {
 namespace {
 
 constexpr int kSegF32 = 2, kSegBf16 = 3, kMaxSegs = kNsMaxSteps / 2;
+constexpr int kSegStep = kSegBf16;   // of muon_step
 constexpr float kNsDefault[3] = {3.4445f, -4.7750f, 2.0315f};
 
 typedef _Float16 ns_f16x8 __attribute__((ext_vector_type(8)));
@@ -1301,8 +1302,10 @@ double pow2_scale(double bound, int most) {   // the largest power of two (at mo
 }
 
 // The segments of `steps` steps and the scales of their matrices, from bounds on the singular values:
-// they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False where they
-// could grow past 2^10 (planes would no longer resolve them).
+// they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False, and P is not to be
+// run, where they could grow past 2^10 (planes would no longer resolve them), or a segment's product of
+// polynomials past 10^15. Which steps share a segment depends on `most`, so what one length accepts another
+// may not.
 bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
     P.nseg = (steps + most - 1) / most;
     double s = 1.0 + 0x1p-10;
@@ -1501,9 +1504,13 @@ int64_t orth_layout(int prec, int64_t batch, int rows, int cols, int steps, NsAr
 
 }  // namespace
 
-bool muon_coeffs_ok(int steps, const float* coeffs) {
-    NsProgram P;
-    return ns_program(steps, coeffs, kSegBf16, P);   // (shorter segments have smaller products)
+bool muon_coeffs_ok(int prec, int steps, const float* coeffs) {
+    NsProgram P{};
+    return ns_program(steps, coeffs, ns_most(prec), P);
+}
+bool muon_step_coeffs_ok(int steps, const float* coeffs) {
+    NsProgram P{};
+    return ns_program(steps, coeffs, kSegStep, P);
 }
 
 bool muon_orth_small(int64_t batch, int rows, int cols) { return ns_one(batch, rows, cols); }
@@ -1529,8 +1536,8 @@ hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x,
     NsArgs a;
     orth_layout(prec, batch, rows, cols, steps, a);
     a.ws = static_cast<char*>(ws);
-    NsProgram P;
-    ns_program(steps, coeffs, ns_most(prec), P);
+    NsProgram P{};
+    if (!ns_program(steps, coeffs, ns_most(prec), P)) return hipErrorInvalidValue;
     const NsGroup& G = a.g[0];
     MuonElem e{};
     const int64_t sums = batch * G.nsum, planes = batch * int64_t(ns_plane_blocks(G));
@@ -1625,7 +1632,7 @@ MuonPlan muon_plan(int64_t n_params, const std::vector<MuonMat>& mats, int steps
         P.a.info = 0;
         P.a.sums = sums;
         int64_t end = base;   // passes follow each other in the same memory
-        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSegBf16);
+        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSegStep);
         plan.total = std::max(plan.total, end);
         P.e.nblocks = plan.nblocks;
     }
@@ -1641,8 +1648,8 @@ size_t muon_step_ws_bytes(int64_t n_params, const std::vector<MuonMat>& mats, in
 hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void* ws, hipStream_t s) {
     if (m.n <= 0) return hipSuccess;
     MuonPlan plan = muon_plan(m.n, mats, m.steps, m.scale_mode);
-    NsProgram P;
-    ns_program(m.steps, m.coeffs, kSegBf16, P);
+    NsProgram P{};
+    if (!ns_program(m.steps, m.coeffs, kSegStep, P)) return hipErrorInvalidValue;
     ProfScope ps(s, [&] { return "muon/" + std::to_string(m.n); });
     for (MuonPlan::Pass& p : plan.pass) {
         p.a.ws = static_cast<char*>(ws);
