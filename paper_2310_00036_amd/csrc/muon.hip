@@ -1304,7 +1304,7 @@ double pow2_scale(double bound, int most) {   // the largest power of two (at mo
 // The segments of `steps` steps and the scales of their matrices, from bounds on the singular values:
 // they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False, and P is not to be
 // run, where they could grow past 2^10 (planes would no longer resolve them), or a segment's product of
-// polynomials past 10^15. Which steps share a segment depends on `most`, so what one length accepts another
+// polynomials past 10^15, or where they shrink what the planes hold too far. Which steps share a segment depends on `most`, so what one length accepts another
 // may not.
 bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
     P.nseg = (steps + most - 1) / most;
@@ -1315,6 +1315,8 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
         std::memset(&g, 0, sizeof(g));
         g.len = (steps - at + P.nseg - k - 1) / (P.nseg - k);
         double amax = s * s, pmax = 0, tmax = 0, q = 1, qmax = 0;
+        double av[kSegBf16], pv[kSegBf16], qv[kSegBf16];   // each step's bounds on A, P and Q
+        const int first = at;
         for (int t = 0; t < g.len; ++t, ++at) {
             const float* c = coeffs ? coeffs + 3 * at : kNsDefault;
             const double a = c[0], b = c[1], cc = c[2], lam = s * s;
@@ -1336,6 +1338,7 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
                 extremum(-a / (3 * b));
             }
             q *= p;
+            av[at - first] = lam; pv[at - first] = p; qv[at - first] = q;
             pmax = std::max(pmax, p); qmax = std::max(qmax, q); tmax = std::max(tmax, lam * p);
             s = ns * (1 + 0x1p-10);
             if (!(s <= 1024.0) || !(qmax <= 1e15)) return false;
@@ -1350,6 +1353,17 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
         g.su = float(pow2_scale(pmax * qmax, 14));
         g.sv = float(pow2_scale(qmax * v, 14));
         P.xscale[k] = pow2_scale(s, 12);
+        // Planes hold 22 bits of what is 2^-3 or more under its scale (f16's smallest step is 2^-24). Every
+        // matrix of the segment has one scale for all steps, so a step that shrinks it too far is refused; of V
+        // = b Q + c A' Q it is what A' V adds to the next Q that counts.
+        auto held = [](double bound, double scale) { return bound == 0 || bound * scale >= 0x1p-3; };
+        for (int t = 0; t < g.len; ++t) {
+            const bool more = t + 1 < g.len;
+            if (!held(av[t], g.sa) || !held(pv[t], g.sp) || !held(qv[t], g.sq) || (t > 0 && !held(qv[t], g.sv / amax)) ||
+                (more && (!held(av[t] * pv[t], g.st) || !held(pv[t] * qv[t], g.su))))
+                return false;
+        }
+        if (at < steps && !held(s, P.xscale[k])) return false;
         g.alpha = k == 0 ? 0.f : float(1.0 / (P.xscale[k - 1] * P.xscale[k - 1]));
     }
     return true;

@@ -41,3 +41,18 @@ def test_accepted_coefficients_stay_accepted():
                    [(2.0, 0.0, 0.0)], [(1.0, 0.0, 0.0)] * 16):
             assert _orth(prec, co) == EWORKSPACE, co
             assert _step(co) == EWORKSPACE, co
+
+
+def test_coefficients_that_shrink_a_matrix_below_what_its_planes_hold():
+    """The first two steps of a segment multiply by 10^-8 each, the third by 9 x 10^14: under the scale of the third's
+    polynomial, 2^-35, the second's is 0 in f16, and so would be the result, whose exact value is 0.09 X."""
+    one = (1.0, 0.0, 0.0)
+    for co in ([SMALL, SMALL, LARGE], [SMALL, SMALL, LARGE, (100.0, 0.0, 0.0), one], [SMALL, one], [one, SMALL, one, one]):
+        assert _orth(P.PREC_BF16, co) == EUNSUPPORTED, co
+        assert _orth(P.PREC_FP32, co) == EUNSUPPORTED, co
+        assert _step(co) == EUNSUPPORTED, co
+    tenth = (0.1, 0.0, 0.0)
+    for co in ([tenth] * 2, [tenth] * 3, [(0.0, 1.0, 0.0)], [(0.0, 0.0, 0.0)], [one, (0.0, 0.0, 0.0)],
+               [(3.0, 1e-9, 0.0)] * 2, [(8.287, -23.596, 17.301), (4.107, -2.948, 0.545)]):
+        for prec in (P.PREC_FP32, P.PREC_BF16):
+            assert _orth(prec, co) == EWORKSPACE, co
