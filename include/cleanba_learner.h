@@ -261,7 +261,8 @@ typedef struct muon_cfg {
 
 /* Global-norm clip over all of grads (as adam_step), then for each matrix
  *   m <- momentum m + (1 - momentum) g;  u = momentum m + (1 - momentum) g if nesterov, else m;
- *   p <- p (1 - lr weight_decay) - lr scale O(u),  O as muon_orthogonalize in float32,
+ *   p <- p (1 - lr weight_decay) - lr scale O(u),  O to muon_orthogonalize's float32 precision (not
+ *   bit for bit: it takes small matrices another way),
  * and one Adam step (step 1-based, adam_lr, no weight decay) on every parameter that no matrix
  * covers. params, m, v are updated in place; v is left alone inside the matrices; grads is read
  * only. mats: HOST array of n_mats matrices in any order, disjoint, inside the buffer; at most 512,

@@ -635,7 +635,7 @@ impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n
     const std::string e = check_muon_call(n_params, mats, n_mats, cfg, mv);
     if (!e.empty()) return fail(IMPALA_EINVAL, "muon_step: %s", e.c_str());
     if (step < 1) return fail(IMPALA_EINVAL, "muon_step: step is 1-based (got %d)", step);
-    if (!muon_step_coeffs_ok(cfg->steps, cfg->coeffs))
+    if (!muon_coeffs_ok(FP32, cfg->steps, cfg->coeffs))
         return fail(IMPALA_EUNSUPPORTED, "muon_step: the coefficients let singular values grow without bound");
     if (n_params == 0) return ok();
     CHECK_PTR(params); CHECK_PTR(grads); CHECK_PTR(m); CHECK_PTR(v); CHECK_PTR(ws);

@@ -307,9 +307,8 @@ hipError_t clip_opt_step(int opt, const OptArgs& a, float* stats, float* partial
 
 // ---- orthogonalised updates (Newton-Schulz products) and the Muon step
 // steps in [1, 16]; coeffs: host [steps][3] or NULL (the default quintic in every step)
-// Whether singular values and the products of a segment's polynomials stay bounded: muon_orth, muon_update.
+// Whether singular values and the products of a segment's polynomials stay bounded (muon_update: as float32).
 bool muon_coeffs_ok(int prec, int steps, const float* coeffs);
-bool muon_step_coeffs_ok(int steps, const float* coeffs);
 bool muon_orth_small(int64_t batch, int rows, int cols);   // one launch, no workspace
 size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps);
 hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,

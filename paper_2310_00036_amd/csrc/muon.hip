@@ -8,10 +8,11 @@
 // L (3 m^2 n + m^3) for the steps one by one. What bounds L is rounding: A squares the singular values
 // and P A P grows what is small by a^2 a step, the rounding of A along with it. A's error is 2^-24 of
 // its norm, so the next segment starts from a fresh Gram matrix. Five steps on gradient-like matrices
-// (a few strong directions over noise) come out as near the exact result as the steps one by one in
-// float32 do, 1e-6 to 3e-6 of their norm, with segments of 2, 2 and 1 steps (kSegF32); with 3 and 2 (kSegBf16)
-// they are off by 6e-6, which bf16 results and parameters that move by a few per cent do not see; one
-// segment of 5 is off by 2^-7 for singular values spread over six decades, more than bf16 resolves.
+// (a few strong directions over noise) are off by 0.7e-6 to 3.5e-6 of their norm with segments of 2, 2 and 1
+// steps (kSegF32: float32 matrices and muon_step), where the steps one by one in float32 are by 1e-6 to 2e-6
+// (at most 2.4 times theirs on one matrix). With 3 and 2 (kSegBf16) they are off by 2e-6 to 14e-6, which bf16
+// results, at 1.7e-3 from their own rounding, do not see; one segment of 5 is off by 2^-7 for singular values
+// spread over six decades, more than bf16 resolves.
 // On square matrices the operations are the same either way; on 15 : 1 they are 1 : 1.4.
 //
 // Every matrix is held as two f16 planes, v = hi + lo with lo = f16(v - hi): 22 bits and more under a
@@ -47,7 +48,6 @@ namespace cb {
 namespace {
 
 constexpr int kSegF32 = 2, kSegBf16 = 3, kMaxSegs = kNsMaxSteps / 2;
-constexpr int kSegStep = kSegBf16;   // of muon_step
 constexpr float kNsDefault[3] = {3.4445f, -4.7750f, 2.0315f};
 
 typedef _Float16 ns_f16x8 __attribute__((ext_vector_type(8)));
@@ -1522,10 +1522,6 @@ bool muon_coeffs_ok(int prec, int steps, const float* coeffs) {
     NsProgram P{};
     return ns_program(steps, coeffs, ns_most(prec), P);
 }
-bool muon_step_coeffs_ok(int steps, const float* coeffs) {
-    NsProgram P{};
-    return ns_program(steps, coeffs, kSegStep, P);
-}
 
 bool muon_orth_small(int64_t batch, int rows, int cols) { return ns_one(batch, rows, cols); }
 
@@ -1646,7 +1642,7 @@ MuonPlan muon_plan(int64_t n_params, const std::vector<MuonMat>& mats, int steps
         P.a.info = 0;
         P.a.sums = sums;
         int64_t end = base;   // passes follow each other in the same memory
-        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSegStep);
+        for (int g = 0; g < P.a.ng; ++g) end = ns_layout(P.a.g[g], end, 2, steps > kSegF32);
         plan.total = std::max(plan.total, end);
         P.e.nblocks = plan.nblocks;
     }
@@ -1663,7 +1659,7 @@ hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void
     if (m.n <= 0) return hipSuccess;
     MuonPlan plan = muon_plan(m.n, mats, m.steps, m.scale_mode);
     NsProgram P{};
-    if (!ns_program(m.steps, m.coeffs, kSegStep, P)) return hipErrorInvalidValue;
+    if (!ns_program(m.steps, m.coeffs, kSegF32, P)) return hipErrorInvalidValue;
     ProfScope ps(s, [&] { return "muon/" + std::to_string(m.n); });
     for (MuonPlan::Pass& p : plan.pass) {
         p.a.ws = static_cast<char*>(ws);
