@@ -155,7 +155,8 @@ impala_status_t impala_maxpool_bwd(impala_prec_t prec, int64_t n, int32_t H, int
  * the backward pass reads, or NULL where none follows. y may be x itself; any other overlap of the
  * two is IMPALA_EINVAL. eps >= 0. 1 <= C <= 1024 with groups dividing C, H * W <= 2^24, any of them
  * odd; addresses aligned to an element (16-byte aligned ones, with C a multiple of 8 in bf16 or 4 in
- * float32, are read 16 bytes at a time). ws: device scratch of
+ * float32, are read 16 bytes at a time). Calls of more elements than a launch holds (about 2^35, fewer
+ * where C is not near a power of two or frames are small) are IMPALA_EUNSUPPORTED. ws: device scratch of
  * impala_groupnorm_fwd_workspace_bytes() bytes (0 where a frame fits one workgroup: ws may then be
  * NULL). */
 typedef enum { IMPALA_ACT_NONE = 0, IMPALA_ACT_RELU = 1, IMPALA_ACT_SILU = 2 } impala_act_t;

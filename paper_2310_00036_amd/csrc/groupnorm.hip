@@ -703,7 +703,7 @@ std::string gn_key(const char* name, int prec, int H, int W, int C) {
 
 int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G) {
     const GnPlan p = gn_plan(prec, n, H, W, C, G, 0, 0, nullptr);   // one-channel columns: the most chunks
-    return n * std::max(256, p.chunks * kGnShapes[p.shape].nt);
+    return n * std::max<int64_t>(256, int64_t(p.chunks) * kGnShapes[p.shape].nt);
 }
 
 size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd) {

@@ -187,7 +187,7 @@ struct GnArgs {
     float* part; float* fsum; float* smean; float* srstd;
 };
 size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd);
-int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G);   // workgroups at most
+int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G);   // of a launch, at most
 hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t s);
 // n == 0: dgamma and dbeta are cleared. Either may be NULL.
 hipError_t groupnorm_bwd(int prec, int H, int W, GnArgs a, float* dgamma, float* dbeta, void* ws, hipStream_t s);
