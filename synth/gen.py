@@ -52,9 +52,16 @@ class Workload:
     beta2: float = 0.999
     adam_eps: float = 1e-5
     max_grad_norm: float = 0.5
-    optimizer: str = "adam"      # "adam" | "rmsprop"
+    optimizer: str = "adam"      # "adam" | "rmsprop" | "muon"
     rms_decay: float = 0.99
     rms_eps: float = 0.01
+    muon_lr: float = 0.02        # "muon": the weight matrices; lr, beta1, beta2, adam_eps for the rest
+    muon_momentum: float = 0.95
+    muon_weight_decay: float = 0.0
+    muon_eps: float = 1e-7
+    muon_nesterov: int = 1
+    muon_steps: int = 5
+    muon_scale: int = 0          # 0: sqrt(max(1, cols / rows)); 1: 0.2 sqrt(max(rows, cols))
     norm_adv: int = 1
     reward_probs: tuple = (0.05, 0.9, 0.05)   # P(r=-1), P(r=0), P(r=+1)
     done_prob: float = 0.02
