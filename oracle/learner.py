@@ -12,12 +12,32 @@ import numpy as np
 from . import losses, net as netmod, optim, targets
 
 
-def _opt_update(params, g, m, v, step, cfg, dtype):
-    """Clip the gradient's global norm, then the configured optimiser: Adam (m, v) or
-    RMSprop (v holds its second-moment estimate; m passes through)."""
+def weight_matrices(net):
+    """(offset, rows, cols) of the conv kernels, [9 cin, cout], and of the dense layer's weights: what Muon
+    orthogonalises. The heads and the biases are left to its Adam."""
+    out = []
+    for name, shape, off in netmod.param_layout(net):
+        if len(shape) == 4:
+            out.append((off, shape[0] * shape[1] * shape[2], shape[3]))
+        elif name == "dense.w":
+            out.append((off, *shape))
+    return out
+
+
+def _opt_update(net, params, g, m, v, step, cfg, dtype):
+    """Clip the gradient's global norm, then the configured optimiser: Adam (m, v), RMSprop (v holds its
+    second-moment estimate; m passes through) or Muon."""
     g, gnorm = optim.clip_by_global_norm(g, cfg.max_grad_norm, dtype)
-    if getattr(cfg, "optimizer", "adam") == "rmsprop":
+    opt = getattr(cfg, "optimizer", "adam")
+    if opt not in ("adam", "rmsprop", "muon"):
+        raise ValueError(f"unknown optimizer {opt!r}")
+    if opt == "rmsprop":
         p, v = optim.rmsprop(params, g, v, cfg.lr, cfg.rms_decay, cfg.rms_eps, dtype)
+        return p, m, v, gnorm
+    if opt == "muon":
+        p, m, v = optim.muon(params, g, m, v, step, weight_matrices(net), cfg.muon_lr, cfg.muon_momentum,
+                             cfg.muon_weight_decay, bool(cfg.muon_nesterov), cfg.muon_steps, cfg.muon_scale, cfg.muon_eps,
+                             cfg.lr, cfg.beta1, cfg.beta2, cfg.adam_eps, dtype)
         return p, m, v, gnorm
     p, m, v = optim.adam(params, g, m, v, step, cfg.lr, cfg.beta1, cfg.beta2, cfg.adam_eps, dtype)
     return p, m, v, gnorm
@@ -48,7 +68,7 @@ def ppo_learner_step(net, cfg, ro, params, m, v, step, perm, prec="fp64"):
                                                  cfg.ent_coef, bool(cfg.norm_adv), dtype=dtype)
             g = netmod.backward(net, cache, dz, dv)
             step += 1
-            p, m_, v_, gn = _opt_update(p, g, m_, v_, step, cfg, dtype)
+            p, m_, v_, gn = _opt_update(net, p, g, m_, v_, step, cfg, dtype)
             out.append(list(st[:6]) + [gn, float(not np.isfinite(gn))])
     return p, m_, v_, step, np.array(out)
 
@@ -90,7 +110,7 @@ def impala_learner_step(net, cfg, ro, params, m, v, step, prec="fp64"):
         dv_all[:n] = dv
         g = netmod.backward(net, cache, dz_all, dv_all)
         step += 1
-        p, m_, v_, gn = _opt_update(p, g, m_, v_, step, cfg, dtype)
+        p, m_, v_, gn = _opt_update(net, p, g, m_, v_, step, cfg, dtype)
         out.append(list(st[:6]) + [gn, float(not np.isfinite(gn))])
     return p, m_, v_, step, np.array(out)
 

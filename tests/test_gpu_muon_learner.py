@@ -66,3 +66,41 @@ def test_pipeline_trains_at_the_workloads_hyperparameters():
     assert rec.rollouts == ref.rollouts and torch.equal(p, p_ref) and np.isfinite(np.concatenate(rec.stats)).all()
     other = wl.replace(muon_lr=0.02)
     assert not torch.equal(PL.run_sequential(agent(other), other, 4, seed=9)[0], p_ref)
+
+
+@pytest.mark.parametrize("kw", [dict(optimizer="muon"), OWN], ids=["defaults", "own"])
+def test_learner_step_against_the_oracle(kw):
+    """One float32 update on certified frames. The momentum against the oracle's at its gradient's tolerance; the
+    parameters against the oracle's update from the learner's own gradient (an orthogonalisation turns a gradient's
+    rounding into up to 485 times as much where singular values are small, and a few frames' gradient has many of
+    those). Per matrix the update is off by the iteration's 2^-14 and the parameters' rounding."""
+    from oracle import learner as olearner, optim
+    from tests.test_gpu_network import FP32_TOL, _certified_rollout, _learner_gpu, _oracle_learner
+    wl = Workload("muon_certified", "ppo", T=2, E=1, net=NetShape(num_actions=6), max_grad_norm=0.0).replace(**kw)
+    params = draw_params(wl.net, 5)
+    wl, raw, ro = _certified_rollout(wl, params)
+    want, _ = _oracle_learner(wl, params, ro, raw["perm"], G.FP32)
+    got = _learner_gpu(wl, G.FP32, params, ro, raw["perm"])
+    p, m, v = (G.host(t) for t in got[:3])
+    assert G.rel_l2(m, want[1]) <= FP32_TOL and G.rel_l2(v, want[2]) <= 2 * FP32_TOL
+    f32 = lambda a: np.float64(np.float32(a))  # noqa: E731
+    mats = olearner.weight_matrices(wl.net)
+    g = m / (1 - f32(wl.beta1))
+    for off, r, c in mats:
+        g[off:off + r * c] = m[off:off + r * c] / (1 - f32(wl.muon_momentum))
+    p0 = params.astype(np.float64)
+    zero = np.zeros_like(p0)
+    pw, _, _ = optim.muon(p0, g, zero, zero, 1, mats, f32(wl.muon_lr), f32(wl.muon_momentum), f32(wl.muon_weight_decay),
+                          bool(wl.muon_nesterov), wl.muon_steps, wl.muon_scale, f32(wl.muon_eps), f32(wl.lr), f32(wl.beta1),
+                          f32(wl.beta2), f32(wl.adam_eps))
+    for off, r, c in mats:
+        at = slice(off, off + r * c)
+        bound = 2.0 ** -14 * np.linalg.norm(pw[at] - p0[at] * (1 - f32(wl.muon_lr) * f32(wl.muon_weight_decay))) \
+            + 2.0 ** -22 * np.linalg.norm(p0[at])
+        err = np.linalg.norm(p[at] - pw[at])
+        print((r, c), "error %.2e of a bound of %.2e" % (err, bound))
+        assert err <= bound, (off, r, c, err, bound)
+    rest = np.ones(p0.size, bool)
+    for off, r, c in mats:
+        rest[off:off + r * c] = False
+    assert G.rel_l2((p - p0)[rest], (pw - p0)[rest]) <= 1e-4
