@@ -157,8 +157,9 @@ impala_status_t impala_maxpool_bwd(impala_prec_t prec, int64_t n, int32_t H, int
  * odd; addresses aligned to an element (16-byte aligned ones, with C a multiple of 8 in bf16 or 4 in
  * float32, are read 16 bytes at a time). Calls of more elements than a launch holds (about 2^35, fewer
  * where C is not near a power of two or frames are small) are IMPALA_EUNSUPPORTED. ws: device scratch of
- * impala_groupnorm_fwd_workspace_bytes() bytes (0 where a frame fits one workgroup: ws may then be
- * NULL). */
+ * impala_groupnorm_fwd_workspace_bytes() bytes, which is enough for any addresses. Where a frame fits
+ * one workgroup none is used and ws may be NULL: H W c <= 8192, with c a pixel's columns (of 16 bytes
+ * where they are read so, else of one channel) rounded up to a power of two. */
 typedef enum { IMPALA_ACT_NONE = 0, IMPALA_ACT_RELU = 1, IMPALA_ACT_SILU = 2 } impala_act_t;
 size_t impala_groupnorm_fwd_workspace_bytes(impala_prec_t prec, int64_t n, int32_t H, int32_t W, int32_t C,
                                             int32_t groups);

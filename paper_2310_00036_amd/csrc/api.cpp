@@ -1040,7 +1040,7 @@ impala_status_t impala_groupnorm_fwd(impala_prec_t prec, int64_t n, int32_t H, i
     CHECK_PTR(x); CHECK_PTR(y);
     const size_t bytes = size_t(n) * H * W * C * (prec == IMPALA_PREC_BF16 ? 2 : 4);
     if (partial_overlap(x, y, bytes)) return fail(IMPALA_EINVAL, "impala_groupnorm_fwd: x and y overlap");
-    const size_t need = groupnorm_ws_bytes(prec, n, H, W, C, groups, 0);
+    const size_t need = groupnorm_fwd_whole(prec, n, H, W, C, groups, x, y) ? 0 : groupnorm_ws_bytes(prec, n, H, W, C, groups, 0);
     if (need > 0) CHECK_PTR(ws);
     if (ws_bytes < need)
         return fail(IMPALA_EWORKSPACE, "impala_groupnorm_fwd: workspace %zu < %zu bytes", ws_bytes, need);

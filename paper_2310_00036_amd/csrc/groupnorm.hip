@@ -711,6 +711,10 @@ size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int b
     return C % (prec == BF16 ? 8 : 4) ? a : std::max(a, gn_plan(prec, n, H, W, C, G, bwd, 1, nullptr).total);
 }
 
+bool groupnorm_fwd_whole(int prec, int64_t n, int H, int W, int C, int G, const void* x, const void* y) {
+    return gn_plan(prec, n, H, W, C, G, 0, gn_vec_ok(prec, C, {x, y}), nullptr).whole;
+}
+
 hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t s) {
     const GnPlan p = gn_plan(prec, a.n, H, W, a.C, a.G, 0, gn_vec_ok(prec, a.C, {a.x, a.y}), &a);
     char* w = static_cast<char*>(ws);

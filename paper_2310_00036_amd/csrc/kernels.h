@@ -186,7 +186,9 @@ struct GnArgs {
     int cv, cvp, cvs, crows, chunks;
     float* part; float* fsum; float* smean; float* srstd;
 };
-size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd);
+size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd);   // at any alignment
+// Whether a forward on these addresses takes a frame a workgroup, and so no workspace.
+bool groupnorm_fwd_whole(int prec, int64_t n, int H, int W, int C, int G, const void* x, const void* y);
 int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G);   // of a launch, at most
 hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t s);
 // n == 0: dgamma and dbeta are cleared. Either may be NULL.
