@@ -266,8 +266,10 @@ typedef struct muon_cfg {
  * and one Adam step (step 1-based, adam_lr, no weight decay) on every parameter that no matrix
  * covers. params, m, v are updated in place; v is left alone inside the matrices; grads is read
  * only. mats: HOST array of n_mats matrices in any order, disjoint, inside the buffer; at most 512,
- * sides as muon_orthogonalize, their sides rounded up to 192 multiplying to 2^34 in all at most. cfg is HOST memory and, like mats, not kept after the call returns.
- * stats as adam_step. ws: device scratch of muon_workspace_bytes() bytes, 16-byte aligned. */
+ * sides as muon_orthogonalize, their sides rounded up to 192 multiplying to 2^34 in all at most (other
+ * sides are IMPALA_EINVAL here, like matrices that do not lie in the buffer). Coefficients are read in
+ * muon_orthogonalize's float32 segments, and refused as there by both calls. cfg is HOST memory and,
+ * like mats, not kept after the call returns. stats as adam_step. ws: device scratch of muon_workspace_bytes() bytes, 16-byte aligned. */
 size_t muon_workspace_bytes(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,
                             const muon_cfg_t* cfg);
 impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n_mats,

@@ -568,6 +568,8 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
     return hip_status(clip_opt_step(OPT_RMSPROP, a, stats, static_cast<float*>(ws), stream), "rmsprop_step");
 }
 
+static const char kMuonGrow[] = "the coefficients let singular values grow without bound, or shrink them too far";
+
 static std::string check_orth(int prec, int64_t batch, int rows, int cols, int steps) {
     if (!valid_prec(prec)) return "bad prec";
     if (batch < 0 || rows < 1 || cols < 1) return "batch >= 0 and sides >= 1";
@@ -600,7 +602,7 @@ impala_status_t muon_orthogonalize(impala_prec_t prec, int64_t batch, int32_t ro
     if (!(eps >= 0.f)) return fail(IMPALA_EINVAL, "muon_orthogonalize: eps must be >= 0");
     if (!orth_supported(batch, rows, cols)) return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: too large");
     if (!muon_coeffs_ok(prec, steps, coeffs))
-        return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: the coefficients let singular values grow without bound");
+        return fail(IMPALA_EUNSUPPORTED, "muon_orthogonalize: %s", kMuonGrow);
     if (batch == 0) return ok();
     CHECK_PTR(x); CHECK_PTR(y); CHECK_PTR(ws);
     if (partial_overlap(x, y, size_t(batch) * rows * cols * (prec == IMPALA_PREC_BF16 ? 2 : 4)))
@@ -624,6 +626,10 @@ size_t muon_workspace_bytes(int64_t n_params, const muon_matrix_t* mats, int32_t
     std::vector<MuonMat> v;
     const std::string e = check_muon_call(n_params, mats, n_mats, cfg, v);
     if (!e.empty()) { fail(IMPALA_EINVAL, "muon_workspace_bytes: %s", e.c_str()); return 0; }
+    if (!muon_coeffs_ok(FP32, cfg->steps, cfg->coeffs)) {
+        fail(IMPALA_EUNSUPPORTED, "muon_workspace_bytes: %s", kMuonGrow);
+        return 0;
+    }
     ok();
     return muon_step_ws_bytes(n_params, v, cfg->steps);
 }
@@ -636,7 +642,7 @@ impala_status_t muon_step(int64_t n_params, const muon_matrix_t* mats, int32_t n
     if (!e.empty()) return fail(IMPALA_EINVAL, "muon_step: %s", e.c_str());
     if (step < 1) return fail(IMPALA_EINVAL, "muon_step: step is 1-based (got %d)", step);
     if (!muon_coeffs_ok(FP32, cfg->steps, cfg->coeffs))
-        return fail(IMPALA_EUNSUPPORTED, "muon_step: the coefficients let singular values grow without bound");
+        return fail(IMPALA_EUNSUPPORTED, "muon_step: %s", kMuonGrow);
     if (n_params == 0) return ok();
     CHECK_PTR(params); CHECK_PTR(grads); CHECK_PTR(m); CHECK_PTR(v); CHECK_PTR(ws);
     const size_t need = muon_step_ws_bytes(n_params, mv, cfg->steps);

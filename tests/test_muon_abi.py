@@ -56,3 +56,12 @@ def test_coefficients_that_shrink_a_matrix_below_what_its_planes_hold():
                [(3.0, 1e-9, 0.0)] * 2, [(8.287, -23.596, 17.301), (4.107, -2.948, 0.545)]):
         for prec in (P.PREC_FP32, P.PREC_BF16):
             assert _orth(prec, co) == EWORKSPACE, co
+
+
+def test_the_workspace_query_refuses_the_coefficients_that_the_step_refuses():
+    mats = P.muon_matrices([(0, 200, 100)])
+    for co in ([(9.0, 9.0, 9.0)] * 5, [SMALL, SMALL, LARGE, (100.0, 0.0, 0.0), (1.0, 0.0, 0.0)]):
+        assert _step(co) == EUNSUPPORTED
+        assert P.muon_workspace_bytes(20000, mats, P.muon_cfg(lr=0.02, steps=5, coeffs=co)) == 0, co
+        assert b"grow" in P.lib.impala_last_error()
+    assert P.muon_workspace_bytes(20000, mats, P.muon_cfg(lr=0.02, steps=1, coeffs=[(1.5, -0.5, 0.0)])) > 0
