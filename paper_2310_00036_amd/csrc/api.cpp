@@ -12,7 +12,9 @@
 #include "../../include/cleanba_layers.h"
 #include "../../include/cleanba_learner.h"
 #include "../../include/cleanba_profile.h"
+#include "groupnorm.h"
 #include "kernels.h"
+#include "muon.h"
 #include "plan.h"
 
 using namespace cb;

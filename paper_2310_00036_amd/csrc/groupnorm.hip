@@ -29,6 +29,7 @@
 // allow it) for all its pixels; columns are padded to a power of two per pixel so that the threads of
 // a wave that share a column are found by their lane's high bits.
 #include "common.h"
+#include "groupnorm.h"
 #include "kernels.h"
 
 #include <algorithm>

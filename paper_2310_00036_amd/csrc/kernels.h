@@ -5,8 +5,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <vector>
-
 #include "prof.h"
 
 namespace cb {
@@ -171,29 +169,6 @@ hipError_t maxpool_fwd(int prec, int n, int H, int W, int C, const void* x, void
 hipError_t maxpool_bwd(int prec, int n, int H, int W, int C, const uint8_t* arg, const void* dy,
                        void* dx, hipStream_t s);
 
-// ---- group norm with an activation, channels last; x, y, dy [n, HW, C] in the storage type
-constexpr int kGnMaxC = 1024;
-struct GnArgs {
-    const void* x; const void* dy; void* y;        // backward: y is dx
-    const float* gamma; const float* beta;         // [C] or NULL (1, 0)
-    float* mean; float* rstd;                      // [n, G]; forward: may be NULL
-    float eps;
-    int act;                                       // 0 none, 1 relu, 2 silu
-    int64_t n;
-    int HW, C, G, cg;                              // cg = C / G channels per group
-    // filled by the launcher: columns of V channels per pixel, padded to cvp = 2^cvs; pixels and
-    // number of a frame's chunks; workspace
-    int cv, cvp, cvs, crows, chunks;
-    float* part; float* fsum; float* smean; float* srstd;
-};
-size_t groupnorm_ws_bytes(int prec, int64_t n, int H, int W, int C, int G, int bwd);   // at any alignment
-// Whether a forward on these addresses takes a frame a workgroup, and so no workspace.
-bool groupnorm_fwd_whole(int prec, int64_t n, int H, int W, int C, int G, const void* x, const void* y);
-int64_t groupnorm_threads(int prec, int64_t n, int H, int W, int C, int G);   // of a launch, at most
-hipError_t groupnorm_fwd(int prec, int H, int W, GnArgs a, void* ws, hipStream_t s);
-// n == 0: dgamma and dbeta are cleared. Either may be NULL.
-hipError_t groupnorm_bwd(int prec, int H, int W, GnArgs a, float* dgamma, float* dbeta, void* ws, hipStream_t s);
-
 // ---- GEMM D[m][n] = sum_k A(m,k) B(k,n) on MFMA, output out[n*ld + m]
 struct GemmArgs {
     const void* a; int a_f32; int a_kcontig; int64_t lda;   // A(m,k) = a[m*lda+k] or a[k*lda+m]
@@ -306,30 +281,6 @@ struct OptArgs {
 };
 // Global-norm clip then one optimiser step; stats [2] = [pre-clip norm, nonfinite] or NULL.
 hipError_t clip_opt_step(int opt, const OptArgs& a, float* stats, float* partial, hipStream_t s);
-
-// ---- orthogonalised updates (Newton-Schulz products) and the Muon step
-// steps in [1, 16]; coeffs: host [steps][3] or NULL (the default quintic in every step)
-// Whether singular values and the products of a segment's polynomials stay bounded (muon_update: as float32).
-bool muon_coeffs_ok(int prec, int steps, const float* coeffs);
-bool muon_orth_small(int64_t batch, int rows, int cols);   // one launch, no workspace
-size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps);
-hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,
-                     float eps, void* y, void* ws, hipStream_t s);
-struct MuonMat { int64_t offset; int rows, cols; };   // a matrix of the flat buffer
-struct MuonStep {
-    int64_t n;
-    OptArgs adam;             // buffers, the clip, Adam's constants for what no matrix covers, the mirror
-    float lr, decay;          // p <- decay p - lr scale O
-    float momentum, omu;      // momentum, 1 - momentum (formed in double)
-    int nesterov, steps, scale_mode;
-    float eps;
-    const float* coeffs;
-    float* stats;
-};
-size_t muon_step_ws_bytes(int64_t n_params, const std::vector<MuonMat>& mats, int steps);
-// mats sorted by offset, disjoint.
-hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void* ws, hipStream_t s);
-
 // Largest dynamic LDS allocation per workgroup on the current device (bytes).
 size_t lds_limit();
 // Compute units of the current device.

@@ -4,7 +4,34 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <vector>
+
+#include "kernels.h"
+
 namespace cb {
+
+// Orthogonalised updates (Newton-Schulz products) and the Muon step:
+// steps in [1, 16]; coeffs: host [steps][3] or NULL (the default quintic in every step)
+// Whether singular values and the products of a segment's polynomials stay bounded (muon_update: as float32).
+bool muon_coeffs_ok(int prec, int steps, const float* coeffs);
+bool muon_orth_small(int64_t batch, int rows, int cols);   // one launch, no workspace
+size_t muon_orth_ws_bytes(int prec, int64_t batch, int rows, int cols, int steps);
+hipError_t muon_orth(int prec, int64_t batch, int rows, int cols, const void* x, int steps, const float* coeffs,
+                     float eps, void* y, void* ws, hipStream_t s);
+struct MuonMat { int64_t offset; int rows, cols; };   // a matrix of the flat buffer
+struct MuonStep {
+    int64_t n;
+    OptArgs adam;             // buffers, the clip, Adam's constants for what no matrix covers, the mirror
+    float lr, decay;          // p <- decay p - lr scale O
+    float momentum, omu;      // momentum, 1 - momentum (formed in double)
+    int nesterov, steps, scale_mode;
+    float eps;
+    const float* coeffs;
+    float* stats;
+};
+size_t muon_step_ws_bytes(int64_t n_params, const std::vector<MuonMat>& mats, int steps);
+// mats sorted by offset, disjoint.
+hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void* ws, hipStream_t s);
 
 constexpr int kNsGroups = 8;       // shapes per pass
 constexpr int kNsMats = 64;        // matrices with offsets of their own per pass
