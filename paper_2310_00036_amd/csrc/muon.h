@@ -61,7 +61,6 @@ struct NsArgs {
 };
 
 struct MuonElem {                     // the elementwise part of muon_step
-    int64_t n_params;
     float* p; const float* g; float* m; float* v;
     float mu, omu, c1, c2;            // momentum, 1 - momentum; u = c1 s g + c2 m
     int nesterov;

@@ -18,8 +18,10 @@
 // Every matrix is held as two f16 planes, v = hi + lo with lo = f16(v - hi): 22 bits and more under a
 // power-of-two scale that keeps values in f16's normal range (at least 2^-40 of a matrix's bound is
 // resolved). A product is hi hi + hi lo + lo hi in f16 MFMAs with float32 accumulation, at a third of
-// the f16 rate, where float32 MFMAs run at a sixteenth. bf16 inputs are exact in one plane (their 8
-// bits under a power-of-two scale), so they need one product in the Gram matrix and two with Q.
+// the f16 rate, where float32 MFMAs are issued at a sixteenth (large library products: 0.153 of 1.49
+// PFLOP/s, a tenth); what it drops, lo lo, is 2^-22 of a product at most. bf16 inputs take one plane: their
+// 8 bits are exact under a power-of-two scale, but for elements below 2^-17 of the root mean square, which
+// f16 holds to 2^-25 of it; so they need one product in the Gram matrix and two with Q.
 // Sums of squares, norms and the clip are 64 bits.
 //
 // Launches of a pass: sums of squares; planes of X (for muon_step with the momentum update and Adam
@@ -48,6 +50,9 @@ namespace cb {
 namespace {
 
 constexpr int kSegF32 = 2, kSegBf16 = 3, kMaxSegs = kNsMaxSteps / 2;
+// What the tile rules count workgroups against. Not the current device's number: the layout of a workspace
+// follows from the rules, and its size is asked for without a device. On fewer they are slower, not wrong.
+constexpr int kNsCus = 256;
 constexpr float kNsDefault[3] = {3.4445f, -4.7750f, 2.0315f};
 
 typedef _Float16 ns_f16x8 __attribute__((ext_vector_type(8)));
@@ -635,9 +640,9 @@ __global__ __launch_bounds__(NT) void ns_reduce_kernel(NsArgs a, NsSeg s) {
 }
 
 // The products of symmetric matrices that commute: tiles of the lower triangle and their mirror images, one
-// or two products a launch. Tiles of up to 64 read what is added early, behind the product. m = 256: 5 us
-// (36 tiles of 32), a launch and eight trips to memory in turn; 1001 x 2: 30 us for one product or two (72 or
-// 144 tiles of 128; tiles of 64, 272 or 544, took 24 and 38); 4096: 195 us, 1.21 PFLOP/s.
+// or two products a launch. m = 256: 5 us (36 tiles of 32), a launch and eight trips to memory in turn;
+// 1001 x 2: 30 us for one product or two (72 or 144 tiles of 128; tiles of 64, 272 or 544, took 24 and 38);
+// 4096: 195 us, 1.21 PFLOP/s.
 enum { NS_A = 0, NS_T, NS_P, NS_V, NS_Q0, NS_Q1 };
 struct NsJob {                 // dst = diag I + fa add + f lhs rhs (scales included)
     int lhs, rhs, dst, add;
@@ -650,8 +655,7 @@ CB_DEV char* ns_buf(const NsArgs& a, const NsGroup& G, int id, int b) {
     return a.ws + o + int64_t(b) * 2 * G.ms;
 }
 
-// Products of symmetric matrices that commute: the lower triangle's tiles, and their mirror images. With
-// tiles of 32 and 64, where a launch is a row of latencies, `add` is read before the product.
+// With tiles of 32 and 64, where a launch is a row of latencies, `add` is read before the product.
 template <int BT, int BK, int ST>
 __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -1230,7 +1234,7 @@ bool ns_one(int64_t batch, int rows, int cols) {
 // below 1024 would be padded too far by 192.
 int ns_bt(int m, int64_t batch) {
     auto tiles = [&](int bt) { const int64_t t = (m + bt - 1) / bt; return batch * t * (t + 1) / 2; };
-    return tiles(32) <= 512 ? 32 : tiles(64) <= 256 ? 64 : tiles(128) <= 256 || m < 1024 ? 128 : 192;
+    return tiles(32) <= 2 * kNsCus ? 32 : tiles(64) <= kNsCus ? 64 : tiles(128) <= kNsCus || m < 1024 ? 128 : 192;
 }
 
 void ns_shape(NsGroup& G, int rows, int cols, int batch) {
@@ -1242,7 +1246,7 @@ void ns_shape(NsGroup& G, int rows, int cols, int batch) {
     G.bg = std::max(G.bt, 64);
     // tiles of Q X: the same rule on their own number
     const int64_t wide = int64_t(batch) * ((rows + 63) / 64) * ((cols + 63) / 64);
-    G.ba = G.bt == 192 ? 192 : G.small || (wide <= 256 && G.bt <= 64) ? 64 : 128;
+    G.ba = G.bt == 192 ? 192 : G.small || (wide <= kNsCus && G.bt <= 64) ? 64 : 128;
     const int pad = std::max(G.bg, G.ba);
     G.rp = int(up(rows, pad)); G.cp = int(up(cols, pad));
     G.mp = std::min(G.rp, G.cp); G.np = std::max(G.rp, G.cp);
@@ -1252,7 +1256,7 @@ void ns_shape(NsGroup& G, int rows, int cols, int batch) {
     // the Gram product's k in splits of at least two 64-blocks, towards what the CUs hold
     const int nb = G.np / 64;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::max(1, nb / 2),
-                                                                256 / (int64_t(batch) * G.gtiles)));
+                                                                kNsCus / (int64_t(batch) * G.gtiles)));
     const int each = int((nb + want - 1) / want);
     G.kchunk = each * 64;
     G.splits = (nb + each - 1) / each;
@@ -1414,8 +1418,8 @@ void ns_apply(const NsArgs& a, const NsApply& ap, int np, hipStream_t s) {
     if (!n) return;
     if constexpr (BT == 64 && ST > 2)
         // More tiles than CUs: two stages, so that a CU holds two of them and there is no second round (the base
-        // net's 305: 14 -> 11 us, muon_step 129 -> 124; the 244 of 3872 x 256 take 0.4 us longer with two).
-        if (n > 256) {
+        // net's 305: 14 -> 11 us; the 244 of 3872 x 256 take 0.4 us longer with two).
+        if (n > kNsCus) {
             ns_apply<BT, BK, 2>(a, ap, np, s);
             return;
         }
@@ -1436,7 +1440,7 @@ int ns_chain(const NsArgs& a, const NsSeg& g, hipStream_t s) {
     // The chip holds two products at once (m = 256: two cost 5.2 us, one 5.1; at m = 512, 272 tiles, 8.1 and
     // 6.4, and both ways take the same time).
     bool wide = true;
-    for (int i = 0; i < a.ng; ++i) wide = wide && (a.g[i].small || 2 * int64_t(a.g[i].batch) * a.g[i].tiles <= 256);
+    for (int i = 0; i < a.ng; ++i) wide = wide && (a.g[i].small || 2 * int64_t(a.g[i].batch) * a.g[i].tiles <= kNsCus);
     if (wide) {
         // A step more in three launches of two products each, where the other way takes four: with R = P A and
         // U = P Q the next A is A' = R P, and the next Q = P' Q = a Q + A' (b Q + c A' Q), A' Q = R U; the P'
@@ -1665,7 +1669,7 @@ hipError_t muon_update(const MuonStep& m, const std::vector<MuonMat>& mats, void
         p.a.ws = static_cast<char*>(ws);
         MuonElem& e = p.e;
         const OptArgs& o = m.adam;
-        e.n_params = m.n; e.p = o.p; e.g = o.g; e.m = o.m; e.v = o.v;
+        e.p = o.p; e.g = o.g; e.m = o.m; e.v = o.v;
         e.mu = m.momentum; e.omu = m.omu; e.nesterov = m.nesterov;
         e.c1 = m.nesterov ? m.omu * (1.f + m.momentum) : m.omu;
         e.c2 = m.nesterov ? m.momentum * m.momentum : m.momentum;

@@ -23,10 +23,10 @@ def test_coefficients_that_shrink_as_far_as_is_allowed(prec):
 
 # Gradient-like matrices in float32, five default steps in segments of 2, 2 and 1. An operand's pair of f16 numbers
 # is off by at most 2^-23 of its element, uniformly (2^-23 / sqrt 3 rms), so a product of two by 2^-23 x 0.82, and the
-# dropped lo lo product adds 2^-24 / 3: A is off by 2^-23 x 0.84 of its norm. A second step of a segment multiplies
-# that by a^2 = 11.9 where singular values are small, and P by |b| / a = 1.4: 1.7e-6 of the result for each segment of
-# two. Float32 sums of hundreds to thousands of products are off by about as much (a float32 evaluation: 1e-6 to 2e-6).
-# Added linearly: 5e-6. A segment of three multiplies by 11.9 once more: 7e-6 to 17e-6 on the first of these.
+# dropped lo lo product, 2^-11 / sqrt 3 squared, adds 2^-23 x 0.67: A is off by 2^-23 x 1.05 of its norm. A second step
+# of a segment multiplies that by a^2 = 11.9 where singular values are small, and P by |b| / a = 1.4: 2.1e-6 of the
+# result, 2.9e-6 for two segments of two, independent of each other. Float32 sums of hundreds to thousands of products
+# are off by as much as a float32 evaluation's, 1e-6 to 2e-6. Added: 5e-6. A segment of three multiplies by 11.9 once more: 7e-6 to 17e-6 on the first of these.
 F32_GRADIENT = 5e-6
 # against a float32 evaluation: two bits fewer an operand
 F32_RATIO = 4
