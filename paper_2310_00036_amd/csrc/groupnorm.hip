@@ -17,6 +17,12 @@
 // (57.8 M elements at 60 instructions are 88 us, their traffic 68), so an element's work is folded into
 // per-channel constants: z = (x - mu) k + beta, dx = da k + (x - mu) c2 + c3.
 //
+// Sums of a chunk (at most 65536 elements, up to 8 in a row per thread, then pairwise) are float32; those
+// over chunks and frames are 64 bits. The silu's sigmoid takes the hardware's exponential and reciprocal:
+// the first is off by |z| 2^-24, which is what z's own rounding leaves of it, the second by 2^-23. Float32
+// results are off by 9.1e-8 (forward) and 1.4e-7 (backward) of their norm, the plain torch form's, summed in
+// 64 bits over the frames, by 8.9e-8 and 8.3e-8.
+//
 // Measured, against a copy's 5.1 TB/s: 2048 x 42x42x16 bf16 forward 44 us, 5.3 TB/s; 2048 x 21x21x64 bf16
 // backward 102 us, 3.4 TB/s (two tensors in registers leave two workgroups a CU, whose loads, arithmetic and
 // stores overlap only with each other's); 2048 x 42x42x32 bf16 forward 117 us, 4.0 TB/s (a workgroup of 1024

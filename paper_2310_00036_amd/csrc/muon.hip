@@ -10,7 +10,7 @@
 // its norm, so the next segment starts from a fresh Gram matrix. Five steps on gradient-like matrices
 // (a few strong directions over noise) are off by 0.7e-6 to 3.5e-6 of their norm with segments of 2, 2 and 1
 // steps (kSegF32: float32 matrices and muon_step), where the steps one by one in float32 are by 1e-6 to 2e-6
-// (at most 2.4 times theirs on one matrix). With 3 and 2 (kSegBf16) they are off by 2e-6 to 14e-6, which bf16
+// (at most 2.5 times theirs on one matrix). With 3 and 2 (kSegBf16) they are off by 2e-6 to 14e-6, which bf16
 // results, at 1.7e-3 from their own rounding, do not see; one segment of 5 is off by 2^-7 for singular values
 // spread over six decades, more than bf16 resolves.
 // On square matrices the operations are the same either way; on 15 : 1 they are 1 : 1.4.
@@ -32,7 +32,7 @@
 // of muon_orthogonalize do without all that: one launch, a workgroup each (ns_one_kernel).
 //
 // What bounds a call: up to m = 512 or so the latency of its 20 launches, 4 to 8 us each (3872 x 256
-// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 124 us);
+// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 136 us);
 // from there on the tile product (4096 x 4096 bf16 3.55 ms, 390 TFLOP/s of the result's operations,
 // 1.2 PFLOP/s of f16 products where a large library product of f16 matrices reaches 1.49).
 #include "common.h"
@@ -854,7 +854,7 @@ CB_DEV void ns_sum256(double (&v)[N], double* sh) {
 }
 
 // Blocks [0, start[ng]) sum a matrix's elements in G.nsum shares; (STEP) those after them the gaps'.
-// Memory-bound where it is long (the wide net's 35 MB of g and m: 10 us), else latency: 5 to 7 us.
+// Memory-bound where it is long (the wide net's 35 MB of g and m: 11 us), else latency: 5 to 7 us.
 // Three doubles a block: sum g^2, sum g m, sum m^2 (others: sum x^2, 0, 0).
 template <int SRC>
 __global__ __launch_bounds__(256) void ns_sums_kernel(NsArgs a, MuonElem e, const void* src, int block0) {
