@@ -219,8 +219,8 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * longer ones first, with L = 2 in float32 and 3 in bf16 (five steps: 2, 2, 1 and 3, 2). Coefficients
  * that let a singular value of [0, 1] grow past 2^10, or the product of the polynomials of a segment's
  * steps past 10^15, are IMPALA_EUNSUPPORTED, whatever the sides; so are those that shrink the bound on
- * X, A X, a polynomial or such a product to less than 2^-17 of one or of its largest in the segment
- * (not to zero), which the pairs of f16 numbers would no longer resolve.
+ * X, A X, a polynomial or such a product to less than 2^-17 of one or of its largest in the segment,
+ * which the pairs of f16 numbers would no longer resolve (a polynomial of zeros among them).
  * Any sides with rows * cols <= 2^28 and min(rows, cols) <= 16384, one row or column included, whose
  * product rounded up to multiples of 192 is <= 2^29; batch <= 2^21, and, but for small matrices that
  * fit one CU, batch times that product <= 2^34 (more: IMPALA_EUNSUPPORTED).

@@ -1360,7 +1360,7 @@ bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
         // Planes hold 22 bits of what is 2^-3 or more under its scale (f16's smallest step is 2^-24). Every
         // matrix of the segment has one scale for all steps, so a step that shrinks it too far is refused; of V
         // = b Q + c A' Q it is what A' V adds to the next Q that counts.
-        auto held = [](double bound, double scale) { return bound == 0 || bound * scale >= 0x1p-3; };
+        auto held = [](double bound, double scale) { return bound * scale >= 0x1p-3; };
         for (int t = 0; t < g.len; ++t) {
             const bool more = t + 1 < g.len;
             if (!held(av[t], g.sa) || !held(pv[t], g.sp) || !held(qv[t], g.sq) || (t > 0 && !held(qv[t], g.sv / amax)) ||

@@ -47,12 +47,16 @@ def test_coefficients_that_shrink_a_matrix_below_what_its_planes_hold():
     """The first two steps of a segment multiply by 10^-8 each, the third by 9 x 10^14: under the scale of the third's
     polynomial, 2^-35, the second's is 0 in f16, and so would be the result, whose exact value is 0.09 X."""
     one = (1.0, 0.0, 0.0)
-    for co in ([SMALL, SMALL, LARGE], [SMALL, SMALL, LARGE, (100.0, 0.0, 0.0), one], [SMALL, one], [one, SMALL, one, one]):
+    for co in ([SMALL, SMALL, LARGE], [SMALL, SMALL, LARGE, (100.0, 0.0, 0.0), one], [SMALL, one], [one, SMALL, one, one],
+               [(0.0, 0.0, 0.0)] * 5):
         assert _orth(P.PREC_BF16, co) == EUNSUPPORTED, co
         assert _orth(P.PREC_FP32, co) == EUNSUPPORTED, co
         assert _step(co) == EUNSUPPORTED, co
+    # after a polynomial of zeros the scales followed from nothing: the factors of the next ones were infinite
+    zeros = [(6.78e13, -244.5, -1.25e-4), (-9.87e14, 1e-5, -3.6e16), (0.0, -1e-18, 0.0), (5e12, 0.0, -3.7e5)]
+    assert _orth(P.PREC_FP32, [(0.0, 0.0, 0.0)] + zeros) == EUNSUPPORTED
     tenth = (0.1, 0.0, 0.0)
-    for co in ([tenth] * 2, [tenth] * 3, [(0.0, 1.0, 0.0)], [(0.0, 0.0, 0.0)], [one, (0.0, 0.0, 0.0)],
+    for co in ([tenth] * 2, [tenth] * 3, [(0.0, 1.0, 0.0)],
                [(3.0, 1e-9, 0.0)] * 2, [(8.287, -23.596, 17.301), (4.107, -2.948, 0.545)]):
         for prec in (P.PREC_FP32, P.PREC_BF16):
             assert _orth(prec, co) == EWORKSPACE, co
