@@ -228,7 +228,9 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * float32 accumulation (small matrices: on float32 matrix cores); ||x|| is a 64-bit
  * sum. Five default steps of gradient-like matrices leave IMPALA_PREC_FP32 results off by 0.7e-6 to
  * 3.5e-6 of their norm, where the steps one by one in float32 leave 1e-6 to 2e-6 (at most 2.5 times those
- * on one matrix; less than them for small ones), and IMPALA_PREC_BF16 results by their own rounding. A
+ * on one matrix; less than them for small ones), and IMPALA_PREC_BF16 results by their own rounding.
+ * Other coefficients with every a_k >= 1 leave up to 1e-5. With smaller ones, which shrink what is small,
+ * errors are relative to the largest values that the coefficients allow instead of to the result's own. A
  * zero matrix gives zeros; one with an element that is not finite gives NaN in all of its own.
  * ws: device scratch of muon_orthogonalize_workspace_bytes() bytes, 16-byte aligned. */
 size_t muon_orthogonalize_workspace_bytes(impala_prec_t prec, int64_t batch, int32_t rows, int32_t cols,
