@@ -227,8 +227,8 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
  * Precision: the products run on f16 matrix cores, each operand as the sum of two f16 numbers, with
  * float32 accumulation (small matrices: on float32 matrix cores); ||x|| is a 64-bit
  * sum. Five default steps of gradient-like matrices leave IMPALA_PREC_FP32 results off by 0.7e-6 to
- * 3.5e-6 of their norm, where the steps one by one in float32 leave 1e-6 to 2e-6 (at most 2.5 times those
- * on one matrix; less than them for small ones), and IMPALA_PREC_BF16 results by their own rounding.
+ * 2.8e-6 of their norm, where the steps one by one in float32 leave 1e-6 to 2e-6 (at most twice those on
+ * one matrix; less than them for small and for large ones), and IMPALA_PREC_BF16 results by their own rounding.
  * Other coefficients with every a_k >= 1 leave up to 1e-5. With smaller ones, which shrink what is small,
  * errors are relative to the largest values that the coefficients allow instead of to the result's own. A
  * zero matrix gives zeros; one with an element that is not finite gives NaN in all of its own.

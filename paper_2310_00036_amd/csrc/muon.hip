@@ -8,9 +8,9 @@
 // L (3 m^2 n + m^3) for the steps one by one. What bounds L is rounding: A squares the singular values
 // and P A P grows what is small by a^2 a step, the rounding of A along with it. A's error is 2^-24 of
 // its norm, so the next segment starts from a fresh Gram matrix. Five steps on gradient-like matrices
-// (a few strong directions over noise) are off by 0.7e-6 to 3.5e-6 of their norm with segments of 2, 2 and 1
+// (a few strong directions over noise) are off by 0.7e-6 to 2.8e-6 of their norm with segments of 2, 2 and 1
 // steps (kSegF32: float32 matrices and muon_step), where the steps one by one in float32 are by 1e-6 to 2e-6
-// (at most 2.5 times theirs on one matrix). With 3 and 2 (kSegBf16) they are off by 2e-6 to 14e-6, which bf16
+// (at most twice theirs on one matrix). With 3 and 2 (kSegBf16) they are off by 2e-6 to 14e-6, which bf16
 // results, at 1.7e-3 from their own rounding, do not see; one segment of 5 is off by 2^-7 for singular values
 // spread over six decades, more than bf16 resolves.
 // On square matrices the operations are the same either way; on 15 : 1 they are 1 : 1.4.
@@ -32,7 +32,7 @@
 // of muon_orthogonalize do without all that: one launch, a workgroup each (ns_one_kernel).
 //
 // What bounds a call: up to m = 512 or so the latency of its 20 launches, 4 to 8 us each (3872 x 256
-// float32 118 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 136 us);
+// float32 119 us, its bytes 2 us and its products 2 at the f16 rate; the base net's muon_step 137 us);
 // from there on the tile product (4096 x 4096 bf16 3.55 ms, 390 TFLOP/s of the result's operations,
 // 1.2 PFLOP/s of f16 products where a large library product of f16 matrices reaches 1.49).
 #include "common.h"
@@ -252,7 +252,19 @@ constexpr int ns_lds_bytes() { return ST * (NA + NB) * BT * BK * 2; }
 template <int BT>
 using NsAcc = cb_f32x4[NsWaves<BT>::FM][NsWaves<BT>::FN];
 
-template <int BT, int BK, int ST, int NA, int NB>
+template <int BT>
+CB_DEV void ns_clear(NsAcc<BT>& acc) {
+#pragma unroll
+    for (int i = 0; i < NsWaves<BT>::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < NsWaves<BT>::FN; ++j) acc[i][j] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// CROSS: the products with a lo plane are summed apart from the hi hi ones and added at the end. The matrix
+// cores seem to cut off what a sum cannot hold rather than round it (a model of sums so cut has the errors
+// measured here, one of rounded sums a third of them), and so a third as many additions to the large sum leave
+// less of that bias. It matters in the m x m chain, whose errors the later products multiply: ns_cross.
+template <int BT, int BK, int ST, int NA, int NB, bool CROSS = false>
 CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char* B, int64_t bbytes, int ldb, int brow,
                     int k0, int k1, unsigned char* smem, NsAcc<BT>& acc) {
     using W = NsWaves<BT>;
@@ -281,14 +293,14 @@ CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char
     };
     // x y row by row; with(ks, i) before row i of step ks: reads and loads go between the products, for
     // one block of either would hold the matrix core up
-    auto mul = [&](const uint4 (&x)[KS][FM], const uint4 (&y)[KS][FN], auto&& with) CB_INLINE_LAMBDA {
+    auto mul = [&](NsAcc<BT>& sum, const uint4 (&x)[KS][FM], const uint4 (&y)[KS][FN], auto&& with) CB_INLINE_LAMBDA {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 with(ks, i);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = ns_mma(x[ks][i], y[ks][j], acc[i][j]);
+                for (int j = 0; j < FN; ++j) sum[i][j] = ns_mma(x[ks][i], y[ks][j], sum[i][j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
@@ -298,6 +310,9 @@ CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char
     // half of that product; the others are read during the products before. No product waits for LDS. The
     // freed buffer's loads are issued half in that product and half in the next stage's first one.
     constexpr int R = KS * FM, HALF = NA > 1 || NB > 1 ? LPS / 2 : LPS;
+    NsAcc<BT> apart;
+    if constexpr (CROSS) ns_clear<BT>(apart);
+    NsAcc<BT>& cross = CROSS ? apart : acc;
     uint4 a0[KS][FM], b0[KS][FN], a1[KS][FM], b1[KS][FN], na[KS][FM], nbf[KS][FN];
     for (int s = 0; s < ST - 1; ++s)
 #pragma unroll
@@ -311,9 +326,9 @@ CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char
         a0[q / FM][q % FM] = read_a(0, 0, q / FM, q % FM);
         b0[q / FM][q % FM] = read_b(0, 0, q / FM, q % FM);
     }
-    for (int it = 0; it < nb; ++it) {
+    auto stage = [&](int it, uint4 (&x0)[KS][FM], uint4 (&y0)[KS][FN], uint4 (&nx)[KS][FM], uint4 (&ny)[KS][FN]) CB_INLINE_LAMBDA {
         if constexpr (NA > 1 || NB > 1)
-            mul(a0, b0, [&](int ks, int i) CB_INLINE_LAMBDA {
+            mul(acc, x0, y0, [&](int ks, int i) CB_INLINE_LAMBDA {
                 if constexpr (NB > 1) b1[ks][i] = read_b(it, 1, ks, i);
                 else a1[ks][i] = read_a(it, 1, ks, i);
                 const int at = ks * FM + i;
@@ -321,38 +336,40 @@ CB_DEV void ns_gemm(const char* A, int64_t abytes, int lda, int arow, const char
                 for (int d = HALF + at * (LPS - HALF) / R; d < HALF + (at + 1) * (LPS - HALF) / R; ++d) issue(it + ST - 1, d);
             });
         if constexpr (NA > 1 && NB > 1)
-            mul(a0, b1, [&](int ks, int i) CB_INLINE_LAMBDA { a1[ks][i] = read_a(it, 1, ks, i); });
+            mul(cross, x0, b1, [&](int ks, int i) CB_INLINE_LAMBDA { a1[ks][i] = read_a(it, 1, ks, i); });
         ns_wait<(ST - 2) * LPS>();
         lds_barrier();
-        mul(NA > 1 ? a1 : a0, NA > 1 ? b0 : NB > 1 ? b1 : b0, [&](int ks, int i) CB_INLINE_LAMBDA {
+        mul(NA > 1 || NB > 1 ? cross : acc, NA > 1 ? a1 : x0, NA > 1 ? y0 : NB > 1 ? b1 : y0, [&](int ks, int i) CB_INLINE_LAMBDA {
             const int at = ks * FM + i;
 #pragma unroll
             for (int q = 2 * at; q < 2 * at + 2; ++q)
                 if (q < R) {
-                    na[q / FM][q % FM] = read_a(it + 1, 0, q / FM, q % FM);
-                    nbf[q / FM][q % FM] = read_b(it + 1, 0, q / FM, q % FM);
+                    nx[q / FM][q % FM] = read_a(it + 1, 0, q / FM, q % FM);
+                    ny[q / FM][q % FM] = read_b(it + 1, 0, q / FM, q % FM);
                 }
 #pragma unroll
             for (int d = at * HALF / R; d < (at + 1) * HALF / R; ++d) issue(it + ST, d);
         });
+    };
+    for (int it = 0; it < nb; ++it) {
+        stage(it, a0, b0, NA > 1 && NB > 1 ? a0 : na, nbf);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                a0[ks][i] = na[ks][i];
+                if constexpr (!(NA > 1 && NB > 1)) a0[ks][i] = na[ks][i];
                 b0[ks][i] = nbf[ks][i];
             }
     }
     ns_wait<0>();
     lds_barrier();
-}
-
-template <int BT>
-CB_DEV void ns_clear(NsAcc<BT>& acc) {
+    if constexpr (CROSS)
 #pragma unroll
-    for (int i = 0; i < NsWaves<BT>::FM; ++i)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < NsWaves<BT>::FN; ++j) acc[i][j] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += apart[i][j][e];
 }
 
 // f(M, N, acc[i][j], i, j) for every group of four rows M .. M+3 of column N that this lane holds (local).
@@ -656,7 +673,7 @@ CB_DEV char* ns_buf(const NsArgs& a, const NsGroup& G, int id, int b) {
 }
 
 // With tiles of 32 and 64, where a launch is a row of latencies, `add` is read before the product.
-template <int BT, int BK, int ST>
+template <int BT, int BK, int ST, bool CROSS>
 __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a, NsJobs jobs) {
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr bool EARLY = BT <= 64;
@@ -679,8 +696,8 @@ __global__ __launch_bounds__(64 * NsWaves<BT>::NW) void ns_prod_kernel(NsArgs a,
             const uint2 h = *reinterpret_cast<const uint2*>(p), l = *reinterpret_cast<const uint2*>(p + kLo);
             early[i][j] = make_uint4(h.x, h.y, l.x, l.y);
         });
-    ns_gemm<BT, BK, ST, 2, 2>(ns_buf(a, G, J.lhs, b), 2 * G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), 2 * G.ms, G.ldm,
-                              tj * BT, 0, G.mp, smem, acc);
+    ns_gemm<BT, BK, ST, 2, 2, CROSS>(ns_buf(a, G, J.lhs, b), 2 * G.ms, G.ldm, ti * BT, ns_buf(a, G, J.rhs, b), 2 * G.ms, G.ldm,
+                                     tj * BT, 0, G.mp, smem, acc);
     char* D = ns_buf(a, G, J.dst, b);
     const float f = J.f, fa = J.fa, diag = J.diag;
     ns_emit<BT>(acc, D, G.ldm, tj * BT, ti * BT, ti != tj, D, G.ldm,
@@ -1402,12 +1419,19 @@ void ns_gram(const NsArgs& a, const NsSeg& g, int src, int np, hipStream_t s) {
     else NS_TILES((ns_gram_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, g, src);
 }
 
-template <int BT, int BK, int ST>
-void ns_prod(const NsArgs& a, const NsJobs& jobs, hipStream_t s) {
+// Whether a group of a float32 call sums its chain's cross products apart (ns_gemm). Below m = 512 the plain
+// sums are off by more than a float32 evaluation of the steps, from there on by less, as its own sums get longer:
+// 3872 x 256 1.31 to 1.5 times as much as that (1.07 with CROSS, 1 % slower), 70 x 200x260 1.35 (1.08, 4 %),
+// 12 x 400x2000 1.11 (0.81, 3 %); 512 x 512 0.94 (0.70, 2 %), 2 x 1001x1531 0.85 (0.63, 6 %), 3000 x 2000 0.77
+// (0.61, 6 %).
+bool ns_cross(const NsGroup& G) { return G.m < 512; }
+
+template <int BT, int BK, int ST, bool CROSS>
+void ns_prod(const NsArgs& a, const NsJobs& jobs, bool f32, hipStream_t s) {
     int n;
-    const NsArgs r = ns_select(a, [](const NsGroup& G) { return G.bt == BT && !G.small; },
+    const NsArgs r = ns_select(a, [&](const NsGroup& G) { return G.bt == BT && !G.small && (f32 && ns_cross(G)) == CROSS; },
                                [&](const NsGroup& G) { return G.batch * G.tiles * jobs.n; }, n);
-    if (n) NS_TILES((ns_prod_kernel<BT, BK, ST>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, jobs);
+    if (n) NS_TILES((ns_prod_kernel<BT, BK, ST, CROSS>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, jobs);
 }
 
 template <int BT, int BK, int ST>
@@ -1427,13 +1451,16 @@ void ns_apply(const NsArgs& a, const NsApply& ap, int np, hipStream_t s) {
     else NS_TILES((ns_apply_kernel<BT, BK, ST, 2>), n, (ns_lds_bytes<BT, BK, ST, 2, 2>()), r, ap);
 }
 
-// The m x m products of a segment; returns which Q buffer holds Q.
-int ns_chain(const NsArgs& a, const NsSeg& g, hipStream_t s) {
+// The m x m products of a segment; returns which Q buffer holds Q. f32: of a float32 call.
+int ns_chain(const NsArgs& a, const NsSeg& g, bool f32, hipStream_t s) {
     auto run = [&](const NsJobs& j) {
-        ns_prod<32, 64, 4>(a, j, s);
-        ns_prod<64, 64, 4>(a, j, s);
-        ns_prod<128, 32, 4>(a, j, s);
-        ns_prod<192, 32, 3>(a, j, s);
+        ns_prod<32, 64, 4, false>(a, j, f32, s);
+        ns_prod<32, 64, 4, true>(a, j, f32, s);
+        ns_prod<64, 64, 4, false>(a, j, f32, s);
+        ns_prod<64, 64, 4, true>(a, j, f32, s);
+        ns_prod<128, 32, 4, false>(a, j, f32, s);
+        ns_prod<128, 32, 4, true>(a, j, f32, s);
+        ns_prod<192, 32, 3, false>(a, j, f32, s);   // (m >= 1024)
     };
     // the first P is Q
     run({1, {{NS_A, NS_A, NS_Q0, NS_A, g.sq * g.c[0][2] / (g.sa * g.sa), g.sq * g.c[0][1] / g.sa, g.sq * g.c[0][0]}}});
@@ -1494,7 +1521,7 @@ hipError_t ns_run(const NsArgs& a, const NsProgram& P, int np, NsApply last, hip
         for (int i = 0; i < a.ng; ++i) small = small || a.g[i].small;
         if (n && small) hipLaunchKernelGGL(ns_reduce_kernel<kSmThreads>, dim3(unsigned(n)), dim3(kSmThreads), kSmLds, s, r, g);
         else if (n) NS_LAUNCH(ns_reduce_kernel<256>, n, 256 * 17 * int(sizeof(float)), r, g);
-        const int q = ns_chain(a, g, s);
+        const int q = ns_chain(a, g, last.out != NS_OUT_BF16, s);
         const bool end = k + 1 == P.nseg;
         NsApply ap = last;
         if (!end) ap.out = NS_OUT_MID;
