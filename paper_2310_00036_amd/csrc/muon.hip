@@ -1325,8 +1325,8 @@ double pow2_scale(double bound, int most) {   // the largest power of two (at mo
 // The segments of `steps` steps and the scales of their matrices, from bounds on the singular values:
 // they start at one at most, and a step maps them by s -> s (a + b s^2 + c s^4). False, and P is not to be
 // run, where they could grow past 2^10 (planes would no longer resolve them), or a segment's product of
-// polynomials past 10^15, or where they shrink what the planes hold too far. Which steps share a segment depends on `most`, so what one length accepts another
-// may not.
+// polynomials past 10^15, or where they shrink what the planes hold too far. Which steps share a segment
+// depends on `most`, so what one length accepts another may not.
 bool ns_program(int steps, const float* coeffs, int most, NsProgram& P) {
     P.nseg = (steps + most - 1) / most;
     double s = 1.0 + 0x1p-10;
