@@ -185,6 +185,61 @@ impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, i
                                      void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
                                      hipStream_t stream);
 
+/* Linear attention with a decay per head, a policy's memory over the rollout: for each env and head a
+ * state S of dk x dv numbers,
+ *   S_t = (1 - d_t) g S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,   g = exp(log_decay[head]),
+ * with d_t = 1 where s_t starts a new episode, as gae_advantages reads it: an episode start clears the
+ * state, so nothing of an earlier episode, NaN and infinities included, reaches a later one, and no
+ * step reaches an earlier one. impala_linattn_fwd and _bwd take a whole rollout (chunks of steps on the
+ * matrix cores), impala_linattn_step one step of every env, for the actor.
+ * q, k: [T, E, heads, dk] and v, o: [T, E, heads, dv] in the storage type, the last axis contiguous, the
+ * others by strides in elements (>= 0; a broadcast axis has stride 0), so they may be parts of one
+ * projection's output, an env block of a larger rollout, or [E, T, ...]. log_decay: float [heads], <= 0
+ * (-infinity: no memory; above 0 the state grows). dones: uint8 with strides done_t, done_e, or NULL (no
+ * episode starts). States: float32 [E, heads, dk, dv], row-major, in both precisions. 1 <= dk, dv <= 128,
+ * E * heads <= 2^21 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element (16-byte aligned ones with
+ * strides and sizes of whole 16 bytes are read so).
+ * Outputs must not have two elements in one place, and must not overlap inputs or each other: two arrays
+ * with the same strides may lie between each other's elements, any other overlap of their address ranges
+ * is IMPALA_EINVAL. */
+typedef struct linattn_strides { int64_t t, e, h; } linattn_strides_t;
+typedef struct linattn_shape {
+    int32_t prec;              /* impala_prec_t */
+    int32_t T, E, heads, dk, dv;
+    float scale;
+    linattn_strides_t q, k, v, o;       /* o: of the output, in the backward pass of its gradient */
+    linattn_strides_t gq, gk, gv;       /* of dq, dk, dv; read by impala_linattn_bwd only */
+    int64_t done_t, done_e;
+} linattn_shape_t;
+
+/* Scratch of impala_linattn_fwd (backward == 0) or _bwd (1); 0 also on error. */
+size_t impala_linattn_workspace_bytes(const linattn_shape_t* shape, int backward);
+
+/* o over the rollout from the state s0 before it (NULL: zeros), and the state s_out after it (NULL: not
+ * wanted; may be s0 itself). s_out is S_{T-1}: the next rollout's first step applies its own d_0.
+ * shape is HOST memory, not kept. ws: 16-byte aligned, may be NULL where the query gives 0.
+ * bf16 products of q and k are exact, what follows is held in pairs or triples of bf16 numbers, so that
+ * o is off by its own rounding and s_out by a few 2^-24 as the float32 sums are. */
+impala_status_t impala_linattn_fwd(const linattn_shape_t* shape, const void* q, const void* k, const void* v,
+                                   const float* log_decay, const uint8_t* dones, const float* s0, void* o,
+                                   float* s_out, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of it from d_o (of o) and ds_out (of s_out; NULL: zero): with
+ *   G_t = scale q_t d_o_t^T + (1 - d_{t+1}) g G_{t+1}, G_{T-1} = scale q d_o^T + ds_out,
+ *   dq_t = scale S_t d_o_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,  ds0 = (1 - d_0) g G_0.
+ * s0 as the forward's (S is formed again from it); ds0 may be NULL. The decays are constants. Inputs that
+ * the forward broadcast have a gradient for each place that read them, to be summed by the caller. */
+impala_status_t impala_linattn_bwd(const linattn_shape_t* shape, const void* d_o, const void* q, const void* k,
+                                   const void* v, const float* log_decay, const uint8_t* dones, const float* s0,
+                                   const float* ds_out, void* dq, void* dk, void* dv, float* ds0, void* ws,
+                                   size_t ws_bytes, hipStream_t stream);
+
+/* One step (shape->T must be 1): impala_linattn_fwd's recurrence, from s_in (NULL: zeros) to s_out, which
+ * may be s_in itself and is required. No workspace. */
+impala_status_t impala_linattn_step(const linattn_shape_t* shape, const void* q, const void* k, const void* v,
+                                    const float* log_decay, const uint8_t* dones, const float* s_in, void* o,
+                                    float* s_out, hipStream_t stream);
+
 /* Where a training-mode impala_cnn_fwd on n_frames frames (workspace laid out by
  * impala_workspace_bytes(net, n_frames, prec, 1)) leaves the activations that impala_cnn_bwd
  * reads, so a caller can inspect them or replace them between the two calls: the backward

@@ -66,6 +66,17 @@ class MuonCfg(C.Structure):
                 ("coeffs", C.POINTER(C.c_float))]
 
 
+class LinattnStrides(C.Structure):
+    _fields_ = [("t", C.c_int64), ("e", C.c_int64), ("h", C.c_int64)]
+
+
+class LinattnShape(C.Structure):
+    _fields_ = ([("prec", C.c_int32), ("T", C.c_int32), ("E", C.c_int32), ("heads", C.c_int32), ("dk", C.c_int32),
+                 ("dv", C.c_int32), ("scale", C.c_float)] +
+                [(x, LinattnStrides) for x in ("q", "k", "v", "o", "gq", "gk", "gv")] +
+                [("done_t", C.c_int64), ("done_e", C.c_int64)])
+
+
 class Rollout(C.Structure):
     _fields_ = [("obs", C.c_void_p), ("actions", C.c_void_p), ("behav_logp", C.c_void_p),
                 ("rewards", C.c_void_p), ("dones", C.c_void_p), ("values", C.c_void_p),
@@ -128,6 +139,11 @@ _SIGS = {
     "impala_groupnorm_bwd_workspace_bytes": (_SZ, [C.c_int, _I64, _I32, _I32, _I32, _I32]),
     "impala_groupnorm_bwd": (C.c_int, [C.c_int, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _I32, _P, _P,
                                        _P, _P, _SZ, _P]),
+    "impala_linattn_workspace_bytes": (_SZ, [C.POINTER(LinattnShape), C.c_int]),
+    "impala_linattn_fwd": (C.c_int, [C.POINTER(LinattnShape), _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "impala_linattn_bwd": (C.c_int, [C.POINTER(LinattnShape), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ,
+                                     _P]),
+    "impala_linattn_step": (C.c_int, [C.POINTER(LinattnShape), _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "impala_gumbel_sample": (C.c_int, [_I64, _I32, _P, _P, _P, _P, _P]),
     "impala_action_logp": (C.c_int, [_I64, _I32, _P, _P, _P, _P]),
     "impala_profile_begin": (C.c_int, [C.c_char_p, _I32]),
@@ -511,6 +527,63 @@ def impala_groupnorm_bwd(prec, n, H, W, C_, groups, dy, x, gamma, beta, mean, rs
     _check("impala_groupnorm_bwd", lib.impala_groupnorm_bwd(
         prec, n, H, W, C_, groups, ptr(dy), ptr(x), ptr(gamma), ptr(beta), ptr(mean), ptr(rstd), act, ptr(dx),
         ptr(dgamma), ptr(dbeta), *_ws_args(ws), stream_handle(stream)))
+
+
+def _strided(name, t, shape, dtype):
+    """A tensor's first three strides, after the checks that its shape, type and last axis need."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name}: expected {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    if t.shape[-1] > 1 and t.numel() > 0 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    return LinattnStrides(*t.stride()[:3])
+
+
+def linattn_shape(q, k, v, o, dones=None, scale=1.0, dq=None, dk=None, dv=None) -> LinattnShape:
+    """Sizes, type and strides of the linear attention's tensors: q, k [T, E, heads, dk], v, o [T, E, heads, dv]
+    (o: the output or its gradient), dones [T, E]; dq, dk, dv for the backward pass."""
+    import torch
+    if q.dim() != 4 or v.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("q and v must be [T, E, heads, d] in bfloat16 or float32")
+    s = LinattnShape()
+    s.prec = PREC_BF16 if q.dtype == torch.bfloat16 else PREC_FP32
+    s.T, s.E, s.heads, s.dk = q.shape
+    s.dv, s.scale = v.shape[3], scale
+    for name, t, like in (("q", q, q), ("k", k, q), ("v", v, v), ("o", o, v), ("gq", dq, q), ("gk", dk, q), ("gv", dv, v)):
+        if t is not None:
+            setattr(s, name, _strided(name, t, like.shape, q.dtype))
+    if dones is not None:
+        if tuple(dones.shape) != (s.T, s.E) or dones.dtype != torch.uint8:
+            raise ValueError("dones must be uint8 [T, E]")
+        s.done_t, s.done_e = dones.stride()
+    return s
+
+
+def _at(t):
+    """Device pointer of a tensor whose strides its shape struct holds (None passes NULL)."""
+    return t if t is None or isinstance(t, int) else t.data_ptr()
+
+
+def impala_linattn_workspace_bytes(shape: LinattnShape, backward: int = 0) -> int:
+    return int(lib.impala_linattn_workspace_bytes(C.byref(shape), backward))
+
+
+def impala_linattn_fwd(shape: LinattnShape, q, k, v, log_decay, dones, s0, o, s_out, ws=None, stream=None):
+    _check("impala_linattn_fwd", lib.impala_linattn_fwd(
+        C.byref(shape), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s0), _at(o), ptr(s_out), *_ws_args(ws),
+        stream_handle(stream)))
+
+
+def impala_linattn_bwd(shape: LinattnShape, d_o, q, k, v, log_decay, dones, s0, ds_out, dq, dk, dv, ds0, ws=None,
+                       stream=None):
+    _check("impala_linattn_bwd", lib.impala_linattn_bwd(
+        C.byref(shape), _at(d_o), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s0), ptr(ds_out), _at(dq),
+        _at(dk), _at(dv), ptr(ds0), *_ws_args(ws), stream_handle(stream)))
+
+
+def impala_linattn_step(shape: LinattnShape, q, k, v, log_decay, dones, s_in, o, s_out, stream=None):
+    _check("impala_linattn_step", lib.impala_linattn_step(
+        C.byref(shape), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s_in), _at(o), ptr(s_out),
+        stream_handle(stream)))
 
 
 def impala_gumbel_sample(n, A, logits, gumbel, actions, logp, stream=None):

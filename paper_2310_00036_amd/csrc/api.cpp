@@ -16,12 +16,17 @@
 #include "kernels.h"
 #include "muon.h"
 #include "plan.h"
+#include "status.h"
 
 using namespace cb;
 
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
+
+namespace cb {
 
 impala_status_t fail(impala_status_t code, const char* fmt, ...) {
     char buf[512];
@@ -43,16 +48,9 @@ impala_status_t hip_status(hipError_t e, const char* where) {
     return fail(IMPALA_EHIP, "%s: %s", where, hipGetErrorString(e));
 }
 
-#define CHECK_PTR(p) \
-    if (!(p)) return fail(IMPALA_EINVAL, "%s: argument '%s' is NULL", __func__, #p)
+}  // namespace cb
 
-bool valid_prec(int p) { return p == IMPALA_PREC_BF16 || p == IMPALA_PREC_FP32; }
-
-// Whether the byte ranges [a, a + bytes) and [b, b + bytes) overlap without being the same.
-bool partial_overlap(const void* a, const void* b, size_t bytes) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x != y && x < y + bytes && y < x + bytes;
-}
+namespace {
 
 // Learner workspace layout (bytes from the start of ws).
 struct LearnerLayout {
