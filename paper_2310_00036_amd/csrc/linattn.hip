@@ -27,19 +27,20 @@ __global__ __launch_bounds__(64) void la_steps_kernel(LaArgs a, int y0) {
     const int n = int(blockIdx.x % nbs) * 64 + lane;
     const int64_t e = eh / a.H, h = eh % a.H;
     const bool on = n < P.dv;
-    const float g = expf(a.log_decay[h]);
+    const float g = float(exp(double(a.log_decay[h])));
     const int64_t dir = P.back ? -1 : 1;
     int64_t t = P.back ? a.T - 1 : 0;
     const T* q = static_cast<const T*>(P.q.p) + e * P.q.e + h * P.q.h + t * P.q.t;
     const T* k = static_cast<const T*>(P.k.p) + e * P.k.e + h * P.k.h + t * P.k.t;
     const T* v = static_cast<const T*>(P.v.p) + e * P.v.e + h * P.v.h + t * P.v.t + n;
     T* o = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h + t * P.o.t + n;
-    auto keep_at = [&](int64_t td) { return a.dones && a.dones[td * a.d_t + e * a.d_e] ? 0.f : g; };
+    auto starts = [&](int64_t td) { return a.dones && a.dones[td * a.d_t + e * a.d_e]; };
     float R[DK];
 #pragma unroll
     for (int i = 0; i < DK; ++i) R[i] = 0.f;
-    float keep = P.back ? 1.f : keep_at(0);
-    if (P.x0 && keep != 0.f && on) {
+    bool cut = !P.back && starts(0);
+    float keep = P.back ? 1.f : g;
+    if (P.x0 && !cut && on) {
         const float* x = P.x0 + eh * P.dk * P.dv + int64_t(n) * P.xn;
 #pragma unroll
         for (int i = 0; i < DK; ++i)
@@ -69,23 +70,24 @@ __global__ __launch_bounds__(64) void la_steps_kernel(LaArgs a, int y0) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < DK; ++i) {
-            R[i] = (keep == 0.f ? 0.f : keep * R[i]) + sk[i] * vn;
+            R[i] = (cut ? 0.f : keep * R[i]) + sk[i] * vn;
             s += sq[i] * R[i];
         }
         if (on) *o = Pr::store(s * P.out);
         o += dir * P.o.t;
         // what lies between this row and the next: the later one's episode start
-        if (P.back) keep = keep_at(t);
-        else if (p + 1 < a.T) keep = keep_at(t + 1);
+        if (P.back) cut = starts(t);
+        else if (p + 1 < a.T) cut = starts(t + 1);
+        keep = g;
         t += dir;
         __syncthreads();
     }
     if (P.x1 && on) {
-        if (!P.back) keep = 1.f;
+        if (!P.back) { keep = 1.f; cut = false; }
         float* x = P.x1 + eh * P.dk * P.dv + int64_t(n) * P.xn;
 #pragma unroll
         for (int i = 0; i < DK; ++i)
-            if (i < P.dk) x[i * P.xk] = keep == 0.f ? 0.f : keep * R[i];
+            if (i < P.dk) x[i * P.xk] = cut ? 0.f : keep * R[i];
     }
 }
 
@@ -101,6 +103,529 @@ hipError_t la_steps(const LaArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- chunks of 64 rows on the matrix cores
+//
+// Rows i of a chunk with the state X before it (c_i: episode starts up to row i, counting its own going forward and not
+// going back; l = 1 forward, 0 back; n rows):
+//   o_i = [c_i = 0] g^(i+l) X^T q_i + sum_{j <= i, c_j = c_i} g^(i-j) (q_i . k_j) v_j,
+//   X  <- [c = 0] g^n X + sum_{j: c_j = c} g^(n-l-j) k_j v_j^T.
+// A wave owns 16 columns of v, o and X. X stays in its registers as results of the matrix products, laid out so that they
+// are, without moving between lanes, the operand of X^T q. The 64 x 64 products q_i . k_j are formed once by the waves
+// together and handed round in LDS.
+
+constexpr int kL = 64;
+
+// bf16: products of two bf16 numbers are exact; what is no bf16 number (the decayed products, X, the decayed v) goes into
+// a product as two of them, or three where the result is a float32 output (X).
+struct LaB {
+    using T = uint16_t;
+    using Frag = uint4;
+    static constexpr int KB = 32, KPL = 8;   // contraction per fragment, elements of it a lane holds (at KPL * group)
+    static constexpr int NP = 2, NX = 2, NV = 3;
+    static CB_DEV cb_f32x4 mma(Frag a, Frag b, cb_f32x4 c) { return PrecBF16::mma(a, b, c); }
+    static CB_DEV float load(T v) { return bf2f(v); }
+    static CB_DEV void unpack(Frag f, float* x) {
+        x[0] = bf_lo(f.x); x[1] = bf_hi(f.x); x[2] = bf_lo(f.y); x[3] = bf_hi(f.y);
+        x[4] = bf_lo(f.z); x[5] = bf_hi(f.z); x[6] = bf_lo(f.w); x[7] = bf_hi(f.w);
+    }
+    static CB_DEV uint32_t finite2(uint32_t u) {
+        return ((u & 0x7f80u) == 0x7f80u ? 0u : u & 0xffffu) | ((u & 0x7f800000u) == 0x7f800000u ? 0u : u & 0xffff0000u);
+    }
+    static CB_DEV Frag finite(Frag f) { return make_uint4(finite2(f.x), finite2(f.y), finite2(f.z), finite2(f.w)); }
+    // x as a sum of bf16 numbers, the first plane the nearest one, each further plane nearest to the rest
+    template <int N>
+    static CB_DEV void split(float* x, Frag (&f)[N]) {
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            f[p] = make_uint4(pack2bf(x[0], x[1]), pack2bf(x[2], x[3]), pack2bf(x[4], x[5]), pack2bf(x[6], x[7]));
+            float y[8];
+            unpack(f[p], y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] -= y[i];
+        }
+    }
+    // four neighbouring entries of a row of the decayed products, plane by plane
+    static CB_DEV void store_p(unsigned char* p, int plane, float (&x)[4]) {
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+            const uint2 v = make_uint2(pack2bf(x[0], x[1]), pack2bf(x[2], x[3]));
+            *reinterpret_cast<uint2*>(p + u * plane) = v;
+            x[0] -= bf_lo(v.x); x[1] -= bf_hi(v.x); x[2] -= bf_lo(v.y); x[3] -= bf_hi(v.y);
+        }
+    }
+    // Fragment with the contraction along the tile's rows row0 .. row0+31, of 16 columns: operand row (or column) r is
+    // column col + 4 (r / 4) CS + r % 4, so CS = 1 takes neighbours and CS = 2 skips every other four.
+    template <int CS>
+    static CB_DEV Frag cols(const unsigned char* tile, int rs, int row0, int col) {
+        const int l = threadIdx.x & 63, g = l >> 4, c = l & 15;
+        const unsigned char* p = tile + (row0 + 8 * g + (c >> 2)) * rs + (col + 4 * CS * (c & 3)) * 2;
+        const uint2 a = lds_read_tr16(p), b = lds_read_tr16(p + 4 * rs);
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+    // X's 16 x 16 results: result m holds rows k0(m) + group * KG + r, so that two of them are a fragment
+    static CB_DEV int krow(int m, int g, int r) { return 32 * (m >> 1) + 8 * g + 4 * (m & 1) + r; }
+    static CB_DEV Frag kcols(const unsigned char* tile, int rs, int row0, int m) {
+        return cols<2>(tile, rs, row0, 32 * (m >> 1) + 4 * (m & 1));
+    }
+    template <int NT>
+    static CB_DEV void xfrag(const cb_f32x4 (&X)[NT], int kb, Frag (&f)[NX]) {
+        float x[8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { x[r] = X[2 * kb][r]; x[4 + r] = X[2 * kb + 1][r]; }
+        split(x, f);
+    }
+    static CB_DEV void store4o(T* p, const float* x) { store4(p, x[0], x[1], x[2], x[3]); }
+    static CB_DEV T store(float x) { return f2bf(x); }
+};
+
+struct LaF {
+    using T = float;
+    using Frag = float4;
+    static constexpr int KB = 16, KPL = 4;
+    static constexpr int NP = 1, NX = 1, NV = 1;
+    static CB_DEV cb_f32x4 mma(Frag a, Frag b, cb_f32x4 c) {
+        c = PrecF32::mma(a.x, b.x, c);
+        c = PrecF32::mma(a.y, b.y, c);
+        c = PrecF32::mma(a.z, b.z, c);
+        return PrecF32::mma(a.w, b.w, c);
+    }
+    static CB_DEV float load(T v) { return v; }
+    static CB_DEV void unpack(Frag f, float* x) { x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w; }
+    static CB_DEV Frag finite(Frag f) {
+        return make_float4(isfinite(f.x) ? f.x : 0.f, isfinite(f.y) ? f.y : 0.f, isfinite(f.z) ? f.z : 0.f,
+                           isfinite(f.w) ? f.w : 0.f);
+    }
+    template <int N>
+    static CB_DEV void split(float* x, Frag (&f)[N]) { f[0] = make_float4(x[0], x[1], x[2], x[3]); }
+    static CB_DEV void store_p(unsigned char* p, int, float (&x)[4]) {
+        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    }
+    template <int CS>
+    static CB_DEV Frag cols(const unsigned char* tile, int rs, int row0, int col) {
+        const int l = threadIdx.x & 63, g = l >> 4, c = l & 15;
+        const unsigned char* p = tile + (row0 + 4 * g) * rs + (col + c) * 4;
+        return make_float4(*reinterpret_cast<const float*>(p), *reinterpret_cast<const float*>(p + rs),
+                           *reinterpret_cast<const float*>(p + 2 * rs), *reinterpret_cast<const float*>(p + 3 * rs));
+    }
+    static CB_DEV int krow(int m, int g, int r) { return 16 * m + 4 * g + r; }
+    static CB_DEV Frag kcols(const unsigned char* tile, int rs, int row0, int m) { return cols<1>(tile, rs, row0, 16 * m); }
+    template <int NT>
+    static CB_DEV void xfrag(const cb_f32x4 (&X)[NT], int kb, Frag (&f)[NX]) {
+        f[0] = make_float4(X[kb][0], X[kb][1], X[kb][2], X[kb][3]);
+    }
+    static CB_DEV void store4o(T* p, const float* x) { store4(p, x[0], x[1], x[2], x[3]); }
+    static CB_DEV T store(float x) { return x; }
+};
+
+// Where a pass is cut along the rollout, each segment's own contribution to the state, then the states before them.
+struct LaSegs {
+    int segs, chunks;          // segments, chunks in each but the last
+    float* state[kLaMaxPasses];    // [segs][E H][dk dv]
+    float* factor[kLaMaxPasses];   // [segs][E H]: what a segment leaves of the state before it; -1: an episode starts in it
+};
+
+template <class Tr, int DK, int NW>
+struct LaTile {
+    static constexpr int ES = sizeof(typename Tr::T);
+    static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16, RSP = kL * ES + 16;
+    static constexpr int Q = 0, K = kL * RSK, V = 2 * kL * RSK, P = V + kL * RSV, PP = kL * RSP;
+    static constexpr int TAB = P + Tr::NP * PP;       // g^0 .. g^64, in g^0 .. in g^64, then X's and v's weights by row
+    static constexpr int BYTES = TAB + (2 * 68 + 2 * kL) * 4;
+    static constexpr int UQ = DK * ES / 16 / NW > 0 ? DK * ES / 16 / NW : 1;   // 16-byte pieces of q and k a thread moves
+    static constexpr int UV = ES;                                             // of v
+};
+
+// 16 bytes of a row, `left` elements of which exist; zeros behind them.
+template <class T>
+CB_DEV uint4 la_load16(const T* p, int left, bool vec) {
+    constexpr int VE = 16 / sizeof(T);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (left <= 0) return v;
+    if (vec) return *reinterpret_cast<const uint4*>(p);
+    T x[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) x[i] = i < left ? p[i] : T(0);
+    __builtin_memcpy(&v, x, 16);
+    return v;
+}
+
+// f(j, column -> v_j there) for the rows of v's fragments: one lane's own column from whichever lane holds row j of it.
+template <class Tr, int NJ, class F>
+CB_DEV void la_each_row(const typename Tr::Frag (&fv)[NJ], F&& f) {
+#pragma unroll
+    for (int jb = 0; jb < NJ; ++jb) {
+        float x[Tr::KPL];
+        Tr::unpack(fv[jb], x);
+        for (int gj = 0; gj < 4; ++gj)
+#pragma unroll
+            for (int u = 0; u < Tr::KPL; ++u)
+                f(jb * Tr::KB + Tr::KPL * gj + u, [&](int col) { return __shfl(x[u], 16 * gj + col); });
+    }
+}
+
+template <class Tr, int DK, int NW, bool STATE>
+__global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0) {
+    using T = typename Tr::T;
+    using Frag = typename Tr::Frag;
+    using L = LaTile<Tr, DK, NW>;
+    constexpr int VE = 16 / sizeof(T), KB = Tr::KB, KPL = Tr::KPL, NT = DK / 16, NJ = kL / KB;
+    extern __shared__ __align__(16) unsigned char lds[];
+    float* pw = reinterpret_cast<float*>(lds + L::TAB);
+    float* pin = pw + 68;
+    float* xw = pin + 68;      // [c_i = 0] g^(i+l)
+    float* vw = xw + kL;       // [c_j = c] in g^(n-l-j)
+
+    const int y = y0 + blockIdx.y;
+    const LaPass& P = a.pass[y];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int nbs = (P.dv + 16 * NW - 1) / (16 * NW);
+    const int64_t EH = int64_t(a.E) * a.H;
+    const int64_t id = blockIdx.x / nbs;
+    const int nb0 = int(blockIdx.x % nbs) * 16 * NW, n0 = nb0 + 16 * wave;   // columns of the workgroup, of the wave
+    const int seg = int(id / EH);
+    const int64_t eh = id % EH, e = eh / a.H, h = eh % a.H;
+    const int p0 = seg * sg.chunks * kL;
+    const int p1 = sg.segs == 1 ? a.T : int(min(int64_t(a.T), int64_t(p0) + int64_t(sg.chunks) * kL));
+
+    const int64_t dir = P.back ? -1 : 1, t0 = P.back ? a.T - 1 - p0 : p0;
+    const int64_t qs = dir * P.q.t, ks = dir * P.k.t, vs = dir * P.v.t, os = dir * P.o.t;
+    const T* q = static_cast<const T*>(P.q.p) + e * P.q.e + h * P.q.h + t0 * P.q.t;
+    const T* k = static_cast<const T*>(P.k.p) + e * P.k.e + h * P.k.h + t0 * P.k.t;
+    const T* v = static_cast<const T*>(P.v.p) + e * P.v.e + h * P.v.h + t0 * P.v.t;
+    T* o = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h + t0 * P.o.t;
+    const uint8_t* dn = a.dones ? a.dones + e * a.d_e + t0 * a.d_t : nullptr;
+    const int64_t ds = dir * a.d_t;
+    const int later = P.back ? 0 : 1;
+
+    if (tid <= kL) {
+        const float w = float(exp(double(tid) * double(tid ? a.log_decay[h] : 0.f)));
+        pw[tid] = w;
+        pin[tid] = w * P.in;
+    }
+    if (!STATE && KB == 32) {   // products above the diagonal that a fragment of 32 rows takes along
+        for (int u = tid; u < 2 * 16 * Tr::NP * 4; u += 64 * NW) {
+            const int pl = u / (2 * 16 * 4), b = u / 64 % 2, i = u / 4 % 16, j = u % 4;
+            *reinterpret_cast<uint2*>(lds + L::P + pl * L::PP + (32 * b + i) * L::RSP + (32 * b + 16 + 4 * j) * L::ES) =
+                make_uint2(0, 0);
+        }
+    }
+
+    __syncthreads();
+    cb_f32x4 X[NT];
+    {
+        const float* x = P.x0 ? P.x0 + eh * P.dk * P.dv : nullptr;
+        int xk = P.xk, xn = P.xn;
+        if (STATE) x = nullptr;
+        else if (sg.segs > 1) { x = sg.state[y] + (seg * EH + eh) * P.dk * P.dv; xk = P.dv; xn = 1; }
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int kk = Tr::krow(m, g, r), n = n0 + c;
+                X[m][r] = x && kk < P.dk && n < P.dv ? x[kk * xk + n * xn] : 0.f;
+            }
+    }
+
+    // the chunk's q, k and v on their way to LDS: 16-byte pieces, 64 rows of CQ or CV of them
+    constexpr int CQ = DK * L::ES / 16, CV = 16 * NW * L::ES / 16;
+    uint4 rq[L::UQ], rk[L::UQ], rv[L::UV];
+    bool rd = false;
+    auto fetch = [&](int n) {
+#pragma unroll
+        for (int u = 0; u < L::UQ; ++u) {
+            const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ * VE;
+            const int left = row < n ? P.dk - col : 0;
+            if (!STATE) rq[u] = la_load16(q + row * qs + col, left, P.vec & 1);
+            rk[u] = la_load16(k + row * ks + col, left, P.vec & 2);
+        }
+#pragma unroll
+        for (int u = 0; u < L::UV; ++u) {
+            const int id2 = tid + 64 * NW * u, row = id2 / CV, col = nb0 + id2 % CV * VE;
+            rv[u] = la_load16(v + row * vs + col, row < n ? P.dv - col : 0, P.vec & 4);
+        }
+        rd = dn && lane < n && dn[lane * ds];
+    };
+    const int ob = n0 + 4 * g;   // this lane's four columns of o
+    float factor = 1.f;
+    fetch(min(kL, p1 - p0));
+    for (int p = p0; p < p1; p += kL) {
+        const int n = min(kL, p1 - p);
+#pragma unroll
+        for (int u = 0; u < L::UQ; ++u) {
+            const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ;
+            if (row < kL) {
+                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + col * 16) = rq[u];
+                *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + col * 16) = rk[u];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < L::UV; ++u) {
+            const int id2 = tid + 64 * NW * u, row = id2 / CV, col = id2 % CV;
+            *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + col * 16) = rv[u];
+        }
+        const uint64_t m = __ballot(rd);
+        // episode starts before what row i holds
+        auto count = [&](int i) { return __popcll(P.back ? m & ((uint64_t(1) << i) - 1) : m & (~uint64_t(0) >> (63 - i))); };
+        const int total = __popcll(m);
+        if (wave == 0) {
+            const int ci = count(lane);
+            xw[lane] = ci == 0 ? pw[lane + later] : 0.f;
+            vw[lane] = lane < n && ci == total ? pin[n - later - lane] : 0.f;
+        }
+        const float over = pw[n];
+        lds_barrier();
+        if (p + kL < p1) {
+            q += kL * qs; k += kL * ks; v += kL * vs;
+            if (dn) dn += kL * ds;
+            fetch(min(kL, p1 - p - kL));
+        }
+
+        if (!STATE) {   // in g^(i-j) q_i . k_j by tiles on and below the diagonal
+            for (int u = wave; u < 10; u += NW) {
+                const int b = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3, t = u - b * (b + 1) / 2;
+                cb_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kb = 0; kb < DK / KB; ++kb) {
+                    const Frag fk = *reinterpret_cast<const Frag*>(lds + L::K + (16 * t + c) * L::RSK + kb * 64 + 16 * g);
+                    const Frag fq = *reinterpret_cast<const Frag*>(lds + L::Q + (16 * b + c) * L::RSK + kb * 64 + 16 * g);
+                    d = Tr::mma(fk, fq, d);
+                }
+                const int i = 16 * b + c, j = 16 * t + 4 * g;
+                float x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = j + r <= i ? d[r] * pin[max(i - j - r, 0)] : 0.f;
+                if (m) {
+                    const int ci = count(i);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = count(j + r) == ci ? x[r] : 0.f;
+                }
+                Tr::store_p(lds + L::P + i * L::RSP + j * L::ES, L::PP, x);
+            }
+        }
+
+        Frag fv[NJ];
+#pragma unroll
+        for (int jb = 0; jb < NJ; ++jb) fv[jb] = Tr::template cols<1>(lds + L::V, L::RSV, jb * KB, 16 * wave);
+
+        cb_f32x4 O[4];
+        if (!STATE) {   // X^T q, columns i
+#pragma unroll
+            for (int b = 0; b < 4; ++b) O[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < DK / KB; ++kb) {
+                Frag fx[Tr::NX];
+                Tr::xfrag(X, kb, fx);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const Frag fq = *reinterpret_cast<const Frag*>(lds + L::Q + (16 * b + c) * L::RSK + kb * 64 + 16 * g);
+#pragma unroll
+                    for (int u = 0; u < Tr::NX; ++u) O[b] = Tr::mma(fx[u], fq, O[b]);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float w = xw[16 * b + c];
+                const bool cut = m && count(16 * b + c) != 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) O[b][r] = cut ? 0.f : O[b][r] * w;
+            }
+        }
+
+        {   // X <- over X + sum_j w_j k_j v_j^T
+            cb_f32x4 U[NT];
+            auto rows = [&](auto clean) CB_INLINE_LAMBDA {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) U[t] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int jb = 0; jb < NJ; ++jb) {
+                    float x[KPL];
+                    Tr::unpack(clean(fv[jb]), x);
+#pragma unroll
+                    for (int u = 0; u < KPL; ++u) x[u] *= vw[jb * KB + KPL * g + u];
+                    Frag fw[Tr::NV];
+                    Tr::split(x, fw);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const Frag fk = clean(Tr::kcols(lds + L::K, L::RSK, jb * KB, t));
+#pragma unroll
+                        for (int u = Tr::NV - 1; u >= 0; --u) U[t] = Tr::mma(fk, fw[u], U[t]);
+                    }
+                }
+            };
+            rows([](Frag f) { return f; });
+            float sum = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sum += (U[t][0] + U[t][1]) + (U[t][2] + U[t][3]);
+            // A number that is not finite comes through a weight of zero as NaN. Then without all such, and theirs added
+            // for the rows that the state sees.
+            if (__any(sum != sum)) {
+                rows([](Frag f) { return Tr::finite(f); });
+                la_each_row<Tr>(fv, [&](int j, auto vat) {
+                    const float x = vat(c), w = vw[j] * x;
+                    if (j >= n || count(j) != total) return;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float kk = Tr::load(*reinterpret_cast<const T*>(lds + L::K + j * L::RSK +
+                                                                                  Tr::krow(t, g, r) * L::ES));
+                            if (!isfinite(x) || !isfinite(kk)) U[t][r] += w * kk;
+                        }
+                });
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) X[t][r] = (total ? 0.f : over * X[t][r]) + U[t][r];
+            if (STATE) factor = total || factor < 0.f ? -1.f : factor * over;
+        }
+        lds_barrier();
+
+        if (!STATE) {   // sum over j of the products with v
+            cb_f32x4 A[4];
+            auto rows = [&](auto clean) CB_INLINE_LAMBDA {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    A[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int jb = 0; jb < NJ; ++jb) {
+                        if (jb * KB > 16 * b + 15) continue;
+#pragma unroll
+                        for (int u = Tr::NP - 1; u >= 0; --u) {
+                            const Frag fp = *reinterpret_cast<const Frag*>(lds + L::P + u * L::PP + (16 * b + c) * L::RSP +
+                                                                           jb * 64 + 16 * g);
+                            A[b] = Tr::mma(clean(fv[jb]), fp, A[b]);
+                        }
+                    }
+                }
+            };
+            rows([](Frag f) { return f; });
+            float sum = 0.f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) sum += (A[b][0] + A[b][1]) + (A[b][2] + A[b][3]);
+            if (__any(sum != sum)) {   // as above: a later row's, or one's of another episode
+                rows([](Frag f) { return Tr::finite(f); });
+                la_each_row<Tr>(fv, [&](int j, auto vat) {
+                    float x[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = vat(4 * g + r);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int i = 16 * b + c;
+                        if (j > i || count(j) != count(i)) continue;
+                        float w = 0.f;
+#pragma unroll
+                        for (int u = 0; u < Tr::NP; ++u)
+                            w += Tr::load(*reinterpret_cast<const T*>(lds + L::P + u * L::PP + i * L::RSP + j * L::ES));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (!isfinite(x[r])) A[b][r] += w * x[r];
+                    }
+                });
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int i = 16 * b + c;
+                if (i >= n || ob >= P.dv) continue;
+                T* po = o + i * os + ob;
+                float x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = (O[b][r] + A[b][r]) * P.out;
+                if (P.vec & 8) Tr::store4o(po, x);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (ob + r < P.dv) po[r] = Tr::store(x[r]);
+            }
+            o += kL * os;
+        }
+    }
+
+    float* x = STATE ? sg.state[y] + (seg * EH + eh) * P.dk * P.dv : seg == sg.segs - 1 && P.x1 ? P.x1 + eh * P.dk * P.dv : nullptr;
+    if (x) {
+        const int xk = STATE ? P.dv : P.xk, xn = STATE ? 1 : P.xn;
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int kk = Tr::krow(m, g, r), n = n0 + c;
+                if (kk < P.dk && n < P.dv) x[kk * xk + n * xn] = X[m][r];
+            }
+    }
+    if (STATE && tid == 0 && nb0 == 0) sg.factor[y][seg * EH + eh] = factor;
+}
+
+// The states before the segments, in place of their contributions.
+__global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, LaSegs sg) {
+    const LaPass& P = a.pass[blockIdx.y];
+    const int64_t EH = int64_t(a.E) * a.H, S = int64_t(P.dk) * P.dv, i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= EH * S) return;
+    const int64_t eh = i / S;
+    const int kn = int(i - eh * S);
+    float x = P.x0 ? P.x0[eh * S + int64_t(kn / P.dv) * P.xk + int64_t(kn % P.dv) * P.xn] : 0.f;
+    float* st = sg.state[blockIdx.y] + i;
+    const float* f = sg.factor[blockIdx.y] + eh;
+    for (int s = 0; s + 1 < sg.segs; ++s) {
+        const float u = st[s * EH * S], w = f[s * EH];
+        st[s * EH * S] = x;
+        x = (w < 0.f ? 0.f : w * x) + u;
+    }
+    st[(sg.segs - 1) * EH * S] = x;
+}
+
+template <class Tr, int DK, int NW>
+hipError_t la_chunks_launch(const LaArgs& a, const LaSegs& sg, int y0, int ny, bool state, hipStream_t s) {
+    using L = LaTile<Tr, DK, NW>;
+    const int64_t nbs = (a.pass[y0].dv + 16 * NW - 1) / (16 * NW);
+    const dim3 grid(unsigned(int64_t(a.E) * a.H * nbs * (state ? sg.segs - 1 : sg.segs)), unsigned(ny));
+    if (state) hipLaunchKernelGGL((la_chunk_kernel<Tr, DK, NW, true>), grid, dim3(64 * NW), L::BYTES, s, a, sg, y0);
+    else hipLaunchKernelGGL((la_chunk_kernel<Tr, DK, NW, false>), grid, dim3(64 * NW), L::BYTES, s, a, sg, y0);
+    return hipGetLastError();
+}
+
+int la_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+template <class Tr, int DK>
+hipError_t la_chunks_nw(const LaArgs& a, const LaSegs& sg, int y0, int ny, bool state, hipStream_t s) {
+    switch (la_dim(a.pass[y0].dv)) {
+        case 32: return la_chunks_launch<Tr, DK, 2>(a, sg, y0, ny, state, s);
+        case 64: return la_chunks_launch<Tr, DK, 4>(a, sg, y0, ny, state, s);
+        default: return la_chunks_launch<Tr, DK, 8>(a, sg, y0, ny, state, s);
+    }
+}
+
+// Passes whose kernels are the same go in one launch.
+template <class Tr>
+hipError_t la_chunks(const LaArgs& a, const LaSegs& sg, bool state, hipStream_t s) {
+    for (int y = 0, ny; y < a.np; y += ny) {
+        for (ny = 1; y + ny < a.np && la_dim(a.pass[y + ny].dk) == la_dim(a.pass[y].dk) &&
+                     la_dim(a.pass[y + ny].dv) == la_dim(a.pass[y].dv); ++ny) {}
+        hipError_t e;
+        switch (la_dim(a.pass[y].dk)) {
+            case 32: e = la_chunks_nw<Tr, 32>(a, sg, y, ny, state, s); break;
+            case 64: e = la_chunks_nw<Tr, 64>(a, sg, y, ny, state, s); break;
+            default: e = la_chunks_nw<Tr, 128>(a, sg, y, ny, state, s); break;
+        }
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+constexpr int kLaSteps = 16;   // rollouts up to here go row by row
+
+// Segments of the rollout that run at once: as many as give the chip 512 workgroups, of two chunks at least.
+int la_segs(int T, int64_t chains, int* chunks) {
+    const int64_t nc = (int64_t(T) + kL - 1) / kL;
+    *chunks = int(nc);
+    if (T <= kLaSteps || chains <= 0 || chains >= 256 || nc < 4) return 1;
+    const int64_t want = std::min<int64_t>((512 + chains - 1) / chains, nc / 2);
+    *chunks = int((nc + want - 1) / want);
+    return int((nc + *chunks - 1) / *chunks);
+}
+
+int64_t la_a256(int64_t b) { return (b + 255) / 256 * 256; }
+
 // No rows: the state goes through (a gradient too: nothing is between the two).
 __global__ void la_empty_kernel(const float* x0, float* x1, int64_t n) {
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256)
@@ -109,9 +634,14 @@ __global__ void la_empty_kernel(const float* x0, float* x1, int64_t n) {
 
 }  // namespace
 
-size_t linattn_ws_bytes(int, int, int, int, int, int, int) { return 0; }
+size_t linattn_ws_bytes(int, int T, int E, int H, int dk, int dv, int passes) {
+    int chunks;
+    const int64_t EH = int64_t(E) * H, segs = la_segs(T, EH * passes, &chunks);
+    if (segs == 1) return 0;
+    return size_t(passes * (la_a256(segs * EH * dk * dv * 4) + la_a256(segs * EH * 4)));
+}
 
-hipError_t linattn(int prec, LaArgs a, void*, hipStream_t s) {
+hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     if (int64_t(a.E) * a.H == 0) return hipSuccess;
     if (a.T == 0) {
         for (int y = 0; y < a.np; ++y) {
@@ -127,7 +657,32 @@ hipError_t linattn(int prec, LaArgs a, void*, hipStream_t s) {
         return cb_key("linattn", prec, std::to_string(a.T) + "x" + std::to_string(a.E) + "x" + std::to_string(a.H) + "x" +
                                            cb_dims(a.pass[0].dk, a.pass[0].dv) + (a.np > 1 ? "/bwd" : ""));
     });
-    return prec == 0 ? la_steps<PrecBF16>(a, s) : la_steps<PrecF32>(a, s);
+    if (a.T <= kLaSteps) return prec == 0 ? la_steps<PrecBF16>(a, s) : la_steps<PrecF32>(a, s);
+    const int es = prec == 0 ? 2 : 4, ve = 16 / es;
+    auto whole = [&](const LaView& v, int d, int k) {   // rows of whole pieces of k elements, at their alignment
+        return reinterpret_cast<uintptr_t>(v.p) % (k * es) == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && d % k == 0;
+    };
+    LaSegs sg{};
+    const int64_t EH = int64_t(a.E) * a.H;
+    sg.segs = la_segs(a.T, EH * a.np, &sg.chunks);
+    char* w = static_cast<char*>(ws);
+    for (int y = 0; y < a.np; ++y) {
+        LaPass& P = a.pass[y];
+        P.vec = whole(P.q, P.dk, ve) | whole(P.k, P.dk, ve) << 1 | whole(P.v, P.dv, ve) << 2 | whole(P.o, P.dv, 4) << 3;
+        if (sg.segs == 1) continue;
+        sg.state[y] = reinterpret_cast<float*>(w);
+        w += la_a256(sg.segs * EH * P.dk * P.dv * 4);
+        sg.factor[y] = reinterpret_cast<float*>(w);
+        w += la_a256(sg.segs * EH * 4);
+    }
+    auto run = [&](bool state) { return prec == 0 ? la_chunks<LaB>(a, sg, state, s) : la_chunks<LaF>(a, sg, state, s); };
+    if (sg.segs > 1) {
+        hipError_t e = run(true);
+        if (e != hipSuccess) return e;
+        const int64_t n = EH * a.pass[0].dk * a.pass[0].dv;
+        hipLaunchKernelGGL(la_scan_kernel, dim3(unsigned((n + 255) / 256), unsigned(a.np)), dim3(256), 0, s, a, sg);
+    }
+    return run(false);
 }
 
 }  // namespace cb
