@@ -240,6 +240,54 @@ impala_status_t impala_linattn_step(const linattn_shape_t* shape, const void* q,
                                     const float* log_decay, const uint8_t* dones, const float* s_in, void* o,
                                     float* s_out, hipStream_t stream);
 
+/* What lies between two blocks of a residual network, in one pass: the norm after a block, its gate, its
+ * scale and the residual sum, and the norm before the next block. Per row of C channels
+ *   z = norm(h) gamma + beta,  out = res + rscale z act(gate),  out2 = norm2(out) gamma2 + beta2,
+ * out2 of out as it is stored. norm over each of the row's `groups` equal groups of channels (a head's
+ * channels, say), norm2 over the whole row: IMPALA_NORM_NONE x, _LAYER (x - mean) / sqrt(var + eps),
+ * _RMS x / sqrt(mean(x^2) + eps). act: gate itself, gate / (1 + exp(-gate)) or 1 / (1 + exp(-gate)).
+ * Left out where NULL: gamma, rscale, gamma2 (1), beta, beta2, res (0), gate (act = 1), out2 with its norm.
+ * So a norm before a block is h, gamma -> out alone; a block without a norm after it has norm NONE.
+ * h, gate, res, out, out2: [n, C] in the storage type with row strides ld_* in elements (>= C; read only
+ * for arrays that are there). gamma, beta, rscale, gamma2, beta2: float [C]. Statistics are float32, a
+ * mean's first, then the squares about it. n >= 0; 1 <= C <= 8192 (more: IMPALA_EUNSUPPORTED), any size;
+ * groups divides C, and is 1 where out2 is there (else IMPALA_EUNSUPPORTED). eps >= 0. Addresses aligned
+ * to an element. An output may be one of h, gate and res itself (same address and stride); any other
+ * overlap of address ranges is IMPALA_EINVAL. */
+typedef enum { IMPALA_NORM_NONE = 0, IMPALA_NORM_LAYER = 1, IMPALA_NORM_RMS = 2 } impala_norm_t;
+typedef enum { IMPALA_GATE_LINEAR = 0, IMPALA_GATE_SILU = 1, IMPALA_GATE_SIGMOID = 2 } impala_gate_t;
+typedef struct blocknorm_shape {
+    int32_t prec;              /* impala_prec_t */
+    int32_t C, groups;
+    int32_t norm, norm2;       /* impala_norm_t */
+    int32_t gate_act;          /* impala_gate_t */
+    float eps;
+    int64_t n;
+    int64_t ld_h, ld_gate, ld_res, ld_out, ld_out2;
+    int64_t ld_dout, ld_dout2, ld_dh, ld_dgate, ld_dres;   /* impala_blocknorm_bwd */
+} blocknorm_shape_t;
+impala_status_t impala_blocknorm_fwd(const blocknorm_shape_t* shape, const void* h, const float* gamma,
+                                     const float* beta, const void* gate, const float* rscale, const void* res,
+                                     void* out, const float* gamma2, const float* beta2, void* out2,
+                                     hipStream_t stream);
+
+/* Backward of it from dout (at out) and dout2 (at out2; NULL where the forward had none; dout may be NULL,
+ * zero, where dout2 is there), with the forward's h, gate and, for dout2, its out. With xh the normalised
+ * rows and <.> a mean over a group:
+ *   ds = dout + norm2'(dout2 gamma2),  dgamma2 = sum dout2 xh2,  dbeta2 = sum dout2,  dres = ds,
+ *   drscale = sum ds z act,  dgate = ds rscale z act'(gate),  dz = ds rscale act,
+ *   dgamma = sum dz xh,  dbeta = sum dz,  dh = rstd (g - <g> - xh <g xh>) of g = dz gamma (RMS: no <g>).
+ * dh is required, the other gradients may be NULL where not wanted; dgate needs gate. Sums over rows are
+ * float [C], overwritten (zero for n = 0). An output may be one of dout, dout2, h, gate and out itself.
+ * ws: impala_blocknorm_bwd_workspace_bytes() bytes, 16-byte aligned. */
+size_t impala_blocknorm_bwd_workspace_bytes(const blocknorm_shape_t* shape);
+impala_status_t impala_blocknorm_bwd(const blocknorm_shape_t* shape, const void* dout, const void* dout2,
+                                     const void* h, const float* gamma, const float* beta, const void* gate,
+                                     const float* rscale, const void* out, const float* gamma2, void* dh,
+                                     float* dgamma, float* dbeta, void* dgate, float* drscale, void* dres,
+                                     float* dgamma2, float* dbeta2, void* ws, size_t ws_bytes,
+                                     hipStream_t stream);
+
 /* Where a training-mode impala_cnn_fwd on n_frames frames (workspace laid out by
  * impala_workspace_bytes(net, n_frames, prec, 1)) leaves the activations that impala_cnn_bwd
  * reads, so a caller can inspect them or replace them between the two calls: the backward

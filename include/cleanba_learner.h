@@ -209,6 +209,29 @@ impala_status_t rmsprop_step(int64_t n_params, float* params, const float* grads
                              float lr, float decay, float eps, float max_grad_norm, float* stats,
                              void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* A gradient tensor of grad_clip: `count` numbers at src, whose clipped values go to dst. prec: impala_prec_t
+ * of each (bf16 or float32). dst may be src itself (same prec), or NULL: the tensor counts in the norm only. */
+typedef struct grad_tensor {
+    const void* src;
+    void* dst;
+    int64_t count;
+    int32_t src_prec, dst_prec;
+} grad_tensor_t;
+
+/* Global-norm clip over many tensors, for gradients that do not lie in one buffer (a trunk's and those of
+ * the layers around it): n = ||all src||_2 (squares summed in 64 bits), dst = src (max_grad_norm / n) if
+ * max_grad_norm > 0 and n > max_grad_norm, else dst = src, bit for bit where the types are the same. With
+ * dst in a flat float32 buffer it gathers what adam_step and the others step (with their own
+ * max_grad_norm <= 0).
+ * tensors: HOST array of n_tensors >= 0 entries (at most 65536), not kept; empty ones are passed over; a
+ * src that is listed twice counts twice. A dst must not overlap another entry's src or dst, nor its own
+ * src in part. Addresses aligned to an element. stats (device, float [2] or NULL): [norm, 1 if the norm is
+ * not finite]; tensors with NaN are not clipped, with infinities they are scaled by zero (NaN and zeros).
+ * ws: device scratch of grad_clip_workspace_bytes() bytes, 8-byte aligned; the query reads counts only. */
+size_t grad_clip_workspace_bytes(const grad_tensor_t* tensors, int32_t n_tensors);
+impala_status_t grad_clip(const grad_tensor_t* tensors, int32_t n_tensors, float max_grad_norm, float* stats,
+                          void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Orthogonalised matrices: y = the polynomial iteration of Newton and Schulz on each x,
  *   X_0 = x / max(||x||_F, eps),  X_k = a_k X + (b_k A + c_k A^2) X with A = X X^T,  y = X_steps,
  * which moves every singular value towards one and keeps the singular vectors (the update of the

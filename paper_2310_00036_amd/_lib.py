@@ -19,6 +19,8 @@ LEARNER_OPT_ADAM, LEARNER_OPT_RMSPROP, LEARNER_OPT_MUON = 0, 1, 2
 MUON_SCALE_SPECTRAL, MUON_SCALE_RMS = 0, 1
 X_PLAIN, X_RELU, X_U8 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+GATE_LINEAR, GATE_SILU, GATE_SIGMOID = 0, 1, 2
 STATUS = {0: "OK", -1: "EINVAL", -2: "EWORKSPACE", -3: "EUNSUPPORTED", -4: "EHIP"}
 
 
@@ -75,6 +77,17 @@ class LinattnShape(C.Structure):
                  ("dv", C.c_int32), ("scale", C.c_float)] +
                 [(x, LinattnStrides) for x in ("q", "k", "v", "o", "gq", "gk", "gv")] +
                 [("done_t", C.c_int64), ("done_e", C.c_int64)])
+
+
+class BlocknormShape(C.Structure):
+    _fields_ = ([(x, C.c_int32) for x in ("prec", "C", "groups", "norm", "norm2", "gate_act")] +
+                [("eps", C.c_float), ("n", C.c_int64)] +
+                [("ld_" + x, C.c_int64) for x in ("h", "gate", "res", "out", "out2", "dout", "dout2", "dh", "dgate", "dres")])
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("count", C.c_int64), ("src_prec", C.c_int32),
+                ("dst_prec", C.c_int32)]
 
 
 class Rollout(C.Structure):
@@ -144,6 +157,11 @@ _SIGS = {
     "impala_linattn_bwd": (C.c_int, [C.POINTER(LinattnShape), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ,
                                      _P]),
     "impala_linattn_step": (C.c_int, [C.POINTER(LinattnShape), _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "impala_blocknorm_fwd": (C.c_int, [C.POINTER(BlocknormShape)] + [_P] * 11),
+    "impala_blocknorm_bwd_workspace_bytes": (_SZ, [C.POINTER(BlocknormShape)]),
+    "impala_blocknorm_bwd": (C.c_int, [C.POINTER(BlocknormShape)] + [_P] * 18 + [_SZ, _P]),
+    "grad_clip_workspace_bytes": (_SZ, [C.POINTER(GradTensor), _I32]),
+    "grad_clip": (C.c_int, [C.POINTER(GradTensor), _I32, _F, _P, _P, _SZ, _P]),
     "impala_gumbel_sample": (C.c_int, [_I64, _I32, _P, _P, _P, _P, _P]),
     "impala_action_logp": (C.c_int, [_I64, _I32, _P, _P, _P, _P]),
     "impala_profile_begin": (C.c_int, [C.c_char_p, _I32]),
@@ -584,6 +602,62 @@ def impala_linattn_step(shape: LinattnShape, q, k, v, log_decay, dones, s_in, o,
     _check("impala_linattn_step", lib.impala_linattn_step(
         C.byref(shape), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s_in), _at(o), ptr(s_out),
         stream_handle(stream)))
+
+
+def blocknorm_shape(prec, n, C_, groups=1, norm=NORM_RMS, norm2=NORM_NONE, gate_act=GATE_LINEAR, eps=1e-5,
+                    **ld) -> BlocknormShape:
+    """Sizes and kinds of the block norm; row strides of C_ elements but for those given as ld_h=..., ld_gate=... ."""
+    s = BlocknormShape(prec, C_, groups, norm, norm2, gate_act, eps, n)
+    for name, _ in BlocknormShape._fields_[8:]:
+        setattr(s, name, ld.pop(name, C_))
+    if ld:
+        raise ValueError(f"unknown row strides {sorted(ld)}")
+    return s
+
+
+def impala_blocknorm_fwd(shape: BlocknormShape, h, gamma, beta, gate, rscale, res, out, gamma2=None, beta2=None,
+                         out2=None, stream=None):
+    _check("impala_blocknorm_fwd", lib.impala_blocknorm_fwd(
+        C.byref(shape), _at(h), ptr(gamma), ptr(beta), _at(gate), ptr(rscale), _at(res), _at(out), ptr(gamma2), ptr(beta2),
+        _at(out2), stream_handle(stream)))
+
+
+def impala_blocknorm_bwd_workspace_bytes(shape: BlocknormShape) -> int:
+    return int(lib.impala_blocknorm_bwd_workspace_bytes(C.byref(shape)))
+
+
+def impala_blocknorm_bwd(shape: BlocknormShape, dout, dout2, h, gamma, beta, gate, rscale, out, gamma2, dh, dgamma, dbeta,
+                         dgate, drscale, dres, dgamma2, dbeta2, ws, stream=None):
+    _check("impala_blocknorm_bwd", lib.impala_blocknorm_bwd(
+        C.byref(shape), _at(dout), _at(dout2), _at(h), ptr(gamma), ptr(beta), _at(gate), ptr(rscale), _at(out), ptr(gamma2),
+        _at(dh), ptr(dgamma), ptr(dbeta), _at(dgate), ptr(drscale), _at(dres), ptr(dgamma2), ptr(dbeta2), *_ws_args(ws),
+        stream_handle(stream)))
+
+
+def grad_tensors(pairs):
+    """The host array that grad_clip takes, from a sequence of (src, dst): contiguous tensors, bfloat16 or float32, of
+    equal sizes; dst may be src, or None (it counts in the norm only)."""
+    import torch
+    precs = {torch.bfloat16: PREC_BF16, torch.float32: PREC_FP32}
+    pairs = list(pairs)
+    out = (GradTensor * max(1, len(pairs)))()
+    out.used = len(pairs)
+    for e, (s, d) in zip(out, pairs):
+        d_ = s if d is None else d
+        if s.dtype not in precs or d_.dtype not in precs or s.numel() != d_.numel():
+            raise ValueError("grad_tensors: bfloat16 or float32 tensors, src and dst of one size")
+        e.src, e.dst, e.count, e.src_prec, e.dst_prec = ptr(s), ptr(d), s.numel(), precs[s.dtype], precs[d_.dtype]
+    return out
+
+
+def grad_clip_workspace_bytes(tensors) -> int:
+    return int(lib.grad_clip_workspace_bytes(tensors, tensors.used))
+
+
+def grad_clip(tensors, max_grad_norm, stats, ws, stream=None):
+    """tensors: grad_tensors(...)."""
+    _check("grad_clip", lib.grad_clip(tensors, tensors.used, max_grad_norm, ptr(stats), *_ws_args(ws),
+                                      stream_handle(stream)))
 
 
 def impala_gumbel_sample(n, A, logits, gumbel, actions, logp, stream=None):

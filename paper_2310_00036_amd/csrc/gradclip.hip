@@ -1,0 +1,211 @@
+// The global norm over many gradient tensors and their clipped values. HBM-bound: every source is read once for the norm
+// and once more for the values (from the caches where it fits them), every target written once. The tensors go by tables
+// in the kernels' arguments, so that a call is two launches for up to kGcTable of them and copies nothing to the device.
+#include <algorithm>
+
+#include "common.h"
+#include "gradclip.h"
+#include "kernels.h"
+
+namespace cb {
+
+namespace {
+
+constexpr int kGcTable = 96;       // tensors of a launch
+constexpr int kGcSeg = 8192;       // elements a workgroup takes at a time
+constexpr int kGcBlocks = 1024;    // workgroups of a launch, each with one partial sum
+
+struct GcEntry {
+    const void* src;
+    void* dst;
+    int64_t n;
+    int32_t first;                 // its first segment in the launch
+    int32_t type;                  // bit 0: src float32, bit 1: dst float32
+};
+struct GcTable {
+    GcEntry e[kGcTable];
+    int n, segs;
+};
+
+// 16 bytes at any alignment of an element: global memory takes them so.
+typedef uint32_t gc_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+
+// f(entry, first element, elements) for this workgroup's segments.
+template <class F>
+CB_DEV void gc_segments(const GcTable& t, F&& f) {
+    for (int s = blockIdx.x; s < t.segs; s += gridDim.x) {
+        int lo = 0, hi = t.n - 1;
+        while (lo < hi) {   // the last entry that starts at or before s
+            const int mid = (lo + hi + 1) / 2;
+            if (t.e[mid].first <= s) lo = mid; else hi = mid - 1;
+        }
+        const GcEntry& e = t.e[lo];
+        const int64_t at = int64_t(s - e.first) * kGcSeg;
+        f(e, at, int(min(int64_t(kGcSeg), e.n - at)));
+    }
+}
+
+// Eight elements of a source as floats, `left` of which exist.
+CB_DEV void gc_load8(const GcEntry& e, int64_t i, int left, float* x) {
+    if (e.type & 1) {
+        const float* p = static_cast<const float*>(e.src) + i;
+        if (left >= 8) {
+            const gc_u32x4 a = *reinterpret_cast<const gc_u32x4*>(p), b = *reinterpret_cast<const gc_u32x4*>(p + 4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { x[u] = __uint_as_float(a[u]); x[4 + u] = __uint_as_float(b[u]); }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = u < left ? p[u] : 0.f;
+        }
+    } else {
+        const uint16_t* p = static_cast<const uint16_t*>(e.src) + i;
+        if (left >= 8) {
+            const gc_u32x4 a = *reinterpret_cast<const gc_u32x4*>(p);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { x[2 * u] = bf_lo(a[u]); x[2 * u + 1] = bf_hi(a[u]); }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = u < left ? bf2f(p[u]) : 0.f;
+        }
+    }
+}
+
+CB_DEV void gc_store8(const GcEntry& e, int64_t i, int left, const float* x) {
+    if (e.type & 2) {
+        float* p = static_cast<float*>(e.dst) + i;
+        if (left >= 8) {
+            gc_u32x4 a, b;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { a[u] = __float_as_uint(x[u]); b[u] = __float_as_uint(x[4 + u]); }
+            *reinterpret_cast<gc_u32x4*>(p) = a;
+            *reinterpret_cast<gc_u32x4*>(p + 4) = b;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (u < left) p[u] = x[u];
+        }
+    } else {
+        uint16_t* p = static_cast<uint16_t*>(e.dst) + i;
+        if (left >= 8) {
+            gc_u32x4 a;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) a[u] = pack2bf(x[2 * u], x[2 * u + 1]);
+            *reinterpret_cast<gc_u32x4*>(p) = a;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (u < left) p[u] = f2bf(x[u]);
+        }
+    }
+}
+
+// Squares are summed in 64 bits: a float32 number's square fits them, whatever its size.
+__global__ __launch_bounds__(256) void gc_norm_kernel(GcTable t, double* part) {
+    __shared__ double sh[256];
+    double s = 0.0;
+    gc_segments(t, [&](const GcEntry& e, int64_t at, int n) {
+        for (int i = 8 * int(threadIdx.x); i < n; i += 8 * 256) {
+            float x[8];
+            gc_load8(e, at + i, n - i, x);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += double(x[u]) * x[u];
+        }
+    });
+    const double tot = block_sum<256>(s, sh);
+    if (threadIdx.x == 0) part[blockIdx.x] = tot;
+}
+
+CB_DEV double gc_total(const double* part, int nparts, double* sh) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < nparts; i += 256) s += part[i];
+    return block_sum<256>(s, sh);
+}
+
+// Many partial sums to one, where they are of several launches.
+__global__ __launch_bounds__(256) void gc_sum_kernel(const double* part, int nparts, double* total) {
+    __shared__ double sh[256];
+    const double s = gc_total(part, nparts, sh);
+    if (threadIdx.x == 0) *total = s;
+}
+
+__global__ __launch_bounds__(256) void gc_scale_kernel(GcTable t, const double* part, int nparts, float max_norm, float* stats) {
+    __shared__ double sh[256];
+    const double norm = sqrt(gc_total(part, nparts, sh));
+    if (stats && blockIdx.x == 0 && threadIdx.x == 0) {
+        stats[0] = float(norm);
+        stats[1] = isfinite(norm) ? 0.f : 1.f;
+    }
+    const bool clip = max_norm > 0.f && norm > double(max_norm);
+    const float f = clip ? float(double(max_norm) / norm) : 1.f;
+    gc_segments(t, [&](const GcEntry& e, int64_t at, int n) {
+        if (!e.dst || (!clip && e.dst == e.src)) return;
+        for (int i = 8 * int(threadIdx.x); i < n; i += 8 * 256) {
+            float x[8];
+            gc_load8(e, at + i, n - i, x);
+            if (clip)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] *= f;
+            gc_store8(e, at + i, n - i, x);
+        }
+    });
+}
+
+// Fills a table with tensors from i on; returns the next tensor. Empty ones are passed over.
+int gc_fill(GcTable& t, const grad_tensor_t* g, int i, int n) {
+    t.n = 0;
+    int64_t segs = 0;
+    for (; i < n && t.n < kGcTable; ++i) {
+        if (g[i].count == 0) continue;
+        const int64_t k = (g[i].count + kGcSeg - 1) / kGcSeg;
+        if (t.n > 0 && segs + k > (int64_t(1) << 30)) break;
+        t.e[t.n++] = GcEntry{g[i].src, g[i].dst, g[i].count, int32_t(segs),
+                             (g[i].src_prec == IMPALA_PREC_FP32 ? 1 : 0) | (g[i].dst_prec == IMPALA_PREC_FP32 ? 2 : 0)};
+        segs += k;
+    }
+    t.segs = int(segs);
+    return i;
+}
+
+int gc_blocks(const GcTable& t) { return std::min(t.segs, kGcBlocks); }
+
+}  // namespace
+
+size_t grad_clip_ws_bytes(const grad_tensor_t* g, int n) {
+    GcTable t;
+    int64_t parts = 1;
+    for (int i = 0; i < n;) {
+        i = gc_fill(t, g, i, n);
+        parts += gc_blocks(t);
+    }
+    return size_t(parts) * sizeof(double);
+}
+
+hipError_t grad_clip_run(const grad_tensor_t* g, int n, float max_norm, float* stats, void* ws, hipStream_t s) {
+    double* total = static_cast<double*>(ws);
+    double* part = total + 1;
+    ProfScope ps(s, [&] { return "grad_clip/" + std::to_string(n); });
+    GcTable t;
+    int nparts = 0, launches = 0;
+    for (int i = 0; i < n;) {
+        i = gc_fill(t, g, i, n);
+        if (t.n == 0) break;
+        hipLaunchKernelGGL(gc_norm_kernel, dim3(unsigned(gc_blocks(t))), dim3(256), 0, s, t, part + nparts);
+        nparts += gc_blocks(t);
+        ++launches;
+    }
+    if (launches != 1) {
+        hipLaunchKernelGGL(gc_sum_kernel, dim3(1), dim3(256), 0, s, part, nparts, total);
+        part = total;
+        nparts = 1;
+    }
+    int done = 0;
+    for (int i = 0; i < n || done == 0; ++done) {
+        i = gc_fill(t, g, i, n);
+        if (t.n == 0 && done > 0) break;
+        hipLaunchKernelGGL(gc_scale_kernel, dim3(unsigned(std::max(1, gc_blocks(t)))), dim3(256), 0, s, t, part, nparts,
+                           max_norm, done == 0 ? stats : nullptr);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace cb

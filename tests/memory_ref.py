@@ -62,3 +62,90 @@ def assert_close(name, got, want, mag, terms, bf16, elem_bf16=None):
     norm = float((got - want).norm())
     limit = (2 * terms ** 0.5 * 2.0 ** -24 + rel) * float(mag.norm()) + (2.0 ** -8 * float(want.norm()) if out16 else 0.0)
     assert norm <= limit + 1e-37, (name, norm, limit)
+
+
+# ------------------------------------------------------------------------------- block norms
+
+
+def _act(g, kind):
+    """(act, slope) of a gate in 64 bits; kind 0 linear, 1 silu, 2 sigmoid."""
+    if kind == 0:
+        return g, torch.ones_like(g)
+    s = torch.sigmoid(g)
+    return (s, s * (1 - s)) if kind == 2 else (g * s, s * (1 + g * (1 - s)))
+
+
+def _rows(x, kind, eps, size):
+    """(xh, rstd, xh's magnitude) of x [n, G, cg]; kind 0 none, 1 layer, 2 rms. size: |x| with the rounded mean's."""
+    if kind == 0:
+        return x, torch.ones_like(x[..., :1]), size
+    if kind == 1:
+        size = size + size.mean(-1, keepdim=True)
+        x = x - x.mean(-1, keepdim=True)
+    r = 1 / torch.sqrt(x.square().mean(-1, keepdim=True) + eps)
+    return x * r, r, size * r
+
+
+def blocknorm(h, gamma, beta, gate, rscale, res, groups, kind, act, eps):
+    """(out, its magnitude), before out is rounded."""
+    n, C = h.shape
+    h = h.double()
+    xh, _, xm = _rows(h.reshape(n, groups, -1), kind, eps, h.abs().reshape(n, groups, -1))
+    z = xh.reshape(n, C) * gamma.double() + beta.double()
+    zm = xm.reshape(n, C) * gamma.double().abs() + beta.double().abs()
+    if gate is not None:
+        a = _act(gate.double(), act)[0]
+        z, zm = z * a, zm * a.abs()
+    z, zm = z * rscale.double(), zm * rscale.double().abs()
+    return (z, zm) if res is None else (z + res.double(), zm + res.double().abs())
+
+
+def blocknorm_second(out, gamma2, beta2, kind, eps):
+    x = out.double()[:, None]
+    xh, _, xm = _rows(x, kind, eps, x.abs())
+    return xh[:, 0] * gamma2.double() + beta2.double(), xm[:, 0] * gamma2.double().abs() + beta2.double().abs()
+
+
+def blocknorm_grads(dout, dout2, h, gamma, beta, gate, rscale, out, gamma2, groups, kind, kind2, act, eps):
+    """name -> (gradient, magnitude), by the formulas."""
+    n, C = h.shape
+    gamma, beta, rscale = gamma.double(), beta.double(), rscale.double()
+
+    def back(g, gm, xh, xm, r, kind):
+        if kind == 0:
+            return g, gm
+        m = lambda t: t.mean(-1, keepdim=True)   # noqa: E731
+        d, dm = g - xh * m(g * xh), gm + xm * m(gm * xm)
+        if kind == 1:
+            d, dm = d - m(g), dm + m(gm)
+        return r * d, r * dm
+
+    res = {}
+    ds = torch.zeros(n, C, dtype=torch.float64) if dout is None else dout.double()
+    dm = ds.abs()
+    if dout2 is not None:
+        x = out.double()
+        xh, r, xm = _rows(x, kind2, eps, x.abs())
+        d2 = dout2.double()
+        res["dgamma2"] = (d2 * xh).sum(0), (d2.abs() * xm).sum(0)
+        res["dbeta2"] = d2.sum(0), d2.abs().sum(0)
+        g, gm = back(d2 * gamma2.double(), d2.abs() * gamma2.double().abs(), xh, xm, r, kind2)
+        ds, dm = ds + g, dm + gm
+    res["dres"] = ds, dm
+    x = h.double().reshape(n, groups, -1)
+    xh, r, xm = _rows(x, kind, eps, x.abs())
+    z, zm = xh.reshape(n, C) * gamma + beta, xm.reshape(n, C) * gamma.abs() + beta.abs()
+    a, slope, am, sm = 1.0, None, 1.0, None
+    if gate is not None:
+        a, slope = _act(gate.double(), act)
+        am, sm = a.abs(), slope.abs() + (0 if act == 0 else a.abs())   # s (1 + g (1 - s)) may cancel
+    res["drscale"] = (ds * z * a).sum(0), (dm * zm * am).sum(0)
+    du, um = ds * rscale, dm * rscale.abs()
+    if gate is not None:
+        res["dgate"] = du * z * slope, um * zm * sm
+    dz, dzm = du * a, um * am
+    res["dgamma"] = (dz * xh.reshape(n, C)).sum(0), (dzm * xm.reshape(n, C)).sum(0)
+    res["dbeta"] = dz.sum(0), dzm.sum(0)
+    d, m = back((dz * gamma).reshape(x.shape), (dzm * gamma.abs()).reshape(x.shape), xh, xm, r, kind)
+    res["dh"] = d.reshape(n, C), m.reshape(n, C)
+    return res

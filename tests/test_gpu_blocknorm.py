@@ -1,0 +1,260 @@
+"""Block norms, forward and backward, against plain evaluations in 64 bits: all norms and gates, what may be left out,
+odd sizes, groups, row strides, in place, no rows."""
+import itertools
+
+import pytest
+import torch
+
+from tests import memory_ref as ref
+
+P = pytest.importorskip("paper_2310_00036_amd")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+PREC = {"bf16": P.PREC_BF16, "f32": P.PREC_FP32}
+# Roundings on the way to one element: the statistics' sums (8 in a thread, 10 shuffles or 16 waves' sums), twice, their
+# roots and products, the gate's exponential, and as many in the second norm.
+TERMS = 100
+
+#        n, C, groups
+SIZES = [(1, 1, 1), (3, 7, 1), (5, 64, 1), (4, 64, 8), (7, 60, 5), (2, 96, 96), (1, 40, 2), (130, 512, 8), (9, 513, 1),
+         (1000, 256, 1), (33, 1024, 1), (5, 1531, 1), (6, 2000, 4), (3, 4097, 1), (2, 8192, 1), (3, 8190, 2), (5000, 24, 3)]
+
+
+def make(n, C, ty, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)   # noqa: E731
+    x = {k: (0.4 + r(n, C)).to(TYPES[ty]) for k in ("h", "gate", "res", "out", "dout", "dout2")}
+    x.update(gamma=1 + 0.3 * r(C), beta=0.3 * r(C), rscale=0.5 + 0.2 * r(C), gamma2=1 + 0.3 * r(C), beta2=0.3 * r(C))
+    return x
+
+
+def dev(x):
+    return None if x is None else x.to(DEV)
+
+
+def shape_of(x, ty, groups, norm, norm2, act, eps=1e-5, **ld):
+    n, C = x["h"].shape
+    return P.blocknorm_shape(PREC[ty], n, C, groups, norm, norm2, act, eps, **ld)
+
+
+def run_forward(x, ty, groups, norm, norm2, act, two):
+    a = {k: dev(v) for k, v in x.items()}
+    out = torch.empty_like(a["h"])
+    out2 = torch.empty_like(out) if two else None
+    P.impala_blocknorm_fwd(shape_of(x, ty, groups, norm, norm2, act), a["h"], a["gamma"], a["beta"], a["gate"], a["rscale"],
+                           a["res"], out, a["gamma2"], a["beta2"], out2)
+    return out, out2
+
+
+def one(x, like, value):
+    return torch.full(like.shape[1:], value) if x is None else x
+
+
+def check_forward(x, ty, groups, norm, norm2, act, got):
+    h = x["h"]
+    want, mag = ref.blocknorm(h, one(x["gamma"], h, 1.0), one(x["beta"], h, 0.0), x["gate"], one(x["rscale"], h, 1.0),
+                              x["res"], groups, norm, act, 1e-5)
+    ref.assert_close("out", got[0], want, mag, TERMS, False, ty == "bf16")
+    if got[1] is not None:
+        want, mag = ref.blocknorm_second(got[0].cpu(), one(x["gamma2"], h, 1.0), one(x["beta2"], h, 0.0), norm2, 1e-5)
+        ref.assert_close("out2", got[1], want, mag, TERMS, False, ty == "bf16")
+
+
+NAMES = ("dh", "dgamma", "dbeta", "dgate", "drscale", "dres", "dgamma2", "dbeta2")
+
+
+def run_backward(x, ty, groups, norm, norm2, act, wanted=NAMES):
+    a = {k: dev(v) for k, v in x.items()}
+    n, C = x["h"].shape
+    o = {}
+    for k in NAMES:
+        rows = k in ("dh", "dgate", "dres")
+        o[k] = None if k not in wanted else torch.full((n, C) if rows else (C,), 9.0, device=DEV,
+                                                       dtype=TYPES[ty] if rows else torch.float32)
+    if x["gate"] is None:
+        o["dgate"] = None
+    if x["dout2"] is None:
+        o["dgamma2"] = o["dbeta2"] = None
+    s = shape_of(x, ty, groups, norm, norm2, act)
+    ws = torch.empty(P.impala_blocknorm_bwd_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    P.impala_blocknorm_bwd(s, a["dout"], a["dout2"], a["h"], a["gamma"], a["beta"], a["gate"], a["rscale"], a["out"],
+                           a["gamma2"], o["dh"], o["dgamma"], o["dbeta"], o["dgate"], o["drscale"], o["dres"], o["dgamma2"],
+                           o["dbeta2"], ws)
+    return o
+
+
+def check_backward(x, ty, groups, norm, norm2, act, got):
+    h = x["h"]
+    want = ref.blocknorm_grads(x["dout"], x["dout2"], h, one(x["gamma"], h, 1.0), one(x["beta"], h, 0.0), x["gate"],
+                               one(x["rscale"], h, 1.0), x["out"], one(x["gamma2"], h, 1.0), groups, norm, norm2, act, 1e-5)
+    for k, g in got.items():
+        if g is not None:
+            rows = k in ("dh", "dgate", "dres")
+            ref.assert_close(k, g, *want[k], TERMS + (0 if rows else h.shape[0]), False, ty == "bf16" and rows)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("size", SIZES)
+def test_sizes(size, ty):
+    """Everything on, with both kinds of norm; the second norm where the rows are whole."""
+    n, C, groups = size
+    for i, (norm, act) in enumerate(((P.NORM_LAYER, P.GATE_SILU), (P.NORM_RMS, P.GATE_SIGMOID))):
+        x = make(n, C, ty, seed=i)
+        two = groups == 1
+        norm2 = P.NORM_RMS if norm == P.NORM_LAYER else P.NORM_LAYER
+        check_forward(x, ty, groups, norm, norm2, act, run_forward(x, ty, groups, norm, norm2, act, two))
+        if not two:
+            x["dout2"] = None
+        check_backward(x, ty, groups, norm, norm2, act, run_backward(x, ty, groups, norm, norm2, act))
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("norm,norm2,act", itertools.product((0, 1, 2), (0, 1, 2), (0, 1, 2)))
+def test_kinds_and_what_is_left_out(norm, norm2, act, ty):
+    for i, gone in enumerate(((), ("gate",), ("res", "beta", "beta2"), ("gamma", "rscale", "gamma2"), ("gate", "rscale", "res"))):
+        for two in (False, True):
+            x = make(37, 200, ty, seed=20 + i)
+            x.update({k: None for k in gone})
+            check_forward(x, ty, 1, norm, norm2, act, run_forward(x, ty, 1, norm, norm2, act, two))
+            if not two:
+                x["dout2"] = None
+            elif i == 1:
+                x["dout"] = None
+            check_backward(x, ty, 1, norm, norm2, act, run_backward(x, ty, 1, norm, norm2, act))
+    x = make(37, 200, ty)
+    check_backward(x, ty, 1, norm, norm2, act, run_backward(x, ty, 1, norm, norm2, act, wanted=("dh", "dbeta")))
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("n,C,groups", [(6, 64, 4), (50, 130, 1), (3, 1100, 1)])
+def test_row_strides_and_in_place(n, C, groups, ty):
+    """Rows inside wider ones, odd offsets included, give the same bits and leave what lies between alone; so do outputs
+    that are an input itself."""
+    x = make(n, C, ty, seed=3)
+    two = groups == 1
+    if not two:
+        x["dout2"] = None
+    args = (ty, groups, P.NORM_LAYER, P.NORM_RMS, P.GATE_SILU)
+    want = run_forward(x, *args, two)
+    grads = run_backward(x, *args)
+    vecs = {k: dev(x[k]) for k in ("gamma", "beta", "rscale", "gamma2", "beta2")}
+    for off in (0, 1, 8):
+        wide, ld = {}, {}
+        for i, k in enumerate(("h", "gate", "res", "out", "out2", "dout", "dout2", "dh", "dgate", "dres")):
+            w = C + 8 * (i % 3) + 2 * off
+            wide[k] = torch.full((n, w), 5.0, dtype=TYPES[ty], device=DEV)
+            ld["ld_" + k] = w
+        at = {k: w[:, off:off + C] for k, w in wide.items()}
+        for k in ("h", "gate", "res", "dout", "dout2"):
+            if x[k] is not None:
+                at[k].copy_(dev(x[k]))
+        s = shape_of(x, *args, **ld)
+        P.impala_blocknorm_fwd(s, at["h"], vecs["gamma"], vecs["beta"], at["gate"], vecs["rscale"], at["res"], at["out"],
+                               vecs["gamma2"], vecs["beta2"], at["out2"] if two else None)
+        assert torch.equal(at["out"], want[0]) and (not two or torch.equal(at["out2"], want[1]))
+        at["out"].copy_(dev(x["out"]))
+        ws = torch.empty(P.impala_blocknorm_bwd_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+        small = {k: torch.empty_like(vecs[k[1:]]) for k in ("dgamma", "dbeta", "drscale", "dgamma2", "dbeta2")}
+        P.impala_blocknorm_bwd(s, at["dout"], at["dout2"] if two else None, at["h"], vecs["gamma"], vecs["beta"], at["gate"],
+                               vecs["rscale"], at["out"], vecs["gamma2"], at["dh"], small["dgamma"], small["dbeta"],
+                               at["dgate"], small["drscale"], at["dres"], small["dgamma2"] if two else None,
+                               small["dbeta2"] if two else None, ws)
+        for k, g in grads.items():
+            if g is not None:
+                assert torch.equal(at[k] if k in at else small[k], g), (off, k)
+        for w in wide.values():
+            assert (w[:, :off] == 5).all() and (w[:, off + C:] == 5).all()
+
+    for over in ("h", "gate", "res"):
+        a = {k: dev(v) for k, v in x.items()}
+        P.impala_blocknorm_fwd(shape_of(x, *args), a["h"], a["gamma"], a["beta"], a["gate"], a["rscale"], a["res"], a[over],
+                               a["gamma2"], a["beta2"], None)
+        assert torch.equal(a[over], want[0])
+    a = {k: dev(v) for k, v in x.items()}
+    P.impala_blocknorm_bwd(shape_of(x, *args), a["dout"], a["dout2"], a["h"], a["gamma"], a["beta"], a["gate"], a["rscale"],
+                           a["out"], a["gamma2"], a["h"], None, None, a["gate"], None, a["dout"], None, None, ws)
+    for k, t in (("dh", a["h"]), ("dgate", a["gate"]), ("dres", a["dout"])):
+        assert torch.equal(t, grads[k])
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+def test_no_rows(ty):
+    x = {k: (v[:0] if v.dim() == 2 else v) for k, v in make(2, 48, ty).items()}
+    run_forward(x, ty, 1, 1, 2, 1, True)
+    got = run_backward(x, ty, 1, 1, 2, 1)
+    assert all((got[k] == 0).all() for k in ("dgamma", "dbeta", "drscale", "dgamma2", "dbeta2"))
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+def test_rows_that_are_not_finite_stay_alone(ty):
+    x = make(40, 72, ty)
+    want, grads = run_forward(x, ty, 1, 1, 2, 1, True), run_backward(x, ty, 1, 1, 2, 1)
+    rows = torch.ones(40, dtype=torch.bool)
+    for r, (k, v) in enumerate((("h", float("nan")), ("gate", float("inf")), ("res", -float("inf")), ("dout", float("nan")))):
+        x[k][3 * r, 5] = v
+        rows[3 * r] = False
+    got, g2 = run_forward(x, ty, 1, 1, 2, 1, True), run_backward(x, ty, 1, 1, 2, 1)
+    for g, w in zip(got, want):
+        assert torch.equal(g[rows.to(DEV)], w[rows.to(DEV)])
+    for k in ("dh", "dgate", "dres"):
+        assert torch.equal(g2[k][rows.to(DEV)], grads[k][rows.to(DEV)])
+
+
+def test_gradients_against_differences():
+    """Along a direction, against central differences of the 64-bit forward."""
+    n, C = 12, 40
+    x = make(n, C, "f32", seed=8)
+    x = {k: v for k, v in x.items()}
+    g = torch.Generator().manual_seed(4)
+    u = {k: torch.randn(*x[k].shape, generator=g).double() for k in ("h", "gamma", "beta", "gate", "rscale", "res", "gamma2",
+                                                                    "beta2")}
+
+    def loss(t):
+        y = {k: x[k].double() + t * u[k] for k in u}
+        out, _ = ref.blocknorm(y["h"], y["gamma"], y["beta"], y["gate"], y["rscale"], y["res"], 1, 1, 1, 1e-5)
+        out2, _ = ref.blocknorm_second(out, y["gamma2"], y["beta2"], 2, 1e-5)
+        return float((out * x["dout"].double()).sum() + (out2 * x["dout2"].double()).sum())
+
+    x["out"] = ref.blocknorm(x["h"], x["gamma"], x["beta"], x["gate"], x["rscale"], x["res"], 1, 1, 1, 1e-5)[0].float()
+    got = run_backward(x, "f32", 1, 1, 2, 1)
+    parts = [(got["d" + k].double().cpu() * u[k]) for k in u]
+    t = 1e-5
+    slope = (loss(t) - loss(-t)) / (2 * t)
+    assert abs(sum(float(p.sum()) for p in parts) - slope) < 1e-5 * sum(float(p.abs().sum()) for p in parts)
+
+
+def test_streams_graphs_and_repeats():
+    xs = [make(300, 512, "bf16", seed=i) for i in range(2)]
+    args = ("bf16", 1, 1, 2, 1)
+    want = [(run_forward(x, *args, True), run_backward(x, *args)) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(3):
+        got = []
+        for x, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                got.append((run_forward(x, *args, True), run_backward(x, *args)))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(g[0], w[0])) and all(torch.equal(g[1][k], w[1][k]) for k in NAMES)
+    a = {k: dev(v) for k, v in xs[0].items()}
+    s = shape_of(xs[0], *args)
+    out, out2 = torch.empty_like(a["h"]), torch.empty_like(a["h"])
+    o = {k: torch.empty_like(v) for k, v in want[0][1].items()}
+    ws = torch.empty(P.impala_blocknorm_bwd_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.impala_blocknorm_fwd(s, a["h"], a["gamma"], a["beta"], a["gate"], a["rscale"], a["res"], out, a["gamma2"], a["beta2"],
+                               out2)
+        P.impala_blocknorm_bwd(s, a["dout"], a["dout2"], a["h"], a["gamma"], a["beta"], a["gate"], a["rscale"], a["out"],
+                               a["gamma2"], *(o[k] for k in NAMES), ws)
+    for i in (0, 1, 0):
+        for k in a:
+            a[k].copy_(xs[i][k])
+        graph.replay()
+        run_forward(xs[1 - i], *args, True)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i][0][0]) and torch.equal(out2, want[i][0][1])
+        assert all(torch.equal(o[k], want[i][1][k]) for k in NAMES)
