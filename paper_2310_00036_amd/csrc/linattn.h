@@ -19,7 +19,7 @@ struct LaPass {
     int dk, dv, back;
     int xk, xn;                // element strides of a state's two axes
     float in, out;
-    int vec;                   // bits 0..3: q, k, v, o may be moved in 16-byte pieces (o: in fours)
+    int vec;                   // bit 0: o is written in fours; 1: rows end inside a 16-byte piece; 2: q, k, v are read by it
 };
 constexpr int kLaMaxPasses = 3;
 constexpr int kLaMaxDim = 128;

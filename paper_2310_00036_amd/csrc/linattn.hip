@@ -114,6 +114,7 @@ hipError_t la_steps(const LaArgs& a, hipStream_t s) {
 // together and handed round in LDS.
 
 constexpr int kL = 64;
+typedef uint32_t cb_u32x2 __attribute__((ext_vector_type(2)));
 
 // bf16: products of two bf16 numbers are exact; what is no bf16 number (the decayed products, X, the decayed v) goes into
 // a product as two of them, or three where the result is a float32 output (X).
@@ -174,7 +175,9 @@ struct LaB {
         for (int r = 0; r < 4; ++r) { x[r] = X[2 * kb][r]; x[4 + r] = X[2 * kb + 1][r]; }
         split(x, f);
     }
-    static CB_DEV void store4o(T* p, const float* x) { store4(p, x[0], x[1], x[2], x[3]); }
+    static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, const float* x) {
+        __builtin_amdgcn_raw_buffer_store_b64(cb_u32x2{pack2bf(x[0], x[1]), pack2bf(x[2], x[3])}, r, off, 0, 0);
+    }
     static CB_DEV T store(float x) { return f2bf(x); }
 };
 
@@ -213,7 +216,10 @@ struct LaF {
     static CB_DEV void xfrag(const cb_f32x4 (&X)[NT], int kb, Frag (&f)[NX]) {
         f[0] = make_float4(X[kb][0], X[kb][1], X[kb][2], X[kb][3]);
     }
-    static CB_DEV void store4o(T* p, const float* x) { store4(p, x[0], x[1], x[2], x[3]); }
+    static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, const float* x) {
+        buf_store16(r, off, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                                       __float_as_uint(x[3])));
+    }
     static CB_DEV T store(float x) { return x; }
 };
 
@@ -235,40 +241,70 @@ struct LaTile {
     static constexpr int UV = ES;                                             // of v
 };
 
-// 16 bytes of a row, `left` elements of which exist; zeros behind them.
+// Rows of one array as 16-byte pieces of a buffer resource that is moved from chunk to chunk: pieces of rows behind the
+// chunk's last or of columns behind the array's read zero. Rows step by st bytes; going back (dir < 0) the resource starts
+// at the chunk's last row.
+struct LaRows {
+    const char* p;             // the chunk's first row
+    int64_t st;
+    int bytes;                 // of a row
+    bool back;
+    CB_DEV __amdgpu_buffer_rsrc_t rsrc(int n) const {
+        return buf_rsrc(back ? p - (n - 1) * st : p, uint32_t((n - 1) * st) + bytes);
+    }
+    CB_DEV uint32_t at(int row, int byte, int n) const {
+        return byte >= bytes ? kOOB : uint32_t((back ? n - 1 - row : row) * int(st) + byte);
+    }
+    CB_DEV void next() { p += back ? -kL * st : kL * st; }
+};
+
+// The piece's elements behind the row's last, which are the next ones' in memory, as zeros.
 template <class T>
-CB_DEV uint4 la_load16(const T* p, int left, bool vec) {
+CB_DEV uint4 la_cut(uint4 v, int left) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) w[i] = 2 * i + 1 < left ? w[i] : 2 * i < left ? w[i] & 0xffffu : 0u;
+        else w[i] = i < left ? w[i] : 0u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The same piece element by element, where the array's alignment or strides allow no more.
+template <class T>
+CB_DEV uint4 la_gather(const LaRows& r, int row, int byte, int n) {
     constexpr int VE = 16 / sizeof(T);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (left <= 0) return v;
-    if (vec) return *reinterpret_cast<const uint4*>(p);
+    const T* p = reinterpret_cast<const T*>(r.p + (r.back ? -row : row) * r.st + byte);
+    const int left = row < n ? (r.bytes - byte) / int(sizeof(T)) : 0;
     T x[VE];
 #pragma unroll
     for (int i = 0; i < VE; ++i) x[i] = i < left ? p[i] : T(0);
+    uint4 v;
     __builtin_memcpy(&v, x, 16);
     return v;
 }
 
-// f(j, column -> v_j there) for the rows of v's fragments: one lane's own column from whichever lane holds row j of it.
-template <class Tr, int NJ, class F>
-CB_DEV void la_each_row(const typename Tr::Frag (&fv)[NJ], F&& f) {
+// Row j's numbers from v's fragments at column col of the wave's 16: whichever lane holds it hands it over. j is the same
+// in all lanes. (Selections instead of an index keep the fragments in registers.)
+template <class Tr, int NJ>
+CB_DEV float la_row_at(const typename Tr::Frag (&fv)[NJ], int j, int col) {
+    float y = 0.f;
 #pragma unroll
     for (int jb = 0; jb < NJ; ++jb) {
         float x[Tr::KPL];
         Tr::unpack(fv[jb], x);
-        for (int gj = 0; gj < 4; ++gj)
 #pragma unroll
-            for (int u = 0; u < Tr::KPL; ++u)
-                f(jb * Tr::KB + Tr::KPL * gj + u, [&](int col) { return __shfl(x[u], 16 * gj + col); });
+        for (int u = 0; u < Tr::KPL; ++u) y = j / Tr::KB == jb && j % Tr::KPL == u ? x[u] : y;
     }
+    return __shfl(y, j / Tr::KPL % 4 * 16 + col);
 }
 
-template <class Tr, int DK, int NW, bool STATE>
-__global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0) {
+template <class Tr, int DK, int NW, bool STATE, bool FAST>
+__global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0) {
     using T = typename Tr::T;
     using Frag = typename Tr::Frag;
     using L = LaTile<Tr, DK, NW>;
-    constexpr int VE = 16 / sizeof(T), KB = Tr::KB, KPL = Tr::KPL, NT = DK / 16, NJ = kL / KB;
+    constexpr int KB = Tr::KB, KPL = Tr::KPL, NT = DK / 16, NJ = kL / KB;
     extern __shared__ __align__(16) unsigned char lds[];
     float* pw = reinterpret_cast<float*>(lds + L::TAB);
     float* pin = pw + 68;
@@ -289,11 +325,11 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
     const int p1 = sg.segs == 1 ? a.T : int(min(int64_t(a.T), int64_t(p0) + int64_t(sg.chunks) * kL));
 
     const int64_t dir = P.back ? -1 : 1, t0 = P.back ? a.T - 1 - p0 : p0;
-    const int64_t qs = dir * P.q.t, ks = dir * P.k.t, vs = dir * P.v.t, os = dir * P.o.t;
-    const T* q = static_cast<const T*>(P.q.p) + e * P.q.e + h * P.q.h + t0 * P.q.t;
-    const T* k = static_cast<const T*>(P.k.p) + e * P.k.e + h * P.k.h + t0 * P.k.t;
-    const T* v = static_cast<const T*>(P.v.p) + e * P.v.e + h * P.v.h + t0 * P.v.t;
-    T* o = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h + t0 * P.o.t;
+    auto rows = [&](const LaView& x, int d) {
+        return LaRows{static_cast<const char*>(x.p) + (e * x.e + h * x.h + t0 * x.t) * L::ES, x.t * L::ES, d * L::ES,
+                      P.back != 0};
+    };
+    LaRows q = rows(P.q, P.dk), k = rows(P.k, P.dk), v = rows(P.v, P.dv), o = rows(P.o, P.dv);
     const uint8_t* dn = a.dones ? a.dones + e * a.d_e + t0 * a.d_t : nullptr;
     const int64_t ds = dir * a.d_t;
     const int later = P.back ? 0 : 1;
@@ -331,38 +367,60 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
     constexpr int CQ = DK * L::ES / 16, CV = 16 * NW * L::ES / 16;
     uint4 rq[L::UQ], rk[L::UQ], rv[L::UV];
     bool rd = false;
-    auto fetch = [&](int n) {
+    auto fetch = [&](int n) CB_INLINE_LAMBDA {
+        if (FAST) {
+            const auto bq = q.rsrc(n), bk = k.rsrc(n), bv = v.rsrc(n);
 #pragma unroll
-        for (int u = 0; u < L::UQ; ++u) {
-            const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ * VE;
-            const int left = row < n ? P.dk - col : 0;
-            if (!STATE) rq[u] = la_load16(q + row * qs + col, left, P.vec & 1);
-            rk[u] = la_load16(k + row * ks + col, left, P.vec & 2);
-        }
+            for (int u = 0; u < L::UQ; ++u) {
+                const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ * 16;
+                if (!STATE) rq[u] = buf_load16(bq, q.at(row, col, n));
+                rk[u] = buf_load16(bk, k.at(row, col, n));
+            }
 #pragma unroll
-        for (int u = 0; u < L::UV; ++u) {
-            const int id2 = tid + 64 * NW * u, row = id2 / CV, col = nb0 + id2 % CV * VE;
-            rv[u] = la_load16(v + row * vs + col, row < n ? P.dv - col : 0, P.vec & 4);
+            for (int u = 0; u < L::UV; ++u) {
+                const int id2 = tid + 64 * NW * u, row = id2 / CV, col = nb0 * L::ES + id2 % CV * 16;
+                rv[u] = buf_load16(bv, v.at(row, col, n));
+            }
         }
         rd = dn && lane < n && dn[lane * ds];
     };
+    const bool tail = P.vec & 2;
     const int ob = n0 + 4 * g;   // this lane's four columns of o
     float factor = 1.f;
     fetch(min(kL, p1 - p0));
     for (int p = p0; p < p1; p += kL) {
         const int n = min(kL, p1 - p);
+        if (FAST) {
 #pragma unroll
-        for (int u = 0; u < L::UQ; ++u) {
-            const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ;
-            if (row < kL) {
-                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + col * 16) = rq[u];
-                *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + col * 16) = rk[u];
+            for (int u = 0; u < L::UQ; ++u) {
+                const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ * 16;
+                if (tail) {
+                    rq[u] = la_cut<T>(rq[u], P.dk - col / L::ES);
+                    rk[u] = la_cut<T>(rk[u], P.dk - col / L::ES);
+                }
+                if (row < kL) {
+                    if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + col) = rq[u];
+                    *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + col) = rk[u];
+                }
             }
-        }
 #pragma unroll
-        for (int u = 0; u < L::UV; ++u) {
-            const int id2 = tid + 64 * NW * u, row = id2 / CV, col = id2 % CV;
-            *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + col * 16) = rv[u];
+            for (int u = 0; u < L::UV; ++u) {
+                const int id2 = tid + 64 * NW * u, row = id2 / CV, col = id2 % CV * 16;
+                if (tail) rv[u] = la_cut<T>(rv[u], P.dv - nb0 - col / L::ES);
+                *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + col) = rv[u];
+            }
+        } else {
+#pragma unroll 1
+            for (int id2 = tid; id2 < kL * CQ; id2 += 64 * NW) {
+                const int row = id2 / CQ, col = id2 % CQ * 16;
+                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + col) = la_gather<T>(q, row, col, n);
+                *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + col) = la_gather<T>(k, row, col, n);
+            }
+#pragma unroll 1
+            for (int id2 = tid; id2 < kL * CV; id2 += 64 * NW) {
+                const int row = id2 / CV, col = id2 % CV * 16;
+                *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + col) = la_gather<T>(v, row, nb0 * L::ES + col, n);
+            }
         }
         const uint64_t m = __ballot(rd);
         // episode starts before what row i holds
@@ -375,8 +433,8 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
         }
         const float over = pw[n];
         lds_barrier();
+        q.next(); k.next(); v.next();
         if (p + kL < p1) {
-            q += kL * qs; k += kL * ks; v += kL * vs;
             if (dn) dn += kL * ds;
             fetch(min(kL, p1 - p - kL));
         }
@@ -404,6 +462,7 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
             }
         }
 
+        __builtin_amdgcn_sched_barrier(0);
         Frag fv[NJ];
 #pragma unroll
         for (int jb = 0; jb < NJ; ++jb) fv[jb] = Tr::template cols<1>(lds + L::V, L::RSV, jb * KB, 16 * wave);
@@ -432,6 +491,7 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
             }
         }
 
+        __builtin_amdgcn_sched_barrier(0);
         {   // X <- over X + sum_j w_j k_j v_j^T
             cb_f32x4 U[NT];
             auto rows = [&](auto clean) CB_INLINE_LAMBDA {
@@ -460,10 +520,12 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
             // A number that is not finite comes through a weight of zero as NaN. Then without all such, and theirs added
             // for the rows that the state sees.
             if (__any(sum != sum)) {
+                asm volatile("" ::: "memory");   // the fragments are read again, not kept for this
                 rows([](Frag f) { return Tr::finite(f); });
-                la_each_row<Tr>(fv, [&](int j, auto vat) {
-                    const float x = vat(c), w = vw[j] * x;
-                    if (j >= n || count(j) != total) return;
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
+                    const float x = la_row_at<Tr>(fv, j, c), w = vw[j] * x;
+                    if (count(j) != total) continue;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -472,7 +534,7 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
                                                                                   Tr::krow(t, g, r) * L::ES));
                             if (!isfinite(x) || !isfinite(kk)) U[t][r] += w * kk;
                         }
-                });
+                }
             }
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -505,11 +567,13 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
 #pragma unroll
             for (int b = 0; b < 4; ++b) sum += (A[b][0] + A[b][1]) + (A[b][2] + A[b][3]);
             if (__any(sum != sum)) {   // as above: a later row's, or one's of another episode
+                asm volatile("" ::: "memory");
                 rows([](Frag f) { return Tr::finite(f); });
-                la_each_row<Tr>(fv, [&](int j, auto vat) {
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
                     float x[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = vat(4 * g + r);
+                    for (int r = 0; r < 4; ++r) x[r] = la_row_at<Tr>(fv, j, 4 * g + r);
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
                         const int i = 16 * b + c;
@@ -522,23 +586,23 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_kernel(LaArgs a, LaSegs sg, 
                         for (int r = 0; r < 4; ++r)
                             if (!isfinite(x[r])) A[b][r] += w * x[r];
                     }
-                });
+                }
             }
+            const auto bo = o.rsrc(n);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int i = 16 * b + c;
-                if (i >= n || ob >= P.dv) continue;
-                T* po = o + i * os + ob;
                 float x[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] = (O[b][r] + A[b][r]) * P.out;
-                if (P.vec & 8) Tr::store4o(po, x);
-                else
+                if (P.vec & 1) Tr::store4o(bo, o.at(i, ob * L::ES, n), x);
+                else if (i < n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (ob + r < P.dv) po[r] = Tr::store(x[r]);
+                        if (ob + r < P.dv)
+                            reinterpret_cast<T*>(const_cast<char*>(o.p) + (P.back ? -i : i) * o.st)[ob + r] = Tr::store(x[r]);
             }
-            o += kL * os;
+            o.next();
         }
     }
 
@@ -579,8 +643,11 @@ hipError_t la_chunks_launch(const LaArgs& a, const LaSegs& sg, int y0, int ny, b
     using L = LaTile<Tr, DK, NW>;
     const int64_t nbs = (a.pass[y0].dv + 16 * NW - 1) / (16 * NW);
     const dim3 grid(unsigned(int64_t(a.E) * a.H * nbs * (state ? sg.segs - 1 : sg.segs)), unsigned(ny));
-    if (state) hipLaunchKernelGGL((la_chunk_kernel<Tr, DK, NW, true>), grid, dim3(64 * NW), L::BYTES, s, a, sg, y0);
-    else hipLaunchKernelGGL((la_chunk_kernel<Tr, DK, NW, false>), grid, dim3(64 * NW), L::BYTES, s, a, sg, y0);
+    bool fast = true;
+    for (int y = y0; y < y0 + ny; ++y) fast &= a.pass[y].vec >> 2 & 1;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), L::BYTES, s, a, sg, y0); };
+    if (state) fast ? go(la_chunk_kernel<Tr, DK, NW, true, true>) : go(la_chunk_kernel<Tr, DK, NW, true, false>);
+    else fast ? go(la_chunk_kernel<Tr, DK, NW, false, true>) : go(la_chunk_kernel<Tr, DK, NW, false, false>);
     return hipGetLastError();
 }
 
@@ -659,8 +726,11 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     });
     if (a.T <= kLaSteps) return prec == 0 ? la_steps<PrecBF16>(a, s) : la_steps<PrecF32>(a, s);
     const int es = prec == 0 ? 2 : 4, ve = 16 / es;
-    auto whole = [&](const LaView& v, int d, int k) {   // rows of whole pieces of k elements, at their alignment
-        return reinterpret_cast<uintptr_t>(v.p) % (k * es) == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && d % k == 0;
+    // Rows that a buffer resource reaches: at whole words, each behind the last one's end, 64 of them within 2^31 bytes.
+    auto reach = [&](const LaView& v, int d) {
+        const int k = 4 / es;
+        return reinterpret_cast<uintptr_t>(v.p) % 4 == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && v.t >= d &&
+               v.t < (int64_t(1) << 30) / kL / es;
     };
     LaSegs sg{};
     const int64_t EH = int64_t(a.E) * a.H;
@@ -668,7 +738,8 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     char* w = static_cast<char*>(ws);
     for (int y = 0; y < a.np; ++y) {
         LaPass& P = a.pass[y];
-        P.vec = whole(P.q, P.dk, ve) | whole(P.k, P.dk, ve) << 1 | whole(P.v, P.dv, ve) << 2 | whole(P.o, P.dv, 4) << 3;
+        P.vec = (reach(P.o, P.dv) && P.dv % 4 == 0) | (P.dk % ve != 0 || P.dv % ve != 0) << 1 |
+                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv)) << 2;
         if (sg.segs == 1) continue;
         sg.state[y] = reinterpret_cast<float*>(w);
         w += la_a256(sg.segs * EH * P.dk * P.dv * 4);
