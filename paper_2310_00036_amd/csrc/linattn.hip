@@ -241,21 +241,19 @@ struct LaTile {
     static constexpr int UV = ES;                                             // of v
 };
 
-// Rows of one array as 16-byte pieces of a buffer resource that is moved from chunk to chunk: pieces of rows behind the
-// chunk's last or of columns behind the array's read zero. Rows step by st bytes; going back (dir < 0) the resource starts
-// at the chunk's last row.
+// Rows of one array through a buffer resource that is moved from chunk to chunk, at 32-bit offsets: what lies behind the
+// chunk's last row, or in columns behind the array's, reads zero and is not written. A row steps by st bytes; going back,
+// st is negative and the resource starts at the chunk's last row, so offsets have -(n - 1) st added.
 struct LaRows {
     const char* p;             // the chunk's first row
-    int64_t st;
-    int bytes;                 // of a row
-    bool back;
+    int st, bytes;             // bytes: of a row
     CB_DEV __amdgpu_buffer_rsrc_t rsrc(int n) const {
-        return buf_rsrc(back ? p - (n - 1) * st : p, uint32_t((n - 1) * st) + bytes);
+        const int span = (n - 1) * st;
+        return buf_rsrc(span < 0 ? p + span : p, uint32_t(abs(span)) + bytes);
     }
-    CB_DEV uint32_t at(int row, int byte, int n) const {
-        return byte >= bytes ? kOOB : uint32_t((back ? n - 1 - row : row) * int(st) + byte);
-    }
-    CB_DEV void next() { p += back ? -kL * st : kL * st; }
+    CB_DEV uint32_t first(int n) const { return uint32_t(max(0, -(n - 1) * st)); }
+    CB_DEV uint32_t at(int row, int byte) const { return byte >= bytes ? kOOB : uint32_t(row * st + byte); }
+    CB_DEV void next() { p += int64_t(kL) * st; }
 };
 
 // The piece's elements behind the row's last, which are the next ones' in memory, as zeros.
@@ -272,16 +270,21 @@ CB_DEV uint4 la_cut(uint4 v, int left) {
 
 // The same piece element by element, where the array's alignment or strides allow no more.
 template <class T>
-CB_DEV uint4 la_gather(const LaRows& r, int row, int byte, int n) {
+CB_DEV uint4 la_gather(const T* p, int left) {
     constexpr int VE = 16 / sizeof(T);
-    const T* p = reinterpret_cast<const T*>(r.p + (r.back ? -row : row) * r.st + byte);
-    const int left = row < n ? (r.bytes - byte) / int(sizeof(T)) : 0;
     T x[VE];
 #pragma unroll
     for (int i = 0; i < VE; ++i) x[i] = i < left ? p[i] : T(0);
     uint4 v;
     __builtin_memcpy(&v, x, 16);
     return v;
+}
+
+// The same number, but for the compiler: what rare paths derive from it is not computed ahead of the main loop and kept in
+// registers throughout (60 of them here).
+CB_DEV int la_here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
 }
 
 // Row j's numbers from v's fragments at column col of the wave's 16: whichever lane holds it hands it over. j is the same
@@ -325,14 +328,15 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
     const int p1 = sg.segs == 1 ? a.T : int(min(int64_t(a.T), int64_t(p0) + int64_t(sg.chunks) * kL));
 
     const int64_t dir = P.back ? -1 : 1, t0 = P.back ? a.T - 1 - p0 : p0;
+    const int dk = P.dk, dv = P.dv, back = P.back, vec = P.vec;
+    const float out = P.out;
     auto rows = [&](const LaView& x, int d) {
-        return LaRows{static_cast<const char*>(x.p) + (e * x.e + h * x.h + t0 * x.t) * L::ES, x.t * L::ES, d * L::ES,
-                      P.back != 0};
+        return LaRows{static_cast<const char*>(x.p) + (e * x.e + h * x.h + t0 * x.t) * L::ES, int(dir * x.t) * L::ES, d * L::ES};
     };
-    LaRows q = rows(P.q, P.dk), k = rows(P.k, P.dk), v = rows(P.v, P.dv), o = rows(P.o, P.dv);
+    LaRows q = rows(P.q, dk), k = rows(P.k, dk), v = rows(P.v, dv), o = rows(P.o, dv);
     const uint8_t* dn = a.dones ? a.dones + e * a.d_e + t0 * a.d_t : nullptr;
     const int64_t ds = dir * a.d_t;
-    const int later = P.back ? 0 : 1;
+    const int later = back ? 0 : 1;
 
     if (tid <= kL) {
         const float w = float(exp(double(tid) * double(tid ? a.log_decay[h] : 0.f)));
@@ -366,26 +370,28 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
     // the chunk's q, k and v on their way to LDS: 16-byte pieces, 64 rows of CQ or CV of them
     constexpr int CQ = DK * L::ES / 16, CV = 16 * NW * L::ES / 16;
     uint4 rq[L::UQ], rk[L::UQ], rv[L::UV];
-    bool rd = false;
+    uint32_t rd = 0;
+    constexpr int RQ = 64 * NW / CQ, RV = 64 * NW / CV;   // rows from one of a thread's pieces to the next
+    static_assert(RQ * CQ == 64 * NW && RV * CV == 64 * NW, "a thread's pieces lie in one column");
+    const int rowq = tid / CQ, colq = tid % CQ * 16, rowv = tid / CV, colv = tid % CV * 16;
+    const uint32_t atq = q.at(rowq, colq), atk = k.at(rowq, colq), atv = v.at(rowv, nb0 * L::ES + colv);
     auto fetch = [&](int n) CB_INLINE_LAMBDA {
         if (FAST) {
             const auto bq = q.rsrc(n), bk = k.rsrc(n), bv = v.rsrc(n);
 #pragma unroll
             for (int u = 0; u < L::UQ; ++u) {
-                const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ * 16;
-                if (!STATE) rq[u] = buf_load16(bq, q.at(row, col, n));
-                rk[u] = buf_load16(bk, k.at(row, col, n));
+                if (!STATE) rq[u] = buf_load16(bq, atq + (q.first(n) + u * RQ * q.st));
+                rk[u] = buf_load16(bk, atk + (k.first(n) + u * RQ * k.st));
             }
 #pragma unroll
-            for (int u = 0; u < L::UV; ++u) {
-                const int id2 = tid + 64 * NW * u, row = id2 / CV, col = nb0 * L::ES + id2 % CV * 16;
-                rv[u] = buf_load16(bv, v.at(row, col, n));
-            }
+            for (int u = 0; u < L::UV; ++u) rv[u] = buf_load16(bv, atv + (v.first(n) + u * RV * v.st));
         }
-        rd = dn && lane < n && dn[lane * ds];
+        // (Kept as it is loaded: a comparison here would wait for it and all loads before it.)
+        rd = 0;
+        if (dn && lane < n) rd = dn[lane * ds];
     };
-    const bool tail = P.vec & 2;
-    const int ob = n0 + 4 * g;   // this lane's four columns of o
+    const bool tail = vec & 2;
+    const uint32_t ato = o.at(c, (n0 + 4 * g) * L::ES);
     float factor = 1.f;
     fetch(min(kL, p1 - p0));
     for (int p = p0; p < p1; p += kL) {
@@ -393,38 +399,38 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         if (FAST) {
 #pragma unroll
             for (int u = 0; u < L::UQ; ++u) {
-                const int id2 = tid + 64 * NW * u, row = id2 / CQ, col = id2 % CQ * 16;
                 if (tail) {
-                    rq[u] = la_cut<T>(rq[u], P.dk - col / L::ES);
-                    rk[u] = la_cut<T>(rk[u], P.dk - col / L::ES);
+                    const int left = dk - la_here(colq) / L::ES;
+                    rq[u] = la_cut<T>(rq[u], left);
+                    rk[u] = la_cut<T>(rk[u], left);
                 }
-                if (row < kL) {
-                    if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + col) = rq[u];
-                    *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + col) = rk[u];
+                if (rowq + RQ * u < kL) {
+                    if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + (rowq + RQ * u) * L::RSK + colq) = rq[u];
+                    *reinterpret_cast<uint4*>(lds + L::K + (rowq + RQ * u) * L::RSK + colq) = rk[u];
                 }
             }
 #pragma unroll
             for (int u = 0; u < L::UV; ++u) {
-                const int id2 = tid + 64 * NW * u, row = id2 / CV, col = id2 % CV * 16;
-                if (tail) rv[u] = la_cut<T>(rv[u], P.dv - nb0 - col / L::ES);
-                *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + col) = rv[u];
+                if (tail) rv[u] = la_cut<T>(rv[u], dv - nb0 - la_here(colv) / L::ES);
+                *reinterpret_cast<uint4*>(lds + L::V + (rowv + RV * u) * L::RSV + colv) = rv[u];
             }
         } else {
+            auto piece = [&](const LaView& x, int row, int col, int d) {
+                const T* r = static_cast<const T*>(x.p) + e * x.e + h * x.h + (t0 + dir * (p - p0 + row)) * x.t + col;
+                return la_gather<T>(r, row < n ? d - col : 0);
+            };
 #pragma unroll 1
-            for (int id2 = tid; id2 < kL * CQ; id2 += 64 * NW) {
-                const int row = id2 / CQ, col = id2 % CQ * 16;
-                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + col) = la_gather<T>(q, row, col, n);
-                *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + col) = la_gather<T>(k, row, col, n);
+            for (int row = rowq; row < kL; row += RQ) {
+                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + colq) = piece(P.q, row, colq / L::ES, dk);
+                *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + colq) = piece(P.k, row, colq / L::ES, dk);
             }
 #pragma unroll 1
-            for (int id2 = tid; id2 < kL * CV; id2 += 64 * NW) {
-                const int row = id2 / CV, col = id2 % CV * 16;
-                *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + col) = la_gather<T>(v, row, nb0 * L::ES + col, n);
-            }
+            for (int row = rowv; row < kL; row += RV)
+                *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + colv) = piece(P.v, row, nb0 + colv / L::ES, dv);
         }
-        const uint64_t m = __ballot(rd);
+        const uint64_t m = __ballot(rd != 0);
         // episode starts before what row i holds
-        auto count = [&](int i) { return __popcll(P.back ? m & ((uint64_t(1) << i) - 1) : m & (~uint64_t(0) >> (63 - i))); };
+        auto count = [&](int i) { return __popcll(back ? m & ((uint64_t(1) << i) - 1) : m & (~uint64_t(0) >> (63 - i))); };
         const int total = __popcll(m);
         if (wave == 0) {
             const int ci = count(lane);
@@ -439,26 +445,37 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             fetch(min(kL, p1 - p - kL));
         }
 
-        if (!STATE) {   // in g^(i-j) q_i . k_j by tiles on and below the diagonal
-            for (int u = wave; u < 10; u += NW) {
-                const int b = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3, t = u - b * (b + 1) / 2;
-                cb_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+        if (!STATE) {   // in g^(i-j) q_i . k_j by tiles on and below the diagonal, a wave's few at once
+            constexpr int MT = (10 + NW - 1) / NW;
+            cb_f32x4 d[MT];
+            int tb[MT], tt[MT];
 #pragma unroll
-                for (int kb = 0; kb < DK / KB; ++kb) {
-                    const Frag fk = *reinterpret_cast<const Frag*>(lds + L::K + (16 * t + c) * L::RSK + kb * 64 + 16 * g);
-                    const Frag fq = *reinterpret_cast<const Frag*>(lds + L::Q + (16 * b + c) * L::RSK + kb * 64 + 16 * g);
-                    d = Tr::mma(fk, fq, d);
+            for (int y = 0; y < MT; ++y) {
+                const int u = min(wave + NW * y, 9);
+                tb[y] = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3;
+                tt[y] = u - tb[y] * (tb[y] + 1) / 2;
+                d[y] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int kb = 0; kb < DK / KB; ++kb)
+#pragma unroll
+                for (int y = 0; y < MT; ++y) {
+                    const Frag fk = *reinterpret_cast<const Frag*>(lds + L::K + (16 * tt[y] + c) * L::RSK + kb * 64 + 16 * g);
+                    const Frag fq = *reinterpret_cast<const Frag*>(lds + L::Q + (16 * tb[y] + c) * L::RSK + kb * 64 + 16 * g);
+                    d[y] = Tr::mma(fk, fq, d[y]);
                 }
-                const int i = 16 * b + c, j = 16 * t + 4 * g;
+#pragma unroll
+            for (int y = 0; y < MT; ++y) {
+                const int i = 16 * tb[y] + c, j = 16 * tt[y] + 4 * g;
                 float x[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = j + r <= i ? d[r] * pin[max(i - j - r, 0)] : 0.f;
+                for (int r = 0; r < 4; ++r) x[r] = j + r <= i ? d[y][r] * pin[max(i - j - r, 0)] : 0.f;
                 if (m) {
-                    const int ci = count(i);
+                    const int ci = count(la_here(i)), j0 = la_here(j);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = count(j + r) == ci ? x[r] : 0.f;
+                    for (int r = 0; r < 4; ++r) x[r] = count(j0 + r) == ci ? x[r] : 0.f;
                 }
-                Tr::store_p(lds + L::P + i * L::RSP + j * L::ES, L::PP, x);
+                if (wave + NW * y < 10) Tr::store_p(lds + L::P + i * L::RSP + j * L::ES, L::PP, x);
             }
         }
 
@@ -485,7 +502,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const float w = xw[16 * b + c];
-                const bool cut = m && count(16 * b + c) != 0;
+                const bool cut = m && count(la_here(16 * b + c)) != 0;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) O[b][r] = cut ? 0.f : O[b][r] * w;
             }
@@ -522,16 +539,17 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             if (__any(sum != sum)) {
                 asm volatile("" ::: "memory");   // the fragments are read again, not kept for this
                 rows([](Frag f) { return Tr::finite(f); });
+                const int cc = la_here(c), gg = la_here(g);
 #pragma unroll 1
                 for (int j = 0; j < n; ++j) {
-                    const float x = la_row_at<Tr>(fv, j, c), w = vw[j] * x;
+                    const float x = la_row_at<Tr>(fv, j, cc), w = vw[j] * x;
                     if (count(j) != total) continue;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float kk = Tr::load(*reinterpret_cast<const T*>(lds + L::K + j * L::RSK +
-                                                                                  Tr::krow(t, g, r) * L::ES));
+                                                                                  Tr::krow(t, gg, r) * L::ES));
                             if (!isfinite(x) || !isfinite(kk)) U[t][r] += w * kk;
                         }
                 }
@@ -569,14 +587,15 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             if (__any(sum != sum)) {   // as above: a later row's, or one's of another episode
                 asm volatile("" ::: "memory");
                 rows([](Frag f) { return Tr::finite(f); });
+                const int cc = la_here(c), gg = la_here(g);
 #pragma unroll 1
                 for (int j = 0; j < n; ++j) {
                     float x[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = la_row_at<Tr>(fv, j, 4 * g + r);
+                    for (int r = 0; r < 4; ++r) x[r] = la_row_at<Tr>(fv, j, 4 * gg + r);
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
-                        const int i = 16 * b + c;
+                        const int i = 16 * b + cc;
                         if (j > i || count(j) != count(i)) continue;
                         float w = 0.f;
 #pragma unroll
@@ -589,18 +608,20 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                 }
             }
             const auto bo = o.rsrc(n);
+            const uint32_t f = o.first(n);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const int i = 16 * b + c;
                 float x[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = (O[b][r] + A[b][r]) * P.out;
-                if (P.vec & 1) Tr::store4o(bo, o.at(i, ob * L::ES, n), x);
-                else if (i < n)
+                for (int r = 0; r < 4; ++r) x[r] = (O[b][r] + A[b][r]) * out;
+                if (vec & 1) Tr::store4o(bo, ato + (f + 16 * b * o.st), x);
+                else if (const int i = la_here(16 * b + c), col = la_here(n0 + 4 * g); i < n) {
+                    T* po = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h +
+                            (t0 + dir * (p - p0 + i)) * P.o.t;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (ob + r < P.dv)
-                            reinterpret_cast<T*>(const_cast<char*>(o.p) + (P.back ? -i : i) * o.st)[ob + r] = Tr::store(x[r]);
+                        if (col + r < dv) po[col + r] = Tr::store(x[r]);
+                }
             }
             o.next();
         }
