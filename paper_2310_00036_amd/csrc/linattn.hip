@@ -146,7 +146,7 @@ struct LaB {
         }
     }
     // four neighbouring entries of a row of the decayed products, plane by plane
-    static CB_DEV void store_p(unsigned char* p, int plane, float (&x)[4]) {
+    static CB_DEV void store_p(unsigned char* p, int plane, cb_f32x4 x) {
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
             const uint2 v = make_uint2(pack2bf(x[0], x[1]), pack2bf(x[2], x[3]));
@@ -175,7 +175,7 @@ struct LaB {
         for (int r = 0; r < 4; ++r) { x[r] = X[2 * kb][r]; x[4 + r] = X[2 * kb + 1][r]; }
         split(x, f);
     }
-    static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, const float* x) {
+    static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, cb_f32x4 x) {
         __builtin_amdgcn_raw_buffer_store_b64(cb_u32x2{pack2bf(x[0], x[1]), pack2bf(x[2], x[3])}, r, off, 0, 0);
     }
     static CB_DEV T store(float x) { return f2bf(x); }
@@ -200,7 +200,7 @@ struct LaF {
     }
     template <int N>
     static CB_DEV void split(float* x, Frag (&f)[N]) { f[0] = make_float4(x[0], x[1], x[2], x[3]); }
-    static CB_DEV void store_p(unsigned char* p, int, float (&x)[4]) {
+    static CB_DEV void store_p(unsigned char* p, int, cb_f32x4 x) {
         *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
     }
     template <int CS>
@@ -216,7 +216,7 @@ struct LaF {
     static CB_DEV void xfrag(const cb_f32x4 (&X)[NT], int kb, Frag (&f)[NX]) {
         f[0] = make_float4(X[kb][0], X[kb][1], X[kb][2], X[kb][3]);
     }
-    static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, const float* x) {
+    static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, cb_f32x4 x) {
         buf_store16(r, off, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
                                        __float_as_uint(x[3])));
     }
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         if (FAST) {
 #pragma unroll
             for (int u = 0; u < L::UQ; ++u) {
-                if (tail) {
+                if (__builtin_expect(tail, 0)) {
                     const int left = dk - la_here(colq) / L::ES;
                     rq[u] = la_cut<T>(rq[u], left);
                     rk[u] = la_cut<T>(rk[u], left);
@@ -411,7 +411,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             }
 #pragma unroll
             for (int u = 0; u < L::UV; ++u) {
-                if (tail) rv[u] = la_cut<T>(rv[u], dv - nb0 - la_here(colv) / L::ES);
+                if (__builtin_expect(tail, 0)) rv[u] = la_cut<T>(rv[u], dv - nb0 - la_here(colv) / L::ES);
                 *reinterpret_cast<uint4*>(lds + L::V + (rowv + RV * u) * L::RSV + colv) = rv[u];
             }
         } else {
@@ -467,16 +467,21 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
 #pragma unroll
             for (int y = 0; y < MT; ++y) {
                 const int i = 16 * tb[y] + c, j = 16 * tt[y] + 4 * g;
-                float x[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = j + r <= i ? d[y][r] * pin[max(i - j - r, 0)] : 0.f;
-                if (m) {
-                    const int ci = count(la_here(i)), j0 = la_here(j);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = count(j0 + r) == ci ? x[r] : 0.f;
-                }
-                if (wave + NW * y < 10) Tr::store_p(lds + L::P + i * L::RSP + j * L::ES, L::PP, x);
+                for (int r = 0; r < 4; ++r) d[y][r] = j + r <= i ? d[y][r] * pin[max(i - j - r, 0)] : 0.f;
             }
+            if (__builtin_expect(m != 0, 0)) {
+#pragma unroll
+                for (int y = 0; y < MT; ++y) {
+                    const int ci = count(la_here(16 * tb[y] + c)), j0 = la_here(16 * tt[y] + 4 * g);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) d[y][r] = count(j0 + r) == ci ? d[y][r] : 0.f;
+                }
+            }
+            // (Behind the tenth tile a wave repeats it: the same numbers in the same place.)
+#pragma unroll
+            for (int y = 0; y < MT; ++y)
+                Tr::store_p(lds + L::P + (16 * tb[y] + c) * L::RSP + (16 * tt[y] + 4 * g) * L::ES, L::PP, d[y]);
         }
 
         __builtin_amdgcn_sched_barrier(0);
@@ -500,11 +505,11 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                 }
             }
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const float w = xw[16 * b + c];
-                const bool cut = m && count(la_here(16 * b + c)) != 0;
+            for (int b = 0; b < 4; ++b) O[b] *= xw[16 * b + c];
+            if (__builtin_expect(m != 0, 0)) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) O[b][r] = cut ? 0.f : O[b][r] * w;
+                for (int b = 0; b < 4; ++b)
+                    if (count(la_here(16 * b + c)) != 0) O[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
             }
         }
 
@@ -536,7 +541,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             for (int t = 0; t < NT; ++t) sum += (U[t][0] + U[t][1]) + (U[t][2] + U[t][3]);
             // A number that is not finite comes through a weight of zero as NaN. Then without all such, and theirs added
             // for the rows that the state sees.
-            if (__any(sum != sum)) {
+            if (__builtin_expect(__any(sum != sum), 0)) {
                 asm volatile("" ::: "memory");   // the fragments are read again, not kept for this
                 rows([](Frag f) { return Tr::finite(f); });
                 const int cc = la_here(c), gg = la_here(g);
@@ -584,7 +589,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             float sum = 0.f;
 #pragma unroll
             for (int b = 0; b < 4; ++b) sum += (A[b][0] + A[b][1]) + (A[b][2] + A[b][3]);
-            if (__any(sum != sum)) {   // as above: a later row's, or one's of another episode
+            if (__builtin_expect(__any(sum != sum), 0)) {   // as above: a later row's, or one's of another episode
                 asm volatile("" ::: "memory");
                 rows([](Frag f) { return Tr::finite(f); });
                 const int cc = la_here(c), gg = la_here(g);
@@ -607,20 +612,25 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                     }
                 }
             }
-            const auto bo = o.rsrc(n);
-            const uint32_t f = o.first(n);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                float x[4];
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = (O[b][r] + A[b][r]) * out;
-                if (vec & 1) Tr::store4o(bo, ato + (f + 16 * b * o.st), x);
-                else if (const int i = la_here(16 * b + c), col = la_here(n0 + 4 * g); i < n) {
+                for (int r = 0; r < 4; ++r) O[b][r] = (O[b][r] + A[b][r]) * out;
+            if (FAST && __builtin_expect(vec & 1, 1)) {
+                const auto bo = o.rsrc(n);
+                const uint32_t f = o.first(n);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) Tr::store4o(bo, ato + (f + 16 * b * o.st), O[b]);
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int i = la_here(16 * b + c), col = la_here(n0 + 4 * g);
+                    if (i >= n) continue;
                     T* po = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h +
                             (t0 + dir * (p - p0 + i)) * P.o.t;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (col + r < dv) po[col + r] = Tr::store(x[r]);
+                        if (col + r < dv) po[col + r] = Tr::store(O[b][r]);
                 }
             }
             o.next();
