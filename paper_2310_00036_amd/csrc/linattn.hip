@@ -235,8 +235,8 @@ struct LaTile {
     static constexpr int ES = sizeof(typename Tr::T);
     static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16, RSP = kL * ES + 16;
     static constexpr int Q = 0, K = kL * RSK, V = 2 * kL * RSK, P = V + kL * RSV, PP = kL * RSP;
-    static constexpr int TAB = P + Tr::NP * PP;       // g^0 .. g^64, in g^0 .. in g^64, then X's and v's weights by row
-    static constexpr int BYTES = TAB + (2 * 68 + 2 * kL) * 4;
+    static constexpr int TAB = P + Tr::NP * PP;       // g^0 .. g^64, 16 zeros, in g^0 .. in g^64, X's and v's weights by row
+    static constexpr int BYTES = TAB + (2 * 68 + 16 + 2 * kL + 2) * 4;
     static constexpr int UQ = DK * ES / 16 / NW > 0 ? DK * ES / 16 / NW : 1;   // 16-byte pieces of q and k a thread moves
     static constexpr int UV = ES;                                             // of v
 };
@@ -248,8 +248,11 @@ struct LaRows {
     const char* p;             // the chunk's first row
     int st, bytes;             // bytes: of a row
     CB_DEV __amdgpu_buffer_rsrc_t rsrc(int n) const {
-        const int span = (n - 1) * st;
-        return buf_rsrc(span < 0 ? p + span : p, uint32_t(abs(span)) + bytes);
+        const int span = __builtin_amdgcn_readfirstlane((n - 1) * st);
+        const uint64_t b = reinterpret_cast<uint64_t>(span < 0 ? p + span : p);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(b)), hi = __builtin_amdgcn_readfirstlane(uint32_t(b >> 32));
+        return buf_rsrc(reinterpret_cast<const void*>(uint64_t(hi) << 32 | lo),
+                        __builtin_amdgcn_readfirstlane(abs(span) + bytes));
     }
     CB_DEV uint32_t first(int n) const { return uint32_t(max(0, -(n - 1) * st)); }
     CB_DEV uint32_t at(int row, int byte) const { return byte >= bytes ? kOOB : uint32_t(row * st + byte); }
@@ -295,7 +298,9 @@ CB_DEV float la_row_at(const typename Tr::Frag (&fv)[NJ], int j, int col) {
 #pragma unroll
     for (int jb = 0; jb < NJ; ++jb) {
         float x[Tr::KPL];
-        Tr::unpack(fv[jb], x);
+        typename Tr::Frag f = fv[jb];
+        asm volatile("" : "+v"(f.x), "+v"(f.y), "+v"(f.z), "+v"(f.w));   // unpacked here, not ahead of the rows' loop
+        Tr::unpack(f, x);
 #pragma unroll
         for (int u = 0; u < Tr::KPL; ++u) y = j / Tr::KB == jb && j % Tr::KPL == u ? x[u] : y;
     }
@@ -310,20 +315,23 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
     constexpr int KB = Tr::KB, KPL = Tr::KPL, NT = DK / 16, NJ = kL / KB;
     extern __shared__ __align__(16) unsigned char lds[];
     float* pw = reinterpret_cast<float*>(lds + L::TAB);
-    float* pin = pw + 68;
+    float* pin = pw + 68 + 16;
     float* xw = pin + 68;      // [c_i = 0] g^(i+l)
     float* vw = xw + kL;       // [c_j = c] in g^(n-l-j)
+    uint64_t* starts = reinterpret_cast<uint64_t*>(vw + kL);   // bit i: an episode starts at row i
 
     const int y = y0 + blockIdx.y;
     const LaPass& P = a.pass[y];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int nbs = (P.dv + 16 * NW - 1) / (16 * NW);
-    const int64_t EH = int64_t(a.E) * a.H;
-    const int64_t id = blockIdx.x / nbs;
-    const int nb0 = int(blockIdx.x % nbs) * 16 * NW, n0 = nb0 + 16 * wave;   // columns of the workgroup, of the wave
-    const int seg = int(id / EH);
-    const int64_t eh = id % EH, e = eh / a.H, h = eh % a.H;
+    const uint32_t nbs = (P.dv + 16 * NW - 1) / (16 * NW), EH = uint32_t(a.E) * a.H;   // EH <= 2^21
+    // (Quotients come from vector instructions; as scalars again, what is addressed by them needs no loop over lanes.)
+    auto quot = [](uint32_t x, uint32_t y) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x / y))); };
+    const uint32_t id = quot(blockIdx.x, nbs);
+    const int nb0 = int(blockIdx.x - id * nbs) * 16 * NW, n0 = nb0 + 16 * wave;   // columns of the workgroup, of the wave
+    const int seg = sg.segs > 1 ? int(quot(id, EH)) : 0;
+    const uint32_t eh32 = id - seg * EH, e32 = quot(eh32, a.H);
+    const int64_t eh = eh32, e = e32, h = eh32 - e32 * a.H;
     const int p0 = seg * sg.chunks * kL;
     const int p1 = sg.segs == 1 ? a.T : int(min(int64_t(a.T), int64_t(p0) + int64_t(sg.chunks) * kL));
 
@@ -334,38 +342,9 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         return LaRows{static_cast<const char*>(x.p) + (e * x.e + h * x.h + t0 * x.t) * L::ES, int(dir * x.t) * L::ES, d * L::ES};
     };
     LaRows q = rows(P.q, dk), k = rows(P.k, dk), v = rows(P.v, dv), o = rows(P.o, dv);
-    const uint8_t* dn = a.dones ? a.dones + e * a.d_e + t0 * a.d_t : nullptr;
-    const int64_t ds = dir * a.d_t;
+    LaRows dn{reinterpret_cast<const char*>(a.dones + (a.dones ? e * a.d_e + t0 * a.d_t : 0)), a.dones ? int(dir * a.d_t) : 0,
+              a.dones ? 1 : 0};
     const int later = back ? 0 : 1;
-
-    if (tid <= kL) {
-        const float w = float(exp(double(tid) * double(tid ? a.log_decay[h] : 0.f)));
-        pw[tid] = w;
-        pin[tid] = w * P.in;
-    }
-    if (!STATE && KB == 32) {   // products above the diagonal that a fragment of 32 rows takes along
-        for (int u = tid; u < 2 * 16 * Tr::NP * 4; u += 64 * NW) {
-            const int pl = u / (2 * 16 * 4), b = u / 64 % 2, i = u / 4 % 16, j = u % 4;
-            *reinterpret_cast<uint2*>(lds + L::P + pl * L::PP + (32 * b + i) * L::RSP + (32 * b + 16 + 4 * j) * L::ES) =
-                make_uint2(0, 0);
-        }
-    }
-
-    __syncthreads();
-    cb_f32x4 X[NT];
-    {
-        const float* x = P.x0 ? P.x0 + eh * P.dk * P.dv : nullptr;
-        int xk = P.xk, xn = P.xn;
-        if (STATE) x = nullptr;
-        else if (sg.segs > 1) { x = sg.state[y] + (seg * EH + eh) * P.dk * P.dv; xk = P.dv; xn = 1; }
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int kk = Tr::krow(m, g, r), n = n0 + c;
-                X[m][r] = x && kk < P.dk && n < P.dv ? x[kk * xk + n * xn] : 0.f;
-            }
-    }
 
     // the chunk's q, k and v on their way to LDS: 16-byte pieces, 64 rows of CQ or CV of them
     constexpr int CQ = DK * L::ES / 16, CV = 16 * NW * L::ES / 16;
@@ -387,13 +366,43 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             for (int u = 0; u < L::UV; ++u) rv[u] = buf_load16(bv, atv + (v.first(n) + u * RV * v.st));
         }
         // (Kept as it is loaded: a comparison here would wait for it and all loads before it.)
-        rd = 0;
-        if (dn && lane < n) rd = dn[lane * ds];
+        if (FAST && wave == 0) rd = __builtin_amdgcn_raw_buffer_load_b8(dn.rsrc(n), uint32_t(lane * dn.st) + dn.first(n), 0, 0);
     };
     const bool tail = vec & 2;
     const uint32_t ato = o.at(c, (n0 + 4 * g) * L::ES);
-    float factor = 1.f;
     fetch(min(kL, p1 - p0));
+
+    cb_f32x4 X[NT];
+    {
+        const float* x = P.x0 ? P.x0 + eh * P.dk * P.dv : nullptr;
+        int xk = P.xk, xn = P.xn;
+        if (STATE) x = nullptr;
+        else if (sg.segs > 1) { x = sg.state[y] + (int64_t(seg) * EH + eh) * P.dk * P.dv; xk = P.dv; xn = 1; }
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int kk = Tr::krow(m, g, r), n = n0 + c;
+                X[m][r] = x && kk < P.dk && n < P.dv ? x[kk * xk + n * xn] : 0.f;
+            }
+    }
+
+    if (tid < 16) pin[tid - 16] = 0.f;
+    if (tid <= kL) {
+        const float w = float(exp(double(tid) * double(tid ? a.log_decay[h] : 0.f)));
+        pw[tid] = w;
+        pin[tid] = w * P.in;
+    }
+    if (!STATE && KB == 32) {   // products above the diagonal that a fragment of 32 rows takes along
+        for (int u = tid; u < 2 * 16 * Tr::NP * 4; u += 64 * NW) {
+            const int pl = u / (2 * 16 * 4), b = u / 64 % 2, i = u / 4 % 16, j = u % 4;
+            *reinterpret_cast<uint2*>(lds + L::P + pl * L::PP + (32 * b + i) * L::RSP + (32 * b + 16 + 4 * j) * L::ES) =
+                make_uint2(0, 0);
+        }
+    }
+
+    lds_barrier();
+    float factor = 1.f;
     for (int p = p0; p < p1; p += kL) {
         const int n = min(kL, p1 - p);
         if (FAST) {
@@ -428,26 +437,34 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             for (int row = rowv; row < kL; row += RV)
                 *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + colv) = piece(P.v, row, nb0 + colv / L::ES, dv);
         }
-        const uint64_t m = __ballot(rd != 0);
-        // episode starts before what row i holds
-        auto count = [&](int i) { return __popcll(back ? m & ((uint64_t(1) << i) - 1) : m & (~uint64_t(0) >> (63 - i))); };
-        const int total = __popcll(m);
+        // episode starts before what row i holds, of the chunk's starts m
+        auto count_in = [&](uint64_t m, int i) {
+            return __popcll(back ? m & ((uint64_t(1) << i) - 1) : m & (~uint64_t(0) >> (63 - i)));
+        };
         if (wave == 0) {
-            const int ci = count(lane);
+            if (!FAST) rd = a.dones && lane < n ? a.dones[e * a.d_e + (t0 + dir * (p - p0 + lane)) * a.d_t] : 0;
+            const uint64_t m = __ballot(rd != 0 && lane < n);
+            const int ci = count_in(m, lane);
             xw[lane] = ci == 0 ? pw[lane + later] : 0.f;
-            vw[lane] = lane < n && ci == total ? pin[n - later - lane] : 0.f;
+            vw[lane] = lane < n && ci == __popcll(m) ? pin[n - later - lane] : 0.f;
+            if (lane == 0) *starts = m;
         }
         const float over = pw[n];
         lds_barrier();
-        q.next(); k.next(); v.next();
+        const uint64_t ms = *starts;
+        const uint64_t m = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(ms >> 32)))) << 32 |
+                           uint32_t(__builtin_amdgcn_readfirstlane(int(ms)));
+        auto count = [&](int i) { return count_in(m, i); };
+        const int total = __popcll(m);
+        q.next(); k.next(); v.next(); dn.next();
         if (p + kL < p1) {
-            if (dn) dn += kL * ds;
             fetch(min(kL, p1 - p - kL));
         }
 
         if (!STATE) {   // in g^(i-j) q_i . k_j by tiles on and below the diagonal, a wave's few at once
             constexpr int MT = (10 + NW - 1) / NW;
             cb_f32x4 d[MT];
+            float w[MT][4];
             int tb[MT], tt[MT];
 #pragma unroll
             for (int y = 0; y < MT; ++y) {
@@ -455,6 +472,8 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                 tb[y] = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3;
                 tt[y] = u - tb[y] * (tb[y] + 1) / 2;
                 d[y] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[y][r] = pin[16 * (tb[y] - tt[y]) + c - 4 * g - r];   // zero above the diagonal
             }
 #pragma unroll
             for (int kb = 0; kb < DK / KB; ++kb)
@@ -466,9 +485,13 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                 }
 #pragma unroll
             for (int y = 0; y < MT; ++y) {
-                const int i = 16 * tb[y] + c, j = 16 * tt[y] + 4 * g;
+                const int ij = 16 * (tb[y] - tt[y]) + c - 4 * g;   // i - j of the first of four rows j
 #pragma unroll
-                for (int r = 0; r < 4; ++r) d[y][r] = j + r <= i ? d[y][r] * pin[max(i - j - r, 0)] : 0.f;
+                for (int r = 0; r < 4; ++r) {
+                    float z = d[y][r] * w[y][r];
+                    asm("" : "+v"(z));   // a selection after it (for what is not finite), not a branch around the load
+                    d[y][r] = r <= ij ? z : 0.f;
+                }
             }
             if (__builtin_expect(m != 0, 0)) {
 #pragma unroll
@@ -495,14 +518,16 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             for (int b = 0; b < 4; ++b) O[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < DK / KB; ++kb) {
-                Frag fx[Tr::NX];
+                Frag fx[Tr::NX], fq[4];
                 Tr::xfrag(X, kb, fx);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const Frag fq = *reinterpret_cast<const Frag*>(lds + L::Q + (16 * b + c) * L::RSK + kb * 64 + 16 * g);
+                for (int b = 0; b < 4; ++b)
+                    fq[b] = *reinterpret_cast<const Frag*>(lds + L::Q + (16 * b + c) * L::RSK + kb * 64 + 16 * g);
+                // (Neighbouring products go to different sums: one on another's result waits for it.)
 #pragma unroll
-                    for (int u = 0; u < Tr::NX; ++u) O[b] = Tr::mma(fx[u], fq, O[b]);
-                }
+                for (int u = 0; u < Tr::NX; ++u)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) O[b] = Tr::mma(fx[u], fq[b], O[b]);
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) O[b] *= xw[16 * b + c];
@@ -527,11 +552,16 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                     for (int u = 0; u < KPL; ++u) x[u] *= vw[jb * KB + KPL * g + u];
                     Frag fw[Tr::NV];
                     Tr::split(x, fw);
+                    constexpr int TG = NT < 4 ? NT : 4;   // at a time
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const Frag fk = clean(Tr::kcols(lds + L::K, L::RSK, jb * KB, t));
+                    for (int t0 = 0; t0 < NT; t0 += TG) {
+                        Frag fk[TG];
 #pragma unroll
-                        for (int u = Tr::NV - 1; u >= 0; --u) U[t] = Tr::mma(fk, fw[u], U[t]);
+                        for (int t = 0; t < TG; ++t) fk[t] = clean(Tr::kcols(lds + L::K, L::RSK, jb * KB, t0 + t));
+#pragma unroll
+                        for (int u = Tr::NV - 1; u >= 0; --u)
+#pragma unroll
+                            for (int t = 0; t < TG; ++t) U[t0 + t] = Tr::mma(fk[t], fw[u], U[t0 + t]);
                     }
                 }
             };
@@ -571,19 +601,21 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             cb_f32x4 A[4];
             auto rows = [&](auto clean) CB_INLINE_LAMBDA {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    A[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int b = 0; b < 4; ++b) A[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int jb = 0; jb < NJ; ++jb) {
-                        if (jb * KB > 16 * b + 15) continue;
+                for (int jb = 0; jb < NJ; ++jb)
 #pragma unroll
-                        for (int u = Tr::NP - 1; u >= 0; --u) {
-                            const Frag fp = *reinterpret_cast<const Frag*>(lds + L::P + u * L::PP + (16 * b + c) * L::RSP +
-                                                                           jb * 64 + 16 * g);
-                            A[b] = Tr::mma(clean(fv[jb]), fp, A[b]);
-                        }
+                    for (int u = Tr::NP - 1; u >= 0; --u) {
+                        Frag fp[4];
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            if (jb * KB <= 16 * b + 15)
+                                fp[b] = *reinterpret_cast<const Frag*>(lds + L::P + u * L::PP + (16 * b + c) * L::RSP +
+                                                                       jb * 64 + 16 * g);
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            if (jb * KB <= 16 * b + 15) A[b] = Tr::mma(clean(fv[jb]), fp[b], A[b]);
                     }
-                }
             };
             rows([](Frag f) { return f; });
             float sum = 0.f;
@@ -637,7 +669,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         }
     }
 
-    float* x = STATE ? sg.state[y] + (seg * EH + eh) * P.dk * P.dv : seg == sg.segs - 1 && P.x1 ? P.x1 + eh * P.dk * P.dv : nullptr;
+    float* x = STATE ? sg.state[y] + (int64_t(seg) * EH + eh) * P.dk * P.dv : seg == sg.segs - 1 && P.x1 ? P.x1 + eh * P.dk * P.dv : nullptr;
     if (x) {
         const int xk = STATE ? P.dv : P.xk, xn = STATE ? 1 : P.xn;
 #pragma unroll
@@ -648,7 +680,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                 if (kk < P.dk && n < P.dv) x[kk * xk + n * xn] = X[m][r];
             }
     }
-    if (STATE && tid == 0 && nb0 == 0) sg.factor[y][seg * EH + eh] = factor;
+    if (STATE && tid == 0 && nb0 == 0) sg.factor[y][int64_t(seg) * EH + eh] = factor;
 }
 
 // The states before the segments, in place of their contributions.
@@ -770,7 +802,7 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     for (int y = 0; y < a.np; ++y) {
         LaPass& P = a.pass[y];
         P.vec = (reach(P.o, P.dv) && P.dv % 4 == 0) | (P.dk % ve != 0 || P.dv % ve != 0) << 1 |
-                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv)) << 2;
+                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv) && a.d_t < (int64_t(1) << 24)) << 2;
         if (sg.segs == 1) continue;
         sg.state[y] = reinterpret_cast<float*>(w);
         w += la_a256(sg.segs * EH * P.dk * P.dv * 4);
