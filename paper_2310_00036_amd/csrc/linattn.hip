@@ -372,24 +372,41 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
     const uint32_t ato = o.at(c, (n0 + 4 * g) * L::ES);
     fetch(min(kL, p1 - p0));
 
+    // X's numbers in a state: results m, rows krow(m, g, r), column n0 + c; what the state has not is zero, and not written.
     cb_f32x4 X[NT];
+    const int xcol = n0 + c;
+    auto state = [&](const float* x) {
+        const uint64_t q = reinterpret_cast<uint64_t>(x + eh * dk * dv);
+        return buf_rsrc(reinterpret_cast<const void*>(q), x ? uint32_t(dk * dv * 4) : 0u);
+    };
+    auto xat = [&](int kk, int xk, int xn) { return kk < dk && xcol < dv ? uint32_t(kk * xk + xcol * xn) * 4 : kOOB; };
     {
-        const float* x = P.x0 ? P.x0 + eh * P.dk * P.dv : nullptr;
+        const float* x = P.x0;
         int xk = P.xk, xn = P.xn;
         if (STATE) x = nullptr;
-        else if (sg.segs > 1) { x = sg.state[y] + (int64_t(seg) * EH + eh) * P.dk * P.dv; xk = P.dv; xn = 1; }
+        else if (sg.segs > 1) { x = sg.state[y] + int64_t(seg) * EH * dk * dv; xk = dv; xn = 1; }
+        const auto bx = state(x);
+        if (xk == 1 && dk % 4 == 0) {
 #pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int kk = Tr::krow(m, g, r), n = n0 + c;
-                X[m][r] = x && kk < P.dk && n < P.dv ? x[kk * xk + n * xn] : 0.f;
+            for (int m = 0; m < NT; ++m) {
+                const uint4 v = buf_load16(bx, xat(Tr::krow(m, g, 0), 1, xn));
+                X[m] = cb_f32x4{__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
             }
+        } else {
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    X[m][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(bx, xat(Tr::krow(m, g, r), xk, xn), 0, 0));
+        }
     }
 
     if (tid < 16) pin[tid - 16] = 0.f;
     if (tid <= kL) {
-        const float w = float(exp(double(tid) * double(tid ? a.log_decay[h] : 0.f)));
+        // exp(tid log g), the product's rounding error made good
+        const float ld = a.log_decay[h], x = tid ? float(tid) * ld : 0.f, lo = fmaf(float(tid), ld, -x);
+        float w = expf(x);
+        w = tid && isfinite(x) ? fmaf(w, lo, w) : w;
         pw[tid] = w;
         pin[tid] = w * P.in;
     }
@@ -669,16 +686,15 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         }
     }
 
-    float* x = STATE ? sg.state[y] + (int64_t(seg) * EH + eh) * P.dk * P.dv : seg == sg.segs - 1 && P.x1 ? P.x1 + eh * P.dk * P.dv : nullptr;
+    float* x = STATE ? sg.state[y] + int64_t(seg) * EH * dk * dv : seg == sg.segs - 1 ? P.x1 : nullptr;
     if (x) {
-        const int xk = STATE ? P.dv : P.xk, xn = STATE ? 1 : P.xn;
+        const int xk = STATE ? dv : P.xk, xn = STATE ? 1 : P.xn;
+        const auto bx = state(x);
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int kk = Tr::krow(m, g, r), n = n0 + c;
-                if (kk < P.dk && n < P.dv) x[kk * xk + n * xn] = X[m][r];
-            }
+            for (int r = 0; r < 4; ++r)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(X[m][r]), bx, xat(Tr::krow(m, g, r), xk, xn), 0, 0);
     }
     if (STATE && tid == 0 && nb0 == 0) sg.factor[y][int64_t(seg) * EH + eh] = factor;
 }
