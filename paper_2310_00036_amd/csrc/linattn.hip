@@ -235,7 +235,7 @@ struct LaTile {
     static constexpr int ES = sizeof(typename Tr::T);
     static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16, RSP = kL * ES + 16;
     static constexpr int Q = 0, K = kL * RSK, V = 2 * kL * RSK, P = V + kL * RSV, PP = kL * RSP;
-    static constexpr int TAB = P + Tr::NP * PP;       // g^0 .. g^64, 16 zeros, in g^0 .. in g^64, X's and v's weights by row
+    static constexpr int TAB = P + Tr::NP * PP;       // g^0 .. g^64, 16 zeros, in out g^0 .. in out g^64, X's and v's weights by row
     static constexpr int BYTES = TAB + (2 * 68 + 16 + 2 * kL + 2) * 4;
     static constexpr int UQ = DK * ES / 16 / NW > 0 ? DK * ES / 16 / NW : 1;   // 16-byte pieces of q and k a thread moves
     static constexpr int UV = ES;                                             // of v
@@ -308,7 +308,7 @@ CB_DEV float la_row_at(const typename Tr::Frag (&fv)[NJ], int j, int col) {
 }
 
 template <class Tr, int DK, int NW, bool STATE, bool FAST>
-__global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0) {
+__global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0, int ny, int blocks) {
     using T = typename Tr::T;
     using Frag = typename Tr::Frag;
     using L = LaTile<Tr, DK, NW>;
@@ -316,19 +316,24 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
     extern __shared__ __align__(16) unsigned char lds[];
     float* pw = reinterpret_cast<float*>(lds + L::TAB);
     float* pin = pw + 68 + 16;
-    float* xw = pin + 68;      // [c_i = 0] g^(i+l)
+    float* xw = pin + 68;      // [c_i = 0] out g^(i+l)
     float* vw = xw + kL;       // [c_j = c] in g^(n-l-j)
     uint64_t* starts = reinterpret_cast<uint64_t*>(vw + kL);   // bit i: an episode starts at row i
 
-    const int y = y0 + blockIdx.y;
+    // Workgroups go round the 8 XCDs one by one: those of the passes on one state, which read the same arrays, are 8 apart,
+    // so they share an L2 at about the same time.
+    // (Quotients come from vector instructions; as scalars again, what is addressed by them needs no loop over lanes.)
+    auto quot = [](uint32_t x, uint32_t y) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x / y))); };
+    const uint32_t turn = blockIdx.x >> 3, turn_y = ny > 1 ? quot(turn, ny) : turn;
+    const int y = y0 + int(turn - turn_y * ny);
+    const uint32_t bid = turn_y * 8 + (blockIdx.x & 7);
+    if (int(bid) >= blocks) return;
     const LaPass& P = a.pass[y];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const uint32_t nbs = (P.dv + 16 * NW - 1) / (16 * NW), EH = uint32_t(a.E) * a.H;   // EH <= 2^21
-    // (Quotients come from vector instructions; as scalars again, what is addressed by them needs no loop over lanes.)
-    auto quot = [](uint32_t x, uint32_t y) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x / y))); };
-    const uint32_t id = quot(blockIdx.x, nbs);
-    const int nb0 = int(blockIdx.x - id * nbs) * 16 * NW, n0 = nb0 + 16 * wave;   // columns of the workgroup, of the wave
+    const uint32_t id = nbs > 1 ? quot(bid, nbs) : bid;
+    const int nb0 = int(bid - id * nbs) * 16 * NW, n0 = nb0 + 16 * wave;   // columns of the workgroup, of the wave
     const int seg = sg.segs > 1 ? int(quot(id, EH)) : 0;
     const uint32_t eh32 = id - seg * EH, e32 = quot(eh32, a.H);
     const int64_t eh = eh32, e = e32, h = eh32 - e32 * a.H;
@@ -393,11 +398,15 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                 X[m] = cb_f32x4{__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
             }
         } else {
+            // rows behind the last are behind the state's end where rows are its outer axis
+            const uint32_t at = xat(Tr::krow(0, g, 0), xk, xn);
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    X[m][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(bx, xat(Tr::krow(m, g, r), xk, xn), 0, 0));
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t off = xn == 1 ? (at == kOOB ? kOOB : at + Tr::krow(m, 0, r) * xk * 4) : xat(Tr::krow(m, g, r), xk, xn);
+                    X[m][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(bx, off, 0, 0));
+                }
         }
     }
 
@@ -408,7 +417,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         float w = expf(x);
         w = tid && isfinite(x) ? fmaf(w, lo, w) : w;
         pw[tid] = w;
-        pin[tid] = w * P.in;
+        pin[tid] = w * P.in * out;
     }
     if (!STATE && KB == 32) {   // products above the diagonal that a fragment of 32 rows takes along
         for (int u = tid; u < 2 * 16 * Tr::NP * 4; u += 64 * NW) {
@@ -462,8 +471,8 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             if (!FAST) rd = a.dones && lane < n ? a.dones[e * a.d_e + (t0 + dir * (p - p0 + lane)) * a.d_t] : 0;
             const uint64_t m = __ballot(rd != 0 && lane < n);
             const int ci = count_in(m, lane);
-            xw[lane] = ci == 0 ? pw[lane + later] : 0.f;
-            vw[lane] = lane < n && ci == __popcll(m) ? pin[n - later - lane] : 0.f;
+            xw[lane] = ci == 0 ? pw[lane + later] * out : 0.f;
+            vw[lane] = lane < n && ci == __popcll(m) ? pw[n - later - lane] * P.in : 0.f;
             if (lane == 0) *starts = m;
         }
         const float over = pw[n];
@@ -478,7 +487,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             fetch(min(kL, p1 - p - kL));
         }
 
-        if (!STATE) {   // in g^(i-j) q_i . k_j by tiles on and below the diagonal, a wave's few at once
+        if (!STATE) {   // in out g^(i-j) q_i . k_j by tiles on and below the diagonal, a wave's few at once
             constexpr int MT = (10 + NW - 1) / NW;
             cb_f32x4 d[MT];
             float w[MT][4];
@@ -501,15 +510,9 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                     d[y] = Tr::mma(fk, fq, d[y]);
                 }
 #pragma unroll
-            for (int y = 0; y < MT; ++y) {
-                const int ij = 16 * (tb[y] - tt[y]) + c - 4 * g;   // i - j of the first of four rows j
+            for (int y = 0; y < MT; ++y)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float z = d[y][r] * w[y][r];
-                    asm("" : "+v"(z));   // a selection after it (for what is not finite), not a branch around the load
-                    d[y][r] = r <= ij ? z : 0.f;
-                }
-            }
+                for (int r = 0; r < 4; ++r) d[y][r] *= w[y][r];
             if (__builtin_expect(m != 0, 0)) {
 #pragma unroll
                 for (int y = 0; y < MT; ++y) {
@@ -585,7 +588,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             rows([](Frag f) { return f; });
             float sum = 0.f;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) sum += (U[t][0] + U[t][1]) + (U[t][2] + U[t][3]);
+            for (int t = 0; t < NT; ++t) sum = fmaf(U[t][0], U[t][1], fmaf(U[t][2], U[t][3], sum));
             // A number that is not finite comes through a weight of zero as NaN. Then without all such, and theirs added
             // for the rows that the state sees.
             if (__builtin_expect(__any(sum != sum), 0)) {
@@ -631,13 +634,13 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                                                                        jb * 64 + 16 * g);
 #pragma unroll
                         for (int b = 0; b < 4; ++b)
-                            if (jb * KB <= 16 * b + 15) A[b] = Tr::mma(clean(fv[jb]), fp[b], A[b]);
+                            if (jb * KB <= 16 * b + 15) A[b] = Tr::mma(clean(fv[jb]), clean(fp[b]), A[b]);
                     }
             };
             rows([](Frag f) { return f; });
             float sum = 0.f;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) sum += (A[b][0] + A[b][1]) + (A[b][2] + A[b][3]);
+            for (int b = 0; b < 4; ++b) sum = fmaf(A[b][0], A[b][1], fmaf(A[b][2], A[b][3], sum));
             if (__builtin_expect(__any(sum != sum), 0)) {   // as above: a later row's, or one's of another episode
                 asm volatile("" ::: "memory");
                 rows([](Frag f) { return Tr::finite(f); });
@@ -657,14 +660,14 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                             w += Tr::load(*reinterpret_cast<const T*>(lds + L::P + u * L::PP + i * L::RSP + j * L::ES));
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (!isfinite(x[r])) A[b][r] += w * x[r];
+                            if (!isfinite(x[r]) || !isfinite(w)) A[b][r] += w * x[r];
                     }
                 }
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) O[b][r] = (O[b][r] + A[b][r]) * out;
+                for (int r = 0; r < 4; ++r) O[b][r] += A[b][r];
             if (FAST && __builtin_expect(vec & 1, 1)) {
                 const auto bo = o.rsrc(n);
                 const uint32_t f = o.first(n);
@@ -721,10 +724,11 @@ template <class Tr, int DK, int NW>
 hipError_t la_chunks_launch(const LaArgs& a, const LaSegs& sg, int y0, int ny, bool state, hipStream_t s) {
     using L = LaTile<Tr, DK, NW>;
     const int64_t nbs = (a.pass[y0].dv + 16 * NW - 1) / (16 * NW);
-    const dim3 grid(unsigned(int64_t(a.E) * a.H * nbs * (state ? sg.segs - 1 : sg.segs)), unsigned(ny));
+    const int blocks = int(int64_t(a.E) * a.H * nbs * (state ? sg.segs - 1 : sg.segs));
+    const dim3 grid(unsigned((blocks + 7) / 8 * 8 * ny));
     bool fast = true;
     for (int y = y0; y < y0 + ny; ++y) fast &= a.pass[y].vec >> 2 & 1;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), L::BYTES, s, a, sg, y0); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), L::BYTES, s, a, sg, y0, ny, blocks); };
     if (state) fast ? go(la_chunk_kernel<Tr, DK, NW, true, true>) : go(la_chunk_kernel<Tr, DK, NW, true, false>);
     else fast ? go(la_chunk_kernel<Tr, DK, NW, false, true>) : go(la_chunk_kernel<Tr, DK, NW, false, false>);
     return hipGetLastError();
