@@ -91,6 +91,105 @@ __global__ __launch_bounds__(64) void la_steps_kernel(LaArgs a, int y0) {
     }
 }
 
+// One step from state to state, HBM-bound: the state is read and written once. A workgroup has one state, a thread four
+// neighbouring columns of every (NT / LR)th row, all loaded before anything waits (LR: the lanes of a row, a power of two).
+// 4096 envs x 8 heads of 128 x 128: 4.3 GB in 0.9 ms.
+template <class Pr, int NT, int LR>
+__global__ __launch_bounds__(NT) void la_step_kernel(LaArgs a) {
+    using T = typename Pr::T;
+    constexpr int RP = NT / LR;                      // rows at a time
+    constexpr int UN = (kLaMaxDim + RP - 1) / RP;    // of them, at most
+    __shared__ float sq[kLaMaxDim], sk[kLaMaxDim];
+    __shared__ float4 red[NT / 64][LR];
+    const LaPass& P = a.pass[0];
+    const int tid = threadIdx.x, col = tid % LR * 4, r0 = tid / LR, dk = P.dk, dv = P.dv;
+    const uint32_t eh = blockIdx.x, e = eh / uint32_t(a.H), h = eh - e * a.H;
+    const bool cut = a.dones && a.dones[int64_t(e) * a.d_e];
+    const int64_t base = int64_t(eh) * dk * dv;
+    const bool whole = dv % 4 == 0;
+    float4 x[UN];
+    const float* px = P.x0 && !cut && col < dv ? P.x0 + base + col : nullptr;
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+        const int kk = r0 + u * RP;
+        x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (u * RP >= dk) break;
+        if (px && kk < dk) {
+            const float* p = px + kk * dv;
+            if (whole) x[u] = load_f4(p);
+            else {
+                x[u].x = p[0];
+                if (col + 1 < dv) x[u].y = p[1];
+                if (col + 2 < dv) x[u].z = p[2];
+                if (col + 3 < dv) x[u].w = p[3];
+            }
+        }
+    }
+    const T* v = static_cast<const T*>(P.v.p) + e * P.v.e + h * P.v.h;
+    const T* q = static_cast<const T*>(P.q.p) + e * P.q.e + h * P.q.h;
+    const T* k = static_cast<const T*>(P.k.p) + e * P.k.e + h * P.k.h;
+    for (int i = tid; i < dk; i += NT) { sq[i] = Pr::load(q[i]); sk[i] = Pr::load(k[i]); }
+    float vv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vv[i] = col + i < dv ? Pr::load(v[col + i]) : 0.f;
+    const float gd = float(exp(double(a.log_decay[h])));
+    __syncthreads();
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float* py = P.x1 ? P.x1 + base + col : nullptr;
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+        const int kk = r0 + u * RP;
+        if (u * RP >= dk) break;
+        if (kk < dk && col < dv) {
+            const float kf = sk[kk], qf = sq[kk];
+            // (without a state before it there is nothing to decay: zero times a decay of infinity is none)
+            x[u].x = (px ? gd * x[u].x : 0.f) + kf * vv[0];
+            x[u].y = (px ? gd * x[u].y : 0.f) + kf * vv[1];
+            x[u].z = (px ? gd * x[u].z : 0.f) + kf * vv[2];
+            x[u].w = (px ? gd * x[u].w : 0.f) + kf * vv[3];
+            o.x += qf * x[u].x; o.y += qf * x[u].y; o.z += qf * x[u].z; o.w += qf * x[u].w;
+            if (py) {
+                float* p = py + kk * dv;
+                if (whole) *reinterpret_cast<cb_f32x4_a4*>(p) = cb_f32x4_a4{x[u].x, x[u].y, x[u].z, x[u].w};
+                else {
+                    p[0] = x[u].x;
+                    if (col + 1 < dv) p[1] = x[u].y;
+                    if (col + 2 < dv) p[2] = x[u].z;
+                    if (col + 3 < dv) p[3] = x[u].w;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int d = LR; d < 64; d *= 2) {
+        o.x += __shfl_xor(o.x, d); o.y += __shfl_xor(o.y, d); o.z += __shfl_xor(o.z, d); o.w += __shfl_xor(o.w, d);
+    }
+    if ((tid & 63) < LR) red[tid >> 6][tid & 63] = o;
+    __syncthreads();
+    if (tid < LR && col < dv) {
+#pragma unroll
+        for (int w = 1; w < NT / 64; ++w) {
+            const float4 t = red[w][tid];
+            o.x += t.x; o.y += t.y; o.z += t.z; o.w += t.w;
+        }
+        T* po = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h + col;
+        const float y[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < dv) po[i] = Pr::store(y[i] * P.out);
+    }
+}
+
+template <class Pr>
+hipError_t la_step(const LaArgs& a, hipStream_t s) {
+    const LaPass& P = a.pass[0];
+    const dim3 grid(unsigned(int64_t(a.E) * a.H));
+    if (P.dv <= 32) hipLaunchKernelGGL((la_step_kernel<Pr, 64, 8>), grid, dim3(64), 0, s, a);
+    else if (P.dv <= 64) hipLaunchKernelGGL((la_step_kernel<Pr, 256, 16>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((la_step_kernel<Pr, 256, 32>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
 template <class Pr>
 hipError_t la_steps(const LaArgs& a, hipStream_t s) {
     for (int y = 0; y < a.np; ++y) {
@@ -230,12 +329,12 @@ struct LaSegs {
     float* factor[kLaMaxPasses];   // [segs][E H]: what a segment leaves of the state before it; -1: an episode starts in it
 };
 
-template <class Tr, int DK, int NW>
-struct LaTile {
+template <class Tr, int DK, int NW, bool STATE>
+struct LaTile {   // STATE: without q and the products
     static constexpr int ES = sizeof(typename Tr::T);
     static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16, RSP = kL * ES + 16;
-    static constexpr int Q = 0, K = kL * RSK, V = 2 * kL * RSK, P = V + kL * RSV, PP = kL * RSP;
-    static constexpr int TAB = P + Tr::NP * PP;       // g^0 .. g^64, 16 zeros, in out g^0 .. in out g^64, X's and v's weights by row
+    static constexpr int Q = 0, K = STATE ? 0 : kL * RSK, V = K + kL * RSK, P = V + kL * RSV, PP = kL * RSP;
+    static constexpr int TAB = STATE ? P : P + Tr::NP * PP;       // g^0 .. g^64, 16 zeros, in out g^0 .. in out g^64, X's and v's weights by row
     static constexpr int BYTES = TAB + (2 * 68 + 16 + 2 * kL + 2) * 4;
     static constexpr int UQ = DK * ES / 16 / NW > 0 ? DK * ES / 16 / NW : 1;   // 16-byte pieces of q and k a thread moves
     static constexpr int UV = ES;                                             // of v
@@ -308,10 +407,10 @@ CB_DEV float la_row_at(const typename Tr::Frag (&fv)[NJ], int j, int col) {
 }
 
 template <class Tr, int DK, int NW, bool STATE, bool FAST>
-__global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0, int ny, int blocks) {
+__global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T) == 2 ? 4 : 2) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0, int ny, int blocks) {
     using T = typename Tr::T;
     using Frag = typename Tr::Frag;
-    using L = LaTile<Tr, DK, NW>;
+    using L = LaTile<Tr, DK, NW, STATE>;
     constexpr int KB = Tr::KB, KPL = Tr::KPL, NT = DK / 16, NJ = kL / KB;
     extern __shared__ __align__(16) unsigned char lds[];
     float* pw = reinterpret_cast<float*>(lds + L::TAB);
@@ -375,6 +474,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
     };
     const bool tail = vec & 2;
     const uint32_t ato = o.at(c, (n0 + 4 * g) * L::ES);
+    const bool busy = n0 < dv;   // a wave behind the last column only moves rows and forms products
     fetch(min(kL, p1 - p0));
 
     // X's numbers in a state: results m, rows krow(m, g, r), column n0 + c; what the state has not is zero, and not written.
@@ -482,7 +582,8 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                            uint32_t(__builtin_amdgcn_readfirstlane(int(ms)));
         auto count = [&](int i) { return count_in(m, i); };
         const int total = __popcll(m);
-        q.next(); k.next(); v.next(); dn.next();
+        if (STATE) factor = total || factor < 0.f ? -1.f : factor * over;
+        q.next(); k.next(); v.next(); dn.next(); if (p > p0) o.next();
         if (p + kL < p1) {
             fetch(min(kL, p1 - p - kL));
         }
@@ -528,6 +629,7 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
         }
 
         __builtin_amdgcn_sched_barrier(0);
+        if (!busy) { lds_barrier(); continue; }
         Frag fv[NJ];
 #pragma unroll
         for (int jb = 0; jb < NJ; ++jb) fv[jb] = Tr::template cols<1>(lds + L::V, L::RSV, jb * KB, 16 * wave);
@@ -613,7 +715,6 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) X[t][r] = (total ? 0.f : over * X[t][r]) + U[t][r];
-            if (STATE) factor = total || factor < 0.f ? -1.f : factor * over;
         }
         lds_barrier();
 
@@ -685,7 +786,6 @@ __global__ __launch_bounds__(64 * NW, 2) void la_chunk_kernel(LaArgs a, LaSegs s
                         if (col + r < dv) po[col + r] = Tr::store(O[b][r]);
                 }
             }
-            o.next();
         }
     }
 
@@ -722,27 +822,31 @@ __global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, LaSegs sg) {
 
 template <class Tr, int DK, int NW>
 hipError_t la_chunks_launch(const LaArgs& a, const LaSegs& sg, int y0, int ny, bool state, hipStream_t s) {
-    using L = LaTile<Tr, DK, NW>;
     const int64_t nbs = (a.pass[y0].dv + 16 * NW - 1) / (16 * NW);
     const int blocks = int(int64_t(a.E) * a.H * nbs * (state ? sg.segs - 1 : sg.segs));
     const dim3 grid(unsigned((blocks + 7) / 8 * 8 * ny));
     bool fast = true;
     for (int y = y0; y < y0 + ny; ++y) fast &= a.pass[y].vec >> 2 & 1;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), L::BYTES, s, a, sg, y0, ny, blocks); };
+    const int lds = state ? LaTile<Tr, DK, NW, true>::BYTES : LaTile<Tr, DK, NW, false>::BYTES;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), lds, s, a, sg, y0, ny, blocks); };
     if (state) fast ? go(la_chunk_kernel<Tr, DK, NW, true, true>) : go(la_chunk_kernel<Tr, DK, NW, true, false>);
     else fast ? go(la_chunk_kernel<Tr, DK, NW, false, true>) : go(la_chunk_kernel<Tr, DK, NW, false, false>);
     return hipGetLastError();
 }
 
 int la_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+// Waves of a workgroup, 16 columns each. Float32 rows of 128 take eight whatever the columns, to move the rows.
+int la_waves(int prec, int dk, int dv) { return prec == 1 && la_dim(dk) == 128 ? 8 : la_dim(dv) / 16; }
 
 template <class Tr, int DK>
 hipError_t la_chunks_nw(const LaArgs& a, const LaSegs& sg, int y0, int ny, bool state, hipStream_t s) {
-    switch (la_dim(a.pass[y0].dv)) {
-        case 32: return la_chunks_launch<Tr, DK, 2>(a, sg, y0, ny, state, s);
-        case 64: return la_chunks_launch<Tr, DK, 4>(a, sg, y0, ny, state, s);
-        default: return la_chunks_launch<Tr, DK, 8>(a, sg, y0, ny, state, s);
+    if constexpr (!(sizeof(typename Tr::T) == 4 && DK == 128)) {
+        switch (la_waves(sizeof(typename Tr::T) == 4, DK, a.pass[y0].dv)) {
+            case 2: return la_chunks_launch<Tr, DK, 2>(a, sg, y0, ny, state, s);
+            case 4: return la_chunks_launch<Tr, DK, 4>(a, sg, y0, ny, state, s);
+        }
     }
+    return la_chunks_launch<Tr, DK, 8>(a, sg, y0, ny, state, s);
 }
 
 // Passes whose kernels are the same go in one launch.
@@ -764,12 +868,20 @@ hipError_t la_chunks(const LaArgs& a, const LaSegs& sg, bool state, hipStream_t 
 
 constexpr int kLaSteps = 16;   // rollouts up to here go row by row
 
-// Segments of the rollout that run at once: as many as give the chip 512 workgroups, of two chunks at least.
-int la_segs(int T, int64_t chains, int* chunks) {
+// Segments of the rollout that run at once: as many as fill the chip's places for workgroups once, of four chunks at
+// least. Each segment's state has to be known first, which reads k and v again and takes two launches more: less than
+// three segments gain nothing. (16384 x 2 envs x 8 heads of 128: 16 chains of 256 chunks, which take 5.8 us each;
+// in 16 segments 145 us in all.)
+int la_segs(int prec, int T, int64_t EH, int dk, int dv, int passes, int* chunks) {
     const int64_t nc = (int64_t(T) + kL - 1) / kL;
     *chunks = int(nc);
-    if (T <= kLaSteps || chains <= 0 || chains >= 256 || nc < 4) return 1;
-    const int64_t want = std::min<int64_t>((512 + chains - 1) / chains, nc / 2);
+    if (T <= kLaSteps || EH == 0) return 1;
+    // passes of a launch: of the backward's three, the two that contract over v's axis, or all where the kernels are one
+    const int together = passes > 1 ? (la_dim(dk) == la_dim(dv) ? 3 : 2) : 1, out = passes > 1 ? dk : dv;
+    const int waves = la_waves(prec, passes > 1 ? dv : dk, out);
+    const int64_t chains = EH * together, places = 256 * (8 / waves);   // a CU holds 8 waves
+    const int64_t want = std::min(places / chains, nc / 4);
+    if (want < 3) return 1;
     *chunks = int((nc + want - 1) / want);
     return int((nc + *chunks - 1) / *chunks);
 }
@@ -784,9 +896,9 @@ __global__ void la_empty_kernel(const float* x0, float* x1, int64_t n) {
 
 }  // namespace
 
-size_t linattn_ws_bytes(int, int T, int E, int H, int dk, int dv, int passes) {
+size_t linattn_ws_bytes(int prec, int T, int E, int H, int dk, int dv, int passes) {
     int chunks;
-    const int64_t EH = int64_t(E) * H, segs = la_segs(T, EH * passes, &chunks);
+    const int64_t EH = int64_t(E) * H, segs = la_segs(prec, T, EH, dk, dv, passes, &chunks);
     if (segs == 1) return 0;
     return size_t(passes * (la_a256(segs * EH * dk * dv * 4) + la_a256(segs * EH * 4)));
 }
@@ -807,6 +919,7 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
         return cb_key("linattn", prec, std::to_string(a.T) + "x" + std::to_string(a.E) + "x" + std::to_string(a.H) + "x" +
                                            cb_dims(a.pass[0].dk, a.pass[0].dv) + (a.np > 1 ? "/bwd" : ""));
     });
+    if (a.T == 1 && a.np == 1) return prec == 0 ? la_step<PrecBF16>(a, s) : la_step<PrecF32>(a, s);
     if (a.T <= kLaSteps) return prec == 0 ? la_steps<PrecBF16>(a, s) : la_steps<PrecF32>(a, s);
     const int es = prec == 0 ? 2 : 4, ve = 16 / es;
     // Rows that a buffer resource reaches: at whole words, each behind the last one's end, 64 of them within 2^31 bytes.
@@ -817,7 +930,8 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     };
     LaSegs sg{};
     const int64_t EH = int64_t(a.E) * a.H;
-    sg.segs = la_segs(a.T, EH * a.np, &sg.chunks);
+    const LaPass& last = a.pass[a.np - 1];   // the one whose axes are k's and v's, in either direction
+    sg.segs = la_segs(prec, a.T, EH, last.dk, last.dv, a.np, &sg.chunks);
     char* w = static_cast<char*>(ws);
     for (int y = 0; y < a.np; ++y) {
         LaPass& P = a.pass[y];
