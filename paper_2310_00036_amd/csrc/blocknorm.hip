@@ -20,20 +20,26 @@ typedef uint32_t bn_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 template <class T>
 struct BnVec {
     static constexpr int N = 16 / sizeof(T);
-    static CB_DEV void load(const T* p, int left, float* x) {
+    static CB_DEV uint4 raw(const T* p, int left) {   // zeros behind `left` elements
         if (left >= N) {
             const bn_u32x4 v = *reinterpret_cast<const bn_u32x4*>(p);
+            return make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(T) == 2) { x[2 * i] = bf_lo(v[i]); x[2 * i + 1] = bf_hi(v[i]); }
-                else x[i] = __uint_as_float(v[i]);
+        for (int i = 0; i < N; ++i)
+            if (i < left) {
+                if constexpr (sizeof(T) == 2) w[i / 2] |= uint32_t(p[i]) << (16 * (i & 1));
+                else w[i] = __float_as_uint(p[i]);
             }
-        } else {
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static CB_DEV void unpack(uint4 v, float* x) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if constexpr (sizeof(T) == 2) x[i] = i < left ? bf2f(p[i]) : 0.f;
-                else x[i] = i < left ? p[i] : 0.f;
-            }
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2) { x[2 * i] = bf_lo(w[i]); x[2 * i + 1] = bf_hi(w[i]); }
+            else x[i] = __uint_as_float(w[i]);
         }
     }
     static CB_DEV void store(T* p, int left, const float* x) {
@@ -77,57 +83,100 @@ struct BnPlace {
     }
 };
 
-// Sums of K numbers over the tpr threads of a row, in every one of them, in a fixed order.
+// x plus that of the lane that `ctrl` names, by a data-parallel-primitive move.
+template <int CTRL>
+CB_DEV float dpp_add(float x) {
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false));
+}
+typedef unsigned bn_u32x2 __attribute__((ext_vector_type(2)));
+
+// Sums of K numbers over the tpr threads of a row, in every one of them, in a fixed order: neighbours, quads (mirrored
+// halves once four lanes agree), rows of 16, of 32, the wave; then the row's waves through LDS, whose two halves the
+// calls take in turn (`flip`), so that one barrier a call is enough.
 template <int K>
-CB_DEV void row_sum(float (&v)[K], int tpr, float* sh) {
-    for (int d = min(tpr, 64) / 2; d > 0; d >>= 1)
+CB_DEV void row_sum(float (&v)[K], int tpr, float* sh, int& flip) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
+    for (int k = 0; k < K; ++k) {
+        if (tpr >= 2) v[k] = dpp_add<0xB1>(v[k]);
+        if (tpr >= 4) v[k] = dpp_add<0x4E>(v[k]);
+        if (tpr >= 8) v[k] = dpp_add<0x141>(v[k]);
+        if (tpr >= 16) v[k] = dpp_add<0x140>(v[k]);
+        if (tpr >= 32) {
+            const unsigned u = __float_as_uint(v[k]);
+            const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+            v[k] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+        if (tpr >= 64) {
+            const unsigned u = __float_as_uint(v[k]);
+            const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            v[k] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+    }
     if (tpr > 64) {
         const int wave = threadIdx.x >> 6, w = tpr >> 6, first = wave / w * w;
-        __syncthreads();
+        float* h = sh + flip * 16 * 4;
+        flip ^= 1;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < K; ++k) sh[wave * K + k] = v[k];
-        __syncthreads();
+            for (int k = 0; k < K; ++k) h[wave * K + k] = v[k];
+        lds_barrier();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            v[k] = sh[first * K + k];
-            for (int i = 1; i < w; ++i) v[k] += sh[(first + i) * K + k];
+            v[k] = h[first * K + k];
+            for (int i = 1; i < w; ++i) v[k] += h[(first + i) * K + k];
         }
     }
 }
 
-// x <- (x - mean) rstd in place (padding stays out of the sums by `width`); returns rstd. Two passes over the registers.
-// MEAN: a norm of the kernel may be a layer norm; the kinds are told apart by selections, not by branches around sums.
-template <bool MEAN, int V, int N>
-CB_DEV float bn_normalise(float (&x)[V], int kind, int width, int t, int tpr, float inv, float eps, float* sh) {
-    float s[1] = {0.f};
+// The columns that are the row's own: x, or zero.
+template <int V, int N, class F>
+CB_DEV void bn_own(float (&x)[V], int width, int t, int tpr, F&& f) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = (i / N * tpr + t) * N + i % N < width ? f(x[i]) : 0.f;
+}
+
+// x <- (x - mean) rstd in place for M rows side by side (padding stays out of the sums by `width`); r: rstd. Two passes
+// over the registers. MEAN: a norm of the kernel may be a layer norm; the kinds are told apart by selections.
+template <bool MEAN, int M, int V, int N>
+CB_DEV void bn_normalise(float (*const (&x)[M])[V], const int (&kind)[M], float (&r)[M], int width, int t, int tpr, float inv,
+                         float eps, float* sh, int& flip) {
+    float s[M];
     if constexpr (MEAN) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[0] += x[i];
-        row_sum(s, tpr, sh);
-        const float mean = kind == 1 ? s[0] * inv : 0.f;
+        for (int m = 0; m < M; ++m) {
+            s[m] = 0.f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = (i / N * tpr + t) * N + i % N < width ? x[i] - mean : 0.f;
-        s[0] = 0.f;
+            for (int i = 0; i < V; ++i) s[m] += (*x[m])[i];
+        }
+        row_sum(s, tpr, sh, flip);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const float mean = kind[m] == 1 ? s[m] * inv : 0.f;
+            bn_own<V, N>(*x[m], width, t, tpr, [&](float v) { return v - mean; });
+        }
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[0] += x[i] * x[i];
-    row_sum(s, tpr, sh);
-    const float r = kind == 0 ? 1.f : 1.f / sqrtf(s[0] * inv + eps);
+    for (int m = 0; m < M; ++m) {
+        s[m] = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] *= r;
-    return r;
+        for (int i = 0; i < V; ++i) s[m] += (*x[m])[i] * (*x[m])[i];
+    }
+    row_sum(s, tpr, sh, flip);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        r[m] = kind[m] == 0 ? 1.f : 1.f / sqrtf(s[m] * inv + eps);
+#pragma unroll
+        for (int i = 0; i < V; ++i) (*x[m])[i] *= r[m];
+    }
 }
 
 // Gradient at a norm's input from d at its normalised output xh: rstd (d - mean(d) - xh mean(d xh)).
-template <int V, int N>
-CB_DEV void bn_back(float (&d)[V], const float (&xh)[V], float r, int kind, int tpr, float inv, float* sh) {
+template <int V>
+CB_DEV void bn_back(float (&d)[V], const float (&xh)[V], float r, int kind, int tpr, float inv, float* sh, int& flip) {
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < V; ++i) { s[0] += d[i]; s[1] += d[i] * xh[i]; }
-    row_sum(s, tpr, sh);
+    row_sum(s, tpr, sh, flip);
     const float m = kind == 1 ? s[0] * inv : 0.f, mx = kind == 0 ? 0.f : s[1] * inv;
 #pragma unroll
     for (int i = 0; i < V; ++i) d[i] = r * (d[i] - m - (kind == 0 ? 0.f : xh[i] * mx));
@@ -138,13 +187,20 @@ CB_DEV float bn_sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 template <class T, int V>
 struct BnRow {
     static constexpr int N = BnVec<T>::N;
-    static CB_DEV void load(const BnMat& m, const BnArgs& a, const BnPlace& p, int64_t row, float (&x)[V]) {
+    struct Raw { uint4 v[V / N]; };
+    static CB_DEV Raw load(const BnMat& m, const BnArgs& a, const BnPlace& p, int64_t row, bool on) {
+        Raw r;
         const T* q = static_cast<const T*>(m.p) + row * m.ld + int64_t(p.grp) * a.cg;
 #pragma unroll
         for (int j = 0; j < V / N; ++j) {
             const int c = (j * a.tpr + p.t) * N;
-            BnVec<T>::load(q + c, p.width - c, x + j * N);
+            r.v[j] = BnVec<T>::raw(q + c, on ? p.width - c : 0);
         }
+        return r;
+    }
+    static CB_DEV void unpack(const Raw& r, float (&x)[V]) {
+#pragma unroll
+        for (int j = 0; j < V / N; ++j) BnVec<T>::unpack(r.v[j], x + j * N);
     }
     static CB_DEV void store(const BnMat& m, const BnArgs& a, const BnPlace& p, int64_t row, const float (&x)[V]) {
         T* q = static_cast<T*>(m.p) + row * m.ld + int64_t(p.grp) * a.cg;
@@ -166,31 +222,40 @@ struct BnRow {
 };
 
 template <class T, int V, bool GATE, bool TWO, bool MEAN>
-__global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_fwd_kernel(BnArgs a) {
+__global__ __launch_bounds__(512) void bn_fwd_kernel(BnArgs a) {
     using R = BnRow<T, V>;
     constexpr int N = BnVec<T>::N;
-    __shared__ float sh[32];
+    __shared__ float sh[2 * 16 * 4];
     const BnPlace p(a);
     const float inv = 1.f / float(a.cg);
+    int flip = 0;
     float gamma[V], beta[V], rs[V], gamma2[V], beta2[V];
     R::vec(a.gamma, 1.f, a, p, gamma);
     R::vec(a.beta, 0.f, a, p, beta);
     R::vec(a.rscale, 1.f, a, p, rs);
     if (TWO) { R::vec(a.gamma2, 1.f, a, p, gamma2); R::vec(a.beta2, 0.f, a, p, beta2); }
-    // whole workgroups go round together: row_sum has barriers
-    for (int64_t base = int64_t(blockIdx.x) * a.rb; base < a.n; base += p.step) {
+    // whole workgroups go round together (row_sum has barriers), the next round's rows on their way
+    int64_t base = int64_t(blockIdx.x) * a.rb;
+    typename R::Raw rh, rg, rr;
+    auto fetch = [&](int64_t base) {
+        const int64_t row = base + p.slot;
+        const bool on = row < a.n;
+        rh = R::load(a.h, a, p, row, on);
+        if (GATE) rg = R::load(a.gate, a, p, row, on);
+        rr = R::load(a.res, a, p, row, on && a.res.p);
+    };
+    fetch(base);
+    for (; base < a.n; base += p.step) {
         const int64_t row = base + p.slot;
         BnPlace q = p;
         if (row >= a.n) q.width = 0;
-        float x[V], y[V];
-        R::load(a.h, a, q, row, x);
-        float gt[V];
-        if (GATE) R::load(a.gate, a, q, row, gt);
-        if (a.res.p) R::load(a.res, a, q, row, y);
-        else
-#pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = 0.f;
-        bn_normalise<MEAN, V, N>(x, a.norm, q.width, p.t, a.tpr, inv, a.eps, sh);
+        float x[V], y[V], gt[V];
+        R::unpack(rh, x);
+        R::unpack(rr, y);
+        if (GATE) R::unpack(rg, gt);
+        if (base + p.step < a.n) fetch(base + p.step);
+        float r[1];
+        bn_normalise<MEAN, 1, V, N>({&x}, {a.norm}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float u = x[i] * gamma[i] + beta[i];
@@ -199,12 +264,8 @@ __global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_fwd_kernel(BnArgs a) {
         }
         R::store(a.out, a, q, row, y);
         if (TWO) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = (i / N * a.tpr + p.t) * N + i % N;
-                y[i] = c < q.width ? BnVec<T>::round(y[i]) : 0.f;
-            }
-            bn_normalise<MEAN, V, N>(y, a.norm2, q.width, p.t, a.tpr, inv, a.eps, sh);
+            bn_own<V, N>(y, q.width, p.t, a.tpr, [](float v) { return BnVec<T>::round(v); });
+            bn_normalise<MEAN, 1, V, N>({&y}, {a.norm2}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = y[i] * gamma2[i] + beta2[i];
             R::store(a.out2, a, q, row, y);
@@ -213,13 +274,14 @@ __global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_fwd_kernel(BnArgs a) {
 }
 
 template <class T, int V, bool GATE, bool TWO, bool MEAN>
-__global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_bwd_kernel(BnArgs a) {
+__global__ __launch_bounds__(512) void bn_bwd_kernel(BnArgs a) {
     using R = BnRow<T, V>;
     constexpr int N = BnVec<T>::N, Q = TWO ? 5 : 3;
-    __shared__ float sh[32];
+    __shared__ float sh[2 * 16 * 4];
     extern __shared__ float cols[];   // [threads][V]
     const BnPlace p(a);
     const float inv = 1.f / float(a.cg);
+    int flip = 0;
     float gamma[V], beta[V], rs[V], gamma2[V];
     R::vec(a.gamma, 1.f, a, p, gamma);
     R::vec(a.beta, 0.f, a, p, beta);
@@ -230,34 +292,45 @@ __global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_bwd_kernel(BnArgs a) {
     for (int k = 0; k < Q; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[k][i] = 0.f;
-    for (int64_t base = int64_t(blockIdx.x) * a.rb; base < a.n; base += p.step) {
+    int64_t base = int64_t(blockIdx.x) * a.rb;
+    typename R::Raw rd, rh, rg, rd2, ro;
+    auto fetch = [&](int64_t base) {
+        const int64_t row = base + p.slot;
+        const bool on = row < a.n;
+        rh = R::load(a.h, a, p, row, on);
+        if (TWO) {
+            ro = R::load(a.out, a, p, row, on);
+            rd2 = R::load(a.dout2, a, p, row, on);
+        }
+        rd = R::load(a.dout, a, p, row, on && a.dout.p);
+        if (GATE) rg = R::load(a.gate, a, p, row, on);
+    };
+    fetch(base);
+    for (; base < a.n; base += p.step) {
         const int64_t row = base + p.slot;
         BnPlace q = p;
         if (row >= a.n) q.width = 0;
-        float ds[V], x[V], gt[V];
-        if (a.dout.p) R::load(a.dout, a, q, row, ds);
-        else
-#pragma unroll
-            for (int i = 0; i < V; ++i) ds[i] = 0.f;
-        R::load(a.h, a, q, row, x);
-        if (GATE) R::load(a.gate, a, q, row, gt);
-        if (TWO) {
-            float d[V], y[V];
-            R::load(a.dout2, a, q, row, d);
-            R::load(a.out, a, q, row, y);
-            const float r = bn_normalise<MEAN, V, N>(y, a.norm2, q.width, p.t, a.tpr, inv, a.eps, sh);
+        float ds[V], x[V], gt[V], d[V], y[V], r[TWO ? 2 : 1];
+        R::unpack(rh, x);
+        R::unpack(rd, ds);
+        if (GATE) R::unpack(rg, gt);
+        if (TWO) { R::unpack(rd2, d); R::unpack(ro, y); }
+        if (base + p.step < a.n) fetch(base + p.step);
+        if constexpr (TWO) {
+            bn_normalise<MEAN, 2, V, N>({&x, &y}, {a.norm, a.norm2}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 sum[Q - 2][i] += d[i] * y[i];
                 sum[Q - 1][i] += d[i];
                 d[i] *= gamma2[i];
             }
-            bn_back<V, N>(d, y, r, a.norm2, a.tpr, inv, sh);
+            bn_back<V>(d, y, r[1], a.norm2, a.tpr, inv, sh, flip);
 #pragma unroll
             for (int i = 0; i < V; ++i) ds[i] += d[i];
+        } else {
+            bn_normalise<MEAN, 1, V, N>({&x}, {a.norm}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
         }
         if (a.dres.p) R::store(a.dres, a, q, row, ds);
-        const float r = bn_normalise<MEAN, V, N>(x, a.norm, q.width, p.t, a.tpr, inv, a.eps, sh);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float z = x[i] * gamma[i] + beta[i], du = ds[i] * rs[i];
@@ -279,7 +352,7 @@ __global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_bwd_kernel(BnArgs a) {
             ds[i] = dz * gamma[i];
         }
         if (GATE && a.dgate.p) R::store(a.dgate, a, q, row, gt);
-        bn_back<V, N>(ds, x, r, a.norm, a.tpr, inv, sh);
+        bn_back<V>(ds, x, r[0], a.norm, a.tpr, inv, sh, flip);
         R::store(a.dh, a, q, row, ds);
     }
     // the workgroup's column sums: over its row slots, then one partial row
@@ -301,32 +374,43 @@ __global__ __launch_bounds__(V == 8 ? 256 : 512) void bn_bwd_kernel(BnArgs a) {
     }
 }
 
-// Column sums over the workgroups' partial rows: 32 columns a workgroup, 8 slices of the partials each.
-__global__ __launch_bounds__(256) void bn_cols_kernel(BnArgs a, int blocks, int nq) {
-    __shared__ double sh[8][33];
+// Column sums over the workgroups' partial rows: 32 columns a workgroup, 32 slices of the partials each.
+__global__ __launch_bounds__(1024) void bn_cols_kernel(BnArgs a, int blocks, int nq) {
+    __shared__ double sh[32][33];
     const int k = blockIdx.y, lane = threadIdx.x & 31, sl = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float* out = a.grads[k];
     if (!out) return;
     double s = 0.0;
-    if (c < a.C)
-        for (int b = sl; b < blocks; b += 8) s += a.part[(int64_t(b) * nq + k) * a.C + c];
+    if (c < a.C) {
+        const float* p = a.part + int64_t(k) * a.C + c;
+        const int64_t st = int64_t(nq) * a.C;
+        int b = sl;
+        for (; b + 7 * 32 < blocks; b += 8 * 32) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = p[(b + 32 * u) * st];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += v[u];
+        }
+        for (; b < blocks; b += 32) s += p[b * st];
+    }
     sh[sl][lane] = s;
     __syncthreads();
     if (sl == 0 && c < a.C) {
 #pragma unroll
-        for (int u = 1; u < 8; ++u) s += sh[u][lane];
+        for (int u = 1; u < 32; ++u) s += sh[u][lane];
         out[c] = float(s);
     }
 }
 
 struct BnPlan { int V, threads, tpr, gb, rb; int64_t blocks; int gy; };
 
-constexpr int kBnBlocks = 1024;   // of a backward pass: each leaves a row of partial column sums
+constexpr int kBnBlocks = 512;   // of a backward pass: each leaves a row of partial column sums
 
 BnPlan bn_plan(int64_t n, int C, int G) {
     BnPlan p;
     const int cg = C / G;
-    p.V = cg <= 512 ? 8 : 16;
+    p.V = cg <= 4096 ? 8 : 16;
     p.tpr = 1;
     while (p.tpr * p.V < cg) p.tpr *= 2;
     p.threads = std::max(256, p.tpr);
@@ -395,7 +479,7 @@ hipError_t blocknorm_bwd(int prec, BnArgs a, void* ws, hipStream_t s) {
     const hipError_t e = bn_run(prec, a, p, true, s);
     if (e != hipSuccess) return e;
     const int nq = two ? 5 : 3;
-    hipLaunchKernelGGL(bn_cols_kernel, dim3(unsigned((a.C + 31) / 32), unsigned(nq)), dim3(256), 0, s, a, int(p.blocks), nq);
+    hipLaunchKernelGGL(bn_cols_kernel, dim3(unsigned((a.C + 31) / 32), unsigned(nq)), dim3(1024), 0, s, a, int(p.blocks), nq);
     return hipGetLastError();
 }
 
