@@ -128,6 +128,27 @@ CB_DEV void row_sum(float (&v)[K], int tpr, float* sh, int& flip) {
     }
 }
 
+// 1 / (1 + exp(-x)) from the hardware's 2^t and reciprocal: the product's rounding error and log2(e)'s own are made good
+// on the power, one Newton step on the reciprocal, so that it is off by about an ulp in a third of the instructions of
+// expf and a division (65536 x 1024 bf16 backward, which they bound beside HBM). Beyond +-88 it is 0 or 1 to 32 bits;
+// selections keep NaN.
+CB_DEV float bn_sigmoid(float x) {
+    constexpr float kL2E = 1.44269504f, kL2ELo = 1.92596300e-8f, kLn2 = 0.69314718f;
+    float a = x < -88.f ? 88.f : -x;
+    a = x > 88.f ? -88.f : a;
+    const float t = a * kL2E, lo = fmaf(a, kL2ELo, fmaf(a, kL2E, -t));
+    float e = __builtin_amdgcn_exp2f(t);
+    e = fmaf(e, lo * kLn2, e);
+    const float d = 1.f + e, r = __builtin_amdgcn_rcpf(d);
+    return fmaf(fmaf(-d, r, 1.f), r, r);
+}
+
+// 1 / sqrt(v), v >= 0, with one Newton step (none from 0 or infinity, where it would make NaN).
+CB_DEV float bn_rsqrt(float v) {
+    const float r = __builtin_amdgcn_rsqf(v);
+    return r > 0.f && r < INFINITY ? fmaf(r * 0.5f, fmaf(-v * r, r, 1.f), r) : r;
+}
+
 // The columns that are the row's own: x, or zero.
 template <int V, int N, class F>
 CB_DEV void bn_own(float (&x)[V], int width, int t, int tpr, F&& f) {
@@ -164,7 +185,7 @@ CB_DEV void bn_normalise(float (*const (&x)[M])[V], const int (&kind)[M], float 
     row_sum(s, tpr, sh, flip);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-        r[m] = kind[m] == 0 ? 1.f : 1.f / sqrtf(s[m] * inv + eps);
+        r[m] = kind[m] == 0 ? 1.f : bn_rsqrt(s[m] * inv + eps);
 #pragma unroll
         for (int i = 0; i < V; ++i) (*x[m])[i] *= r[m];
     }
@@ -181,8 +202,6 @@ CB_DEV void bn_back(float (&d)[V], const float (&xh)[V], float r, int kind, int 
 #pragma unroll
     for (int i = 0; i < V; ++i) d[i] = r * (d[i] - m - (kind == 0 ? 0.f : xh[i] * mx));
 }
-
-CB_DEV float bn_sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
 template <class T, int V>
 struct BnRow {
@@ -214,9 +233,15 @@ struct BnRow {
     // leaves its mean
     static CB_DEV void vec(const float* v, float other, const BnArgs& a, const BnPlace& p, float (&x)[V]) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < V; i += 4) {
             const int c = (i / N * a.tpr + p.t) * N + i % N;
-            x[i] = c >= p.width ? 0.f : v ? v[int64_t(p.grp) * a.cg + c] : other;
+            const float* q = v ? v + int64_t(p.grp) * a.cg + c : nullptr;
+            if (q && c + 4 <= p.width) {
+                const float4 f = load_f4(q);
+                x[i] = f.x; x[i + 1] = f.y; x[i + 2] = f.z; x[i + 3] = f.w;
+            } else
+#pragma unroll
+                for (int u = 0; u < 4; ++u) x[i + u] = c + u >= p.width ? 0.f : q ? q[u] : other;
         }
     }
 };
@@ -405,6 +430,7 @@ __global__ __launch_bounds__(1024) void bn_cols_kernel(BnArgs a, int blocks, int
 
 struct BnPlan { int V, threads, tpr, gb, rb; int64_t blocks; int gy; };
 
+constexpr int kBnFwdBlocks = 1024;
 constexpr int kBnBlocks = 512;   // of a backward pass: each leaves a row of partial column sums
 
 BnPlan bn_plan(int64_t n, int C, int G) {
@@ -459,7 +485,7 @@ size_t blocknorm_bwd_ws_bytes(int, int64_t n, int C, int G, bool two) {
 hipError_t blocknorm_fwd(int prec, BnArgs a, hipStream_t s) {
     if (a.n == 0) return hipSuccess;
     BnPlan p = bn_plan(a.n, a.C, a.G);
-    p.blocks = std::min<int64_t>(p.blocks, 1 << 16);
+    p.blocks = std::min<int64_t>(p.blocks, kBnFwdBlocks);
     return bn_run(prec, a, p, false, s);
 }
 

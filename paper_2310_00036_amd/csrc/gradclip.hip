@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kGcTable = 96;       // tensors of a launch
 constexpr int kGcSeg = 8192;       // elements a workgroup takes at a time
-constexpr int kGcBlocks = 1024;    // workgroups of a launch, each with one partial sum
+constexpr int kGcBlocks = 2048;    // workgroups of a launch, each with one partial sum
 
 struct GcEntry {
     const void* src;
@@ -30,42 +30,80 @@ struct GcTable {
 // 16 bytes at any alignment of an element: global memory takes them so.
 typedef uint32_t gc_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 
-// f(entry, first element, elements) for this workgroup's segments.
+// f(entry, first element, elements) for this workgroup's segments, which are neighbours: the tensor of the first one is
+// looked up, the others follow from it. `back` takes the workgroups and their segments from the end.
 template <class F>
-CB_DEV void gc_segments(const GcTable& t, F&& f) {
-    for (int s = blockIdx.x; s < t.segs; s += gridDim.x) {
-        int lo = 0, hi = t.n - 1;
-        while (lo < hi) {   // the last entry that starts at or before s
-            const int mid = (lo + hi + 1) / 2;
-            if (t.e[mid].first <= s) lo = mid; else hi = mid - 1;
-        }
-        const GcEntry& e = t.e[lo];
-        const int64_t at = int64_t(s - e.first) * kGcSeg;
-        f(e, at, int(min(int64_t(kGcSeg), e.n - at)));
+CB_DEV void gc_segments(const GcTable& t, bool back, F&& f) {
+    const int b = back ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    const int s0 = int(int64_t(t.segs) * b / gridDim.x), s1 = int(int64_t(t.segs) * (b + 1) / gridDim.x);
+    if (s0 >= s1) return;
+    int at = 0, hi = t.n - 1;
+    const int first = back ? s1 - 1 : s0;
+    while (at < hi) {   // the last entry that starts at or before the first segment
+        const int mid = (at + hi + 1) / 2;
+        if (t.e[mid].first <= first) at = mid; else hi = mid - 1;
+    }
+    for (int i = 0; i < s1 - s0; ++i) {
+        const int s = back ? s1 - 1 - i : s0 + i;
+        if (back) { if (s < t.e[at].first) --at; }
+        else if (at + 1 < t.n && s >= t.e[at + 1].first) ++at;
+        const GcEntry& e = t.e[at];
+        const int64_t el = int64_t(s - e.first) * kGcSeg;
+        f(e, el, int(min(int64_t(kGcSeg), e.n - el)));
     }
 }
 
-// Eight elements of a source as floats, `left` of which exist.
-CB_DEV void gc_load8(const GcEntry& e, int64_t i, int left, float* x) {
-    if (e.type & 1) {
+// Eight elements of a source, `left` of which exist: one or two 16-byte words, and as floats.
+struct GcRaw { gc_u32x4 a, b; };
+template <bool F32>
+CB_DEV GcRaw gc_raw(const GcEntry& e, int64_t i, int left) {
+    GcRaw r;
+    if constexpr (F32) {
         const float* p = static_cast<const float*>(e.src) + i;
         if (left >= 8) {
-            const gc_u32x4 a = *reinterpret_cast<const gc_u32x4*>(p), b = *reinterpret_cast<const gc_u32x4*>(p + 4);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) { x[u] = __uint_as_float(a[u]); x[4 + u] = __uint_as_float(b[u]); }
+            r.a = *reinterpret_cast<const gc_u32x4*>(p);
+            r.b = *reinterpret_cast<const gc_u32x4*>(p + 4);
         } else {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = u < left ? p[u] : 0.f;
+            for (int u = 0; u < 4; ++u) {
+                r.a[u] = u < left ? __float_as_uint(p[u]) : 0u;
+                r.b[u] = 4 + u < left ? __float_as_uint(p[4 + u]) : 0u;
+            }
         }
     } else {
         const uint16_t* p = static_cast<const uint16_t*>(e.src) + i;
-        if (left >= 8) {
-            const gc_u32x4 a = *reinterpret_cast<const gc_u32x4*>(p);
+        if (left >= 8) r.a = *reinterpret_cast<const gc_u32x4*>(p);
+        else
 #pragma unroll
-            for (int u = 0; u < 4; ++u) { x[2 * u] = bf_lo(a[u]); x[2 * u + 1] = bf_hi(a[u]); }
-        } else {
+            for (int u = 0; u < 4; ++u)
+                r.a[u] = (2 * u < left ? uint32_t(p[2 * u]) : 0u) | (2 * u + 1 < left ? uint32_t(p[2 * u + 1]) << 16 : 0u);
+        r.b = r.a;
+    }
+    return r;
+}
+template <bool F32>
+CB_DEV void gc_floats(const GcRaw& r, float* x) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = u < left ? bf2f(p[u]) : 0.f;
+    for (int u = 0; u < 4; ++u) {
+        if constexpr (F32) { x[u] = __uint_as_float(r.a[u]); x[4 + u] = __uint_as_float(r.b[u]); }
+        else { x[2 * u] = bf_lo(r.a[u]); x[2 * u + 1] = bf_hi(r.a[u]); }
+    }
+}
+
+// f(offset, elements left, eight floats) over a segment, four pieces of a thread on their way at once.
+template <bool F32, class F>
+CB_DEV void gc_pieces(const GcEntry& e, int64_t at, int n, F&& f) {
+    constexpr int ST = 8 * 256;
+    for (int i0 = 8 * int(threadIdx.x); i0 < n; i0 += 4 * ST) {
+        GcRaw r[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) r[u] = gc_raw<F32>(e, at + i0 + u * ST, n - i0 - u * ST);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u * ST >= n) break;
+            float x[8];
+            gc_floats<F32>(r[u], x);
+            f(at + i0 + u * ST, n - i0 - u * ST, x);
         }
     }
 }
@@ -103,13 +141,12 @@ CB_DEV void gc_store8(const GcEntry& e, int64_t i, int left, const float* x) {
 __global__ __launch_bounds__(256) void gc_norm_kernel(GcTable t, double* part) {
     __shared__ double sh[256];
     double s = 0.0;
-    gc_segments(t, [&](const GcEntry& e, int64_t at, int n) {
-        for (int i = 8 * int(threadIdx.x); i < n; i += 8 * 256) {
-            float x[8];
-            gc_load8(e, at + i, n - i, x);
+    gc_segments(t, false, [&](const GcEntry& e, int64_t at, int n) {
+        auto add = [&](int64_t, int, const float* x) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) s += double(x[u]) * x[u];
-        }
+        };
+        e.type & 1 ? gc_pieces<true>(e, at, n, add) : gc_pieces<false>(e, at, n, add);
     });
     const double tot = block_sum<256>(s, sh);
     if (threadIdx.x == 0) part[blockIdx.x] = tot;
@@ -137,16 +174,16 @@ __global__ __launch_bounds__(256) void gc_scale_kernel(GcTable t, const double* 
     }
     const bool clip = max_norm > 0.f && norm > double(max_norm);
     const float f = clip ? float(double(max_norm) / norm) : 1.f;
-    gc_segments(t, [&](const GcEntry& e, int64_t at, int n) {
+    // from the end: what the norm read last is still in the caches
+    gc_segments(t, true, [&](const GcEntry& e, int64_t at, int n) {
         if (!e.dst || (!clip && e.dst == e.src)) return;
-        for (int i = 8 * int(threadIdx.x); i < n; i += 8 * 256) {
-            float x[8];
-            gc_load8(e, at + i, n - i, x);
+        auto put = [&](int64_t i, int left, float* x) {
             if (clip)
 #pragma unroll
                 for (int u = 0; u < 8; ++u) x[u] *= f;
-            gc_store8(e, at + i, n - i, x);
-        }
+            gc_store8(e, i, left, x);
+        };
+        e.type & 1 ? gc_pieces<true>(e, at, n, put) : gc_pieces<false>(e, at, n, put);
     });
 }
 
