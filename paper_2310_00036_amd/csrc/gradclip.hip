@@ -19,13 +19,14 @@ struct GcEntry {
     const void* src;
     void* dst;
     int64_t n;
-    int32_t first;                 // its first segment in the launch
     int32_t type;                  // bit 0: src float32, bit 1: dst float32
 };
 struct GcTable {
     GcEntry e[kGcTable];
+    int32_t first[kGcTable];       // an entry's first segment in the launch; behind the last, more than there are
     int n, segs;
 };
+static_assert(kGcTable <= 128 && sizeof(GcTable) <= 3584, "two entries a lane, and a kernel's arguments");
 
 // 16 bytes at any alignment of an element: global memory takes them so.
 typedef uint32_t gc_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -37,18 +38,16 @@ CB_DEV void gc_segments(const GcTable& t, bool back, F&& f) {
     const int b = back ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     const int s0 = int(int64_t(t.segs) * b / gridDim.x), s1 = int(int64_t(t.segs) * (b + 1) / gridDim.x);
     if (s0 >= s1) return;
-    int at = 0, hi = t.n - 1;
-    const int first = back ? s1 - 1 : s0;
-    while (at < hi) {   // the last entry that starts at or before the first segment
-        const int mid = (at + hi + 1) / 2;
-        if (t.e[mid].first <= first) at = mid; else hi = mid - 1;
-    }
+    // the last entry that starts at or before the first segment: lanes compare, two entries each
+    const int s = back ? s1 - 1 : s0, lane = threadIdx.x & 63;
+    const int more = min(lane + 64, kGcTable - 1);
+    int at = __popcll(__ballot(t.first[lane] <= s)) + __popcll(__ballot(more == lane + 64 && t.first[more] <= s)) - 1;
     for (int i = 0; i < s1 - s0; ++i) {
         const int s = back ? s1 - 1 - i : s0 + i;
-        if (back) { if (s < t.e[at].first) --at; }
-        else if (at + 1 < t.n && s >= t.e[at + 1].first) ++at;
+        if (back) { if (s < t.first[at]) --at; }
+        else if (at + 1 < t.n && s >= t.first[at + 1]) ++at;
         const GcEntry& e = t.e[at];
-        const int64_t el = int64_t(s - e.first) * kGcSeg;
+        const int64_t el = int64_t(s - t.first[at]) * kGcSeg;
         f(e, el, int(min(int64_t(kGcSeg), e.n - el)));
     }
 }
@@ -195,11 +194,13 @@ int gc_fill(GcTable& t, const grad_tensor_t* g, int i, int n) {
         if (g[i].count == 0) continue;
         const int64_t k = (g[i].count + kGcSeg - 1) / kGcSeg;
         if (t.n > 0 && segs + k > (int64_t(1) << 30)) break;
-        t.e[t.n++] = GcEntry{g[i].src, g[i].dst, g[i].count, int32_t(segs),
+        t.first[t.n] = int32_t(segs);
+        t.e[t.n++] = GcEntry{g[i].src, g[i].dst, g[i].count,
                              (g[i].src_prec == IMPALA_PREC_FP32 ? 1 : 0) | (g[i].dst_prec == IMPALA_PREC_FP32 ? 2 : 0)};
         segs += k;
     }
     t.segs = int(segs);
+    for (int k = t.n; k < kGcTable; ++k) t.first[k] = INT32_MAX;
     return i;
 }
 
