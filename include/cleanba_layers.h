@@ -197,8 +197,9 @@ impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, i
  * projection's output, an env block of a larger rollout, or [E, T, ...]. log_decay: float [heads], <= 0
  * (-infinity: no memory; above 0 the state grows). dones: uint8 with strides done_t, done_e, or NULL (no
  * episode starts). States: float32 [E, heads, dk, dv], row-major, in both precisions. 1 <= dk, dv <= 128,
- * E * heads <= 2^21 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element (16-byte aligned ones with
- * strides and sizes of whole 16 bytes are read so).
+ * E * heads <= 2^21 and T <= 2^30 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element
+ * (sizes, strides and addresses of whole 4 bytes, and steps less than 2^24 bytes apart, are read 16 bytes at a
+ * time, others element by element).
  * Outputs must not have two elements in one place, and must not overlap inputs or each other: two arrays
  * with the same strides may lie between each other's elements, any other overlap of their address ranges
  * is IMPALA_EINVAL. */

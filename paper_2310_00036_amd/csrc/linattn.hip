@@ -11,89 +11,11 @@ namespace cb {
 
 namespace {
 
-CB_DEV const void* la_at(const void* p, int64_t elems, int es) { return static_cast<const char*>(p) + elems * es; }
-
-// The recurrence row by row: one wave for 64 columns of one env's and head's state, a column a lane, its dk numbers in
-// registers.
-template <class Pr, int DK>
-__global__ __launch_bounds__(64) void la_steps_kernel(LaArgs a, int y0) {
-    using T = typename Pr::T;
-    constexpr int KL = (DK + 63) / 64;
-    __shared__ float sq[DK], sk[DK];
-    const LaPass& P = a.pass[y0 + blockIdx.y];
-    const int lane = threadIdx.x;
-    const int nbs = (P.dv + 63) / 64;
-    const int64_t eh = blockIdx.x / nbs;
-    const int n = int(blockIdx.x % nbs) * 64 + lane;
-    const int64_t e = eh / a.H, h = eh % a.H;
-    const bool on = n < P.dv;
-    const float g = float(exp(double(a.log_decay[h])));
-    const int64_t dir = P.back ? -1 : 1;
-    int64_t t = P.back ? a.T - 1 : 0;
-    const T* q = static_cast<const T*>(P.q.p) + e * P.q.e + h * P.q.h + t * P.q.t;
-    const T* k = static_cast<const T*>(P.k.p) + e * P.k.e + h * P.k.h + t * P.k.t;
-    const T* v = static_cast<const T*>(P.v.p) + e * P.v.e + h * P.v.h + t * P.v.t + n;
-    T* o = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h + t * P.o.t + n;
-    auto starts = [&](int64_t td) { return a.dones && a.dones[td * a.d_t + e * a.d_e]; };
-    float R[DK];
-#pragma unroll
-    for (int i = 0; i < DK; ++i) R[i] = 0.f;
-    bool cut = !P.back && starts(0);
-    float keep = P.back ? 1.f : g;
-    if (P.x0 && !cut && on) {
-        const float* x = P.x0 + eh * P.dk * P.dv + int64_t(n) * P.xn;
-#pragma unroll
-        for (int i = 0; i < DK; ++i)
-            if (i < P.dk) R[i] = x[i * P.xk];
-    }
-    T nq[KL], nk[KL], nv = T(0);
-    auto fetch = [&] {
-#pragma unroll
-        for (int u = 0; u < KL; ++u) {
-            const int i = lane + 64 * u;
-            nq[u] = i < P.dk ? q[i] : T(0);
-            nk[u] = i < P.dk ? k[i] : T(0);
-        }
-        nv = on ? *v : T(0);
-    };
-    fetch();
-    for (int p = 0; p < a.T; ++p) {
-#pragma unroll
-        for (int u = 0; u < KL; ++u)
-            if (lane + 64 * u < DK) {
-                sq[lane + 64 * u] = Pr::load(nq[u]);
-                sk[lane + 64 * u] = Pr::load(nk[u]);
-            }
-        const float vn = Pr::load(nv) * P.in;
-        __syncthreads();
-        if (p + 1 < a.T) { q += dir * P.q.t; k += dir * P.k.t; v += dir * P.v.t; fetch(); }
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < DK; ++i) {
-            R[i] = (cut ? 0.f : keep * R[i]) + sk[i] * vn;
-            s += sq[i] * R[i];
-        }
-        if (on) *o = Pr::store(s * P.out);
-        o += dir * P.o.t;
-        // what lies between this row and the next: the later one's episode start
-        if (P.back) cut = starts(t);
-        else if (p + 1 < a.T) cut = starts(t + 1);
-        keep = g;
-        t += dir;
-        __syncthreads();
-    }
-    if (P.x1 && on) {
-        if (!P.back) { keep = 1.f; cut = false; }
-        float* x = P.x1 + eh * P.dk * P.dv + int64_t(n) * P.xn;
-#pragma unroll
-        for (int i = 0; i < DK; ++i)
-            if (i < P.dk) x[i * P.xk] = cut ? 0.f : keep * R[i];
-    }
-}
-
 // One step from state to state, HBM-bound: the state is read and written once. A workgroup has one state, a thread four
 // neighbouring columns of every (NT / LR)th row, all loaded before anything waits (LR: the lanes of a row, a power of two).
-// 4096 envs x 8 heads of 128 x 128: 4.3 GB in 0.9 ms.
+// 4096 envs x 8 heads of 128 x 128: 4.3 GB in 0.86 ms, 5.0 TB/s. (A rollout of 4 steps of 512 envs x 8 heads of 64 takes 47 us
+// as a chunk and took 31 row by row from registers: with one step, where the state is all there is to move, a chunk's
+// set-up would cost more than the step. On 64 envs x 4 heads the chunk is the faster from 4 steps on, 9 us for 18.)
 template <class Pr, int NT, int LR>
 __global__ __launch_bounds__(NT) void la_step_kernel(LaArgs a) {
     using T = typename Pr::T;
@@ -190,18 +112,6 @@ hipError_t la_step(const LaArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <class Pr>
-hipError_t la_steps(const LaArgs& a, hipStream_t s) {
-    for (int y = 0; y < a.np; ++y) {
-        const LaPass& P = a.pass[y];
-        const dim3 grid(unsigned(int64_t(a.E) * a.H * ((P.dv + 63) / 64)));
-        if (P.dk <= 32) hipLaunchKernelGGL((la_steps_kernel<Pr, 32>), grid, dim3(64), 0, s, a, y);
-        else if (P.dk <= 64) hipLaunchKernelGGL((la_steps_kernel<Pr, 64>), grid, dim3(64), 0, s, a, y);
-        else hipLaunchKernelGGL((la_steps_kernel<Pr, 128>), grid, dim3(64), 0, s, a, y);
-    }
-    return hipGetLastError();
-}
-
 // ---------------------------------------------------------------- chunks of 64 rows on the matrix cores
 //
 // Rows i of a chunk with the state X before it (c_i: episode starts up to row i, counting its own going forward and not
@@ -277,6 +187,9 @@ struct LaB {
     static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, cb_f32x4 x) {
         __builtin_amdgcn_raw_buffer_store_b64(cb_u32x2{pack2bf(x[0], x[1]), pack2bf(x[2], x[3])}, r, off, 0, 0);
     }
+    static CB_DEV void store1o(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
+        __builtin_amdgcn_raw_buffer_store_b16(f2bf(x), r, off, 0, 0);
+    }
     static CB_DEV T store(float x) { return f2bf(x); }
 };
 
@@ -318,6 +231,9 @@ struct LaF {
     static CB_DEV void store4o(__amdgpu_buffer_rsrc_t r, uint32_t off, cb_f32x4 x) {
         buf_store16(r, off, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
                                        __float_as_uint(x[3])));
+    }
+    static CB_DEV void store1o(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, off, 0, 0);
     }
     static CB_DEV T store(float x) { return x; }
 };
@@ -412,6 +328,8 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
     using Frag = typename Tr::Frag;
     using L = LaTile<Tr, DK, NW, STATE>;
     constexpr int KB = Tr::KB, KPL = Tr::KPL, NT = DK / 16, NJ = kL / KB;
+    // Float32 products of 16 contracted numbers take 128 cycles: those of padding only are passed over.
+    constexpr bool SKIP = sizeof(T) == 4 && DK == 128;
     extern __shared__ __align__(16) unsigned char lds[];
     float* pw = reinterpret_cast<float*>(lds + L::TAB);
     float* pin = pw + 68 + 16;
@@ -604,6 +522,7 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
             }
 #pragma unroll
             for (int kb = 0; kb < DK / KB; ++kb)
+                if (!SKIP || kb * KB < dk)
 #pragma unroll
                 for (int y = 0; y < MT; ++y) {
                     const Frag fk = *reinterpret_cast<const Frag*>(lds + L::K + (16 * tt[y] + c) * L::RSK + kb * 64 + 16 * g);
@@ -640,6 +559,7 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
             for (int b = 0; b < 4; ++b) O[b] = cb_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < DK / KB; ++kb) {
+                if (SKIP && kb * KB >= dk) break;
                 Frag fx[Tr::NX], fq[4];
                 Tr::xfrag(X, kb, fx);
 #pragma unroll
@@ -674,9 +594,10 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
                     for (int u = 0; u < KPL; ++u) x[u] *= vw[jb * KB + KPL * g + u];
                     Frag fw[Tr::NV];
                     Tr::split(x, fw);
-                    constexpr int TG = NT < 4 ? NT : 4;   // at a time
+                    constexpr int TG = SKIP ? 2 : NT < 4 ? NT : 4;   // at a time
 #pragma unroll
                     for (int t0 = 0; t0 < NT; t0 += TG) {
+                        if (SKIP && t0 * 16 >= dk) break;
                         Frag fk[TG];
 #pragma unroll
                         for (int t = 0; t < TG; ++t) fk[t] = clean(Tr::kcols(lds + L::K, L::RSK, jb * KB, t0 + t));
@@ -769,11 +690,20 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) O[b][r] += A[b][r];
-            if (FAST && __builtin_expect(vec & 1, 1)) {
+            if constexpr (FAST) {
                 const auto bo = o.rsrc(n);
                 const uint32_t f = o.first(n);
+                if (__builtin_expect(vec & 1, 1)) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) Tr::store4o(bo, ato + (f + 16 * b * o.st), O[b]);
+                    for (int b = 0; b < 4; ++b) Tr::store4o(bo, ato + (f + 16 * b * o.st), O[b]);
+                } else {
+                    const int left = dv - la_here(n0 + 4 * g);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            Tr::store1o(bo, r < left ? ato + (f + 16 * b * o.st + r * L::ES) : kOOB, O[b][r]);
+                }
             } else {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
@@ -866,8 +796,6 @@ hipError_t la_chunks(const LaArgs& a, const LaSegs& sg, bool state, hipStream_t 
     return hipSuccess;
 }
 
-constexpr int kLaSteps = 16;   // rollouts up to here go row by row
-
 // Segments of the rollout that run at once: as many as fill the chip's places for workgroups once, of four chunks at
 // least. Each segment's state has to be known first, which reads k and v again and takes two launches more: less than
 // three segments gain nothing. (16384 x 2 envs x 8 heads of 128: 16 chains of 256 chunks, which take 5.8 us each;
@@ -875,7 +803,7 @@ constexpr int kLaSteps = 16;   // rollouts up to here go row by row
 int la_segs(int prec, int T, int64_t EH, int dk, int dv, int passes, int* chunks) {
     const int64_t nc = (int64_t(T) + kL - 1) / kL;
     *chunks = int(nc);
-    if (T <= kLaSteps || EH == 0) return 1;
+    if (EH == 0) return 1;
     // passes of a launch: of the backward's three, the two that contract over v's axis, or all where the kernels are one
     const int together = passes > 1 ? (la_dim(dk) == la_dim(dv) ? 3 : 2) : 1, out = passes > 1 ? dk : dv;
     const int waves = la_waves(prec, passes > 1 ? dv : dk, out);
@@ -920,12 +848,12 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
                                            cb_dims(a.pass[0].dk, a.pass[0].dv) + (a.np > 1 ? "/bwd" : ""));
     });
     if (a.T == 1 && a.np == 1) return prec == 0 ? la_step<PrecBF16>(a, s) : la_step<PrecF32>(a, s);
-    if (a.T <= kLaSteps) return prec == 0 ? la_steps<PrecBF16>(a, s) : la_steps<PrecF32>(a, s);
     const int es = prec == 0 ? 2 : 4, ve = 16 / es;
-    // Rows that a buffer resource reaches: at whole words, each behind the last one's end, 64 of them within 2^31 bytes.
+    // Rows that a buffer resource reaches: of whole words (it ends with the last row's last one), each behind the last
+    // one's end, 64 of them within 2^30 bytes.
     auto reach = [&](const LaView& v, int d) {
         const int k = 4 / es;
-        return reinterpret_cast<uintptr_t>(v.p) % 4 == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && v.t >= d &&
+        return reinterpret_cast<uintptr_t>(v.p) % 4 == 0 && d % k == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && v.t >= d &&
                v.t < (int64_t(1) << 30) / kL / es;
     };
     LaSegs sg{};
@@ -935,8 +863,8 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     char* w = static_cast<char*>(ws);
     for (int y = 0; y < a.np; ++y) {
         LaPass& P = a.pass[y];
-        P.vec = (reach(P.o, P.dv) && P.dv % 4 == 0) | (P.dk % ve != 0 || P.dv % ve != 0) << 1 |
-                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv) && a.d_t < (int64_t(1) << 24)) << 2;
+        P.vec = (P.dv % 4 == 0) | (P.dk % ve != 0 || P.dv % ve != 0) << 1 |
+                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv) && reach(P.o, P.dv) && a.d_t < (int64_t(1) << 24)) << 2;
         if (sg.segs == 1) continue;
         sg.state[y] = reinterpret_cast<float*>(w);
         w += la_a256(sg.segs * EH * P.dk * P.dv * 4);

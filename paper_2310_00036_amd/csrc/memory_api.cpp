@@ -113,8 +113,8 @@ impala_status_t check_linattn(const char* fn, const linattn_shape_t* c) {
         return fail(IMPALA_EINVAL, "%s: shape out of range", fn);
     if (c->dk > kLaMaxDim || c->dv > kLaMaxDim)
         return fail(IMPALA_EUNSUPPORTED, "%s: heads of at most %d (got dk=%d dv=%d)", fn, kLaMaxDim, c->dk, c->dv);
-    if (int64_t(c->E) * c->heads > (int64_t(1) << 21))
-        return fail(IMPALA_EUNSUPPORTED, "%s: at most 2^21 states in a call", fn);
+    if (int64_t(c->E) * c->heads > (int64_t(1) << 21) || c->T > (1 << 30))
+        return fail(IMPALA_EUNSUPPORTED, "%s: at most 2^21 states and 2^30 steps in a call", fn);
     return IMPALA_OK;
 }
 

@@ -214,6 +214,33 @@ def test_strided_arrays(ty, T, d):
     assert all(torch.equal(g, w) for g, w in zip((dq, dk, dv, ds0), backward(full, 0.5)))
 
 
+@pytest.mark.parametrize("d", [7, 27, 66])
+def test_odd_sizes_at_even_strides(d):
+    """bf16 rows that end inside a 4-byte word, or between two, in wider arrays at 4-byte addresses: up to the last row's
+    last element, with infinities behind it."""
+    T, E, H, w = 130, 2, 2, 72
+    x = make(T, E, H, d, d, "bf16", "few", seed=d)
+    want = forward(x, 0.5), backward(x, 0.5)
+    a, s0, ds = dev(x["a"]), dev(x["s0"]), dev(x["ds"])
+
+    def wide(t):
+        base = torch.full((T, E, H, w), float("inf"), dtype=torch.bfloat16, device=DEV)
+        base[..., :d].copy_(t.to(DEV))
+        return base[..., :d]
+
+    q, k, v, do, o = (wide(x[n]) for n in ("q", "k", "v", "do", "do"))
+    dones, s_out = dev(x["d"]), torch.empty_like(s0)
+    shape = P.linattn_shape(q, k, v, o, dones, 0.5)
+    P.impala_linattn_fwd(shape, q, k, v, a, dones, s0, o, s_out, workspace(shape))
+    assert torch.equal(o, want[0][0]) and torch.equal(s_out, want[0][1])
+    dq, dk, dv, ds0 = wide(x["q"]), wide(x["k"]), wide(x["v"]), torch.empty_like(s0)
+    shape = P.linattn_shape(q, k, v, do, dones, 0.5, dq, dk, dv)
+    P.impala_linattn_bwd(shape, do, q, k, v, a, dones, s0, ds, dq, dk, dv, ds0, workspace(shape, 1))
+    assert all(torch.equal(g, y) for g, y in zip((dq, dk, dv, ds0), want[1]))
+    for t in (o, dq, dk, dv):
+        assert torch.isinf(t._base[..., d:]).all()
+
+
 def poison(x, where, value):
     for n in ("q", "k", "v", "do"):
         x[n][where] = value

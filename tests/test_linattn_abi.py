@@ -43,7 +43,7 @@ def test_shapes(call):
     for bad in (dict(prec=2), dict(T=-1), dict(E=-1), dict(heads=0), dict(dk=0), dict(dv=0)):
         assert call(shape(**bad)) == EINVAL, bad
         assert P.impala_linattn_workspace_bytes(shape(**bad)) == 0
-    for bad in (dict(dk=129), dict(dv=129), dict(E=1 << 21, heads=2)):
+    for bad in (dict(dk=129), dict(dv=129), dict(E=1 << 21, heads=2), dict(T=(1 << 30) + 1)):
         assert call(shape(**bad)) == EUNSUPPORTED, bad
     assert call(shape(E=0)) == 0
 
