@@ -250,6 +250,7 @@ template <class T, int V, bool GATE, bool TWO, bool MEAN>
 __global__ __launch_bounds__(512) void bn_fwd_kernel(BnArgs a) {
     using R = BnRow<T, V>;
     constexpr int N = BnVec<T>::N;
+    constexpr bool AHEAD = V == 8;   // with 16 elements a thread the registers are the rows' at hand
     __shared__ float sh[2 * 16 * 4];
     const BnPlace p(a);
     const float inv = 1.f / float(a.cg);
@@ -269,8 +270,9 @@ __global__ __launch_bounds__(512) void bn_fwd_kernel(BnArgs a) {
         if (GATE) rg = R::load(a.gate, a, p, row, on);
         rr = R::load(a.res, a, p, row, on && a.res.p);
     };
-    fetch(base);
+    if (AHEAD) fetch(base);
     for (; base < a.n; base += p.step) {
+        if (!AHEAD) fetch(base);
         const int64_t row = base + p.slot;
         BnPlace q = p;
         if (row >= a.n) q.width = 0;
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(512) void bn_fwd_kernel(BnArgs a) {
         R::unpack(rh, x);
         R::unpack(rr, y);
         if (GATE) R::unpack(rg, gt);
-        if (base + p.step < a.n) fetch(base + p.step);
+        if (AHEAD && base + p.step < a.n) fetch(base + p.step);
         float r[1];
         bn_normalise<MEAN, 1, V, N>({&x}, {a.norm}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
 #pragma unroll
@@ -302,16 +304,19 @@ template <class T, int V, bool GATE, bool TWO, bool MEAN>
 __global__ __launch_bounds__(512) void bn_bwd_kernel(BnArgs a) {
     using R = BnRow<T, V>;
     constexpr int N = BnVec<T>::N, Q = TWO ? 5 : 3;
+    constexpr bool AHEAD = V == 8;
     __shared__ float sh[2 * 16 * 4];
     extern __shared__ float cols[];   // [threads][V]
     const BnPlace p(a);
     const float inv = 1.f / float(a.cg);
     int flip = 0;
     float gamma[V], beta[V], rs[V], gamma2[V];
-    R::vec(a.gamma, 1.f, a, p, gamma);
-    R::vec(a.beta, 0.f, a, p, beta);
-    R::vec(a.rscale, 1.f, a, p, rs);
-    if (TWO) R::vec(a.gamma2, 1.f, a, p, gamma2);
+    if (AHEAD) {
+        R::vec(a.gamma, 1.f, a, p, gamma);
+        R::vec(a.beta, 0.f, a, p, beta);
+        R::vec(a.rscale, 1.f, a, p, rs);
+        if (TWO) R::vec(a.gamma2, 1.f, a, p, gamma2);
+    }
     float sum[Q][V];
 #pragma unroll
     for (int k = 0; k < Q; ++k)
@@ -330,8 +335,9 @@ __global__ __launch_bounds__(512) void bn_bwd_kernel(BnArgs a) {
         rd = R::load(a.dout, a, p, row, on && a.dout.p);
         if (GATE) rg = R::load(a.gate, a, p, row, on);
     };
-    fetch(base);
+    if (AHEAD) fetch(base);
     for (; base < a.n; base += p.step) {
+        if (!AHEAD) fetch(base);
         const int64_t row = base + p.slot;
         BnPlace q = p;
         if (row >= a.n) q.width = 0;
@@ -340,9 +346,10 @@ __global__ __launch_bounds__(512) void bn_bwd_kernel(BnArgs a) {
         R::unpack(rd, ds);
         if (GATE) R::unpack(rg, gt);
         if (TWO) { R::unpack(rd2, d); R::unpack(ro, y); }
-        if (base + p.step < a.n) fetch(base + p.step);
+        if (AHEAD && base + p.step < a.n) fetch(base + p.step);
         if constexpr (TWO) {
             bn_normalise<MEAN, 2, V, N>({&x, &y}, {a.norm, a.norm2}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
+            if (!AHEAD) R::vec(a.gamma2, 1.f, a, p, gamma2);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 sum[Q - 2][i] += d[i] * y[i];
@@ -356,6 +363,11 @@ __global__ __launch_bounds__(512) void bn_bwd_kernel(BnArgs a) {
             bn_normalise<MEAN, 1, V, N>({&x}, {a.norm}, r, q.width, p.t, a.tpr, inv, a.eps, sh, flip);
         }
         if (a.dres.p) R::store(a.dres, a, q, row, ds);
+        if (!AHEAD) {   // held through the loop they would be in memory all the same
+            R::vec(a.gamma, 1.f, a, p, gamma);
+            R::vec(a.beta, 0.f, a, p, beta);
+            R::vec(a.rscale, 1.f, a, p, rs);
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float z = x[i] * gamma[i] + beta[i], du = ds[i] * rs[i];

@@ -1,6 +1,8 @@
 // The global norm over many gradient tensors and their clipped values. HBM-bound: every source is read once for the norm
 // and once more for the values (from the caches where it fits them), every target written once. The tensors go by tables
 // in the kernels' arguments, so that a call is two launches for up to kGcTable of them and copies nothing to the device.
+// 36 tensors of 1.09 M float32 numbers in all: kernels of 4.4 and 5.6 us; 84 of 219 M, nearly all bf16, into float32:
+// 380 us, 4.6 TB/s with the second reading.
 #include <algorithm>
 
 #include "common.h"
@@ -13,7 +15,7 @@ namespace {
 
 constexpr int kGcTable = 96;       // tensors of a launch
 constexpr int kGcSeg = 8192;       // elements a workgroup takes at a time
-constexpr int kGcBlocks = 2048;    // workgroups of a launch, each with one partial sum
+constexpr int kGcBlocks = 4096;    // workgroups of a launch, each with one partial sum (2048: 391 us for 380 below)
 
 struct GcEntry {
     const void* src;
