@@ -615,11 +615,18 @@ def blocknorm_shape(prec, n, C_, groups=1, norm=NORM_RMS, norm2=NORM_NONE, gate_
     return s
 
 
+def _rows(t, ld: int, C_: int):
+    """Device pointer of rows ld elements apart: contiguous ones where that is their width."""
+    return ptr(t) if ld == C_ else _at(t)
+
+
 def impala_blocknorm_fwd(shape: BlocknormShape, h, gamma, beta, gate, rscale, res, out, gamma2=None, beta2=None,
                          out2=None, stream=None):
+    c = shape.C
     _check("impala_blocknorm_fwd", lib.impala_blocknorm_fwd(
-        C.byref(shape), _at(h), ptr(gamma), ptr(beta), _at(gate), ptr(rscale), _at(res), _at(out), ptr(gamma2), ptr(beta2),
-        _at(out2), stream_handle(stream)))
+        C.byref(shape), _rows(h, shape.ld_h, c), ptr(gamma), ptr(beta), _rows(gate, shape.ld_gate, c), ptr(rscale),
+        _rows(res, shape.ld_res, c), _rows(out, shape.ld_out, c), ptr(gamma2), ptr(beta2), _rows(out2, shape.ld_out2, c),
+        stream_handle(stream)))
 
 
 def impala_blocknorm_bwd_workspace_bytes(shape: BlocknormShape) -> int:
@@ -628,10 +635,12 @@ def impala_blocknorm_bwd_workspace_bytes(shape: BlocknormShape) -> int:
 
 def impala_blocknorm_bwd(shape: BlocknormShape, dout, dout2, h, gamma, beta, gate, rscale, out, gamma2, dh, dgamma, dbeta,
                          dgate, drscale, dres, dgamma2, dbeta2, ws, stream=None):
+    c = shape.C
     _check("impala_blocknorm_bwd", lib.impala_blocknorm_bwd(
-        C.byref(shape), _at(dout), _at(dout2), _at(h), ptr(gamma), ptr(beta), _at(gate), ptr(rscale), _at(out), ptr(gamma2),
-        _at(dh), ptr(dgamma), ptr(dbeta), _at(dgate), ptr(drscale), _at(dres), ptr(dgamma2), ptr(dbeta2), *_ws_args(ws),
-        stream_handle(stream)))
+        C.byref(shape), _rows(dout, shape.ld_dout, c), _rows(dout2, shape.ld_dout2, c), _rows(h, shape.ld_h, c), ptr(gamma),
+        ptr(beta), _rows(gate, shape.ld_gate, c), ptr(rscale), _rows(out, shape.ld_out, c), ptr(gamma2),
+        _rows(dh, shape.ld_dh, c), ptr(dgamma), ptr(dbeta), _rows(dgate, shape.ld_dgate, c), ptr(drscale),
+        _rows(dres, shape.ld_dres, c), ptr(dgamma2), ptr(dbeta2), *_ws_args(ws), stream_handle(stream)))
 
 
 def grad_tensors(pairs):
@@ -641,7 +650,7 @@ def grad_tensors(pairs):
     precs = {torch.bfloat16: PREC_BF16, torch.float32: PREC_FP32}
     pairs = list(pairs)
     out = (GradTensor * max(1, len(pairs)))()
-    out.used = len(pairs)
+    out.used, out.kept = len(pairs), pairs   # the array keeps the tensors alive
     for e, (s, d) in zip(out, pairs):
         d_ = s if d is None else d
         if s.dtype not in precs or d_.dtype not in precs or s.numel() != d_.numel():

@@ -19,7 +19,8 @@ struct LaPass {
     int dk, dv, back;
     int xk, xn;                // element strides of a state's two axes
     float in, out;
-    int vec;                   // bit 0: o is written in fours; 1: rows end inside a 16-byte piece; 2: q, k, v are read by it
+    int vec;                   // bit 0: o has whole fours of columns; 1: rows end inside a 16-byte piece; 2: all rows are in
+                               // a buffer resource's reach
 };
 constexpr int kLaMaxPasses = 3;
 constexpr int kLaMaxDim = 128;

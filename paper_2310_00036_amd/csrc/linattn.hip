@@ -123,8 +123,8 @@ hipError_t la_step(const LaArgs& a, hipStream_t s) {
 // together and handed round in LDS.
 //
 // 64 rows: the products on the diagonal grow with the chunk, the state's with its number, and a wave's lanes are the rows.
-// A chunk of 64-wide heads is 32 KB in bf16 and takes a workgroup of four waves 2.7 us (6500 cycles, of which 930 in the
-// matrix cores and 1300 in LDS); two of them share a CU, 2048 x 256 envs x 4 heads at 4.9 TB/s. Heads of 128: eight waves,
+// A chunk of 64-wide heads is 32 KB in bf16 and takes a workgroup of four waves 2.7 us (6500 cycles, about 930 of them in the
+// matrix cores and 1500 in LDS); two of them share a CU, 2048 x 256 envs x 4 heads take 252 us, 4.3 TB/s. Heads of 128: eight waves,
 // alone on a CU, 5.7 us for 64 KB.
 
 constexpr int kL = 64;

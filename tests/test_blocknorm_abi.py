@@ -85,6 +85,13 @@ def test_workspace():
         P.blocknorm_shape(0, 1, 8, ld_x=9)
 
 
+def test_binding_checks_rows():
+    t = torch.zeros(6, 80)[:, :64]
+    s = P.blocknorm_shape(P.PREC_FP32, 6, 64)
+    with pytest.raises(ValueError):
+        P.impala_blocknorm_fwd(s, t, None, None, None, None, None, torch.zeros(6, 64), stream=torch.Stream(device="cpu"))
+
+
 def clip(entries, limit=0.5, stats=None, ws=1 << 30, wsb=BIG, n=None):
     t = (P.GradTensor * max(1, len(entries)))(*(P.GradTensor(*e) for e in entries))
     return lib.grad_clip(t, len(entries) if n is None else n, limit, stats, ws, wsb, None)

@@ -258,3 +258,28 @@ def test_streams_graphs_and_repeats():
         torch.cuda.synchronize()
         assert torch.equal(out, want[i][0][0]) and torch.equal(out2, want[i][0][1])
         assert all(torch.equal(o[k], want[i][1][k]) for k in NAMES)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 128 KB apart, 9 GB from the first to the last: the bits of contiguous rows."""
+    n, C, w = 70000, 24, 65536
+    x = make(n, C, "bf16", seed=6)
+    args = ("bf16", 1, 1, 2, 1)
+    want, grads = run_forward(x, *args, True), run_backward(x, *args)
+    big = torch.empty(n, w, dtype=torch.bfloat16, device=DEV)
+    names = ("h", "gate", "res", "out", "out2", "dout", "dout2", "dh", "dgate", "dres")
+    at = {k: big[:, 1000 * i:1000 * i + C] for i, k in enumerate(names)}
+    for k in ("h", "gate", "res", "dout", "dout2"):
+        at[k].copy_(dev(x[k]))
+    v = {k: dev(x[k]) for k in ("gamma", "beta", "rscale", "gamma2", "beta2")}
+    s = shape_of(x, *args, **{"ld_" + k: w for k in names})
+    P.impala_blocknorm_fwd(s, at["h"], v["gamma"], v["beta"], at["gate"], v["rscale"], at["res"], at["out"], v["gamma2"],
+                           v["beta2"], at["out2"])
+    assert torch.equal(at["out"], want[0]) and torch.equal(at["out2"], want[1])
+    at["out"].copy_(dev(x["out"]))
+    small = {"d" + k: torch.empty_like(t) for k, t in v.items()}
+    ws = torch.empty(P.impala_blocknorm_bwd_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    P.impala_blocknorm_bwd(s, at["dout"], at["dout2"], at["h"], v["gamma"], v["beta"], at["gate"], v["rscale"], at["out"],
+                           v["gamma2"], at["dh"], small["dgamma"], small["dbeta"], at["dgate"], small["drscale"], at["dres"],
+                           small["dgamma2"], small["dbeta2"], ws)
+    assert all(torch.equal((at.get(k) if k in at else small[k]), g) for k, g in grads.items())

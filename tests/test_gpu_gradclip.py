@@ -166,3 +166,17 @@ def test_streams_graphs_and_repeats():
         st = run(zip(sets[0], eager), 0.5)
         torch.cuda.synchronize()
         assert sts[0].cpu().tolist() == st and all(torch.equal(a, b) for a, b in zip(outs[0], eager))
+
+
+def test_a_tensor_of_more_than_2_31_elements():
+    """Zeros with a few numbers about the border and at the end, in place; sources of it by parts give the same norm."""
+    n = 2 ** 31 + 70001
+    t = torch.zeros(n, dtype=B, device=DEV)
+    at = torch.tensor([0, 2 ** 31 - 1, 2 ** 31, 2 ** 31 + 1, n - 2, n - 1], device=DEV)
+    t[at] = torch.tensor([3.0, 4.0, 12.0, 84.0, 5.0, 12.0], dtype=B, device=DEV)
+    whole = math.sqrt(9 + 16 + 144 + 7056 + 25 + 144)
+    stats = run([(t[:2 ** 30], None), (t[2 ** 30:], None)], 1.0)
+    assert stats[0] == pytest.approx(whole, rel=2.0 ** -23)
+    stats = run([(t, t)], whole / 2)
+    assert stats[0] == pytest.approx(whole, rel=2.0 ** -23) and stats[1] == 0
+    assert t[at].tolist() == [1.5, 2.0, 6.0, 42.0, 2.5, 6.0] and int((t != 0).sum()) == 6

@@ -367,3 +367,22 @@ def test_streams_graphs_and_repeats(T, E):
             assert torch.equal(g, w)
         for g, w in zip((dq, dk, dv, ds0), want[i][1]):
             assert torch.equal(g, w)
+
+
+def test_offsets_beyond_32_bits():
+    """Steps 128 KB apart, 9 GB from the first to the last: the bits of contiguous arrays."""
+    T, d, w = 70000, 16, 65536
+    x = make(T, 1, 1, d, d, "bf16", "few", seed=4)
+    x["d"][::1500] = 1
+    big = torch.empty(T, 1, 1, w, dtype=torch.bfloat16, device=DEV)
+    q, k, v, do, o, dq, dk, dv = (big[..., i * 1000:i * 1000 + d] for i in range(8))
+    for n, t in (("q", q), ("k", k), ("v", v), ("do", do)):
+        t.copy_(dev(x[n]))
+    a, s0, ds, dones = dev(x["a"]), dev(x["s0"]), dev(x["ds"]), dev(x["d"])
+    s_out, ds0 = torch.empty_like(s0), torch.empty_like(s0)
+    shape = P.linattn_shape(q, k, v, o, dones, 0.5)
+    P.impala_linattn_fwd(shape, q, k, v, a, dones, s0, o, s_out, workspace(shape))
+    shape = P.linattn_shape(q, k, v, do, dones, 0.5, dq, dk, dv)
+    P.impala_linattn_bwd(shape, do, q, k, v, a, dones, s0, ds, dq, dk, dv, ds0, workspace(shape, 1))
+    for g, want in zip((o, s_out, dq, dk, dv, ds0), (*forward(x, 0.5), *backward(x, 0.5))):
+        assert torch.equal(g, want)
