@@ -177,7 +177,7 @@ struct LaB {
         const uint2 a = lds_read_tr16(p), b = lds_read_tr16(p + 4 * rs);
         return make_uint4(a.x, a.y, b.x, b.y);
     }
-    // X's 16 x 16 results: result m holds rows k0(m) + group * KG + r, so that two of them are a fragment
+    // X's 16 x 16 results: the row that result m has in lane group g as its r-th, so that two results are a fragment
     static CB_DEV int krow(int m, int g, int r) { return 32 * (m >> 1) + 8 * g + 4 * (m & 1) + r; }
     static CB_DEV Frag kcols(const unsigned char* tile, int rs, int row0, int m) {
         return cols<2>(tile, rs, row0, 32 * (m >> 1) + 4 * (m & 1));
@@ -255,7 +255,8 @@ struct LaTile {   // STATE: without q and the products
     static constexpr int ES = sizeof(typename Tr::T);
     static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16, RSP = kL * ES + 16;
     static constexpr int Q = 0, K = STATE ? 0 : kL * RSK, V = K + kL * RSK, P = V + kL * RSV, PP = kL * RSP;
-    static constexpr int TAB = STATE ? P : P + Tr::NP * PP;       // g^0 .. g^64, 16 zeros, in out g^0 .. in out g^64, X's and v's weights by row
+    // g^0 .. g^64, 16 zeros, in out g^0 .. in out g^64, X's and v's weights by row, the rows that start an episode
+    static constexpr int TAB = STATE ? P : P + Tr::NP * PP;
     static constexpr int BYTES = TAB + (2 * 68 + 16 + 2 * kL + 2) * 4;
     static constexpr int UQ = DK * ES / 16 / NW > 0 ? DK * ES / 16 / NW : 1;   // 16-byte pieces of q and k a thread moves
     static constexpr int UV = ES;                                             // of v
@@ -327,8 +328,13 @@ CB_DEV float la_row_at(const typename Tr::Frag (&fv)[NJ], int j, int col) {
     return __shfl(y, j / Tr::KPL % 4 * 16 + col);
 }
 
+// Waves a SIMD is to hold: two of the whole pass's, four of the states' where their registers allow it without memory.
+template <class Tr, int DK, bool STATE>
+constexpr int la_simd_waves = STATE && DK <= 64 && sizeof(typename Tr::T) == 2 ? 4 : 2;
+
 template <class Tr, int DK, int NW, bool STATE, bool FAST>
-__global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T) == 2 ? 4 : 2) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0, int ny, int blocks) {
+__global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_chunk_kernel(LaArgs a, LaSegs sg, int y0, int ny,
+                                                                                          int blocks) {
     using T = typename Tr::T;
     using Frag = typename Tr::Frag;
     using L = LaTile<Tr, DK, NW, STATE>;
@@ -366,7 +372,8 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
     const int dk = P.dk, dv = P.dv, back = P.back, vec = P.vec;
     const float out = P.out;
     auto rows = [&](const LaView& x, int d) {
-        return LaRows{static_cast<const char*>(x.p) + (e * x.e + h * x.h + t0 * x.t) * L::ES, int(dir * x.t) * L::ES, d * L::ES};
+        return LaRows{static_cast<const char*>(x.p) + (e * x.e + h * x.h + t0 * x.t) * L::ES, FAST ? int(dir * x.t) * L::ES : 0,
+                      d * L::ES};
     };
     LaRows q = rows(P.q, dk), k = rows(P.k, dk), v = rows(P.v, dv), o = rows(P.o, dv);
     LaRows dn{reinterpret_cast<const char*>(a.dones + (a.dones ? e * a.d_e + t0 * a.d_t : 0)), a.dones ? int(dir * a.d_t) : 0,
@@ -427,7 +434,8 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
             for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const uint32_t off = xn == 1 ? (at == kOOB ? kOOB : at + Tr::krow(m, 0, r) * xk * 4) : xat(Tr::krow(m, g, r), xk, xn);
+                    const uint32_t off = xk != dv ? xat(Tr::krow(m, g, r), xk, xn)
+                                         : at == kOOB ? kOOB : at + Tr::krow(m, 0, r) * xk * 4;
                     X[m][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(bx, off, 0, 0));
                 }
         }
@@ -506,10 +514,9 @@ __global__ __launch_bounds__(64 * NW, STATE && DK <= 64 && sizeof(typename Tr::T
         auto count = [&](int i) { return count_in(m, i); };
         const int total = __popcll(m);
         if (STATE) factor = total || factor < 0.f ? -1.f : factor * over;
-        q.next(); k.next(); v.next(); dn.next(); if (p > p0) o.next();
-        if (p + kL < p1) {
-            fetch(min(kL, p1 - p - kL));
-        }
+        q.next(); k.next(); v.next(); dn.next();
+        if (p > p0) o.next();   // the chunk at hand's, to be written at its end
+        if (p + kL < p1) fetch(min(kL, p1 - p - kL));
 
         if (!STATE) {   // in out g^(i-j) q_i . k_j by tiles on and below the diagonal, a wave's few at once
             constexpr int MT = (10 + NW - 1) / NW;

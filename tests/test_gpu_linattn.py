@@ -281,6 +281,23 @@ def test_what_is_not_finite_stays_in_its_episode_and_time(ty, T, value):
     assert all(torch.equal(g, w) for g, w in zip(forward(z, 0.5), want))
 
 
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(16, 1), (1, 16), (7, 1), (1, 1), (5, 3)])
+def test_a_states_number_reaches_its_row_and_column_only(dk, dv, ty):
+    x = make(70, 1, 1, dk, dv, ty, "none", seed=dk)
+    clean = forward(x, 1.0), backward(x, 1.0)
+    k, n = dk - 1, dv - 1
+    x["s0"][0, 0, k, n] = float("nan")
+    (o, s), (dq, dkk, dvv, ds0) = forward(x, 1.0), backward(x, 1.0)
+    for g, w, axis, i in ((o, clean[0][0], 3, n), (dq, clean[1][0], 3, k)):
+        keep = [j for j in range(g.shape[axis]) if j != i]
+        assert torch.equal(g[..., keep], w[..., keep]) and g[..., i].isnan().all()
+    bad = torch.zeros_like(s, dtype=torch.bool)
+    bad[0, 0, k, n] = True
+    assert torch.equal(s[~bad], clean[0][1][~bad]) and s[bad].isnan().all()
+    assert all(torch.equal(g, w) for g, w in zip((dkk, dvv, ds0), clean[1][1:]))
+
+
 def test_decays_of_none_and_of_everything():
     """Decay 1 (sums over all steps), decay 0 (log of -infinity: one step's memory) and a fast one that underflows."""
     for T in (3, 200):
