@@ -219,8 +219,8 @@ size_t impala_linattn_workspace_bytes(const linattn_shape_t* shape, int backward
 /* o over the rollout from the state s0 before it (NULL: zeros), and the state s_out after it (NULL: not
  * wanted; may be s0 itself). s_out is S_{T-1}: the next rollout's first step applies its own d_0.
  * shape is HOST memory, not kept. ws: 16-byte aligned, may be NULL where the query gives 0.
- * bf16 products of q and k are exact, what follows is held in pairs or triples of bf16 numbers, so that
- * o is off by its own rounding and s_out by a few 2^-24 as the float32 sums are. */
+ * In bf16 products of q and k are exact and what follows is held in 24 bits or more (three bf16 numbers), so
+ * that before its own rounding o, like s_out, is off by a few 2^-24 of its terms' magnitudes. */
 impala_status_t impala_linattn_fwd(const linattn_shape_t* shape, const void* q, const void* k, const void* v,
                                    const float* log_decay, const uint8_t* dones, const float* s0, void* o,
                                    float* s_out, void* ws, size_t ws_bytes, hipStream_t stream);

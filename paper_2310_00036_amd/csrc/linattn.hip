@@ -131,12 +131,14 @@ constexpr int kL = 64;
 typedef uint32_t cb_u32x2 __attribute__((ext_vector_type(2)));
 
 // bf16: products of two bf16 numbers are exact; what is no bf16 number (the decayed products, X, the decayed v) goes into
-// a product as two of them, or three where the result is a float32 output (X).
+// a product as three of them, each nearest to what the ones before leave: 24 bits, as float32 has. (Two for the decayed
+// products and X, 16 bits, would show wherever a sum's terms cancel; they take 60 us for 65 in the backward pass of 128 x 128
+// envs x 8 heads of 64, 128 for 136 in 16384 x 2 x 8 heads of 128 forward.)
 struct LaB {
     using T = uint16_t;
     using Frag = uint4;
     static constexpr int KB = 32, KPL = 8;   // contraction per fragment, elements of it a lane holds (at KPL * group)
-    static constexpr int NP = 2, NX = 2, NV = 3;
+    static constexpr int NP = 3, NX = 3, NV = 3;
     static CB_DEV cb_f32x4 mma(Frag a, Frag b, cb_f32x4 c) { return PrecBF16::mma(a, b, c); }
     static CB_DEV float load(T v) { return bf2f(v); }
     static CB_DEV void unpack(Frag f, float* x) {
@@ -253,8 +255,15 @@ struct LaSegs {
 template <class Tr, int DK, int NW, bool STATE>
 struct LaTile {   // STATE: without q and the products
     static constexpr int ES = sizeof(typename Tr::T);
-    static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16, RSP = kL * ES + 16;
-    static constexpr int Q = 0, K = STATE ? 0 : kL * RSK, V = K + kL * RSK, P = V + kL * RSV, PP = kL * RSP;
+    static constexpr int RSK = DK * ES + 16, RSV = 16 * NW * ES + 16;
+    // The products' rows. Of 32-wide heads, rows 0 .. 31 have 32 columns (what is above the diagonal is not read), so that
+    // four bf16 workgroups share a CU: 1024 x 64 envs x 16 heads of 32 forward 81 us, with square planes 96. (Wider heads are
+    // no more in a CU with it and pay for the addresses: 2048 x 64 x 4 heads of 64 forward 93 us square, 95 so.)
+    static constexpr int RSP = kL * ES + 16, RSP0 = DK == 32 ? kL / 2 * ES + 16 : RSP;
+    static constexpr int Q = 0, K = STATE ? 0 : kL * RSK, V = K + kL * RSK, P = V + kL * RSV, PP = kL / 2 * (RSP0 + RSP);
+    static CB_DEV int prow(int i) {
+        return RSP0 == RSP ? i * RSP : i < kL / 2 ? i * RSP0 : kL / 2 * RSP0 + (i - kL / 2) * RSP;
+    }
     // g^0 .. g^64, 16 zeros, in out g^0 .. in out g^64, X's and v's weights by row, the rows that start an episode
     static constexpr int TAB = STATE ? P : P + Tr::NP * PP;
     static constexpr int BYTES = TAB + (2 * 68 + 16 + 2 * kL + 2) * 4;
@@ -453,7 +462,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
     if (!STATE && KB == 32) {   // products above the diagonal that a fragment of 32 rows takes along
         for (int u = tid; u < 2 * 16 * Tr::NP * 4; u += 64 * NW) {
             const int pl = u / (2 * 16 * 4), b = u / 64 % 2, i = u / 4 % 16, j = u % 4;
-            *reinterpret_cast<uint2*>(lds + L::P + pl * L::PP + (32 * b + i) * L::RSP + (32 * b + 16 + 4 * j) * L::ES) =
+            *reinterpret_cast<uint2*>(lds + L::P + pl * L::PP + L::prow(32 * b + i) + (32 * b + 16 + 4 * j) * L::ES) =
                 make_uint2(0, 0);
         }
     }
@@ -556,7 +565,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
             // (Behind the tenth tile a wave repeats it: the same numbers in the same place.)
 #pragma unroll
             for (int y = 0; y < MT; ++y)
-                Tr::store_p(lds + L::P + (16 * tb[y] + c) * L::RSP + (16 * tt[y] + 4 * g) * L::ES, L::PP, d[y]);
+                Tr::store_p(lds + L::P + L::prow(16 * tb[y] + c) + (16 * tt[y] + 4 * g) * L::ES, L::PP, d[y]);
         }
 
         __builtin_amdgcn_sched_barrier(0);
@@ -664,7 +673,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
 #pragma unroll
                         for (int b = 0; b < 4; ++b)
                             if (jb * KB <= 16 * b + 15)
-                                fp[b] = *reinterpret_cast<const Frag*>(lds + L::P + u * L::PP + (16 * b + c) * L::RSP +
+                                fp[b] = *reinterpret_cast<const Frag*>(lds + L::P + u * L::PP + L::prow(16 * b + c) +
                                                                        jb * 64 + 16 * g);
 #pragma unroll
                         for (int b = 0; b < 4; ++b)
@@ -691,7 +700,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
                         float w = 0.f;
 #pragma unroll
                         for (int u = 0; u < Tr::NP; ++u)
-                            w += Tr::load(*reinterpret_cast<const T*>(lds + L::P + u * L::PP + i * L::RSP + j * L::ES));
+                            w += Tr::load(*reinterpret_cast<const T*>(lds + L::P + u * L::PP + L::prow(i) + j * L::ES));
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             if (!isfinite(x[r]) || !isfinite(w)) A[b][r] += w * x[r];
