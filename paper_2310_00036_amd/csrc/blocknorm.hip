@@ -157,7 +157,8 @@ CB_DEV void bn_own(float (&x)[V], int width, int t, int tpr, F&& f) {
 }
 
 // x <- (x - mean) rstd in place for M rows side by side (padding stays out of the sums by `width`); r: rstd. Two passes
-// over the registers. MEAN: a norm of the kernel may be a layer norm; the kinds are told apart by selections.
+// over the registers. MEAN: a norm of the kernel may be a layer norm; the kinds are told apart by selections. A slot behind
+// the last row (width 0) has r = 1: with eps = 0 its zeros would make NaN of the column sums.
 template <bool MEAN, int M, int V, int N>
 CB_DEV void bn_normalise(float (*const (&x)[M])[V], const int (&kind)[M], float (&r)[M], int width, int t, int tpr, float inv,
                          float eps, float* sh, int& flip) {
@@ -185,7 +186,7 @@ CB_DEV void bn_normalise(float (*const (&x)[M])[V], const int (&kind)[M], float 
     row_sum(s, tpr, sh, flip);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-        r[m] = kind[m] == 0 ? 1.f : bn_rsqrt(s[m] * inv + eps);
+        r[m] = kind[m] == 0 || width == 0 ? 1.f : bn_rsqrt(s[m] * inv + eps);
 #pragma unroll
         for (int i = 0; i < V; ++i) (*x[m])[i] *= r[m];
     }
