@@ -83,9 +83,9 @@ bool arrays_meet(const Strided& a, const Strided& b) {
     return rows_meet(a, b, ax, 0, d / a.es);
 }
 
-// Strides and aliases of a call's arrays. in_place: an output may be an input itself.
+// Strides and aliases of a call's arrays. Of the first `in_place` ones an output may be an input itself.
 template <size_t N>
-impala_status_t check_arrays(const char* fn, const Strided (&v)[N], bool in_place = false) {
+impala_status_t check_arrays(const char* fn, const Strided (&v)[N], size_t in_place = 0) {
     for (const Strided& x : v) {
         if (!x.p) continue;
         for (int i = 0; i < 3; ++i)
@@ -96,12 +96,11 @@ impala_status_t check_arrays(const char* fn, const Strided (&v)[N], bool in_plac
             return fail(IMPALA_EINVAL, "%s: %s has elements in one place", fn, x.name);
     }
     auto same = [&](const Strided& a, const Strided& b) {
-        return in_place && a.written != b.written && a.p == b.p && a.es == b.es && a.w == b.w && a.n[0] == b.n[0] &&
-               a.s[0] == b.s[0];
+        return a.written != b.written && a.p == b.p && a.es == b.es && a.w == b.w && a.n[0] == b.n[0] && a.s[0] == b.s[0];
     };
     for (size_t i = 0; i < N; ++i)
         for (size_t j = 0; j < i; ++j)
-            if (!same(v[i], v[j]) && (v[i].written || v[j].written) && !v[i].empty() && !v[j].empty() && arrays_meet(v[i], v[j]))
+            if (!(i < in_place && same(v[i], v[j])) && (v[i].written || v[j].written) && !v[i].empty() && !v[j].empty() && arrays_meet(v[i], v[j]))
                 return fail(IMPALA_EINVAL, "%s: %s and %s overlap", fn, v[j].name, v[i].name);
     return IMPALA_OK;
 }
@@ -282,7 +281,7 @@ impala_status_t impala_blocknorm_fwd(const blocknorm_shape_t* shape, const void*
                          bn_rows("out2", out2, c, c.ld_out2, true), bn_cols("gamma", gamma, c, false),
                          bn_cols("beta", beta, c, false), bn_cols("rscale", rscale, c, false),
                          bn_cols("gamma2", gamma2, c, false), bn_cols("beta2", beta2, c, false)};
-    if ((st = check_lds(__func__, c, v, 5)) || (st = check_arrays(__func__, v, true))) return st;
+    if ((st = check_lds(__func__, c, v, 5)) || (st = check_arrays(__func__, v, 5))) return st;
     BnArgs a = bn_args(c);
     a.h = bn_mat(h, c.ld_h); a.gate = bn_mat(gate, c.ld_gate); a.res = bn_mat(res, c.ld_res);
     a.out = bn_mat(out, c.ld_out); a.out2 = bn_mat(out2, c.ld_out2);
@@ -324,7 +323,7 @@ impala_status_t impala_blocknorm_bwd(const blocknorm_shape_t* shape, const void*
                          bn_cols("drscale", drscale, c, true), bn_cols("dgamma2", dgamma2, c, true),
                          bn_cols("dbeta2", dbeta2, c, true)};
     if (rows && (st = check_lds(__func__, c, v, 8))) return st;
-    if ((st = check_arrays(__func__, v, true))) return st;
+    if ((st = check_arrays(__func__, v, 8))) return st;
     if (rows) {
         const size_t need = blocknorm_bwd_ws_bytes(c.prec, c.n, c.C, c.groups, dout2 != nullptr);
         if (ws_bytes < need) return fail(IMPALA_EWORKSPACE, "%s: workspace %zu < %zu bytes", __func__, ws_bytes, need);
