@@ -200,8 +200,9 @@ impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, i
  * E * heads <= 2^21 and T <= 2^30 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element
  * (sizes, strides and addresses of whole 4 bytes, and steps less than 2^24 bytes apart, are read 16 bytes at a
  * time, others element by element).
- * Outputs must not have two elements in one place, and must not overlap inputs or each other: two arrays
- * with the same strides may lie between each other's elements, any other overlap of their address ranges
+ * Outputs must not have two elements in one place, and must not overlap inputs or each other. Two arrays
+ * may lie between each other's rows, as the parts of one buffer do; an axis on which their strides differ
+ * (the heads, where dk is not dv) counts with all that it spans. Any other overlap of their address ranges
  * is IMPALA_EINVAL. */
 typedef struct linattn_strides { int64_t t, e, h; } linattn_strides_t;
 typedef struct linattn_shape {

@@ -72,15 +72,23 @@ bool rows_meet(const Strided& a, const Strided& b, const int* ax, int level, int
 bool arrays_meet(const Strided& a, const Strided& b) {
     if (!a.p || !b.p || !ranges_overlap(a.p, a.bytes(), b.p, b.bytes())) return false;
     if (a.es != b.es) return true;
+    // An axis on which they step differently (the heads of parts of one buffer, where dk is not dv) becomes part of the row,
+    // with all that it spans.
+    Strided x = a, y = b;
     for (int i = 0; i < 3; ++i)
-        if (a.n[i] != b.n[i] || a.s[i] != b.s[i]) return true;
-    Strided wide = a;
-    wide.w = std::max(a.w, b.w);
+        if (a.n[i] != b.n[i] || a.s[i] != b.s[i])
+            for (Strided* r : {&x, &y}) {
+                r->w += (r->n[i] - 1) * r->s[i];
+                r->n[i] = 1;
+                r->s[i] = 0;
+            }
+    Strided wide = x;
+    wide.w = std::max(x.w, y.w);
     const int64_t d = reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p);
     if (!wide.nested() || d % a.es) return true;
     int ax[3];
-    a.order(ax);
-    return rows_meet(a, b, ax, 0, d / a.es);
+    x.order(ax);
+    return rows_meet(x, y, ax, 0, d / a.es);
 }
 
 // Strides and aliases of a call's arrays. Of the first `in_place` ones an output may be an input itself.
