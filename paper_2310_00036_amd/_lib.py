@@ -8,7 +8,10 @@ runs in the library's HIP kernels. Importing it fails loudly when the library is
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
+
+import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcleanba_learner.so")
@@ -72,17 +75,58 @@ class LinattnStrides(C.Structure):
     _fields_ = [("t", C.c_int64), ("e", C.c_int64), ("h", C.c_int64)]
 
 
-class LinattnShape(C.Structure):
+def _flat_of(name, *size):
+    """What a call expects of contiguous float32 numbers."""
+    return name, torch.Size(size), tuple(math.prod(size[i + 1:]) for i in range(len(size))), torch.float32
+
+
+class _Shape(C.Structure):
+    """A struct that keeps what it says of a call's tensors beside itself, formed again whenever its fields change."""
+
+    def expected(self):
+        """{call: [(argument, shape, strides, dtype)] in the call's order}"""
+        raw = bytes(self)
+        known = self.__dict__.get("_known")
+        if known is None or known[0] != raw:
+            known = self._known = raw, self._expected()
+        return known[1]
+
+
+class LinattnShape(_Shape):
     _fields_ = ([("prec", C.c_int32), ("T", C.c_int32), ("E", C.c_int32), ("heads", C.c_int32), ("dk", C.c_int32),
                  ("dv", C.c_int32), ("scale", C.c_float)] +
                 [(x, LinattnStrides) for x in ("q", "k", "v", "o", "gq", "gk", "gv")] +
                 [("done_t", C.c_int64), ("done_e", C.c_int64)])
 
+    def _expected(self):
+        def rows(name, field, d):
+            st = getattr(self, field)
+            return name, torch.Size((self.T, self.E, self.heads, d)), (st.t, st.e, st.h, 1), _DTYPES.get(self.prec)
 
-class BlocknormShape(C.Structure):
+        def state(name):
+            return _flat_of(name, self.E, self.heads, self.dk, self.dv)
+
+        qkv = [rows("q", "q", self.dk), rows("k", "k", self.dk), rows("v", "v", self.dv), _flat_of("log_decay", self.heads),
+               ("dones", torch.Size((self.T, self.E)), (self.done_t, self.done_e), torch.uint8)]
+        return dict(fwd=qkv + [state("s0"), rows("o", "o", self.dv), state("s_out")],
+                    step=qkv + [state("s_in"), rows("o", "o", self.dv), state("s_out")],
+                    bwd=[rows("d_o", "o", self.dv)] + qkv + [state("s0"), state("ds_out"), rows("dq", "gq", self.dk), rows("dk", "gk", self.dk),
+                                                       rows("dv", "gv", self.dv), state("ds0")])
+
+
+class BlocknormShape(_Shape):
     _fields_ = ([(x, C.c_int32) for x in ("prec", "C", "groups", "norm", "norm2", "gate_act")] +
                 [("eps", C.c_float), ("n", C.c_int64)] +
                 [("ld_" + x, C.c_int64) for x in ("h", "gate", "res", "out", "out2", "dout", "dout2", "dh", "dgate", "dres")])
+
+    def _expected(self):
+        def args(*names):   # rows have a stride in the struct, the others are vectors over the channels
+            return [(x, torch.Size((self.n, self.C)), (getattr(self, "ld_" + x), 1), _DTYPES.get(self.prec))
+                    if hasattr(self, "ld_" + x) else _flat_of(x, self.C) for x in names]
+
+        return dict(fwd=args("h", "gamma", "beta", "gate", "rscale", "res", "out", "gamma2", "beta2", "out2"),
+                    bwd=args("dout", "dout2", "h", "gamma", "beta", "gate", "rscale", "out", "gamma2", "dh", "dgamma", "dbeta",
+                             "dgate", "drscale", "dres", "dgamma2", "dbeta2"))
 
 
 class GradTensor(C.Structure):
@@ -559,7 +603,6 @@ def _strided(name, t, shape, dtype):
 def linattn_shape(q, k, v, o, dones=None, scale=1.0, dq=None, dk=None, dv=None) -> LinattnShape:
     """Sizes, type and strides of the linear attention's tensors: q, k [T, E, heads, dk], v, o [T, E, heads, dv]
     (o: the output or its gradient), dones [T, E]; dq, dk, dv for the backward pass."""
-    import torch
     if q.dim() != 4 or v.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("q and v must be [T, E, heads, d] in bfloat16 or float32")
     s = LinattnShape()
@@ -576,9 +619,58 @@ def linattn_shape(q, k, v, o, dones=None, scale=1.0, dq=None, dk=None, dv=None) 
     return s
 
 
-def _at(t):
-    """Device pointer of a tensor whose strides its shape struct holds (None passes NULL)."""
-    return t if t is None or isinstance(t, int) else t.data_ptr()
+_DTYPES = {PREC_BF16: torch.bfloat16, PREC_FP32: torch.float32}
+
+
+def _steps_as(t, size, strides) -> bool:
+    """Whether t's elements in their order are those of `size` and `strides`: axes of one element have no stride, and axes
+    that step evenly count as one."""
+    if t.numel() != math.prod(size) or t.numel() == 0:
+        return t.numel() == math.prod(size)
+
+    def axes(size, strides):   # from the last one on, even ones joined
+        out = []
+        for n, s in zip(reversed(size), reversed(strides)):
+            if n > 1 and out and s == out[-1][0] * out[-1][1]:
+                out[-1] = out[-1][0] * n, out[-1][1]
+            elif n > 1:
+                out.append((n, s))
+        return out
+    return axes(t.shape, t.stride()) == axes(size, strides)
+
+
+def _pointers(fn, expected, tensors, ws=None):
+    """(device pointers, device) of a call's tensors. What a shape struct says of a tensor is what the kernels read and write,
+    so each has to be of the struct's type, size and strides, and on one GPU; None and plain addresses pass as they are."""
+    out, device = [], None
+    for x, t in zip(expected, tensors):
+        if t is None or type(t) is int:
+            out.append(t)
+            continue
+        name, size, strides, dtype = x
+        at = t.get_device()
+        if device is None:
+            device = at
+        if t.dtype is not dtype or (t.shape != size or t.stride() != strides) and not _steps_as(t, size, strides) \
+                or at != device or at < 0:
+            raise ValueError(f"{fn}: {name} has to be {tuple(size)} of {dtype} with strides {strides} on the GPU of the others, "
+                             f"got {tuple(t.shape)} of {t.dtype}, {t.stride()}, on {t.device}")
+        out.append(t.data_ptr())
+    if ws is not None and (ws.get_device() != (ws.get_device() if device is None else device) or ws.get_device() < 0):
+        raise ValueError(f"{fn}: ws has to be on the GPU of the others, got {ws.device}")
+    return out, device
+
+
+def _stream_of(fn, stream, device):
+    """The stream's handle; it has to be of the tensors' device."""
+    if stream is None:
+        at = torch.cuda.current_device()
+        handle = torch._C._cuda_getCurrentRawStream(at)   # torch.cuda.current_stream().cuda_stream, without its object
+    else:
+        at, handle = getattr(stream, "device_index", device), stream.cuda_stream
+    if device is not None and at != device:
+        raise ValueError(f"{fn}: tensors on cuda:{device}, stream on device {at}")
+    return handle
 
 
 def impala_linattn_workspace_bytes(shape: LinattnShape, backward: int = 0) -> int:
@@ -586,22 +678,22 @@ def impala_linattn_workspace_bytes(shape: LinattnShape, backward: int = 0) -> in
 
 
 def impala_linattn_fwd(shape: LinattnShape, q, k, v, log_decay, dones, s0, o, s_out, ws=None, stream=None):
-    _check("impala_linattn_fwd", lib.impala_linattn_fwd(
-        C.byref(shape), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s0), _at(o), ptr(s_out), *_ws_args(ws),
-        stream_handle(stream)))
+    p, at = _pointers("impala_linattn_fwd", shape.expected()["fwd"], (q, k, v, log_decay, dones, s0, o, s_out), ws)
+    _check("impala_linattn_fwd", lib.impala_linattn_fwd(C.byref(shape), *p, *_ws_args(ws),
+                                                        _stream_of("impala_linattn_fwd", stream, at)))
 
 
 def impala_linattn_bwd(shape: LinattnShape, d_o, q, k, v, log_decay, dones, s0, ds_out, dq, dk, dv, ds0, ws=None,
                        stream=None):
-    _check("impala_linattn_bwd", lib.impala_linattn_bwd(
-        C.byref(shape), _at(d_o), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s0), ptr(ds_out), _at(dq),
-        _at(dk), _at(dv), ptr(ds0), *_ws_args(ws), stream_handle(stream)))
+    p, at = _pointers("impala_linattn_bwd", shape.expected()["bwd"],
+                      (d_o, q, k, v, log_decay, dones, s0, ds_out, dq, dk, dv, ds0), ws)
+    _check("impala_linattn_bwd", lib.impala_linattn_bwd(C.byref(shape), *p, *_ws_args(ws),
+                                                        _stream_of("impala_linattn_bwd", stream, at)))
 
 
 def impala_linattn_step(shape: LinattnShape, q, k, v, log_decay, dones, s_in, o, s_out, stream=None):
-    _check("impala_linattn_step", lib.impala_linattn_step(
-        C.byref(shape), _at(q), _at(k), _at(v), ptr(log_decay), _at(dones), ptr(s_in), _at(o), ptr(s_out),
-        stream_handle(stream)))
+    p, at = _pointers("impala_linattn_step", shape.expected()["step"], (q, k, v, log_decay, dones, s_in, o, s_out))
+    _check("impala_linattn_step", lib.impala_linattn_step(C.byref(shape), *p, _stream_of("impala_linattn_step", stream, at)))
 
 
 def blocknorm_shape(prec, n, C_, groups=1, norm=NORM_RMS, norm2=NORM_NONE, gate_act=GATE_LINEAR, eps=1e-5,
@@ -615,18 +707,11 @@ def blocknorm_shape(prec, n, C_, groups=1, norm=NORM_RMS, norm2=NORM_NONE, gate_
     return s
 
 
-def _rows(t, ld: int, C_: int):
-    """Device pointer of rows ld elements apart: contiguous ones where that is their width."""
-    return ptr(t) if ld == C_ else _at(t)
-
-
 def impala_blocknorm_fwd(shape: BlocknormShape, h, gamma, beta, gate, rscale, res, out, gamma2=None, beta2=None,
                          out2=None, stream=None):
-    c = shape.C
-    _check("impala_blocknorm_fwd", lib.impala_blocknorm_fwd(
-        C.byref(shape), _rows(h, shape.ld_h, c), ptr(gamma), ptr(beta), _rows(gate, shape.ld_gate, c), ptr(rscale),
-        _rows(res, shape.ld_res, c), _rows(out, shape.ld_out, c), ptr(gamma2), ptr(beta2), _rows(out2, shape.ld_out2, c),
-        stream_handle(stream)))
+    p, at = _pointers("impala_blocknorm_fwd", shape.expected()["fwd"],
+                      (h, gamma, beta, gate, rscale, res, out, gamma2, beta2, out2))
+    _check("impala_blocknorm_fwd", lib.impala_blocknorm_fwd(C.byref(shape), *p, _stream_of("impala_blocknorm_fwd", stream, at)))
 
 
 def impala_blocknorm_bwd_workspace_bytes(shape: BlocknormShape) -> int:
@@ -635,22 +720,21 @@ def impala_blocknorm_bwd_workspace_bytes(shape: BlocknormShape) -> int:
 
 def impala_blocknorm_bwd(shape: BlocknormShape, dout, dout2, h, gamma, beta, gate, rscale, out, gamma2, dh, dgamma, dbeta,
                          dgate, drscale, dres, dgamma2, dbeta2, ws, stream=None):
-    c = shape.C
-    _check("impala_blocknorm_bwd", lib.impala_blocknorm_bwd(
-        C.byref(shape), _rows(dout, shape.ld_dout, c), _rows(dout2, shape.ld_dout2, c), _rows(h, shape.ld_h, c), ptr(gamma),
-        ptr(beta), _rows(gate, shape.ld_gate, c), ptr(rscale), _rows(out, shape.ld_out, c), ptr(gamma2),
-        _rows(dh, shape.ld_dh, c), ptr(dgamma), ptr(dbeta), _rows(dgate, shape.ld_dgate, c), ptr(drscale),
-        _rows(dres, shape.ld_dres, c), ptr(dgamma2), ptr(dbeta2), *_ws_args(ws), stream_handle(stream)))
+    p, at = _pointers("impala_blocknorm_bwd", shape.expected()["bwd"],
+                      (dout, dout2, h, gamma, beta, gate, rscale, out, gamma2, dh, dgamma, dbeta, dgate, drscale, dres, dgamma2,
+                       dbeta2), ws)
+    _check("impala_blocknorm_bwd", lib.impala_blocknorm_bwd(C.byref(shape), *p, *_ws_args(ws),
+                                                            _stream_of("impala_blocknorm_bwd", stream, at)))
 
 
 def grad_tensors(pairs):
     """The host array that grad_clip takes, from a sequence of (src, dst): contiguous tensors, bfloat16 or float32, of
     equal sizes; dst may be src, or None (it counts in the norm only)."""
-    import torch
-    precs = {torch.bfloat16: PREC_BF16, torch.float32: PREC_FP32}
+    precs = {t: p for p, t in _DTYPES.items()}
     pairs = list(pairs)
     out = (GradTensor * max(1, len(pairs)))()
     out.used, out.kept = len(pairs), pairs   # the array keeps the tensors alive
+    out.devices = {t.get_device() for pair in pairs for t in pair if t is not None and t.numel()}
     for e, (s, d) in zip(out, pairs):
         d_ = s if d is None else d
         if s.dtype not in precs or d_.dtype not in precs or s.numel() != d_.numel():
@@ -665,8 +749,15 @@ def grad_clip_workspace_bytes(tensors) -> int:
 
 def grad_clip(tensors, max_grad_norm, stats, ws, stream=None):
     """tensors: grad_tensors(...)."""
-    _check("grad_clip", lib.grad_clip(tensors, tensors.used, max_grad_norm, ptr(stats), *_ws_args(ws),
-                                      stream_handle(stream)))
+    if len(tensors.devices) > 1 or -1 in tensors.devices:
+        raise ValueError("grad_clip: the tensors have to be on one GPU")
+    n = max(2, stats.numel()) if isinstance(stats, torch.Tensor) else 2
+    p, at = _pointers("grad_clip", (("stats", (n,), (1,), torch.float32),), (stats,), ws)
+    device = next(iter(tensors.devices), at)
+    if at is not None and at != device:
+        raise ValueError("grad_clip: the tensors have to be on one GPU")
+    _check("grad_clip", lib.grad_clip(tensors, tensors.used, max_grad_norm, *p, *_ws_args(ws),
+                                      _stream_of("grad_clip", stream, device)))
 
 
 def impala_gumbel_sample(n, A, logits, gumbel, actions, logp, stream=None):
