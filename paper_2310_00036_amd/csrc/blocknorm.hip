@@ -518,6 +518,7 @@ hipError_t blocknorm_bwd(int prec, BnArgs a, void* ws, hipStream_t s) {
     const hipError_t e = bn_run(prec, a, p, true, s);
     if (e != hipSuccess) return e;
     const int nq = two ? 5 : 3;
+    ProfScope ps(s, [&] { return "blocknorm_params/" + std::to_string(p.blocks) + "x" + cb_dims(a.C, nq); });
     hipLaunchKernelGGL(bn_cols_kernel, dim3(unsigned((a.C + 31) / 32), unsigned(nq)), dim3(1024), 0, s, a, int(p.blocks), nq);
     return hipGetLastError();
 }

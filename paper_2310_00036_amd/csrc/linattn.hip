@@ -860,6 +860,7 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
             const int64_t n = int64_t(a.E) * a.H * P.dk * P.dv;
             if (!P.x1 || P.x1 == P.x0) continue;
             const int64_t blocks = std::min<int64_t>((n + 255) / 256, 4096);
+            ProfScope ps(s, [&] { return "linattn_state/" + std::to_string(n); });
             hipLaunchKernelGGL(la_empty_kernel, dim3(unsigned(blocks)), dim3(256), 0, s, P.x0, P.x1, n);
         }
         return hipGetLastError();
