@@ -110,7 +110,8 @@ CB_DEV void gc_pieces(const GcEntry& e, int64_t at, int n, F&& f) {
     }
 }
 
-CB_DEV void gc_store8(const GcEntry& e, int64_t i, int left, const float* x) {
+// `bits`: what came from bf16 goes there as it came (a conversion would make signalling NaN quiet).
+CB_DEV void gc_store8(const GcEntry& e, int64_t i, int left, const float* x, bool bits) {
     if (e.type & 2) {
         float* p = static_cast<float*>(e.dst) + i;
         if (left >= 8) {
@@ -129,12 +130,14 @@ CB_DEV void gc_store8(const GcEntry& e, int64_t i, int left, const float* x) {
         if (left >= 8) {
             gc_u32x4 a;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) a[u] = pack2bf(x[2 * u], x[2 * u + 1]);
+            for (int u = 0; u < 4; ++u)
+                a[u] = bits ? __float_as_uint(x[2 * u]) >> 16 | (__float_as_uint(x[2 * u + 1]) & 0xffff0000u)
+                            : pack2bf(x[2 * u], x[2 * u + 1]);
             *reinterpret_cast<gc_u32x4*>(p) = a;
         } else {
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-                if (u < left) p[u] = f2bf(x[u]);
+                if (u < left) p[u] = bits ? uint16_t(__float_as_uint(x[u]) >> 16) : f2bf(x[u]);
         }
     }
 }
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(256) void gc_scale_kernel(GcTable t, const double* 
             if (clip)
 #pragma unroll
                 for (int u = 0; u < 8; ++u) x[u] *= f;
-            gc_store8(e, i, left, x);
+            gc_store8(e, i, left, x, !clip && !(e.type & 1));
         };
         e.type & 1 ? gc_pieces<true>(e, at, n, put) : gc_pieces<false>(e, at, n, put);
     });

@@ -1,0 +1,35 @@
+"""Gradients that are not clipped reach their targets bit for bit where the types are the same, NaN of any kind included."""
+import pytest
+import torch
+
+P = pytest.importorskip("paper_2310_00036_amd")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def run(pairs, limit):
+    t = P.grad_tensors(pairs)
+    stats = torch.zeros(2, device=DEV)
+    P.grad_clip(t, limit, stats, torch.empty(P.grad_clip_workspace_bytes(t), dtype=torch.uint8, device=DEV))
+    return stats.cpu().tolist()
+
+
+@pytest.mark.parametrize("limit", [0.0, 0.5])
+@pytest.mark.parametrize("n", [5, 65536, 65536 + 3])
+def test_bf16(n, limit):
+    bits = torch.arange(n, dtype=torch.int32).to(torch.int16).to(DEV)   # all of bf16, quiet and signalling NaN among them
+    src = bits.view(torch.bfloat16)
+    if n < 65536:
+        bits[:] = torch.tensor([0x7f81, 0x7fc1, -0x7f, 1, -0x8000 + 1], dtype=torch.int16)
+    for off in (0, 1):
+        dst = torch.zeros(n + off, dtype=torch.bfloat16, device=DEV)[off:]
+        assert run([(src, dst)], limit)[1] == 1      # its norm is NaN: nothing is clipped
+        assert torch.equal(dst.view(torch.int16), bits)
+
+
+@pytest.mark.parametrize("limit", [0.0, 0.5])
+def test_float32(limit):
+    bits = torch.tensor([0x7f800001, 0x7fc00001, 0x7fffffff, 1, 0x3f800000, 0x7f800000], dtype=torch.int32).repeat(700).to(DEV)
+    dst = torch.zeros(4200, device=DEV)
+    assert run([(bits.view(torch.float32), dst)], limit)[1] == 1
+    assert torch.equal(dst.view(torch.int32), bits)
