@@ -174,8 +174,9 @@ __global__ __launch_bounds__(256) void gc_scale_kernel(GcTable t, const double* 
     __shared__ double sh[256];
     const double norm = sqrt(gc_total(part, nparts, sh));
     if (stats && blockIdx.x == 0 && threadIdx.x == 0) {
-        stats[0] = float(norm);
-        stats[1] = isfinite(norm) ? 0.f : 1.f;
+        const float n = float(norm);
+        stats[0] = n;
+        stats[1] = isfinite(n) ? 0.f : 1.f;   // also where the norm is beyond float32
     }
     const bool clip = max_norm > 0.f && norm > double(max_norm);
     const float f = clip ? float(double(max_norm) / norm) : 1.f;

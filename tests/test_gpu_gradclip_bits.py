@@ -33,3 +33,13 @@ def test_float32(limit):
     dst = torch.zeros(4200, device=DEV)
     assert run([(bits.view(torch.float32), dst)], limit)[1] == 1
     assert torch.equal(dst.view(torch.int32), bits)
+
+
+def test_a_norm_beyond_float32():
+    """The flag is of the norm as it is reported; the values are clipped by the 64-bit one."""
+    src = torch.full((9,), 3e38, device=DEV)
+    dst = torch.empty_like(src)
+    assert run([(src, dst)], 0.5) == [float("inf"), 1]
+    # the factor 0.5 / 9e38 is off by half of 2^-149 (1.26e-6 of it), the product by 2^-24
+    assert ((dst.double() * 6 - 1).abs() < 1.4e-6).all()
+    assert run([(src[:1], dst[:1])], 0.5)[1] == 0
