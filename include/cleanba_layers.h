@@ -198,8 +198,7 @@ impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, i
  * (-infinity: no memory; above 0 the state grows). dones: uint8 with strides done_t, done_e, or NULL (no
  * episode starts). States: float32 [E, heads, dk, dv], row-major, in both precisions. 1 <= dk, dv <= 128,
  * E * heads <= 2^21 and T <= 2^30 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element
- * (sizes, strides and addresses of whole 4 bytes, and steps less than 2^24 bytes apart, are read 16 bytes at a
- * time, others element by element).
+ * (odd bf16 sizes, strides or addresses take up to 1.6 times as long).
  * Outputs must not have two elements in one place, and must not overlap inputs or each other. Two arrays
  * may lie between each other's rows, as the parts of one buffer do; an axis on which their strides differ
  * (the heads, where dk is not dv) counts with all that it spans. Any other overlap of their address ranges

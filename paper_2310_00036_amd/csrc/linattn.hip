@@ -129,6 +129,9 @@ hipError_t la_step(const LaArgs& a, hipStream_t s) {
 
 constexpr int kL = 64;
 typedef uint32_t cb_u32x2 __attribute__((ext_vector_type(2)));
+// words at any alignment of an element, which global memory takes
+typedef uint32_t la_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t la_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 
 // bf16: products of two bf16 numbers are exact; what is no bf16 number (the decayed products, X, the decayed v) goes into
 // a product as three of them, each nearest to what the ones before leave: 24 bits, as float32 has. (Two for the decayed
@@ -198,6 +201,9 @@ struct LaB {
         __builtin_amdgcn_raw_buffer_store_b16(f2bf(x), r, off, 0, 0);
     }
     static CB_DEV T store(float x) { return f2bf(x); }
+    static CB_DEV void store4(T* p, cb_f32x4 x) {
+        *reinterpret_cast<la_u32x2*>(p) = la_u32x2{pack2bf(x[0], x[1]), pack2bf(x[2], x[3])};
+    }
 };
 
 struct LaF {
@@ -243,6 +249,7 @@ struct LaF {
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, off, 0, 0);
     }
     static CB_DEV T store(float x) { return x; }
+    static CB_DEV void store4(T* p, cb_f32x4 x) { *reinterpret_cast<cb_f32x4_a4*>(p) = x; }
 };
 
 // Where a pass is cut along the rollout, each segment's own contribution to the state, then the states before them.
@@ -274,6 +281,11 @@ struct LaTile {   // STATE: without q and the products
 // Rows of one array through a buffer resource that is moved from chunk to chunk, at 32-bit offsets: what lies behind the
 // chunk's last row, or in columns behind the array's, reads zero and is not written. A row steps by st bytes; going back,
 // st is negative and the resource starts at the chunk's last row, so offsets have -(n - 1) st added.
+// With |st| <= 2^25 a resource ends below 2^31 = kOOB, and no offset comes round into it modulo 2^32: rows go to 127 (threads
+// without a row in a chunk of 32-wide bf16 heads among 8 waves), so going forward offsets stay below 127 2^25 + 2^9 < 2^32, and
+// going back that of a row r >= n is 2^32 - (r - n + 1) |st| or more, which is n |st| or more, behind (n - 1) |st| + bytes;
+// in columns behind the array's, rows go to 63: kOOB +- 63 |st| lies within 2^25 and 2^32.
+constexpr int64_t kLaReach = int64_t(1) << 25;
 struct LaRows {
     const char* p;             // the chunk's first row
     int st, bytes;             // bytes: of a row
@@ -285,7 +297,7 @@ struct LaRows {
                         __builtin_amdgcn_readfirstlane(abs(span) + bytes));
     }
     CB_DEV uint32_t first(int n) const { return uint32_t(max(0, -(n - 1) * st)); }
-    CB_DEV uint32_t at(int row, int byte) const { return byte >= bytes ? kOOB : uint32_t(row * st + byte); }
+    CB_DEV uint32_t at(int row, int byte) const { return byte >= bytes ? kOOB : uint32_t(row) * uint32_t(st) + byte; }
     CB_DEV void next() { p += int64_t(kL) * st; }
 };
 
@@ -301,10 +313,15 @@ CB_DEV uint4 la_cut(uint4 v, int left) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The same piece element by element, where the array's alignment or strides allow no more.
+// The same piece by its address, where the array's alignment or strides do not suit a buffer resource. The row's last piece
+// goes element by element.
 template <class T>
 CB_DEV uint4 la_gather(const T* p, int left) {
     constexpr int VE = 16 / sizeof(T);
+    if (left >= VE) {
+        const la_u32x4 w = *reinterpret_cast<const la_u32x4*>(p);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
     T x[VE];
 #pragma unroll
     for (int i = 0; i < VE; ++i) x[i] = i < left ? p[i] : T(0);
@@ -397,7 +414,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
     static_assert(RQ * CQ == 64 * NW && RV * CV == 64 * NW, "a thread's pieces lie in one column");
     const int rowq = tid / CQ, colq = tid % CQ * 16, rowv = tid / CV, colv = tid % CV * 16;
     const uint32_t atq = q.at(rowq, colq), atk = k.at(rowq, colq), atv = v.at(rowv, nb0 * L::ES + colv);
-    auto fetch = [&](int n) CB_INLINE_LAMBDA {
+    auto fetch = [&](int n, int p) CB_INLINE_LAMBDA {   // rows p .. p + n - 1
         if (FAST) {
             const auto bq = q.rsrc(n), bk = k.rsrc(n), bv = v.rsrc(n);
 #pragma unroll
@@ -407,14 +424,27 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
             }
 #pragma unroll
             for (int u = 0; u < L::UV; ++u) rv[u] = buf_load16(bv, atv + (v.first(n) + u * RV * v.st));
+        } else {
+            auto piece = [&](const LaView& x, int row, int col, int d) {
+                const T* r = static_cast<const T*>(x.p) + e * x.e + h * x.h + (t0 + dir * (p - p0 + row)) * x.t + col;
+                return la_gather<T>(r, row < n ? d - col : 0);
+            };
+#pragma unroll
+            for (int u = 0; u < L::UQ; ++u) {
+                if (!STATE) rq[u] = piece(P.q, rowq + RQ * u, colq / L::ES, dk);
+                rk[u] = piece(P.k, rowq + RQ * u, colq / L::ES, dk);
+            }
+#pragma unroll
+            for (int u = 0; u < L::UV; ++u) rv[u] = piece(P.v, rowv + RV * u, nb0 + colv / L::ES, dv);
+            if (wave == 0) rd = a.dones && lane < n ? a.dones[e * a.d_e + (t0 + dir * (p - p0 + lane)) * a.d_t] : 0;
         }
         // (Kept as it is loaded: a comparison here would wait for it and all loads before it.)
         if (FAST && wave == 0) rd = __builtin_amdgcn_raw_buffer_load_b8(dn.rsrc(n), uint32_t(lane * dn.st) + dn.first(n), 0, 0);
     };
-    const bool tail = vec & 2;
+    const bool tail = FAST && (vec & 2);
     const uint32_t ato = o.at(c, (n0 + 4 * g) * L::ES);
     const bool busy = n0 < dv;   // a wave behind the last column only moves rows and forms products
-    fetch(min(kL, p1 - p0));
+    fetch(min(kL, p1 - p0), p0);
 
     // X's numbers in a state: results m, rows krow(m, g, r), column n0 + c; what the state has not is zero, and not written.
     cb_f32x4 X[NT];
@@ -471,44 +501,28 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
     float factor = 1.f;
     for (int p = p0; p < p1; p += kL) {
         const int n = min(kL, p1 - p);
-        if (FAST) {
 #pragma unroll
-            for (int u = 0; u < L::UQ; ++u) {
-                if (__builtin_expect(tail, 0)) {
-                    const int left = dk - la_here(colq) / L::ES;
-                    rq[u] = la_cut<T>(rq[u], left);
-                    rk[u] = la_cut<T>(rk[u], left);
-                }
-                if (rowq + RQ * u < kL) {
-                    if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + (rowq + RQ * u) * L::RSK + colq) = rq[u];
-                    *reinterpret_cast<uint4*>(lds + L::K + (rowq + RQ * u) * L::RSK + colq) = rk[u];
-                }
+        for (int u = 0; u < L::UQ; ++u) {
+            if (__builtin_expect(tail, 0)) {
+                const int left = dk - la_here(colq) / L::ES;
+                rq[u] = la_cut<T>(rq[u], left);
+                rk[u] = la_cut<T>(rk[u], left);
             }
+            if (rowq + RQ * u < kL) {
+                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + (rowq + RQ * u) * L::RSK + colq) = rq[u];
+                *reinterpret_cast<uint4*>(lds + L::K + (rowq + RQ * u) * L::RSK + colq) = rk[u];
+            }
+        }
 #pragma unroll
-            for (int u = 0; u < L::UV; ++u) {
-                if (__builtin_expect(tail, 0)) rv[u] = la_cut<T>(rv[u], dv - nb0 - la_here(colv) / L::ES);
-                *reinterpret_cast<uint4*>(lds + L::V + (rowv + RV * u) * L::RSV + colv) = rv[u];
-            }
-        } else {
-            auto piece = [&](const LaView& x, int row, int col, int d) {
-                const T* r = static_cast<const T*>(x.p) + e * x.e + h * x.h + (t0 + dir * (p - p0 + row)) * x.t + col;
-                return la_gather<T>(r, row < n ? d - col : 0);
-            };
-#pragma unroll 1
-            for (int row = rowq; row < kL; row += RQ) {
-                if (!STATE) *reinterpret_cast<uint4*>(lds + L::Q + row * L::RSK + colq) = piece(P.q, row, colq / L::ES, dk);
-                *reinterpret_cast<uint4*>(lds + L::K + row * L::RSK + colq) = piece(P.k, row, colq / L::ES, dk);
-            }
-#pragma unroll 1
-            for (int row = rowv; row < kL; row += RV)
-                *reinterpret_cast<uint4*>(lds + L::V + row * L::RSV + colv) = piece(P.v, row, nb0 + colv / L::ES, dv);
+        for (int u = 0; u < L::UV; ++u) {
+            if (__builtin_expect(tail, 0)) rv[u] = la_cut<T>(rv[u], dv - nb0 - la_here(colv) / L::ES);
+            *reinterpret_cast<uint4*>(lds + L::V + (rowv + RV * u) * L::RSV + colv) = rv[u];
         }
         // episode starts before what row i holds, of the chunk's starts m
         auto count_in = [&](uint64_t m, int i) {
             return __popcll(back ? m & ((uint64_t(1) << i) - 1) : m & (~uint64_t(0) >> (63 - i)));
         };
         if (wave == 0) {
-            if (!FAST) rd = a.dones && lane < n ? a.dones[e * a.d_e + (t0 + dir * (p - p0 + lane)) * a.d_t] : 0;
             const uint64_t m = __ballot(rd != 0 && lane < n);
             const int ci = count_in(m, lane);
             xw[lane] = ci == 0 ? pw[lane + later] * out : 0.f;
@@ -525,7 +539,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
         if (STATE) factor = total || factor < 0.f ? -1.f : factor * over;
         q.next(); k.next(); v.next(); dn.next();
         if (p > p0) o.next();   // the chunk at hand's, to be written at its end
-        if (p + kL < p1) fetch(min(kL, p1 - p - kL));
+        if (p + kL < p1) fetch(min(kL, p1 - p - kL), p + kL);
 
         if (!STATE) {   // in out g^(i-j) q_i . k_j by tiles on and below the diagonal, a wave's few at once
             constexpr int MT = (10 + NW - 1) / NW;
@@ -732,6 +746,10 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
                     if (i >= n) continue;
                     T* po = static_cast<T*>(const_cast<void*>(P.o.p)) + e * P.o.e + h * P.o.h +
                             (t0 + dir * (p - p0 + i)) * P.o.t;
+                    if (col + 4 <= dv) {
+                        Tr::store4(po + col, O[b]);
+                        continue;
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (col + r < dv) po[col + r] = Tr::store(O[b][r]);
@@ -872,11 +890,13 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     if (a.T == 1 && a.np == 1) return prec == 0 ? la_step<PrecBF16>(a, s) : la_step<PrecF32>(a, s);
     const int es = prec == 0 ? 2 : 4, ve = 16 / es;
     // Rows that a buffer resource reaches: of whole words (it ends with the last row's last one), each behind the last
-    // one's end, 64 of them within 2^30 bytes.
+    // one's end, not too far apart. (Others go by their addresses: 128 x 1024 envs x 8 heads of 64, bf16, in rows of 50 MB forward
+    // 213 us, contiguous 211. 33- and 71-wide ones, 128 x 512 x 8 heads: 287,
+    // backward 812, 34- and 70-wide ones 241 and 522.)
     auto reach = [&](const LaView& v, int d) {
         const int k = 4 / es;
         return reinterpret_cast<uintptr_t>(v.p) % 4 == 0 && d % k == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && v.t >= d &&
-               v.t < (int64_t(1) << 30) / kL / es;
+               v.t * es <= kLaReach;
     };
     LaSegs sg{};
     const int64_t EH = int64_t(a.E) * a.H;
@@ -886,7 +906,7 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     for (int y = 0; y < a.np; ++y) {
         LaPass& P = a.pass[y];
         P.vec = (P.dv % 4 == 0) | (P.dk % ve != 0 || P.dv % ve != 0) << 1 |
-                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv) && reach(P.o, P.dv) && a.d_t < (int64_t(1) << 24)) << 2;
+                (reach(P.q, P.dk) && reach(P.k, P.dk) && reach(P.v, P.dv) && reach(P.o, P.dv) && a.d_t <= kLaReach) << 2;
         if (sg.segs == 1) continue;
         sg.state[y] = reinterpret_cast<float*>(w);
         w += la_a256(sg.segs * EH * P.dk * P.dv * 4);

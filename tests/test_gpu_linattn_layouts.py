@@ -42,3 +42,39 @@ def test_one_buffer_of_parts_with_other_widths(T, E, H, dk, dv, ty):
             at += H * w
         same_bits(x, part, 0.5, want, grads)
         assert (buf[..., row:] == 7).all()
+
+
+# Steps of a rollout's rows in bytes: buffer resources reach 2^25, rows further apart go by their addresses.
+STEPS = [2 ** 24 - 8, 2 ** 24, 2 ** 25, 2 ** 25 + 4, 2 ** 25 + 2]
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("T,dk,dv", [(65, 32, 128), (130, 64, 64), (3, 128, 31)])
+def test_steps_far_apart(T, dk, dv, ty):
+    E, H, es = 2, 2, 2 if ty == "bf16" else 4
+    x = make(T, E, H, dk, dv, ty, "few", seed=T)
+    want, grads = forward(x, 0.5), backward(x, 0.5)
+    flat = torch.empty((T - 1) * (STEPS[-2] // es) + 8192, dtype=TYPES[ty], device=DEV)
+    for step in STEPS:
+        if step % es:
+            continue
+        part = {}
+        for i, (n, d) in enumerate((("q", dk), ("k", dk), ("v", dv), ("do", dv), ("o", dv), ("dq", dk), ("dk", dk), ("dv", dv))):
+            part[n] = flat.as_strided((T, E, H, d), (step // es, H * d, d, 1), 1024 * i)
+        same_bits(x, part, 0.5, want, grads)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [1, 5, 33, 71, 127])
+def test_rows_at_any_address(d, ty):
+    """Odd widths side by side, each row at its own alignment; what lies between stays."""
+    T, E, H = 70, 2, 3
+    x = make(T, E, H, d, d, ty, "few", seed=d)
+    want, grads = forward(x, 0.5), backward(x, 0.5)
+    row = 8 * H * (d + 1) + 1
+    buf = torch.full((T, E, row), 7.0, dtype=TYPES[ty], device=DEV)
+    part = {n: buf[..., i * H * (d + 1):(i + 1) * H * (d + 1)].unflatten(-1, (H, d + 1))[..., :d]
+            for i, n in enumerate(("q", "dq", "k", "dk", "v", "dv", "do", "o"))}
+    same_bits(x, part, 0.5, want, grads)
+    gaps = buf[..., :-1].unflatten(-1, (8 * H, d + 1))[..., d]
+    assert (gaps == 7).all() and (buf[..., -1] == 7).all()
