@@ -890,13 +890,12 @@ hipError_t linattn(int prec, LaArgs a, void* ws, hipStream_t s) {
     if (a.T == 1 && a.np == 1) return prec == 0 ? la_step<PrecBF16>(a, s) : la_step<PrecF32>(a, s);
     const int es = prec == 0 ? 2 : 4, ve = 16 / es;
     // Rows that a buffer resource reaches: of whole words (it ends with the last row's last one), each behind the last
-    // one's end, not too far apart. (Others go by their addresses: 128 x 1024 envs x 8 heads of 64, bf16, in rows of 50 MB forward
-    // 213 us, contiguous 211. 33- and 71-wide ones, 128 x 512 x 8 heads: 287,
-    // backward 812, 34- and 70-wide ones 241 and 522.)
+    // one's end, not too far apart. (Others go by their addresses: 128 x 1024 envs x 8 heads of 64, bf16, in rows of 50 MB
+    // forward 213 us, contiguous 211; 128 x 512 x 8 heads of 33 x 71 forward 287, backward 812, of 34 x 70 241 and 522.)
     auto reach = [&](const LaView& v, int d) {
         const int k = 4 / es;
         return reinterpret_cast<uintptr_t>(v.p) % 4 == 0 && d % k == 0 && v.t % k == 0 && v.e % k == 0 && v.h % k == 0 && v.t >= d &&
-               v.t * es <= kLaReach;
+               v.t <= kLaReach / es;
     };
     LaSegs sg{};
     const int64_t EH = int64_t(a.E) * a.H;

@@ -78,3 +78,22 @@ def test_rows_at_any_address(d, ty):
     same_bits(x, part, 0.5, want, grads)
     gaps = buf[..., :-1].unflatten(-1, (8 * H, d + 1))[..., d]
     assert (gaps == 7).all() and (buf[..., -1] == 7).all()
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+def test_the_step_stride_of_one_step_is_not_used(ty):
+    """Axes of one element have no stride: whatever it says, also where its bytes would come round in 64 bits."""
+    x = make(1, 3, 2, 16, 8, ty, "few")
+    want, grads = forward(x, 0.5), backward(x, 0.5)
+    q, k, v, do, a, d, s0, ds = (dev(x[n]) for n in ("q", "k", "v", "do", "a", "d", "s0", "ds"))
+    for step in (0, -1, 1 << 62, (1 << 62) + 16, -(1 << 63)):
+        o, dq, dk, dv = (torch.empty_like(t) for t in (v, q, k, v))
+        s_out, ds0 = torch.empty_like(s0), torch.empty_like(s0)
+        shape = P.linattn_shape(q, k, v, o, d, 0.5, dq, dk, dv)
+        for n in ("q", "k", "v", "o", "gq", "gk", "gv"):
+            getattr(shape, n).t = step
+        shape.done_t = step
+        P.impala_linattn_fwd(shape, q, k, v, a, d, s0, o, s_out)
+        P.impala_linattn_bwd(shape, do, q, k, v, a, d, s0, ds, dq, dk, dv, ds0)
+        assert torch.equal(o, want[0]) and torch.equal(s_out, want[1]), step
+        assert all(torch.equal(g, w) for g, w in zip((dq, dk, dv, ds0), grads)), step
