@@ -195,7 +195,8 @@ impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, i
  * q, k: [T, E, heads, dk] and v, o: [T, E, heads, dv] in the storage type, the last axis contiguous, the
  * others by strides in elements (>= 0; a broadcast axis has stride 0), so they may be parts of one
  * projection's output, an env block of a larger rollout, or [E, T, ...]. log_decay: float [heads], <= 0
- * (-infinity: no memory; above 0 the state grows). dones: uint8 with strides done_t, done_e, or NULL (no
+ * (-infinity: no memory; above 0 the state grows, and over rollouts g^64 has to be a float32 number: at most
+ * 1.38). What is infinite or overflows leaves the outputs that it reaches infinite or NaN. dones: uint8 with strides done_t, done_e, or NULL (no
  * episode starts). States: float32 [E, heads, dk, dv], row-major, in both precisions. 1 <= dk, dv <= 128,
  * E * heads <= 2^21 and T <= 2^30 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element
  * (odd bf16 sizes, strides or addresses take up to 1.6 times as long).
