@@ -196,10 +196,10 @@ impala_status_t impala_groupnorm_bwd(impala_prec_t prec, int64_t n, int32_t H, i
  * others by strides in elements (>= 0; a broadcast axis has stride 0), so they may be parts of one
  * projection's output, an env block of a larger rollout, or [E, T, ...]. log_decay: float [heads], <= 0
  * (-infinity: no memory; above 0 the state grows, and over rollouts g^64 has to be a float32 number: at most
- * 1.38). What is infinite or overflows leaves the outputs that it reaches infinite or NaN. dones: uint8 with strides done_t, done_e, or NULL (no
- * episode starts). States: float32 [E, heads, dk, dv], row-major, in both precisions. 1 <= dk, dv <= 128,
- * E * heads <= 2^21 and T <= 2^30 (more: IMPALA_EUNSUPPORTED); T, E >= 0. Addresses aligned to an element
- * (odd bf16 sizes, strides or addresses take up to 1.6 times as long).
+ * 1.38). What is infinite or overflows leaves the outputs that it reaches infinite or NaN. dones: uint8 with
+ * strides done_t, done_e, or NULL (no episode starts). States: float32 [E, heads, dk, dv], row-major, in both
+ * precisions. 1 <= dk, dv <= 128, E * heads <= 2^21 and T <= 2^30 (more: IMPALA_EUNSUPPORTED); T, E >= 0.
+ * Addresses aligned to an element (odd bf16 sizes, strides or addresses take up to 1.6 times as long).
  * Outputs must not have two elements in one place, and must not overlap inputs or each other. Two arrays
  * may lie between each other's rows, as the parts of one buffer do; an axis on which their strides differ
  * (the heads, where dk is not dv) counts with all that it spans. Any other overlap of their address ranges

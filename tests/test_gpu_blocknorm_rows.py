@@ -65,3 +65,35 @@ def test_eps_of_zero(n, C, groups, ty):
         if groups > 1:
             x["dout2"] = None
         check(x, ty, groups, kinds, 0.0, forward(x, ty, groups, kinds, 0.0, groups == 1), backward(x, ty, groups, kinds, 0.0))
+
+
+# Workgroups are at most 1024 forward and 512 backward: here each goes round several times, some without a last row.
+MANY = [(9001, 256, 1), (2100, 1531, 1), (1100, 4100, 1), (90001, 24, 3), (3000, 2048, 2)]
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("n,C,groups", MANY)
+def test_more_rows_than_places(n, C, groups, ty):
+    for i, kinds in enumerate(KINDS[:2]):
+        x = make(n, C, ty, seed=i)
+        if groups > 1:
+            x["dout2"] = None
+        check(x, ty, groups, kinds, 1e-5, forward(x, ty, groups, kinds, 1e-5, groups == 1), backward(x, ty, groups, kinds, 1e-5))
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("n,C,groups", MANY)
+def test_more_rows_than_places_in_place(n, C, groups, ty):
+    """An output on an input, the next rows of which may be on their way: the bits of outputs of their own."""
+    kinds, two = KINDS[0], groups == 1
+    x = make(n, C, ty, seed=7)
+    if not two:
+        x["dout2"] = None
+    want, grads = forward(x, ty, groups, kinds, 1e-5, two), backward(x, ty, groups, kinds, 1e-5)
+    for over in (("h", "gate"), ("res", "h"), ("gate", "res")):
+        got = forward(x, ty, groups, kinds, 1e-5, two, over)
+        assert torch.equal(got[0], want[0]) and (not two or torch.equal(got[1], want[1])), over
+    for over in (dict(dh="h", dgate="gate", dres="dout"), dict(dh="gate", dgate="dout", dres="h"),
+                 dict(dh="out", dgate="h", dres="gate") if two else dict(dh="dout")):
+        got = backward(x, ty, groups, kinds, 1e-5, over)
+        assert all(torch.equal(got[k], g) for k, g in grads.items() if g is not None), over
