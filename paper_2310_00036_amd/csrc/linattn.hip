@@ -385,11 +385,10 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
     const LaPass& P = a.pass[y];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const uint32_t nbs = (P.dv + 16 * NW - 1) / (16 * NW), EH = uint32_t(a.E) * a.H;   // EH <= 2^21
-    const uint32_t id = nbs > 1 ? quot(bid, nbs) : bid;
-    const int nb0 = int(bid - id * nbs) * 16 * NW, n0 = nb0 + 16 * wave;   // columns of the workgroup, of the wave
-    const int seg = sg.segs > 1 ? int(quot(id, EH)) : 0;
-    const uint32_t eh32 = id - seg * EH, e32 = quot(eh32, a.H);
+    const uint32_t EH = uint32_t(a.E) * a.H;   // <= 2^21
+    const int n0 = 16 * wave;                  // the wave's columns; the workgroup has all
+    const int seg = sg.segs > 1 ? int(quot(bid, EH)) : 0;
+    const uint32_t eh32 = bid - seg * EH, e32 = quot(eh32, a.H);
     const int64_t eh = eh32, e = e32, h = eh32 - e32 * a.H;
     const int p0 = seg * sg.chunks * kL;
     const int p1 = sg.segs == 1 ? a.T : int(min(int64_t(a.T), int64_t(p0) + int64_t(sg.chunks) * kL));
@@ -413,7 +412,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
     constexpr int RQ = 64 * NW / CQ, RV = 64 * NW / CV;   // rows from one of a thread's pieces to the next
     static_assert(RQ * CQ == 64 * NW && RV * CV == 64 * NW, "a thread's pieces lie in one column");
     const int rowq = tid / CQ, colq = tid % CQ * 16, rowv = tid / CV, colv = tid % CV * 16;
-    const uint32_t atq = q.at(rowq, colq), atk = k.at(rowq, colq), atv = v.at(rowv, nb0 * L::ES + colv);
+    const uint32_t atq = q.at(rowq, colq), atk = k.at(rowq, colq), atv = v.at(rowv, colv);
     auto fetch = [&](int n, int p) CB_INLINE_LAMBDA {   // rows p .. p + n - 1
         if (FAST) {
             const auto bq = q.rsrc(n), bk = k.rsrc(n), bv = v.rsrc(n);
@@ -435,7 +434,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
                 rk[u] = piece(P.k, rowq + RQ * u, colq / L::ES, dk);
             }
 #pragma unroll
-            for (int u = 0; u < L::UV; ++u) rv[u] = piece(P.v, rowv + RV * u, nb0 + colv / L::ES, dv);
+            for (int u = 0; u < L::UV; ++u) rv[u] = piece(P.v, rowv + RV * u, colv / L::ES, dv);
             if (wave == 0) rd = a.dones && lane < n ? a.dones[e * a.d_e + (t0 + dir * (p - p0 + lane)) * a.d_t] : 0;
         }
         // (Kept as it is loaded: a comparison here would wait for it and all loads before it.)
@@ -515,7 +514,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
         }
 #pragma unroll
         for (int u = 0; u < L::UV; ++u) {
-            if (__builtin_expect(tail, 0)) rv[u] = la_cut<T>(rv[u], dv - nb0 - la_here(colv) / L::ES);
+            if (__builtin_expect(tail, 0)) rv[u] = la_cut<T>(rv[u], dv - la_here(colv) / L::ES);
             *reinterpret_cast<uint4*>(lds + L::V + (rowv + RV * u) * L::RSV + colv) = rv[u];
         }
         // episode starts before what row i holds, of the chunk's starts m
@@ -768,7 +767,7 @@ __global__ __launch_bounds__(64 * NW, (la_simd_waves<Tr, DK, STATE>)) void la_ch
             for (int r = 0; r < 4; ++r)
                 __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(X[m][r]), bx, xat(Tr::krow(m, g, r), xk, xn), 0, 0);
     }
-    if (STATE && tid == 0 && nb0 == 0) sg.factor[y][int64_t(seg) * EH + eh] = factor;
+    if (STATE && tid == 0) sg.factor[y][int64_t(seg) * EH + eh] = factor;
 }
 
 // The states before the segments, in place of their contributions.
@@ -791,8 +790,8 @@ __global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, LaSegs sg) {
 
 template <class Tr, int DK, int NW>
 hipError_t la_chunks_launch(const LaArgs& a, const LaSegs& sg, int y0, int ny, bool state, hipStream_t s) {
-    const int64_t nbs = (a.pass[y0].dv + 16 * NW - 1) / (16 * NW);
-    const int blocks = int(int64_t(a.E) * a.H * nbs * (state ? sg.segs - 1 : sg.segs));
+    // A workgroup has a state of its own, all columns (16 NW >= dv, by la_waves), so a state may go through in place.
+    const int blocks = int(int64_t(a.E) * a.H * (state ? sg.segs - 1 : sg.segs));
     const dim3 grid(unsigned((blocks + 7) / 8 * 8 * ny));
     bool fast = true;
     for (int y = y0; y < y0 + ny; ++y) fast &= a.pass[y].vec >> 2 & 1;
