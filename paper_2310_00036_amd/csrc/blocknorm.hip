@@ -143,10 +143,14 @@ CB_DEV float bn_sigmoid(float x) {
     return fmaf(fmaf(-d, r, 1.f), r, r);
 }
 
-// 1 / sqrt(v), v >= 0, with one Newton step (none from 0 or infinity, where it would make NaN).
+// 1 / sqrt(v), v >= 0, with one Newton step (none from 0 or infinity, where it would make NaN). The instruction takes
+// denormal numbers, which are squares of rows about 1e-19, for zero: small numbers are scaled to it and back.
 CB_DEV float bn_rsqrt(float v) {
+    const bool small = v < 0x1p-100f;
+    v = small ? v * 0x1p100f : v;
     const float r = __builtin_amdgcn_rsqf(v);
-    return r > 0.f && r < INFINITY ? fmaf(r * 0.5f, fmaf(-v * r, r, 1.f), r) : r;
+    const float y = r > 0.f && r < INFINITY ? fmaf(r * 0.5f, fmaf(-v * r, r, 1.f), r) : r;
+    return small ? y * 0x1p50f : y;
 }
 
 // The columns that are the row's own: x, or zero.

@@ -97,3 +97,29 @@ def test_more_rows_than_places_in_place(n, C, groups, ty):
                  dict(dh="out", dgate="h", dres="gate") if two else dict(dh="dout")):
         got = backward(x, ty, groups, kinds, 1e-5, over)
         assert all(torch.equal(got[k], g) for k, g in grads.items() if g is not None), over
+
+
+@pytest.mark.parametrize("size", [1e-17, 1e-18, 3e-19, 1e-19, 3e-20, 1e-20])
+def test_rows_whose_squares_are_denormal(size):
+    """eps = 0 and float32 rows down to 1e-20. A square and the sum it goes into are off by half of 2^-149 each, the mean by
+    as much again, so the mean square ms is off by at most 3 2^-150 and its root by 1.5 2^-150 / ms of itself."""
+    n, C = 9, 200
+    x = make(n, C, "f32")
+    h = (torch.randn(n, C, generator=torch.Generator().manual_seed(1)) * size)
+    d = h.double()
+    ms = d.square().mean(-1, keepdim=True)
+    rel = TERMS * 2.0 ** -24 + 1.5 * 2.0 ** -150 / ms
+    assert rel.max() < 1e-4
+    s = P.blocknorm_shape(P.PREC_FP32, n, C, norm=P.NORM_RMS, eps=0.0)
+    out = torch.empty(n, C, device=DEV)
+    P.impala_blocknorm_fwd(s, dev(h), None, None, None, None, None, out)
+    want = d / ms.sqrt()
+    assert ((out.double().cpu() - want).abs() <= rel * want.abs()).all()
+    # dh = r (g - xh <g xh>): r and each xh off by rel, in up to four places a term
+    g = x["dout"]
+    dh, ws = torch.empty_like(out), torch.empty(P.impala_blocknorm_bwd_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    P.impala_blocknorm_bwd(s, dev(g), None, dev(h), None, None, None, None, None, None, dh, *[None] * 7, ws)
+    g, r = g.double(), 1 / ms.sqrt()
+    want_dh = r * (g - want * (g * want).mean(-1, keepdim=True))
+    mag = r * (g.abs() + want.abs() * (g * want).abs().mean(-1, keepdim=True))
+    assert ((dh.double().cpu() - want_dh).abs() <= 4 * rel * mag).all()
