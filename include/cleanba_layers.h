@@ -280,7 +280,8 @@ impala_status_t impala_blocknorm_fwd(const blocknorm_shape_t* shape, const void*
  *   drscale = sum ds z act,  dgate = ds rscale z act'(gate),  dz = ds rscale act,
  *   dgamma = sum dz xh,  dbeta = sum dz,  dh = rstd (g - <g> - xh <g xh>) of g = dz gamma (RMS: no <g>).
  * dh is required, the other gradients may be NULL where not wanted; dgate needs gate. Sums over rows are
- * float [C], overwritten (zero for n = 0). An output may be one of dout, dout2, h, gate and out itself.
+ * float [C], overwritten (zero for n = 0), formed in float32 over the rows of a workgroup (n / 512 or so) and
+ * in 64 bits over those. An output of rows may be one of dout, dout2, h, gate and out itself.
  * ws: impala_blocknorm_bwd_workspace_bytes() bytes, 16-byte aligned. */
 size_t impala_blocknorm_bwd_workspace_bytes(const blocknorm_shape_t* shape);
 impala_status_t impala_blocknorm_bwd(const blocknorm_shape_t* shape, const void* dout, const void* dout2,

@@ -1,8 +1,8 @@
 // The global norm over many gradient tensors and their clipped values. HBM-bound: every source is read once for the norm
 // and once more for the values (from the caches where it fits them), every target written once. The tensors go by tables
 // in the kernels' arguments, so that a call is two launches for up to kGcTable of them and copies nothing to the device.
-// 36 tensors of 1.09 M float32 numbers in all: kernels of 4.4 and 5.6 us; 84 of 219 M, nearly all bf16, into float32:
-// 370 us, 4.7 TB/s with the second reading.
+// 36 tensors of 1.09 M float32 numbers in all: kernels of 5.0 and 7.0 us in the trace; 84 of 219 M, nearly all bf16, into float32:
+// 370 us (381 on another card), 4.7 TB/s with the second reading.
 #include <algorithm>
 
 #include "common.h"
@@ -15,7 +15,8 @@ namespace {
 
 constexpr int kGcTable = 96;       // tensors of a launch
 constexpr int kGcSeg = 16384;       // elements a workgroup takes at a time
-constexpr int kGcBlocks = 4096;    // workgroups of a launch, each with one partial sum (2048: 391 us for 380 below)
+constexpr int kGcBlocks = 4096;    // workgroups of a launch, each with one partial sum (2048: 382 us for
+                                   // the four wide blocks instead of 370)
 
 struct GcEntry {
     const void* src;
@@ -91,8 +92,8 @@ CB_DEV void gc_floats(const GcRaw& r, float* x) {
     }
 }
 
-// f(offset, elements left, eight floats) over a segment, 128 bytes of a thread on their way at once (64: 2% more time for
-// the four wide blocks).
+// f(offset, elements left, eight floats) over a segment, 128 bytes of a thread on their way at once (64: 384 us for the
+// four wide blocks instead of 370).
 template <bool F32, class F>
 CB_DEV void gc_pieces(const GcEntry& e, int64_t at, int n, F&& f) {
     constexpr int ST = 8 * 256, NP = F32 ? 4 : 8;

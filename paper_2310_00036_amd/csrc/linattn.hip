@@ -13,9 +13,9 @@ namespace {
 
 // One step from state to state, HBM-bound: the state is read and written once. A workgroup has one state, a thread four
 // neighbouring columns of every (NT / LR)th row, all loaded before anything waits (LR: the lanes of a row, a power of two).
-// 4096 envs x 8 heads of 128 x 128: 4.3 GB in 0.86 ms, 5.0 TB/s. (A rollout of 4 steps of 512 envs x 8 heads of 64 takes 47 us
+// 4096 envs x 8 heads of 128 x 128: 4.3 GB in 0.86 ms, 5.0 TB/s. (A rollout of 4 steps of 512 envs x 8 heads of 64 takes 49 us
 // as a chunk and took 31 row by row from registers: with one step, where the state is all there is to move, a chunk's
-// set-up would cost more than the step. On 64 envs x 4 heads the chunk is the faster from 4 steps on, 9 us for 18.)
+// set-up would cost more than the step. On 64 envs x 4 heads the chunk is the faster from 4 steps on, 8 us for 18.)
 template <class Pr, int NT, int LR>
 __global__ __launch_bounds__(NT) void la_step_kernel(LaArgs a) {
     using T = typename Pr::T;
@@ -123,9 +123,9 @@ hipError_t la_step(const LaArgs& a, hipStream_t s) {
 // together and handed round in LDS.
 //
 // 64 rows: the products on the diagonal grow with the chunk, the state's with its number, and a wave's lanes are the rows.
-// A chunk of 64-wide heads is 32 KB in bf16 and takes a workgroup of four waves 2.7 us (6500 cycles, about 930 of them in the
-// matrix cores and 1500 in LDS); two of them share a CU, 2048 x 256 envs x 4 heads take 252 us, 4.3 TB/s. Heads of 128: eight waves,
-// alone on a CU, 5.7 us for 64 KB.
+// A chunk of 64-wide heads is 32 KB in bf16 and takes a workgroup of four waves 2.9 us (7000 cycles, about 1150 of them in
+// the matrix cores); two of them share a CU, 2048 x 256 envs x 4 heads take 279 us, 4.0 TB/s. Heads of 128: eight waves, alone on
+// a CU, 5.6 us for 64 KB.
 
 constexpr int kL = 64;
 typedef uint32_t cb_u32x2 __attribute__((ext_vector_type(2)));
@@ -836,8 +836,8 @@ hipError_t la_chunks(const LaArgs& a, const LaSegs& sg, bool state, hipStream_t 
 
 // Segments of the rollout that run at once: as many as fill the chip's places for workgroups once, of four chunks at
 // least. Each segment's state has to be known first, which reads k and v again and takes two launches more: less than
-// three segments gain nothing. (16384 x 2 envs x 8 heads of 128: 16 chains of 256 chunks, which take 5.8 us each;
-// in 16 segments 145 us in all.)
+// three segments gain nothing. (16384 x 2 envs x 8 heads of 128: 16 chains of 256 chunks, which take 5.6 us each;
+// in 16 segments 138 us in all.)
 int la_segs(int prec, int T, int64_t EH, int dk, int dv, int passes, int* chunks) {
     const int64_t nc = (int64_t(T) + kL - 1) / kL;
     *chunks = int(nc);
