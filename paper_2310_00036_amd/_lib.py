@@ -2,8 +2,9 @@
 include/cleanba_layers.h under the same names.
 
 This layer only marshals arguments (torch tensors -> device pointers, the current HIP
-stream, C structs) and turns non-zero statuses into exceptions; every step of the learner
-runs in the library's HIP kernels. Importing it fails loudly when the library is missing.
+stream, C structs; tensors that a struct describes are held against it) and turns non-zero
+statuses into exceptions; every step of the learner runs in the library's HIP kernels.
+Importing it fails loudly when the library is missing.
 """
 from __future__ import annotations
 
@@ -749,11 +750,12 @@ def grad_clip_workspace_bytes(tensors) -> int:
 
 def grad_clip(tensors, max_grad_norm, stats, ws, stream=None):
     """tensors: grad_tensors(...)."""
-    if len(tensors.devices) > 1 or -1 in tensors.devices:
+    devices = getattr(tensors, "devices", ())   # an array of plain addresses has none
+    if len(devices) > 1 or -1 in devices:
         raise ValueError("grad_clip: the tensors have to be on one GPU")
     n = max(2, stats.numel()) if isinstance(stats, torch.Tensor) else 2
     p, at = _pointers("grad_clip", (("stats", (n,), (1,), torch.float32),), (stats,), ws)
-    device = next(iter(tensors.devices), at)
+    device = next(iter(devices), at)
     if at is not None and at != device:
         raise ValueError("grad_clip: the tensors have to be on one GPU")
     _check("grad_clip", lib.grad_clip(tensors, tensors.used, max_grad_norm, *p, *_ws_args(ws),
